@@ -77,6 +77,24 @@ typedef struct {
     int32_t n_blocks;
 } rs_pool_desc;
 
+/* The pool of a cache held in 4 bits (rs_init_kv4; device, caller-allocated, 16-byte aligned).
+ * uint8 [n_layers][n_blocks][n_kv_heads][RS_KV4_BYTES(head_dim)], layer_stride = BYTES between layers (a multiple of 16).
+ * 8.5 bits for each key/value pair of elements: 3.76 times the tokens of the bf16 pools in the same memory.
+ *   Values.  32 consecutive dims of a token's key (after the rotary embedding) or value are a group with a scale
+ *     s = 2^(b-127), b one byte: the smallest power of two with max|x| < 7 s, b clamped to [2, 252]; an element is s times
+ *     the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (ties to the even index, more than 6 to 6) with its sign, code = index + 8 if
+ *     negative.  A group that holds a NaN or an infinity has b = 255 and reads back as NaN.
+ *   Bytes of one (block, kv head), G = head_dim/32:
+ *     K codes  [G][16 tokens][16]     byte j: dims 2j (low half) and 2j+1 of the group
+ *     V codes  [4][16][G][4]          byte (q, j, g, i): dims 32g+2j (low half) and 32g+2j+1 of token 4q+i
+ *     K scales [G][16 tokens], V scales [4][G][4] (token 4q+i at (q, g, i)) */
+#define RS_KV4_BYTES(head_dim) (17 * (head_dim))
+typedef struct {
+    void *pool;
+    int64_t layer_stride;
+    int32_t n_blocks;
+} rs_kv4_desc;
+
 /* Upper bounds that size the two activation workspaces. */
 typedef struct {
     int32_t max_prefill_tokens; /* total tokens of one rs_prefill_layer call */
@@ -116,6 +134,11 @@ typedef struct {
  * split (256,256).  pool may have null pointers only for RS_HOST_ONLY.  prof may be NULL. */
 int32_t rs_init(const rs_model_desc *model, const rs_pool_desc *pool, const rs_limits *limits,
                 const rs_profile *prof, int32_t device, rs_ctx **out);
+/* rs_init for a context whose cache is held in 4 bits.  Allocates two more workspaces, for attention whose rows more than
+ * one workgroup computes (34 MB and what the decode rows' 512-token chunks need, as for the bf16 cache, on each side that
+ * runs such attention). */
+int32_t rs_init_kv4(const rs_model_desc *model, const rs_kv4_desc *pool, const rs_limits *limits,
+                    const rs_profile *prof, int32_t device, rs_ctx **out);
 /* Waits for both sides, frees everything the library owns. */
 int32_t rs_destroy(rs_ctx *ctx);
 /* Registers (borrows) the weights of one layer, and, on a GPU context, makes the library's own
@@ -195,6 +218,43 @@ int32_t rs_prefill_layer(rs_ctx *ctx, int32_t layer, const void *x_in, void *x_o
 int32_t rs_decode_layer(rs_ctx *ctx, int32_t layer, const void *x_in, void *x_out,
                         const int32_t *ctx_lens, const int32_t *block_tables, int32_t max_blk,
                         int32_t B, int32_t max_ctx);
+
+/* ---- the cache held in 4 bits ------------------------------------------------------------------
+ * For contexts of rs_init_kv4 (RS_ERR_STATE on others, and on host-only ones).  Each call enqueues on the named side's
+ * current stream and returns; calls on one side are ordered, between the sides the caller orders them.  Block ids come from
+ * rs_kv_alloc.  Rows are bf16, `row_stride` elements apart (a multiple of 8, and 16-byte aligned; at least the row's own
+ * length).  A block id outside the pool is never dereferenced: what it would have held is skipped (rows that would be read
+ * from it are zero), and rs_sync reports RS_ERR_BAD_BLOCK.
+ *
+ * rs_kv4_write: quantises keys (after the rotary embedding) and values of runs of tokens.  Rows [cu_seqlens[r],
+ * cu_seqlens[r+1]) of k and v, n_kv_heads * head_dim elements each, are the tokens at positions start_pos[r], start_pos[r] + 1,
+ * ... of request r (host arrays; start_pos may be null: all 0; any position may start a run, a run may be empty, n_req is 1 to
+ * RS_MAX_PREFILL_REQS).  Tokens outside the runs keep what they hold.
+ * rs_kv4_append: one token of each of B requests, row i at position ctx_lens[i] (device), -1: no request, nothing is done.
+ * rs_kv4_read: the inverse of rs_kv4_write, exactly what the cache holds as bf16.
+ * RS_ERR_BAD_ARG for a null or misaligned pointer or a bad size, RS_ERR_BAD_BLOCK for a table too short for a run. */
+int32_t rs_kv4_write(rs_ctx *ctx, int32_t side, int32_t layer, const void *k, const void *v, int64_t row_stride,
+                     const int32_t *cu_seqlens, const int32_t *start_pos, int32_t n_req, const int32_t *block_tables,
+                     int32_t max_blk);
+int32_t rs_kv4_append(rs_ctx *ctx, int32_t side, int32_t layer, const void *k, const void *v, int64_t row_stride,
+                      const int32_t *ctx_lens, const int32_t *block_tables, int32_t max_blk, int32_t B);
+int32_t rs_kv4_read(rs_ctx *ctx, int32_t side, int32_t layer, void *k_out, void *v_out, int64_t row_stride,
+                    const int32_t *cu_seqlens, const int32_t *start_pos, int32_t n_req, const int32_t *block_tables,
+                    int32_t max_blk);
+/* Attention over the cache, softmax(q K^T / sqrt(head_dim)) V of every query head, on the DECODE side: row i of q (rotated;
+ * n_q_heads * head_dim elements) attends to ctx_lens[i] + 1 cached tokens (the newest one included, as rs_kv4_append leaves it).
+ * ctx_lens[i] = -1: a row without a request, its output is zero.  B <= max_decode_batch, max_ctx (host) bounds
+ * ctx_lens[i] + 1 as for rs_decode_layer.  Results depend on the sizes alone, not on the CU split.
+ * A score whose key or value group is not finite is NaN, and so is its row's output for that head. */
+int32_t rs_kv4_decode_attention(rs_ctx *ctx, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                                const int32_t *ctx_lens, const int32_t *block_tables, int32_t max_blk, int32_t B,
+                                int32_t max_ctx);
+/* The same for several rows a request, on the PREFILL side: rows [cu_seqlens[r], cu_seqlens[r+1]) are positions start_pos[r] ..
+ * of request r (start_pos null: all 0) and each attends to the cached positions up to its own, which are there already
+ * (rs_kv4_write).  At most max_prefill_tokens rows.  What a later token holds, NaN included, does not reach earlier rows. */
+int32_t rs_kv4_prefill_attention(rs_ctx *ctx, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                                 const int32_t *cu_seqlens, const int32_t *start_pos, int32_t n_req,
+                                 const int32_t *block_tables, int32_t max_blk);
 
 /* The same decode step, replayed from a captured HIP graph (section 4.5.2: decode steps are
  * captured as graphs per batch size; section 4.5.3: the CU mask a graph was captured under stays

@@ -33,6 +33,7 @@ EXPORTS = [
     "rs_debug_cu_histogram", "rs_debug_read_workspace", "rs_debug_stream_read", "rs_debug_mfma_probe", "rs_submit", "rs_step", "rs_request_state", "rs_debug_complete_prefill",
     "rs_set_head", "rs_embed", "rs_lm_head_greedy", "rs_submit_tokens", "rs_step_tokens", "rs_request_output",
     "rs_debug_push_sampled", "rs_request_times", "rs_request_release", "rs_set_step_graphs", "rs_step_graph_stats", "rs_engine_start", "rs_engine_stop", "rs_engine_stats", "rs_release_source_weights", "rs_set_moe_weights", "rs_debug_read_moe_routing",
+    "rs_init_kv4", "rs_kv4_write", "rs_kv4_append", "rs_kv4_read", "rs_kv4_decode_attention", "rs_kv4_prefill_attention",
 ]
 
 
@@ -51,6 +52,15 @@ class ModelDesc(ctypes.Structure):
 class PoolDesc(ctypes.Structure):
     _fields_ = [("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p), ("layer_stride", ctypes.c_int64),
                 ("n_blocks", ctypes.c_int32)]
+
+
+class Kv4Desc(ctypes.Structure):
+    _fields_ = [("pool", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("n_blocks", ctypes.c_int32)]
+
+
+def kv4_bytes(head_dim: int) -> int:
+    """Bytes of one (block, kv head) of a cache held in 4 bits (RS_KV4_BYTES)."""
+    return 17 * head_dim
 
 
 class Limits(ctypes.Structure):
@@ -123,6 +133,15 @@ def _i32(a) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.int32)
 
 
+def _runs(cu_seqlens, start_pos):
+    """cu_seqlens, their number of runs and start_pos (None: null) as ctypes arguments."""
+    n = len(cu_seqlens) - 1
+    if start_pos is not None and len(start_pos) != n:
+        raise ValueError(f"{len(start_pos)} first positions for {n} requests")
+    sp = (ctypes.c_int32 * max(n, 1))(*map(int, start_pos)) if start_pos is not None else None
+    return (ctypes.c_int32 * (n + 1))(*map(int, cu_seqlens)), ctypes.c_int32(n), sp
+
+
 def _ptr(x) -> ctypes.c_void_p:
     """Device pointer of a torch tensor (or an int address)."""
     if x is None:
@@ -150,29 +169,31 @@ class Profile:
 
 
 class Context:
-    """Owns one rs_ctx.  Method names mirror the C entry points without the rs_ prefix."""
+    """Owns one rs_ctx.  Method names mirror the C entry points without the rs_ prefix.  With kv4_pool (uint8
+    [n_layers][n_blocks][n_kv_heads][kv4_bytes(head_dim)]) the cache is held in 4 bits (rs_init_kv4; layer_stride in bytes)."""
 
     def __init__(self, d_model: int, n_q_heads: int, n_kv_heads: int, head_dim: int, ffn_dim: int,
                  n_layers: int, rms_eps: float, rope_base: float, max_pos: int, n_blocks: int,
                  k_pool=None, v_pool=None, layer_stride: int = 0, max_prefill_tokens: int = 0,
                  max_decode_batch: int = 0, max_context: int = 1, profile: Optional[Profile] = None,
-                 device: int = 0):
+                 device: int = 0, kv4_pool=None, kv4: bool = False):
         self._lib = load()
         self._h = ctypes.c_void_p(0)
         m = ModelDesc(d_model, n_q_heads, n_kv_heads, head_dim, ffn_dim, n_layers, rms_eps, rope_base, max_pos)
+        kv4 = kv4 or kv4_pool is not None   # kv4 alone: a host-only context of that kind
         if layer_stride == 0:
-            layer_stride = n_blocks * RS_KV_BLOCK * n_kv_heads * head_dim
-        p = PoolDesc(_ptr(k_pool), _ptr(v_pool), layer_stride, n_blocks)
+            layer_stride = n_blocks * n_kv_heads * (kv4_bytes(head_dim) if kv4 else RS_KV_BLOCK * head_dim)
+        p = Kv4Desc(_ptr(kv4_pool), layer_stride, n_blocks) if kv4 else PoolDesc(_ptr(k_pool), _ptr(v_pool), layer_stride, n_blocks)
         lim = Limits(max_prefill_tokens, max_decode_batch, max_context)
         self._prof = profile
         pd = profile.desc() if profile is not None else None
-        self._keep = [k_pool, v_pool]
+        self._keep = [k_pool, v_pool, kv4_pool]
         self._keep_layers = []
         self.n_layers = n_layers
         self.max_context = max_context
-        _check(self._lib.rs_init(ctypes.byref(m), ctypes.byref(p), ctypes.byref(lim),
-                                 ctypes.byref(pd) if pd is not None else None, ctypes.c_int32(device),
-                                 ctypes.byref(self._h)))
+        init = self._lib.rs_init_kv4 if kv4 else self._lib.rs_init
+        _check(init(ctypes.byref(m), ctypes.byref(p), ctypes.byref(lim), ctypes.byref(pd) if pd is not None else None,
+                    ctypes.c_int32(device), ctypes.byref(self._h)))
 
     @classmethod
     def from_shape(cls, shape, **kw):
@@ -275,6 +296,32 @@ class Context:
         _check(self._lib.rs_decode_layer_graph(self._h, ctypes.c_int32(layer), _ptr(x_in), _ptr(x_out), _ptr(ctx_lens),
                                                _ptr(block_tables), ctypes.c_int32(max_blk), ctypes.c_int32(B),
                                                ctypes.c_int32(max_ctx_bucket)))
+
+    # -- the cache held in 4 bits
+    def kv4_write(self, side: int, layer: int, k, v, row_stride: int, cu_seqlens: Sequence[int], start_pos, block_tables, max_blk: int):
+        cu, n, sp = _runs(cu_seqlens, start_pos)
+        _check(self._lib.rs_kv4_write(self._h, ctypes.c_int32(side), ctypes.c_int32(layer), _ptr(k), _ptr(v), ctypes.c_int64(row_stride),
+                                      cu, sp, n, _ptr(block_tables), ctypes.c_int32(max_blk)))
+
+    def kv4_append(self, side: int, layer: int, k, v, row_stride: int, ctx_lens, block_tables, max_blk: int, B: int):
+        _check(self._lib.rs_kv4_append(self._h, ctypes.c_int32(side), ctypes.c_int32(layer), _ptr(k), _ptr(v), ctypes.c_int64(row_stride),
+                                       _ptr(ctx_lens), _ptr(block_tables), ctypes.c_int32(max_blk), ctypes.c_int32(B)))
+
+    def kv4_read(self, side: int, layer: int, k_out, v_out, row_stride: int, cu_seqlens: Sequence[int], start_pos, block_tables, max_blk: int):
+        cu, n, sp = _runs(cu_seqlens, start_pos)
+        _check(self._lib.rs_kv4_read(self._h, ctypes.c_int32(side), ctypes.c_int32(layer), _ptr(k_out), _ptr(v_out), ctypes.c_int64(row_stride),
+                                     cu, sp, n, _ptr(block_tables), ctypes.c_int32(max_blk)))
+
+    def kv4_decode_attention(self, layer: int, q, q_stride: int, out, out_stride: int, ctx_lens, block_tables, max_blk: int, B: int, max_ctx: int):
+        _check(self._lib.rs_kv4_decode_attention(self._h, ctypes.c_int32(layer), _ptr(q), ctypes.c_int64(q_stride), _ptr(out),
+                                                 ctypes.c_int64(out_stride), _ptr(ctx_lens), _ptr(block_tables), ctypes.c_int32(max_blk),
+                                                 ctypes.c_int32(B), ctypes.c_int32(max_ctx)))
+
+    def kv4_prefill_attention(self, layer: int, q, q_stride: int, out, out_stride: int, cu_seqlens: Sequence[int], start_pos, block_tables,
+                              max_blk: int):
+        cu, n, sp = _runs(cu_seqlens, start_pos)
+        _check(self._lib.rs_kv4_prefill_attention(self._h, ctypes.c_int32(layer), _ptr(q), ctypes.c_int64(q_stride), _ptr(out),
+                                                  ctypes.c_int64(out_stride), cu, sp, n, _ptr(block_tables), ctypes.c_int32(max_blk)))
 
     # -- CU split / manager
     def set_cu_split(self, prefill_cus: int, decode_cus: int):

@@ -69,6 +69,43 @@ enum HybridForm { HYBRID_APART, HYBRID_TEAMS, HYBRID_SMALL };
 HybridForm hybrid_form(const PrefillAttnArgs &p, const DecodeAttnArgs &d);
 void launch_hybrid_attention(hipStream_t st, const PrefillAttnArgs &p, const DecodeAttnArgs &d);
 
+// ---- the KV cache held in 4 bits (kv4.hip) ----
+struct Kv4RowsArgs {
+    const bf16_t *k, *v;      // write, append: rows of Hkv * hd, row_stride elements apart (multiples of 8, 16-byte aligned)
+    bf16_t *k_out, *v_out;    // read
+    size_t row_stride;
+    uint8_t *pool;            // this layer: [n_blocks][Hkv][17 * hd]
+    const int32_t *tables;    // [n_req or B][max_blk]
+    const int32_t *ctx_lens;  // append: position of row m's token, -1: none
+    int32_t *err_flag;
+    int B, Hkv, hd, max_blk, n_blocks;
+    SeqInfo seq;              // write, read: request r's rows are its tokens start[r] ..
+};
+void launch_kv4_write(hipStream_t st, const Kv4RowsArgs &a);
+void launch_kv4_append(hipStream_t st, const Kv4RowsArgs &a);
+void launch_kv4_read(hipStream_t st, const Kv4RowsArgs &a);
+
+struct Kv4AttnArgs {
+    const bf16_t *q;          // rows of Hq * hd, q_stride elements apart
+    size_t q_stride;
+    bf16_t *out;              // row-major, out_stride elements apart, or with out_Mt fragment-packed
+    size_t out_stride;
+    const uint8_t *pool;      // this layer
+    const int32_t *tables;
+    const int32_t *ctx_lens;  // decode: row b sees ctx_lens[b] + 1 tokens
+    int32_t *err_flag;
+    float *part_o, *part_ml;  // [rows][Hq][n_chunks][hd], [..][2]: pieces of rows that more than one workgroup computes
+    int B, Hq, Hkv, hd, max_blk, n_blocks, max_ctx;
+    float scale_log2;         // log2(e) / sqrt(hd)
+    SeqInfo seq;              // prompts
+    int out_row0 = 0, out_Mt = 0;   // first row and row tiles of the packed output matrix
+    int chunk = 0, n_chunks = 0;    // set by the launchers
+};
+#define KV4_SPLIT_WGS 512      // most workgroups of a launch whose rows are cut into key ranges
+int kv4_chunk(int B, int Hkv, int max_ctx);
+void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &a);
+void launch_kv4_prefill(hipStream_t st, const Kv4AttnArgs &a);
+
 enum GemmEpilogue { EPI_STORE = 0, EPI_RESIDUAL = 1, EPI_SWIGLU = 2 };
 
 // out[M,N] = epi(A[M,K] * W[N,K]^T).  EPI_RESIDUAL adds resid[M,N].  EPI_SWIGLU:

@@ -168,6 +168,11 @@ struct rs_ctx {
     struct MoeLayer { int E = 0; const bf16_t *router = nullptr; bf16_t *wg = nullptr, *wu = nullptr, *wd = nullptr;
                       size_t stride_gu = 0, stride_d = 0; };
     std::vector<MoeLayer> moe;
+    // a cache held in 4 bits (rs_init_kv4): its pool, and scratch of attention whose rows several workgroups compute, per side
+    uint8_t *kv4 = nullptr;
+    int64_t kv4_stride = 0;
+    bool is_kv4 = false;
+    float *kv4_part_o[2] = {nullptr, nullptr}, *kv4_part_ml[2] = {nullptr, nullptr};
     CosSin *rope = nullptr;
     // One error word per side (kernels OR bits into it: 1 position outside the rotary table, 2 block id outside
     // the pool, 4 token outside the vocabulary, 8 context length outside [1, max_ctx]) and its pinned host
@@ -540,6 +545,7 @@ int32_t check_layer_call(rs_ctx *c, int side, int32_t layer, const void *x_in, v
     if (!c) return fail(RS_ERR_BAD_ARG, "null context");
     if (!c->gpu) return fail(RS_ERR_STATE, "host-only context cannot run layers");
     if (layer < 0 || layer >= c->m.n_layers) return fail(RS_ERR_BAD_ARG, "layer %d out of range", layer);
+    if (c->is_kv4) return fail(RS_ERR_STATE, "layer passes need the bf16 cache");
     if (!c->have_weights[layer]) return fail(RS_ERR_STATE, "weights of layer %d not set", layer);
     if (!x_in || !x_out || !tables) return fail(RS_ERR_BAD_ARG, "null pointer");
     if (c->side[side].cus <= 0) return fail(RS_ERR_STATE, "side %d has no compute units in the current split", side);
@@ -979,6 +985,118 @@ int32_t enter_mode(rs_ctx *c, int mode) {
     return RS_OK;
 }
 
+// ---- the cache held in 4 bits ----
+
+// The device of a context for the length of a call; the caller's current device again afterwards.
+struct OnDevice {
+    int prev = -1;
+    hipError_t err;
+    explicit OnDevice(int device) {
+        err = hipGetDevice(&prev);
+        if (err == hipSuccess && prev != device) err = hipSetDevice(device);
+        else prev = -1;
+    }
+    ~OnDevice() {
+        if (prev >= 0) (void)hipSetDevice(prev);
+    }
+};
+
+// Rows of partial results that a side's attention can need, as (row, query head) pieces: the split launches' of prompts, and of
+// `rows` decode rows in chunks (a launch with chunks of less than 512 tokens has less than 1024 of them).
+size_t kv4_pieces(const rs_ctx *c, bool prefill, int rows) {
+    const rs_model_desc &m = c->m;
+    const size_t chunks = ((size_t)c->lim.max_context + RS_DECODE_CHUNK - 1) / RS_DECODE_CHUNK;
+    size_t n = prefill ? (size_t)KV4_SPLIT_WGS * 128 : 0;
+    if (rows > 0) n = std::max(n, std::max<size_t>((size_t)rows * m.n_kv_heads * chunks, 1024) * (m.n_q_heads / m.n_kv_heads));
+    return n;
+}
+
+int32_t alloc_kv4(rs_ctx *c) {
+    for (int s = 0; s < 2; ++s) {
+        const int decode_rows = s == RS_SIDE_DECODE ? c->lim.max_decode_batch : std::min(c->lim.max_decode_batch, c->lim.max_prefill_tokens);
+        const size_t n = kv4_pieces(c, s == RS_SIDE_PREFILL && c->lim.max_prefill_tokens > 0, decode_rows);
+        if (n == 0) continue;
+        HIP_TRY(hipMalloc(&c->kv4_part_o[s], n * c->m.head_dim * sizeof(float)));
+        HIP_TRY(hipMalloc(&c->kv4_part_ml[s], n * 2 * sizeof(float)));
+    }
+    return RS_OK;
+}
+
+int32_t check_kv4_call(rs_ctx *c, int32_t side, int32_t layer, const int32_t *tables, int32_t max_blk) {
+    if (!c) return fail(RS_ERR_BAD_ARG, "null context");
+    if (side < 0 || side > 1) return fail(RS_ERR_BAD_ARG, "side %d", side);
+    if (!c->is_kv4) return fail(RS_ERR_STATE, "the context's cache is not held in 4 bits (rs_init_kv4)");
+    if (layer < 0 || layer >= c->m.n_layers) return fail(RS_ERR_BAD_ARG, "layer %d out of range", layer);
+    if (!tables) return fail(RS_ERR_BAD_ARG, "null block tables");
+    if (max_blk < 1) return fail(RS_ERR_BAD_BLOCK, "block tables of %d entries", max_blk);
+    return RS_OK;
+}
+
+// The last check, behind those of the arguments: whether the side can take work.
+int32_t check_kv4_side(rs_ctx *c, int32_t side) {
+    if (!c->gpu) return fail(RS_ERR_STATE, "host-only context: no device work");
+    if (c->side[side].cus <= 0 || !c->side[side].stream) return fail(RS_ERR_STATE, "side %d has no compute units in the current split", side);
+    return RS_OK;
+}
+
+int32_t check_kv4_rows(const char *what, const void *p, int64_t stride, int64_t width) {
+    if (!p || (uintptr_t)p % 16) return fail(RS_ERR_BAD_ARG, "%s: a null pointer or one that is not 16-byte aligned", what);
+    if (stride < width || stride % 8) return fail(RS_ERR_BAD_ARG, "%s: rows %lld elements apart, must be a multiple of 8 and at least %lld", what, (long long)stride, (long long)width);
+    return RS_OK;
+}
+
+// Runs of tokens by request -> their description for the kernels.
+int32_t kv4_runs(const int32_t *cu, const int32_t *start, int32_t n_req, int32_t max_blk, SeqInfo *seq) {
+    if (!cu || n_req < 1 || n_req > RS_MAX_PREFILL_REQS) return fail(RS_ERR_BAD_ARG, "n_req %d out of range, or null cu_seqlens", n_req);
+    if (cu[0] != 0) return fail(RS_ERR_BAD_ARG, "cu_seqlens must start at 0");
+    seq->n_req = n_req;
+    seq->cu[0] = 0;
+    for (int r = 0; r < n_req; ++r) {
+        const int32_t first = start ? start[r] : 0, len = cu[r + 1] - cu[r];
+        if (cu[r + 1] < cu[r]) return fail(RS_ERR_BAD_ARG, "cu_seqlens must ascend");
+        if (first < 0 || (int64_t)first + len > INT32_MAX - 64) return fail(RS_ERR_BAD_ARG, "positions %d .. of request %d out of range", first, r);
+        if (len > 0 && (first + len - 1) / RS_KV_BLOCK >= max_blk)
+            return fail(RS_ERR_BAD_BLOCK, "block table of %d entries too short for %d tokens", max_blk, first + len);
+        seq->cu[r + 1] = cu[r + 1];
+        seq->start[r] = first;
+    }
+    return RS_OK;
+}
+
+Kv4RowsArgs kv4_rows_args(rs_ctx *c, int side, int32_t layer, int64_t row_stride, const int32_t *tables, int32_t max_blk) {
+    Kv4RowsArgs a{};
+    a.row_stride = (size_t)row_stride;
+    a.pool = c->kv4 + (size_t)layer * c->kv4_stride;
+    a.tables = tables;
+    a.err_flag = c->err_flag + side;
+    a.Hkv = c->m.n_kv_heads;
+    a.hd = c->m.head_dim;
+    a.max_blk = max_blk;
+    a.n_blocks = c->pool.n_blocks;
+    return a;
+}
+
+Kv4AttnArgs kv4_attn_args(rs_ctx *c, int side, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                          const int32_t *tables, int32_t max_blk) {
+    Kv4AttnArgs a{};
+    a.q = (const bf16_t *)q;
+    a.q_stride = (size_t)q_stride;
+    a.out = (bf16_t *)out;
+    a.out_stride = (size_t)out_stride;
+    a.pool = c->kv4 + (size_t)layer * c->kv4_stride;
+    a.tables = tables;
+    a.err_flag = c->err_flag + side;
+    a.part_o = c->kv4_part_o[side];
+    a.part_ml = c->kv4_part_ml[side];
+    a.Hq = c->m.n_q_heads;
+    a.Hkv = c->m.n_kv_heads;
+    a.hd = c->m.head_dim;
+    a.max_blk = max_blk;
+    a.n_blocks = c->pool.n_blocks;
+    a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c->m.head_dim));
+    return a;
+}
+
 int32_t check_head_call(rs_ctx *c, int side, int n) {
     if (!c) return fail(RS_ERR_BAD_ARG, "null context");
     if (side < 0 || side > 1) return fail(RS_ERR_BAD_ARG, "side %d", side);
@@ -997,8 +1115,9 @@ extern "C" {
 
 const char *rs_last_error(void) { return g_err.c_str(); }
 
-int32_t rs_init(const rs_model_desc *model, const rs_pool_desc *pool, const rs_limits *limits,
-                const rs_profile *prof, int32_t device, rs_ctx **out) {
+// Both kinds of context: kv4 is the 4-bit pool, or null for the bf16 pools that `pool` describes.
+static int32_t init_ctx(const rs_model_desc *model, const rs_pool_desc *pool, const rs_kv4_desc *kv4, const rs_limits *limits,
+                        const rs_profile *prof, int32_t device, rs_ctx **out) {
     if (!model || !pool || !limits || !out) return fail(RS_ERR_BAD_ARG, "null argument");
     const rs_model_desc &m = *model;
     if (m.head_dim != 64 && m.head_dim != 128) return fail(RS_ERR_BAD_ARG, "head_dim %d: only 64 and 128", m.head_dim);
@@ -1011,10 +1130,13 @@ int32_t rs_init(const rs_model_desc *model, const rs_pool_desc *pool, const rs_l
         return fail(RS_ERR_BAD_ARG, "bad n_layers / max_pos / rope_base / rms_eps");
     if (pool->n_blocks < 1) return fail(RS_ERR_BAD_ARG, "pool needs at least one block");
     const int64_t per_layer = (int64_t)pool->n_blocks * RS_KV_BLOCK * m.n_kv_heads * m.head_dim;
-    if (m.n_layers > 1 && pool->layer_stride < per_layer) return fail(RS_ERR_BAD_ARG, "layer_stride smaller than one layer's pool");
+    if (!kv4 && m.n_layers > 1 && pool->layer_stride < per_layer) return fail(RS_ERR_BAD_ARG, "layer_stride smaller than one layer's pool");
+    if (kv4 && m.n_layers > 1 && kv4->layer_stride < (int64_t)kv4->n_blocks * m.n_kv_heads * RS_KV4_BYTES(m.head_dim))
+        return fail(RS_ERR_BAD_ARG, "layer_stride smaller than one layer's pool");
+    if (kv4 && (kv4->layer_stride % 16 || (uintptr_t)kv4->pool % 16)) return fail(RS_ERR_BAD_ARG, "4-bit pool or its layer_stride not a multiple of 16 bytes");
     if (limits->max_prefill_tokens < 0 || limits->max_decode_batch < 0 || limits->max_context < 1)
         return fail(RS_ERR_BAD_ARG, "bad limits");
-    if (device != RS_HOST_ONLY && (!pool->k_pool || !pool->v_pool)) return fail(RS_ERR_BAD_ARG, "null KV pool");
+    if (device != RS_HOST_ONLY && (kv4 ? !kv4->pool : !pool->k_pool || !pool->v_pool)) return fail(RS_ERR_BAD_ARG, "null KV pool");
     if (prof) {
         if (prof->n_batch < 1 || prof->n_ctx < 1 || prof->n_split < 1 || !prof->batch_edges || !prof->ctx_edges ||
             !prof->decode_cus || !prof->lat_distinct_us || !prof->lat_over_us)
@@ -1028,6 +1150,11 @@ int32_t rs_init(const rs_model_desc *model, const rs_pool_desc *pool, const rs_l
     rs_ctx *c = new rs_ctx();
     c->m = m;
     c->pool = *pool;
+    if (kv4) {
+        c->is_kv4 = true;
+        c->kv4 = (uint8_t *)kv4->pool;
+        c->kv4_stride = kv4->layer_stride;
+    }
     c->lim = *limits;
     c->device = device;
     c->gpu = device != RS_HOST_ONLY;
@@ -1089,6 +1216,7 @@ int32_t rs_init(const rs_model_desc *model, const rs_pool_desc *pool, const rs_l
         if (r) return r;
         r = alloc_ws(c, c->ws[RS_SIDE_DECODE], limits->max_decode_batch, true);
         if (r) return r;
+        if (kv4 && (r = alloc_kv4(c))) return r;
         for (int s = 0; s < 2; ++s) {
             HIP_TRY(hipEventCreateWithFlags(&c->side[s].order, hipEventDisableTiming));
             c->side[s].marks.assign(RS_MAX_MARKS, nullptr);
@@ -1115,6 +1243,18 @@ int32_t rs_init(const rs_model_desc *model, const rs_pool_desc *pool, const rs_l
     return RS_OK;
 }
 
+int32_t rs_init(const rs_model_desc *model, const rs_pool_desc *pool, const rs_limits *limits,
+                const rs_profile *prof, int32_t device, rs_ctx **out) {
+    return init_ctx(model, pool, nullptr, limits, prof, device, out);
+}
+
+int32_t rs_init_kv4(const rs_model_desc *model, const rs_kv4_desc *pool, const rs_limits *limits,
+                    const rs_profile *prof, int32_t device, rs_ctx **out) {
+    if (!pool) return fail(RS_ERR_BAD_ARG, "null argument");
+    const rs_pool_desc none{nullptr, nullptr, 0, pool->n_blocks};
+    return init_ctx(model, &none, pool, limits, prof, device, out);
+}
+
 int32_t rs_destroy(rs_ctx *c) {
     if (!c) return RS_OK;
     if (c->engine) (void)rs_engine_stop(c, 0);
@@ -1131,6 +1271,8 @@ int32_t rs_destroy(rs_ctx *c) {
                 if (e) (void)hipEventDestroy(e);
             for (auto &kv : c->side[s].pool) (void)hipStreamDestroy(kv.second);
             free_ws(c->ws[s]);
+            if (c->kv4_part_o[s]) (void)hipFree(c->kv4_part_o[s]);
+            if (c->kv4_part_ml[s]) (void)hipFree(c->kv4_part_ml[s]);
         }
         for (auto &kv : c->graphs) (void)hipGraphExecDestroy(kv.second);
         drop_step_graphs(c);
@@ -1417,6 +1559,104 @@ int32_t rs_hybrid_layer(rs_ctx *c, int32_t layer, const void *x_in, void *x_out,
     if (rc) return rc;
     return hybrid_layer(c, layer, x_in, x_out, cu_seqlens, start_pos, n_req, prefill_tables, max_blk_prefill, ctx_lens,
                         decode_tables, max_blk_decode, B, max_ctx, 0);
+}
+
+int32_t rs_kv4_write(rs_ctx *c, int32_t side, int32_t layer, const void *k, const void *v, int64_t row_stride,
+                     const int32_t *cu_seqlens, const int32_t *start_pos, int32_t n_req, const int32_t *tables, int32_t max_blk) {
+    int32_t rc = check_kv4_call(c, side, layer, tables, max_blk);
+    if (rc) return rc;
+    const int width = c->m.n_kv_heads * c->m.head_dim;
+    if ((rc = check_kv4_rows("k", k, row_stride, width)) || (rc = check_kv4_rows("v", v, row_stride, width))) return rc;
+    Kv4RowsArgs a = kv4_rows_args(c, side, layer, row_stride, tables, max_blk);
+    if ((rc = kv4_runs(cu_seqlens, start_pos, n_req, max_blk, &a.seq))) return rc;
+    a.k = (const bf16_t *)k;
+    a.v = (const bf16_t *)v;
+    if ((rc = check_kv4_side(c, side))) return rc;
+    OnDevice on(c->device);
+    HIP_TRY(on.err);
+    launch_kv4_write(c->side[side].stream, a);
+    HIP_TRY(hipGetLastError());
+    return RS_OK;
+}
+
+int32_t rs_kv4_append(rs_ctx *c, int32_t side, int32_t layer, const void *k, const void *v, int64_t row_stride,
+                      const int32_t *ctx_lens, const int32_t *tables, int32_t max_blk, int32_t B) {
+    int32_t rc = check_kv4_call(c, side, layer, tables, max_blk);
+    if (rc) return rc;
+    const int width = c->m.n_kv_heads * c->m.head_dim;
+    if ((rc = check_kv4_rows("k", k, row_stride, width)) || (rc = check_kv4_rows("v", v, row_stride, width))) return rc;
+    if (!ctx_lens) return fail(RS_ERR_BAD_ARG, "null ctx_lens");
+    if (B < 1 || B > 65535) return fail(RS_ERR_BAD_ARG, "%d rows", B);
+    Kv4RowsArgs a = kv4_rows_args(c, side, layer, row_stride, tables, max_blk);
+    a.k = (const bf16_t *)k;
+    a.v = (const bf16_t *)v;
+    a.ctx_lens = ctx_lens;
+    a.B = B;
+    if ((rc = check_kv4_side(c, side))) return rc;
+    OnDevice on(c->device);
+    HIP_TRY(on.err);
+    launch_kv4_append(c->side[side].stream, a);
+    HIP_TRY(hipGetLastError());
+    return RS_OK;
+}
+
+int32_t rs_kv4_read(rs_ctx *c, int32_t side, int32_t layer, void *k_out, void *v_out, int64_t row_stride,
+                    const int32_t *cu_seqlens, const int32_t *start_pos, int32_t n_req, const int32_t *tables, int32_t max_blk) {
+    int32_t rc = check_kv4_call(c, side, layer, tables, max_blk);
+    if (rc) return rc;
+    const int width = c->m.n_kv_heads * c->m.head_dim;
+    if ((rc = check_kv4_rows("k_out", k_out, row_stride, width)) || (rc = check_kv4_rows("v_out", v_out, row_stride, width))) return rc;
+    Kv4RowsArgs a = kv4_rows_args(c, side, layer, row_stride, tables, max_blk);
+    if ((rc = kv4_runs(cu_seqlens, start_pos, n_req, max_blk, &a.seq))) return rc;
+    a.k_out = (bf16_t *)k_out;
+    a.v_out = (bf16_t *)v_out;
+    if ((rc = check_kv4_side(c, side))) return rc;
+    OnDevice on(c->device);
+    HIP_TRY(on.err);
+    launch_kv4_read(c->side[side].stream, a);
+    HIP_TRY(hipGetLastError());
+    return RS_OK;
+}
+
+int32_t rs_kv4_decode_attention(rs_ctx *c, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                                const int32_t *ctx_lens, const int32_t *tables, int32_t max_blk, int32_t B, int32_t max_ctx) {
+    int32_t rc = check_kv4_call(c, RS_SIDE_DECODE, layer, tables, max_blk);
+    if (rc) return rc;
+    const int width = c->m.n_q_heads * c->m.head_dim;
+    if ((rc = check_kv4_rows("q", q, q_stride, width)) || (rc = check_kv4_rows("out", out, out_stride, width))) return rc;
+    if (!ctx_lens) return fail(RS_ERR_BAD_ARG, "null ctx_lens");
+    if (B < 1 || B > c->lim.max_decode_batch || B > 65535) return fail(RS_ERR_BAD_ARG, "decode batch %d, the limit is %d", B, c->lim.max_decode_batch);
+    if (max_ctx < 1 || max_ctx > c->lim.max_context) return fail(RS_ERR_BAD_ARG, "max_ctx %d outside [1, %d]", max_ctx, c->lim.max_context);
+    if ((max_ctx + RS_KV_BLOCK - 1) / RS_KV_BLOCK > max_blk)
+        return fail(RS_ERR_BAD_BLOCK, "block table of %d entries too short for context %d", max_blk, max_ctx);
+    Kv4AttnArgs a = kv4_attn_args(c, RS_SIDE_DECODE, layer, q, q_stride, out, out_stride, tables, max_blk);
+    a.ctx_lens = ctx_lens;
+    a.B = B;
+    a.max_ctx = max_ctx;
+    if ((rc = check_kv4_side(c, RS_SIDE_DECODE))) return rc;
+    OnDevice on(c->device);
+    HIP_TRY(on.err);
+    launch_kv4_decode(c->side[RS_SIDE_DECODE].stream, a);
+    HIP_TRY(hipGetLastError());
+    return RS_OK;
+}
+
+int32_t rs_kv4_prefill_attention(rs_ctx *c, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                                 const int32_t *cu_seqlens, const int32_t *start_pos, int32_t n_req, const int32_t *tables, int32_t max_blk) {
+    int32_t rc = check_kv4_call(c, RS_SIDE_PREFILL, layer, tables, max_blk);
+    if (rc) return rc;
+    const int width = c->m.n_q_heads * c->m.head_dim;
+    if ((rc = check_kv4_rows("q", q, q_stride, width)) || (rc = check_kv4_rows("out", out, out_stride, width))) return rc;
+    Kv4AttnArgs a = kv4_attn_args(c, RS_SIDE_PREFILL, layer, q, q_stride, out, out_stride, tables, max_blk);
+    if ((rc = kv4_runs(cu_seqlens, start_pos, n_req, max_blk, &a.seq))) return rc;
+    if (a.seq.cu[n_req] > c->lim.max_prefill_tokens)
+        return fail(RS_ERR_BAD_ARG, "%d rows, the limit is %d", a.seq.cu[n_req], c->lim.max_prefill_tokens);
+    if ((rc = check_kv4_side(c, RS_SIDE_PREFILL))) return rc;
+    OnDevice on(c->device);
+    HIP_TRY(on.err);
+    launch_kv4_prefill(c->side[RS_SIDE_PREFILL].stream, a);
+    HIP_TRY(hipGetLastError());
+    return RS_OK;
 }
 
 int32_t rs_decode_layer_noalloc(rs_ctx *c, int32_t layer, const void *x_in, void *x_out, const int32_t *ctx_lens,
