@@ -70,6 +70,7 @@ HybridForm hybrid_form(const PrefillAttnArgs &p, const DecodeAttnArgs &d);
 void launch_hybrid_attention(hipStream_t st, const PrefillAttnArgs &p, const DecodeAttnArgs &d);
 
 // ---- the KV cache held in 4 bits (kv4.hip) ----
+#define RS_MAX_RUNS 64
 struct Kv4RowsArgs {
     const bf16_t *k, *v;      // write, append: rows of Hkv * hd, row_stride elements apart (multiples of 8, 16-byte aligned)
     bf16_t *k_out, *v_out;    // read
@@ -80,6 +81,7 @@ struct Kv4RowsArgs {
     int32_t *err_flag;
     int B, Hkv, hd, max_blk, n_blocks;
     SeqInfo seq;              // write, read: request r's rows are its tokens start[r] ..
+    int32_t first[RS_MAX_RUNS];   // set by the launchers: blocks that the requests before touch
 };
 void launch_kv4_write(hipStream_t st, const Kv4RowsArgs &a);
 void launch_kv4_append(hipStream_t st, const Kv4RowsArgs &a);
@@ -102,7 +104,10 @@ struct Kv4AttnArgs {
     int chunk = 0, n_chunks = 0;    // set by the launchers
 };
 #define KV4_SPLIT_WGS 512      // most workgroups of a launch whose rows are cut into key ranges
-int kv4_chunk(int B, int Hkv, int max_ctx);
+struct Kv4Cut { int chunk, waves; };
+Kv4Cut kv4_cut(int64_t pairs, int max_ctx);
+int64_t kv4_most_pieces(int64_t pairs, int max_ctx);
+void kv4_kernels_init();
 void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &a);
 void launch_kv4_prefill(hipStream_t st, const Kv4AttnArgs &a);
 

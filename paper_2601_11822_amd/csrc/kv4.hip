@@ -36,8 +36,17 @@ __device__ __forceinline__ uint32_t kv4_scale_byte(uint32_t amax_bits) {
     return amax_bits >= 0x7f80u ? 255u : (uint32_t)min(max(b, 2), 252);
 }
 __device__ __forceinline__ float kv4_scale(uint32_t byte) { return as_float(byte << 23); }   // (255: the conversions give NaN)
+// Byte I of four as a scale: one instruction (the compiler takes a shift and a mask).
 template <int I>
-__device__ __forceinline__ float kv4_scale_of(uint32_t four) { return as_float(((four >> (8 * I)) & 255u) << 23); }
+__device__ __forceinline__ float kv4_scale_of(uint32_t four) {
+    uint32_t r;
+    const uint32_t sh = 23;
+    if (I == 0) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_0" : "=v"(r) : "v"(sh), "v"(four));
+    if (I == 1) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_1" : "=v"(r) : "v"(sh), "v"(four));
+    if (I == 2) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_2" : "=v"(r) : "v"(sh), "v"(four));
+    if (I == 3) asm("v_lshlrev_b32_sdwa %0, %1, %2 dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:DWORD src1_sel:BYTE_3" : "=v"(r) : "v"(sh), "v"(four));
+    return as_float(r);
+}
 
 __device__ __forceinline__ uint32_t absmax2(uint32_t m, uint32_t two) {   // of bf16 magnitudes, as bits
     return max(m, max(two & 0x7fffu, (two >> 16) & 0x7fffu));
@@ -71,22 +80,19 @@ template <int HD> struct Kv4 {
 // A workgroup of 2 hd threads takes one (block, kv head) of one request: a thread 16 dims of one token's key (first half of the
 // threads) or value.  Bound by memory: 4 hd bytes of bf16 and 17/16 hd of cache a (token, head).
 struct RunBlock { int req, bi; };
-// The u-th block of the run of blocks that the requests' tokens touch.
-__device__ __forceinline__ RunBlock run_block(const SeqInfo &seq, int u) {
-    for (int r = 0; r < seq.n_req; ++r) {
-        const int len = seq.cu[r + 1] - seq.cu[r];
-        if (len <= 0) continue;
-        const int b0 = seq.start[r] >> 4, nb = ((seq.start[r] + len - 1) >> 4) - b0 + 1;
-        if (u < nb) return {r, b0 + u};
-        u -= nb;
-    }
-    return {-1, 0};
+// The u-th block of the run of blocks that the requests' tokens touch (u less than their number): every lane looks at one request.
+__device__ __forceinline__ RunBlock run_block(const Kv4RowsArgs &a, int u) {
+    const int lane = threadIdx.x & 63;
+    const unsigned long long before = __ballot(lane < a.seq.n_req && a.first[min(lane, RS_MAX_RUNS - 1)] <= u);
+    const int r = 63 - __builtin_clzll(before);   // (the last: empty runs begin where the next one does; first[0] is 0)
+    return {r, (a.seq.start[r] >> 4) + u - a.first[r]};
 }
-static int run_blocks(const SeqInfo &seq) {
+static int run_blocks(Kv4RowsArgs &a) {
     int n = 0;
-    for (int r = 0; r < seq.n_req; ++r) {
-        const int len = seq.cu[r + 1] - seq.cu[r];
-        if (len > 0) n += ((seq.start[r] + len - 1) >> 4) - (seq.start[r] >> 4) + 1;
+    for (int r = 0; r < a.seq.n_req; ++r) {
+        const int len = a.seq.cu[r + 1] - a.seq.cu[r];
+        a.first[r] = n;
+        if (len > 0) n += ((a.seq.start[r] + len - 1) >> 4) - (a.seq.start[r] >> 4) + 1;
     }
     return n;
 }
@@ -96,8 +102,7 @@ __global__ __launch_bounds__(2 * HD) void kv4_write_kernel(Kv4RowsArgs a) {
     using F = Kv4<HD>;
     __shared__ __attribute__((aligned(16))) uint8_t s_v[8 * HD];
     const int hk = blockIdx.x % a.Hkv, tid = threadIdx.x;
-    const RunBlock u = run_block(a.seq, blockIdx.x / a.Hkv);
-    if (u.req < 0) return;
+    const RunBlock u = run_block(a, blockIdx.x / a.Hkv);
     const int blk = a.tables[(size_t)u.req * a.max_blk + u.bi];
     if ((unsigned)blk >= (unsigned)a.n_blocks) {
         if (tid == 0 && hk == 0) atomicOr(a.err_flag, 2);
@@ -149,8 +154,7 @@ __global__ __launch_bounds__(2 * HD) void kv4_read_kernel(Kv4RowsArgs a) {
     using F = Kv4<HD>;
     __shared__ __attribute__((aligned(16))) uint8_t s_v[8 * HD];
     const int hk = blockIdx.x % a.Hkv, tid = threadIdx.x;
-    const RunBlock u = run_block(a.seq, blockIdx.x / a.Hkv);
-    if (u.req < 0) return;
+    const RunBlock u = run_block(a, blockIdx.x / a.Hkv);
     const int blk = a.tables[(size_t)u.req * a.max_blk + u.bi];
     const bool ok = (unsigned)blk < (unsigned)a.n_blocks;
     if (!ok && tid == 0 && hk == 0) atomicOr(a.err_flag, 2);
@@ -179,15 +183,17 @@ __global__ __launch_bounds__(2 * HD) void kv4_read_kernel(Kv4RowsArgs a) {
     *(u32x4_t *)(dst + 8) = kv4_values8(c[1], s);
 }
 
-void launch_kv4_write(hipStream_t st, const Kv4RowsArgs &a) {
-    const int n = run_blocks(a.seq);
+void launch_kv4_write(hipStream_t st, const Kv4RowsArgs &args) {
+    Kv4RowsArgs a = args;
+    const int n = run_blocks(a);
     if (n <= 0) return;
     if (a.hd == 128) hipLaunchKernelGGL(kv4_write_kernel<128>, dim3(a.Hkv * n), dim3(256), 0, st, a);
     else hipLaunchKernelGGL(kv4_write_kernel<64>, dim3(a.Hkv * n), dim3(128), 0, st, a);
 }
 
-void launch_kv4_read(hipStream_t st, const Kv4RowsArgs &a) {
-    const int n = run_blocks(a.seq);
+void launch_kv4_read(hipStream_t st, const Kv4RowsArgs &args) {
+    Kv4RowsArgs a = args;
+    const int n = run_blocks(a);
     if (n <= 0) return;
     if (a.hd == 128) hipLaunchKernelGGL(kv4_read_kernel<128>, dim3(a.Hkv * n), dim3(256), 0, st, a);
     else hipLaunchKernelGGL(kv4_read_kernel<64>, dim3(a.Hkv * n), dim3(128), 0, st, a);
@@ -255,20 +261,14 @@ __device__ __forceinline__ void q_split(const float *x, float mul, int *hi, int 
         lo[w] = r;
     }
 }
-__device__ __forceinline__ float absmax16(const float *x) {
-    float m = 0.f;
+__device__ __forceinline__ uint32_t absmax16(const float *x) {   // as bits: 0x7f800000 or more if one is not finite
+    uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m = fmaxf(m, fabsf(x[i]));
+    for (int i = 0; i < 16; ++i) m = max(m, as_bits(x[i]) & 0x7fffffffu);
     return m;
 }
-__device__ __forceinline__ bool all_finite16(const float *x) {
-    bool f = true;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) f = f && fabsf(x[i]) < __builtin_huge_valf();   // false for a NaN too
-    return f;
-}
 // Exponent field of the largest magnitude; 255 where it is not finite.
-__device__ __forceinline__ uint32_t q_exponent(float amax) { return min(max(as_bits(amax) >> 23, 12u), 255u); }
+__device__ __forceinline__ uint32_t q_exponent(uint32_t amax_bits) { return max(amax_bits >> 23, 12u); }
 __device__ __forceinline__ float q_mul(uint32_t e) { return as_float((261u - min(e, 254u)) << 23); }
 __device__ __forceinline__ int q_hi_scale(uint32_t e) { return e == 255u ? 255 : (int)e - 7; }
 __device__ __forceinline__ int q_lo_scale(uint32_t e) { return e == 255u ? 255 : (int)e - 11; }
@@ -299,35 +299,135 @@ __device__ __forceinline__ bf16_t *kv4_out(const Kv4AttnArgs &a, int row, int co
     return a.out_Mt ? a.out + packed_offset(a.out_row0 + row, col, a.out_Mt) + (col & 7) : a.out + (size_t)row * a.out_stride + col;
 }
 
+// ---- pieces of rows ---------------------------------------------------------------------------------------------------------
+// A row of one head that several workgroups compute leaves a piece each: the weighted sum of values, relative to the piece's own
+// maximum of raw scores, that maximum and the sum of weights.  A workgroup joins the pieces of the heads of one kv head of one
+// row, in order; a thread takes four dims.  Bound by round trips to memory: up to 8 pieces are asked for at once, whether the
+// row has them or not, beside its length; more in eights behind a pass over the maxima (64 rows of 3 chunks, 8B heads: 4.1 us, 32 rows of
+// 16 chunks 4.7; a launch that does nothing is 2).
+template <int HD>
+__global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
+    __shared__ float s[2 * 16];
+    const int row = blockIdx.y, G = a.Hq / a.Hkv, hq0 = blockIdx.x * G;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const float sc = a.scale_log2;
+    const size_t p0 = ((size_t)row * a.Hq + hq0) * a.n_chunks;
+    const float2 *ml = (const float2 *)a.part_ml + p0;
+    const f32x4 *po = (const f32x4 *)a.part_o + p0 * (HD / 4);
+    auto pieces = [&]() {   // of this row
+        return a.ctx_lens ? (min(max(__builtin_amdgcn_readfirstlane(a.ctx_lens[row]) + 1, 0), a.max_ctx) + a.chunk - 1) / a.chunk : a.n_chunks;
+    };
+    auto store = [&](int g, int d4, f32x4 acc, float l) {
+        bf16x4 w;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = (bf16_t)(l == 0.f ? 0.f : acc[j] / l);   // (0: an empty row, or every block of it refused)
+        *(bf16x4 *)kv4_out(a, row, (hq0 + g) * HD + 4 * d4) = w;
+    };
+    if (a.n_chunks <= 8) {
+        for (int i = tid; i < G * (HD / 4); i += 256) {
+            const int g = i / (HD / 4), d4 = i % (HD / 4);
+            f32x4 v[8];
+            float2 m[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const size_t c = (size_t)g * a.n_chunks + min(j, a.n_chunks - 1);
+                v[j] = po[c * (HD / 4) + d4];
+                m[j] = ml[c];
+            }
+            const int n = pieces();
+            float mx = NEG_INF, l = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) mx = fmaxf(mx, j < n ? m[j].x : NEG_INF);
+            const float ms = mx == NEG_INF ? 0.f : mx;
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (j < n) {
+                    const float e = __builtin_amdgcn_exp2f((m[j].x - ms) * sc);
+                    acc += v[j] * e;
+                    l += m[j].y * e;
+                }
+            store(g, d4, acc, l);
+        }
+        return;
+    }
+    const int n = pieces();
+    for (int g = wave; g < G; g += 4) {
+        const float2 *mg = ml + (size_t)g * a.n_chunks;
+        float mx = NEG_INF, l = 0.f;
+        for (int c = lane; c < n; c += 64) mx = fmaxf(mx, mg[c].x);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
+        const float ms = mx == NEG_INF ? 0.f : mx;
+        for (int c = lane; c < n; c += 64) {
+            const float2 v = mg[c];
+            l += v.y * __builtin_amdgcn_exp2f((v.x - ms) * sc);
+        }
+        l = wave_sum(l);
+        if (lane == 0) {
+            s[2 * g] = ms;
+            s[2 * g + 1] = l;
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < G * (HD / 4); i += 256) {
+        const int g = i / (HD / 4), d4 = i % (HD / 4);
+        const float ms = s[2 * g];
+        const f32x4 *pg = po + (size_t)g * a.n_chunks * (HD / 4) + d4;
+        const float2 *mg = ml + (size_t)g * a.n_chunks;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int c0 = 0; c0 < n; c0 += 8) {
+            f32x4 v[8];
+            float m[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int c = min(c0 + j, n - 1);
+                v[j] = pg[(size_t)c * (HD / 4)];
+                m[j] = mg[c].x;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c0 + j < n) acc += v[j] * __builtin_amdgcn_exp2f((m[j] - ms) * sc);
+        }
+        store(g, d4, acc, s[2 * g + 1]);
+    }
+}
+
+static void launch_kv4_merge(hipStream_t st, const Kv4AttnArgs &a, int rows) {
+    if (a.hd == 128) hipLaunchKernelGGL(kv4_merge_kernel<128>, dim3(a.Hkv, rows), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(kv4_merge_kernel<64>, dim3(a.Hkv, rows), dim3(256), 0, st, a);
+}
+
 // ---- attention: one row per request -----------------------------------------------------------------------------------------
 // Workgroup = (kv head, request, chunk of the context); its four waves take a quarter of the chunk's tokens each, 32 (two
 // blocks) at a time; the G query heads of the kv head are the columns of 16 x 16 tiles.  S^T = K Q^T, then O^T = V^T P^T: a
 // lane's eight scores (tokens 4h..4h+3 of both blocks) are the contraction slice that it supplies to the second product.
-template <int HD>
-__global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4AttnArgs a) {
+// The 4.25 KB of the next 32 tokens are asked for before the present ones are computed, from block ids that the wave holds.
+__device__ __forceinline__ float max_of_quarters(float v) {   // over the four lanes of a column
+    const auto x = __builtin_amdgcn_permlane16_swap(as_bits(v), as_bits(v), false, false);
+    v = fmaxf(as_float((uint32_t)x[0]), as_float((uint32_t)x[1]));
+    const auto y = __builtin_amdgcn_permlane32_swap(as_bits(v), as_bits(v), false, false);
+    return fmaxf(as_float((uint32_t)y[0]), as_float((uint32_t)y[1]));
+}
+
+template <int HD, int NW>
+__global__ __launch_bounds__(64 * NW, NW == 4 ? 3 : 2) void kv4_decode_kernel(Kv4AttnArgs a) {
     using F = Kv4<HD>;
-    constexpr int G = F::G;
+    constexpr int G = F::G, NT = 64 * NW;
+    typedef uint32_t gvec __attribute__((ext_vector_type(G)));
     extern __shared__ float smem_kv4[];
     const int hk = blockIdx.x, b = blockIdx.z, chunk = blockIdx.y;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c16 = lane & 15, h = lane >> 4;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c16 = lane & 15, h = lane >> 4;
     const int Gq = a.Hq / a.Hkv;
-    float *s_o = smem_kv4;               // [4][HD][Gq]
-    float *s_m = smem_kv4 + 4 * HD * Gq; // [4][Gq] maxima, [4][Gq] sums
-    float *s_l = s_m + 4 * Gq;
+    float *s_o = smem_kv4;                // [NW][HD][Gq]
+    float *s_m = smem_kv4 + NW * HD * Gq; // [NW][Gq] maxima, [NW][Gq] sums
+    float *s_l = s_m + NW * Gq;
 
-    int n_keys = a.ctx_lens[b] + 1;
-    if (n_keys < 0 || n_keys > a.max_ctx) {
-        if (tid == 0 && chunk == 0 && hk == 0) atomicOr(a.err_flag, 8);
-        n_keys = min(max(n_keys, 0), a.max_ctx);
-    }
-    if (n_keys == 0) {   // a row without a request
-        if (a.n_chunks == 1)
-            for (int c = tid * 8; c < Gq * HD; c += 2048) *(u32x4_t *)kv4_out(a, b, hk * Gq * HD + c) = u32x4_t{0, 0, 0, 0};
-        return;
-    }
-    if (chunk * a.chunk >= n_keys) return;
-    const int per_wave = a.chunk / 4;
-    const int t0 = chunk * a.chunk + wave * per_wave, t1 = min(t0 + per_wave, n_keys);
+    const int per_wave = a.chunk / NW;    // at most 1024 tokens: a lane holds a block id
+    const int t0 = chunk * a.chunk + wave * per_wave;
+    // asked for beside the length, not after it (within the table: it may end before the chunk does)
+    int my_blk = lane < per_wave / 16 ? a.tables[(size_t)b * a.max_blk + min((t0 >> 4) + lane, a.max_blk - 1)] : -1;
+    int n_keys = __builtin_amdgcn_readfirstlane(a.ctx_lens[b]) + 1;
 
     // the query's terms: bytes 0-15 of a lane's operand are dims 16h.., bytes 16-31 dims 64 + 16h..
     i32x8 qh, ql;
@@ -351,9 +451,9 @@ __global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4AttnArgs a) {
             if (!col)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) x[p][i] = 0.f;
-            uint32_t mine = all_finite16(x[p]) ? as_bits(absmax16(x[p])) : 0x7f800000u;
+            uint32_t mine = absmax16(x[p]);
             mine = max(mine, (uint32_t)__shfl_xor((int)mine, 16, 64));
-            e[p] = q_exponent(as_float(mine));
+            e[p] = q_exponent(mine);
             q_split(x[p], q_mul(e[p]), hi + 4 * p, lo + 4 * p);
         }
 #pragma unroll
@@ -368,56 +468,78 @@ __global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4AttnArgs a) {
         ql_scale = q_lo_scale(mine);
     }
 
+    if (n_keys < 0 || n_keys > a.max_ctx) {
+        if (tid == 0 && chunk == 0 && hk == 0) atomicOr(a.err_flag, 8);
+        n_keys = min(max(n_keys, 0), a.max_ctx);
+    }
+    if (n_keys == 0) {   // a row without a request
+        if (a.n_chunks == 1)
+            for (int c = tid * 8; c < Gq * HD; c += 8 * NT) *(u32x4_t *)kv4_out(a, b, hk * Gq * HD + c) = u32x4_t{0, 0, 0, 0};
+        return;
+    }
+    if (chunk * a.chunk >= n_keys) return;
+    const int t1 = min(t0 + per_wave, n_keys);
+    if (t0 + 16 * lane >= t1) my_blk = -1;
+    else if ((unsigned)my_blk >= (unsigned)a.n_blocks) {
+        atomicOr(a.err_flag, 2);
+        my_blk = -1;
+    }
+
     float m_run = NEG_INF, l_run = 0.f;
     f32x4 o[2 * G];   // (group, parity of the dim)
 #pragma unroll
     for (int i = 0; i < 2 * G; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float sc = a.scale_log2;
-    const int32_t *tab = a.tables + (size_t)b * a.max_blk;
     const uint8_t *head = a.pool + (size_t)hk * F::BYTES;
     const size_t blk_stride = (size_t)a.Hkv * F::BYTES;
+    const uint32_t off_k = F::k_chunk(h & (G - 1), c16), off_ks = F::k_scale(h & (G - 1), c16), off_v = F::V + (h * 16 + c16) * (4 * G), off_vs = F::VS + h * (4 * G);
 
-    for (int base = t0; base < t1; base += 32) {
+    struct Buf {
         u32x4_t kc[2];
-        typedef uint32_t gvec __attribute__((ext_vector_type(G)));
         uint32_t ks[2];
         gvec vc[2], vs[2];
-        bool ok[2];
+    };
+    const int nit = t1 > t0 ? (t1 - t0 + 31) >> 5 : 0;   // the wave's
+    // (always loads, the last tokens again at the end: after a load under a branch, or a way out of the loop between its two halves,
+    // the compiler waits for all loads in flight, not for the older ones)
+    auto issue = [&](int it, Buf &f) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int tok = base + 16 * u;
-            int blk = tok < n_keys ? tab[tok >> 4] : -1;
-            ok[u] = (unsigned)blk < (unsigned)a.n_blocks;
-            if (tok < n_keys && !ok[u] && lane == 0) atomicOr(a.err_flag, 2);
-            const uint8_t *p = head + (size_t)(ok[u] ? blk : 0) * blk_stride;
-            kc[u] = *(const u32x4_t *)(p + F::k_chunk(h & (G - 1), c16));
-            ks[u] = p[F::k_scale(h & (G - 1), c16)];
-            vc[u] = *(const gvec *)(p + F::V + (h * 16 + c16) * (4 * G));
-            vs[u] = *(const gvec *)(p + F::VS + h * (4 * G));
+            const int blk = __builtin_amdgcn_readlane(my_blk, 2 * it + u);
+            const uint8_t *p = head + (size_t)max(blk, 0) * blk_stride;   // a missing block: memory of the pool, masked out
+            f.kc[u] = __builtin_nontemporal_load((const u32x4_t *)(p + off_k));
+            f.vc[u] = __builtin_nontemporal_load((const gvec *)(p + off_v));
+            f.ks[u] = p[off_ks];
+            f.vs[u] = *(const gvec *)(p + off_vs);
         }
+    };
+    auto compute = [&](int it, Buf &f) {
+        const int base = t0 + 32 * it;
+        const int b0 = __builtin_amdgcn_readlane(my_blk, 2 * it), b1 = __builtin_amdgcn_readlane(my_blk, 2 * it + 1);
         f32x4 s[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const i32x8 k = {(int)kc[u][0], (int)kc[u][1], (int)kc[u][2], (int)kc[u][3], 0, 0, 0, 0};
+            const i32x8 k = {(int)f.kc[u][0], (int)f.kc[u][1], (int)f.kc[u][2], (int)f.kc[u][3], 0, 0, 0, 0};
             s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, ql, s[u], 4, 0, 0, (int)ks[u], 0, ql_scale);
-            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, qh, s[u], 4, 0, 0, (int)ks[u], 0, qh_scale);
-            const int nv = ok[u] ? min(max(n_keys - (base + 16 * u + 4 * h), 0), 4) : 0;   // valid tokens of this lane's four
-            if (nv < 4) {
+            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, ql, s[u], 4, 0, 0, (int)f.ks[u], 0, ql_scale);
+            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, qh, s[u], 4, 0, 0, (int)f.ks[u], 0, qh_scale);
+        }
+        if (!(base + 32 <= t1 && b0 >= 0 && b1 >= 0)) {   // uniform
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int nv = (u ? b1 : b0) >= 0 ? min(max(t1 - (base + 16 * u + 4 * h), 0), 4) : 0;   // valid tokens of this lane's four
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (i >= nv) s[u][i] = NEG_INF;
                 const uint32_t keep = nv == 0 ? 0u : 0xffffffffu >> (32 - 8 * nv);
 #pragma unroll
-                for (int g = 0; g < G; ++g) vs[u][g] &= keep;   // what is behind the context may read as NaN
+                for (int g = 0; g < G; ++g) f.vs[u][g] &= keep;   // what is behind the context may read as NaN
             }
         }
-        float m_tile = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-        m_tile = fmaxf(m_tile, __shfl_xor(m_tile, 16, 64));
-        m_tile = fmaxf(m_tile, __shfl_xor(m_tile, 32, 64));
+        const float m_tile = max_of_quarters(fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))));
         const float m_new = fmaxf(m_run, m_tile), m_safe = m_new == NEG_INF ? 0.f : m_new;
         const float ms = m_safe * sc;
-        bf16x8 pf;   // the weights are rounded to bf16 for the second product (at most 2^-9 each); their sum is of the unrounded ones
+        bf16x8 pf;   // the weights are rounded to bf16 for the second product (at most 2^-8 each); their sum is of the unrounded ones
         float psum = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -435,15 +557,29 @@ __global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4AttnArgs a) {
         l_run += psum;
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            const V4 va = v_values(vc[0][g], vs[0][g]), vb = v_values(vc[1][g], vs[1][g]);
+            const V4 va = v_values(f.vc[0][g], f.vs[0][g]), vb = v_values(f.vc[1][g], f.vs[1][g]);
             o[2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join8(va.even, vb.even), pf, o[2 * g], 0, 0, 0);
             o[2 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join8(va.odd, vb.odd), pf, o[2 * g + 1], 0, 0, 0);
+        }
+    };
+    if (nit > 0) {
+        Buf x, y;
+        issue(0, x);
+        for (int it = 0; it < nit; it += 2) {
+            issue(min(it + 1, nit - 1), y);
+            __builtin_amdgcn_sched_barrier(0);
+            compute(it, x);
+            __builtin_amdgcn_sched_barrier(0);
+            issue(min(it + 2, nit - 1), x);
+            __builtin_amdgcn_sched_barrier(0);
+            if (it + 1 < nit) compute(it + 1, y);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
     l_run += __shfl_xor(l_run, 16, 64);
     l_run += __shfl_xor(l_run, 32, 64);
 
-    // the four waves, in order
+    // the waves, in order
     if (c16 < Gq) {
 #pragma unroll
         for (int g = 0; g < G; ++g)
@@ -458,12 +594,15 @@ __global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4AttnArgs a) {
         }
     }
     __syncthreads();
-    for (int idx = tid; idx < Gq * HD; idx += 256) {
+    for (int idx = tid; idx < Gq * HD; idx += NT) {
         const int gg = idx / HD, d = idx % HD;
-        const float mx = fmaxf(fmaxf(s_m[gg], s_m[Gq + gg]), fmaxf(s_m[2 * Gq + gg], s_m[3 * Gq + gg])), ms = mx == NEG_INF ? 0.f : mx;
+        float mx = NEG_INF;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) mx = fmaxf(mx, s_m[w * Gq + gg]);
+        const float ms = mx == NEG_INF ? 0.f : mx;
         float acc = 0.f, l = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < NW; ++w) {
             const float e = __builtin_amdgcn_exp2f((s_m[w * Gq + gg] - ms) * sc);
             acc += s_o[(w * HD + d) * Gq + gg] * e;
             l += s_l[w * Gq + gg] * e;
@@ -481,51 +620,55 @@ __global__ __launch_bounds__(256, 2) void kv4_decode_kernel(Kv4AttnArgs a) {
     }
 }
 
-// The pieces of a row (chunks of its context, or key ranges of a prompt's row), in order.  n: pieces of this row.
-template <int HD>
-__global__ __launch_bounds__(HD) void kv4_merge_kernel(Kv4AttnArgs a) {
-    const int hq = blockIdx.x, row = blockIdx.y, d = threadIdx.x;
-    int n = a.n_chunks;
-    if (a.ctx_lens) {
-        const int keys = min(max(a.ctx_lens[row] + 1, 0), a.max_ctx);
-        n = (keys + a.chunk - 1) / a.chunk;
+// How the rows of a decode launch are cut, from the sizes alone (pairs: rows times kv heads): tokens of a chunk and waves of its
+// workgroup.  A compute unit loads 57 GB/s, 2.4 us for 1024 tokens of 128 dims; pieces cost a launch of their own, 3 us and more:
+// whole contexts in one workgroup while that is the lesser, or while the pairs fill the chip by themselves.  Of eight waves where
+// they are no more than one a unit.  us a pass, 8B heads:
+//   1 row of 900 tokens: whole, 8 waves / 4 waves 8.1 / 8.7, in chunks of 256 8.9;  of 2000: 11.8 / 13.3, 9.0
+//   32 rows of 500 to 2000: 12.4 / 14.0, chunks of 1024 16.3;  32 of 1000 to 4000: 19.6 / 23.5, chunks of 2048 23.8
+//   128 rows of 250 to 1000: 29.9 / 21.9, chunks of 512 29.8;  203 rows of 1 to 1500, 4 heads of 64: whole 17.0, chunks of 1024 26.0
+// Chunks: the shortest of 256 .. that make 512 workgroups at most and 32 pieces a row, up to 1024 tokens, 2048 of contexts beyond 4096.
+//   1 row of 4000 / 32000 tokens in chunks of 256, 512, 1024, 2048: 9.5, 10.2, 12.5, 15.9 / 25, 16.3, 14.4, 18.0
+//   16 rows of 2000 to 8000: 512 26.1, 1024 25.4, 2048 23.6, 4096 27.5;  128 of 750 to 3000: 512 68.0, 1024 57.5, 2048 69.1, whole 62.8
+//   32 rows of 8192 to 32767: 1024 141, 2048 128, 4096 128
+Kv4Cut kv4_cut(int64_t pairs, int max_ctx) {
+    const int whole = pairs < 128 ? 1024 : pairs <= 256 ? 4096 : 2048;
+    if (max_ctx <= whole) {
+        const int waves = pairs <= 256 ? 8 : 4;
+        return {(max_ctx + 32 * waves - 1) / (32 * waves) * (32 * waves), waves};
     }
-    const size_t p0 = ((size_t)row * a.Hq + hq) * a.n_chunks;
-    float mx = NEG_INF;
-    for (int c = 0; c < n; ++c) mx = fmaxf(mx, a.part_ml[2 * (p0 + c)]);
-    const float ms = mx == NEG_INF ? 0.f : mx;
-    float acc = 0.f, l = 0.f;
-    for (int c = 0; c < n; ++c) {
-        const float e = __builtin_amdgcn_exp2f((a.part_ml[2 * (p0 + c)] - ms) * a.scale_log2);
-        acc += a.part_o[(p0 + c) * HD + d] * e;
-        l += a.part_ml[2 * (p0 + c) + 1] * e;
-    }
-    *kv4_out(a, row, hq * HD + d) = (bf16_t)(l == 0.f ? 0.f : acc / l);
+    const int cap = max_ctx <= 4096 ? 1024 : 2048;
+    int c = 256;
+    while (c < cap && (pairs * ((max_ctx + c - 1) / c) > 512 || (max_ctx + c - 1) / c > 32)) c *= 2;
+    return {c, 4};
 }
+// Most pieces, over all contexts up to max_ctx.
+int64_t kv4_most_pieces(int64_t pairs, int max_ctx) { return std::max<int64_t>(512, pairs * std::max(4, (max_ctx + 2047) / 2048)); }
 
-static void launch_kv4_merge(hipStream_t st, const Kv4AttnArgs &a, int rows) {
-    if (a.hd == 128) hipLaunchKernelGGL(kv4_merge_kernel<128>, dim3(a.Hq, rows), dim3(128), 0, st, a);
-    else hipLaunchKernelGGL(kv4_merge_kernel<64>, dim3(a.Hq, rows), dim3(64), 0, st, a);
-}
-
-// Tokens of a chunk: 512, fewer where the launch would not give every compute unit two workgroups.  From the sizes alone.
-int kv4_chunk(int B, int Hkv, int max_ctx) {
-    int c = 512;
-    while (c > 128 && (int64_t)B * Hkv * ((max_ctx + c - 1) / c) < 512) c /= 2;
-    return c;
+template <int HD, int NW>
+static void launch_kv4_decode_form(hipStream_t st, const Kv4AttnArgs &a) {
+    const int Gq = a.Hq / a.Hkv;
+    hipLaunchKernelGGL((kv4_decode_kernel<HD, NW>), dim3(a.Hkv, a.n_chunks, a.B), dim3(64 * NW), (size_t)(NW * HD * Gq + 2 * NW * Gq) * sizeof(float), st, a);
 }
 
 void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &args) {
     Kv4AttnArgs a = args;
     if (a.B <= 0) return;
-    a.chunk = kv4_chunk(a.B, a.Hkv, a.max_ctx);
+    const Kv4Cut cut = kv4_cut((int64_t)a.B * a.Hkv, a.max_ctx);
+    a.chunk = cut.chunk;
     a.n_chunks = (a.max_ctx + a.chunk - 1) / a.chunk;
-    const int Gq = a.Hq / a.Hkv;
-    const size_t lds = (size_t)(4 * a.hd * Gq + 8 * Gq) * sizeof(float);
-    const dim3 grid(a.Hkv, a.n_chunks, a.B);
-    if (a.hd == 128) hipLaunchKernelGGL(kv4_decode_kernel<128>, grid, dim3(256), lds, st, a);
-    else hipLaunchKernelGGL(kv4_decode_kernel<64>, grid, dim3(256), lds, st, a);
+    if (cut.waves == 8) {
+        if (a.hd == 128) launch_kv4_decode_form<128, 8>(st, a);
+        else launch_kv4_decode_form<64, 8>(st, a);
+    } else {
+        if (a.hd == 128) launch_kv4_decode_form<128, 4>(st, a);
+        else launch_kv4_decode_form<64, 4>(st, a);
+    }
     if (a.n_chunks > 1) launch_kv4_merge(st, a, a.B);
+}
+
+void kv4_kernels_init() {
+    (void)hipFuncSetAttribute((const void *)kv4_decode_kernel<128, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * (128 + 2) * 16 * 4);
 }
 
 // ---- attention: prompts and chunks of them ----------------------------------------------------------------------------------
@@ -548,7 +691,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
     constexpr int G = F::G, KSTEP = HD / 64, DT = HD / 32;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem_kv4p[];
     const int hk = blockIdx.x % a.Hkv, split = blockIdx.y, Gq = a.Hq / a.Hkv;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, c32 = lane & 31, h = lane >> 5;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c32 = lane & 31, h = lane >> 5;
 
     int unit = blockIdx.x / a.Hkv, req = 0, units = 0;
     for (; req < a.seq.n_req; ++req) {
@@ -582,9 +725,9 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
                 load16(qp + 64 * s + 32 * p, x[p]);
-                uint32_t mine = all_finite16(x[p]) ? as_bits(absmax16(x[p])) : 0x7f800000u;
+                uint32_t mine = absmax16(x[p]);
                 mine = max(mine, (uint32_t)__shfl_xor((int)mine, 32, 64));
-                e[p] = q_exponent(as_float(mine));
+                e[p] = q_exponent(mine);
                 q_split(x[p], q_mul(e[p]), hi + 4 * p, lo + 4 * p);
             }
 #pragma unroll

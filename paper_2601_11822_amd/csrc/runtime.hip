@@ -1001,13 +1001,11 @@ struct OnDevice {
     }
 };
 
-// Rows of partial results that a side's attention can need, as (row, query head) pieces: the split launches' of prompts, and of
-// `rows` decode rows in chunks (a launch with chunks of less than 512 tokens has less than 1024 of them).
+// (row, query head) pieces that a side's attention can leave: the split launches of prompts, and those of `rows` decode rows.
 size_t kv4_pieces(const rs_ctx *c, bool prefill, int rows) {
     const rs_model_desc &m = c->m;
-    const size_t chunks = ((size_t)c->lim.max_context + RS_DECODE_CHUNK - 1) / RS_DECODE_CHUNK;
     size_t n = prefill ? (size_t)KV4_SPLIT_WGS * 128 : 0;
-    if (rows > 0) n = std::max(n, std::max<size_t>((size_t)rows * m.n_kv_heads * chunks, 1024) * (m.n_q_heads / m.n_kv_heads));
+    if (rows > 0) n = std::max(n, (size_t)kv4_most_pieces((int64_t)rows * m.n_kv_heads, c->lim.max_context) * (m.n_q_heads / m.n_kv_heads));
     return n;
 }
 
@@ -1196,6 +1194,7 @@ static int32_t init_ctx(const rs_model_desc *model, const rs_pool_desc *pool, co
         gemm_kernels_init();
         decode_gemm_kernels_init();
         attention_kernels_init();
+        kv4_kernels_init();
         // rotary table, angles in float64
         const int half = m.head_dim / 2;
         std::vector<CosSin> tab((size_t)m.max_pos * half);
