@@ -13,6 +13,7 @@
 // lane's share of V (4 tokens of a dim pair in every group) is another.  Both halves of a byte belong to one token, so tokens
 // can be appended one by one by anybody without reading what is there.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -283,14 +284,17 @@ __device__ __forceinline__ void load16(const bf16_t *p, float *x) {
 }
 
 // Four tokens of a dim pair (a dword of codes, a dword of scale bytes) -> the even dim's four values and the odd dim's.
-struct V4 { u32x2_t even, odd; };
+struct V4 {
+    u32x2_t even, odd;
+    uint32_t top;   // the largest of the scales, as bits: 0x7f800000 where one is 255
+};
 __device__ __forceinline__ V4 v_values(uint32_t codes, uint32_t scales) {
-    const uint32_t x0 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, kv4_scale_of<0>(scales), 0));
-    const uint32_t x1 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, kv4_scale_of<1>(scales), 1));
-    const uint32_t x2 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, kv4_scale_of<2>(scales), 2));
-    const uint32_t x3 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, kv4_scale_of<3>(scales), 3));
+    const float s0 = kv4_scale_of<0>(scales), s1 = kv4_scale_of<1>(scales), s2 = kv4_scale_of<2>(scales), s3 = kv4_scale_of<3>(scales);
+    const uint32_t x0 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s0, 0)), x1 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s1, 1));
+    const uint32_t x2 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s2, 2)), x3 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s3, 3));
     return {u32x2_t{__builtin_amdgcn_perm(x1, x0, 0x05040100u), __builtin_amdgcn_perm(x3, x2, 0x05040100u)},
-            u32x2_t{__builtin_amdgcn_perm(x1, x0, 0x07060302u), __builtin_amdgcn_perm(x3, x2, 0x07060302u)}};
+            u32x2_t{__builtin_amdgcn_perm(x1, x0, 0x07060302u), __builtin_amdgcn_perm(x3, x2, 0x07060302u)},
+            max(max(max(as_bits(s0), as_bits(s1)), as_bits(s2)), as_bits(s3))};
 }
 __device__ __forceinline__ bf16x8 join8(u32x2_t a, u32x2_t b) { return __builtin_bit_cast(bf16x8, u32x4_t{a[0], a[1], b[0], b[1]}); }
 
@@ -706,7 +710,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
     const bool valid = col < n_cols;
     const int colc = min(col, n_cols - 1), row = colc / Gq, hq = hk * Gq + colc % Gq;
     const int q_pos = prior + row;
-    const int w_min = prior + min(col0 + 32 * wave, n_cols - 1) / Gq, w_max = prior + min(col0 + 32 * wave + 31, n_cols - 1) / Gq;
+    const int w_min = prior + min(col0 + 32 * wave, n_cols - 1) / Gq;
     const int kv_end = prior + min(col0 + KV4_COLS - 1, n_cols - 1) / Gq + 1;
     const int n_tiles = (kv_end + 63) >> 6;
     // this workgroup's share of the key tiles
@@ -754,126 +758,190 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
     // and 2 + v_half, dim pair vj, UG groups from vg on), and the lanes of the first HD/8 bytes of K's scales.
     constexpr int UG = G / 2;   // groups of a lane's V unit
     const int vj = lane & 15, vg = ((lane >> 4) & 1) * UG, v_half = lane >> 5;
-    // A value that is not finite must not reach the rows before it, whose weight of it is zero: where a scale of V says so, the
-    // token's scores are made NaN instead, which only the rows that see it take.
     typedef uint32_t kvec __attribute__((ext_vector_type(HD / 32)));
     typedef uint32_t vvec __attribute__((ext_vector_type(UG)));
     kvec rk;
-    uint32_t rks = 0;
+    uint32_t rks;
     vvec rv[2], rs[2];
-    auto fetch = [&](int kt) {
-        const int tok0 = kt * 64 + 16 * wave;
-        const int blk = tok0 < kv_end ? tab[tok0 >> 4] : -1;
-        const bool ok = (unsigned)blk < (unsigned)a.n_blocks;
-        if (tok0 < kv_end && !ok && lane == 0) atomicOr(a.err_flag, 2);
-        const uint8_t *p = a.pool + ((size_t)(ok ? blk : 0) * a.Hkv + hk) * F::BYTES;
-        rk = ((const kvec *)p)[lane];
-        if (lane < HD / 8) rks = ok ? ((const uint32_t *)(p + F::KS))[lane] : 0;
+    bool r_ok = true;      // whether the block of what was fetched is one of the pool
+    int next_blk = 0;      // block of the tile to fetch next, asked for a tile ahead
+    auto block_at = [&](int kt) { return tab[min(kt * 4 + wave, (kv_end - 1) >> 4)]; };   // (behind the context: its last one, which nobody looks at)
+    auto fetch = [&](int kt) {   // and asks for the block id of the tile after it
+        const int blk = __builtin_amdgcn_readfirstlane(next_blk);
+        r_ok = (unsigned)blk < (unsigned)a.n_blocks;
+        const uint8_t *p = a.pool + ((size_t)(r_ok ? blk : 0) * a.Hkv + hk) * F::BYTES;
+        rk = *(const kvec *)(p + (uint32_t)(lane * (HD / 8)));
+        rks = *(const uint32_t *)(p + (uint32_t)(F::KS + 4 * (lane & (HD / 8 - 1))));
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int q = v_half + 2 * u;
-            rv[u] = *(const vvec *)(p + F::V + ((q * 16 + vj) * G + vg) * 4);
-            rs[u] = *(const vvec *)(p + F::VS + (q * G + vg) * 4);
-            const int nv = ok ? min(max(kv_end - (tok0 + 4 * q), 0), 4) : 0;   // (what is behind the context may read as NaN)
-            const uint32_t keep = nv == 0 ? 0u : 0xffffffffu >> (32 - 8 * nv);
-#pragma unroll
-            for (int g = 0; g < UG; ++g) rs[u][g] &= keep;
+            rv[u] = *(const vvec *)(p + (uint32_t)(F::V + (((v_half + 2 * u) * 16 + vj) * G + vg) * 4));
+            rs[u] = *(const vvec *)(p + (uint32_t)(F::VS + ((v_half + 2 * u) * G + vg) * 4));
         }
+        next_blk = block_at(min(kt + 1, kt1 - 1));
     };
-    auto put = [&](int buf) {
-        uint8_t *t = smem_kv4p + buf * L::TILE;
-        ((kvec *)(t + wave * (8 * HD)))[lane] = rk;
+    auto refuse = [&]() {   // a block that is none: small scores, no values
+        if (r_ok) return;
+        if (lane == 0) atomicOr(a.err_flag, 2);
+        rks = 0;
+        rs[0] = rs[1] = 0;
+    };
+    // What was fetched goes to LDS in parts, which the first product's instructions lie between: K; then of each group the values
+    // of two quads and their stores.  (No branch among them: what the products give is used behind it, and the compiler would move
+    // them there.)
+    constexpr int PARTS = 1 + 3 * UG;
+    V4 px, py;
+    uint32_t top = 0;
+    auto put = [&](int part, uint8_t *t) {
         uint8_t *scales = t + L::K + wave * (HD / 2);
-        if (lane < HD / 8) ((uint32_t *)scales)[lane] = rks;
-        uint32_t bad[2] = {0, 0};   // bytes of 255
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int g = 0; g < UG; ++g) bad[u] |= ((rs[u][g] & 0x7f7f7f7fu) + 0x01010101u) & rs[u][g] & 0x80808080u;
-        if (__any((bad[0] | bad[1]) != 0)) {
-            for (int u = 0; u < 2; ++u) {
-                const uint32_t ff = (bad[u] >> 7) * 255u;
-#pragma unroll
-                for (int g = 0; g < UG; ++g) rs[u][g] &= ~ff;
-                for (int i = 0; i < 4; ++i)
-                    if ((ff >> (8 * i)) & 1) scales[4 * (v_half + 2 * u) + i] = 255;   // of group 0, after the wave's own store above
+        bf16x8 *v = (bf16x8 *)(t + L::K + L::KS) + (wave * 2 + v_half) * HD + 32 * vg + vj;
+        if (part == 0) {
+            *(kvec *)(t + wave * (8 * HD) + lane * (HD / 8)) = rk;
+            ((uint32_t *)scales)[lane & (HD / 8 - 1)] = rks;
+            top = 0;
+        } else {
+            const int g = (part - 1) / 3, what = (part - 1) % 3;
+            if (what == 0) {
+                px = v_values(rv[0][g], rs[0][g]);
+            } else if (what == 1) {
+                py = v_values(rv[1][g], rs[1][g]);
+            } else {
+                top = max(max(top, px.top), py.top);
+                v[32 * g] = join8(px.even, py.even);
+                v[32 * g + 16] = join8(px.odd, py.odd);
             }
         }
-        bf16x8 *v = (bf16x8 *)(t + L::K + L::KS) + (wave * 2 + v_half) * HD;
+    };
+    // A value that is not finite must not reach the rows before it, whose weight of it is zero: the token's scores are made NaN
+    // instead, which only the rows that see it take.
+    auto put_nan = [&](uint8_t *t) {
+        if (!__any(top >= 0x7f800000u)) return;
+        uint8_t *scales = t + L::K + wave * (HD / 2);
+        bf16x8 *v = (bf16x8 *)(t + L::K + L::KS) + (wave * 2 + v_half) * HD + 32 * vg + vj;
+        for (int u = 0; u < 2; ++u) {
+            uint32_t ff = 0;   // bytes of 255
+#pragma unroll
+            for (int g = 0; g < UG; ++g) ff |= ((rs[u][g] & 0x7f7f7f7fu) + 0x01010101u) & rs[u][g] & 0x80808080u;
+            ff = (ff >> 7) * 255u;
+            rs[u] &= ~ff;
+            for (int i = 0; i < 4; ++i)
+                if ((ff >> (8 * i)) & 1) scales[4 * (v_half + 2 * u) + i] = 255;   // of group 0, behind the wave's own store above
+        }
 #pragma unroll
         for (int g = 0; g < UG; ++g) {
             const V4 x = v_values(rv[0][g], rs[0][g]), y = v_values(rv[1][g], rs[1][g]);
-            v[32 * (vg + g) + vj] = join8(x.even, y.even);
-            v[32 * (vg + g) + 16 + vj] = join8(x.odd, y.odd);
+            v[32 * g] = join8(x.even, y.even);
+            v[32 * g + 16] = join8(x.odd, y.odd);
         }
     };
 
-    if (kt0 < kt1) {
-        fetch(kt0);
-        put(0);
-    }
-    __syncthreads();
-    for (int kt = kt0; kt < kt1; ++kt) {
-        if (kt + 1 < kt1) fetch(kt + 1);
+    // A key tile: the tile in buffer B is used while the next one, which is in registers, goes to the other buffer and the one
+    // after that is fetched.  The order of instructions is written out: with two waves a SIMD the matrix unit idles whenever both
+    // wait for vector work at a time.
+    const int k_base = (c32 >> 4) * (8 * HD) + F::k_chunk(h, c32 & 15), s_base = (c32 >> 4) * (HD / 2) + h * 16 + (c32 & 15), v_base = (h * HD + c32) * 16;
+    auto tile = [&](int kt, auto btag) {
+        constexpr int B = decltype(btag)::value;
+        uint8_t *t = smem_kv4p + B * L::TILE, *other = smem_kv4p + (1 - B) * L::TILE;
         const int kv0 = kt * 64;
-        const uint8_t *t = smem_kv4p + ((kt - kt0) & 1) * L::TILE;
-        if (kv0 <= w_max) {
-            f32x16 st[2];
+        refuse();
+        u32x4_t kc[2][KSTEP];
+        int ks[2][KSTEP];
+#pragma unroll
+        for (int s = 0; s < KSTEP; ++s)
 #pragma unroll
             for (int t2 = 0; t2 < 2; ++t2) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) st[t2][i] = 0.f;
-                const int blk = 2 * t2 + (c32 >> 4), tok = c32 & 15;
-#pragma unroll
-                for (int s = 0; s < KSTEP; ++s) {
-                    const u32x4_t kc = *(const u32x4_t *)(t + blk * (8 * HD) + F::k_chunk(2 * s + h, tok));
-                    const int ks = t[L::K + blk * (HD / 2) + (2 * s + h) * 16 + tok];
-                    const i32x8 k = {(int)kc[0], (int)kc[1], (int)kc[2], (int)kc[3], 0, 0, 0, 0};
-                    st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, ql[s], st[t2], 4, 0, 0, ks, 0, qls[s]);
-                    st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, qh[s], st[t2], 4, 0, 0, ks, 0, qhs[s]);
-                }
+                kc[t2][s] = *(const u32x4_t *)(t + k_base + t2 * (16 * HD) + s * 512);
+                ks[t2][s] = t[s_base + L::K + t2 * HD + s * 32];
             }
-            if (kv0 + 63 > w_min) {   // only tiles that touch the diagonal need the mask
+        f32x16 st[2];
 #pragma unroll
-                for (int t2 = 0; t2 < 2; ++t2)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (kv0 + 32 * t2 + (i >> 2) * 8 + 4 * h + (i & 3) > q_pos) st[t2][i] = NEG_INF;
+        for (int i = 0; i < 4 * KSTEP; ++i) {   // the two score tiles in turn
+            const int t2 = i & 1, s = i >> 2;
+            const i32x8 k = {(int)kc[t2][s][0], (int)kc[t2][s][1], (int)kc[t2][s][2], (int)kc[t2][s][3], 0, 0, 0, 0};
+            if (i < 2) {
+                const f32x16 zero = {};
+                st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, ql[s], zero, 4, 0, 0, ks[t2][s], 0, qls[s]);
+            } else {
+                st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, i & 2 ? qh[s] : ql[s], st[t2], 4, 0, 0, ks[t2][s], 0, i & 2 ? qhs[s] : qls[s]);
             }
-            float m_tile = NEG_INF;
+            __builtin_amdgcn_sched_barrier(0);
+            if (i < PARTS) put(i, other);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        asm volatile("" : "+v"(st[0]), "+v"(st[1]));   // the products stay in front of the branch
+        put_nan(other);
+        fetch(min(kt + 2, kt1 - 1));
+        if (kv0 + 63 > w_min) {   // only tiles that touch the diagonal need the mask
 #pragma unroll
             for (int t2 = 0; t2 < 2; ++t2)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) m_tile = fmaxf(m_tile, st[t2][i]);
-            {
-                const auto sw = __builtin_amdgcn_permlane32_swap(as_bits(m_tile), as_bits(m_tile), false, false);
-                m_tile = fmaxf(as_float((uint32_t)sw[0]), as_float((uint32_t)sw[1]));
-            }
-            const float m_new = fmaxf(m_run, m_tile), m_safe = m_new == NEG_INF ? 0.f : m_new;
-            if (__any(m_new != m_run)) {
-                const float alpha = __builtin_amdgcn_exp2f((m_run - m_safe) * sc);
-                l_run *= alpha;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[dt] = o[dt] * alpha;
-                m_run = m_new;
-            }
-            const float ms = m_safe * sc;
-            const bf16x8 *v = (const bf16x8 *)(t + L::K + L::KS);
-#pragma unroll
-            for (int b4 = 0; b4 < 4; ++b4) {
-                bf16x8 pf;   // rounded to bf16 for the product; the sum is of the unrounded weights
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(st[b4 >> 1][8 * (b4 & 1) + i], sc, -ms));
-                    l_run += p;
-                    pf[i] = (bf16_t)p;
-                }
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[(b4 * 2 + h) * HD + 32 * dt + c32], pf, o[dt], 0, 0, 0);
-            }
+                for (int i = 0; i < 16; ++i)
+                    if (kv0 + 32 * t2 + (i >> 2) * 8 + 4 * h + (i & 3) > q_pos) st[t2][i] = NEG_INF;
         }
-        if (kt + 1 < kt1) put((kt + 1 - kt0) & 1);
+        float m_tile = NEG_INF;
+#pragma unroll
+        for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m_tile = fmaxf(m_tile, st[t2][i]);
+        {
+            const auto sw = __builtin_amdgcn_permlane32_swap(as_bits(m_tile), as_bits(m_tile), false, false);
+            m_tile = fmaxf(as_float((uint32_t)sw[0]), as_float((uint32_t)sw[1]));
+        }
+        const float m_new = fmaxf(m_run, m_tile), m_safe = m_new == NEG_INF ? 0.f : m_new;
+        if (__any(m_new != m_run)) {
+            const float alpha = __builtin_amdgcn_exp2f((m_run - m_safe) * sc);
+            l_run *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[dt] = o[dt] * alpha;
+            m_run = m_new;
+        }
+        const float ms = m_safe * sc;
+        // weights of a block, a pair at a time, rounded to bf16 for the product (at most 2^-8 each); their sum is of the rounded ones
+        u32x4_t pw[2];
+        const bf16x2 ones = {(bf16_t)1.f, (bf16_t)1.f};
+        auto weights = [&](int b4, int w0, int n) {
+#pragma unroll
+            for (int w = w0; w < w0 + n; ++w) {
+                bf16x2 p;
+                p[0] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(st[b4 >> 1][8 * (b4 & 1) + 2 * w], sc, -ms));
+                p[1] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(st[b4 >> 1][8 * (b4 & 1) + 2 * w + 1], sc, -ms));
+                l_run = __builtin_amdgcn_fdot2_f32_bf16(p, ones, l_run, false);
+                pw[b4 & 1][w] = as_bits(p);
+            }
+        };
+        constexpr int NV = 4 * DT, R = 4;   // V's fragments are read R - 1 ahead of their products
+        bf16x8 vf[R];
+        auto values = [&](int f) { return *(const bf16x8 *)(t + v_base + L::K + L::KS + (f / DT) * (32 * HD) + (f % DT) * 512); };
+#pragma unroll
+        for (int f = 0; f < R - 1; ++f) vf[f] = values(f);
+        weights(0, 0, 4);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < NV; ++f) {
+            const int b4 = f / DT, dt = f % DT;
+            if (f + R - 1 < NV) vf[(f + R - 1) % R] = values(f + R - 1);
+            o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[f % R], __builtin_bit_cast(bf16x8, pw[b4 & 1]), o[dt], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
+            if (b4 < 3) weights(b4 + 1, dt * (4 / DT), 4 / DT);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    if (kt0 < kt1) {
+        next_blk = block_at(kt0);
+        fetch(kt0);
+        refuse();
+#pragma unroll
+        for (int i = 0; i < PARTS; ++i) put(i, smem_kv4p);
+        put_nan(smem_kv4p);
+        fetch(min(kt0 + 1, kt1 - 1));
+    }
+    __syncthreads();
+    for (int kt = kt0; kt < kt1; kt += 2) {
+        tile(kt, std::integral_constant<int, 0>{});
         __syncthreads();
+        if (kt + 1 < kt1) {
+            tile(kt + 1, std::integral_constant<int, 1>{});
+            __syncthreads();
+        }
     }
     l_run += __shfl_xor(l_run, 32, 64);
     if (!valid) return;
