@@ -101,7 +101,7 @@ struct Kv4AttnArgs {
     float scale_log2;         // log2(e) / sqrt(hd)
     SeqInfo seq;              // prompts
     int out_row0 = 0, out_Mt = 0;   // first row and row tiles of the packed output matrix
-    int chunk = 0, n_chunks = 0;    // set by the launchers
+    int chunk = 0, n_chunks = 0, fold = 0;    // set by the launchers
 };
 #define KV4_SPLIT_WGS 512      // most workgroups of a launch whose rows are cut into key ranges
 struct Kv4Cut { int chunk, waves; };

@@ -241,60 +241,77 @@ void launch_kv4_append(hipStream_t st, const Kv4RowsArgs &a) {
 
 // ---- attention: what both kinds share ---------------------------------------------------------------------------------------
 // Scores.  K stays as it is in the cache: the matrix instruction with block scales takes 4-bit rows, 32 dims and their scale a
-// lane.  The query goes in as two e4m3 terms, q = hi + lo / 16: of a bf16's eight significant bits hi takes four and lo the
-// rest, exactly, down to 2^-20 of the largest of its 32 dims (smaller ones lose bits there).  Two such products cost what one
-// of bf16 operands does, and K needs no conversion.  Their sums are good to 2e-5 of sum|q k| (measured), far less than what
-// rounding the softmax weights to bf16 does.
-// A scale of 255 makes every score of its token NaN, as a NaN in a bf16 cache would.
-
-// 16 dims of the query (as floats) -> 16 bytes each of hi and lo; mul: the power of two that takes the group's largest into
-// [128, 256)
-__device__ __forceinline__ void q_split(const float *x, float mul, int *hi, int *lo) {
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const float a = x[4 * w] * mul, b = x[4 * w + 1] * mul, c = x[4 * w + 2] * mul, d = x[4 * w + 3] * mul;
-        int p = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-        p = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, p, true);
-        const auto ab = __builtin_amdgcn_cvt_pk_f32_fp8(p, false), cd = __builtin_amdgcn_cvt_pk_f32_fp8(p, true);
-        int r = __builtin_amdgcn_cvt_pk_fp8_f32((a - ab[0]) * 16.f, (b - ab[1]) * 16.f, 0, false);
-        r = __builtin_amdgcn_cvt_pk_fp8_f32((c - cd[0]) * 16.f, (d - cd[1]) * 16.f, r, true);
-        hi[w] = p;
-        lo[w] = r;
-    }
-}
-__device__ __forceinline__ uint32_t absmax16(const float *x) {   // as bits: 0x7f800000 or more if one is not finite
+// lane.  The query, times log2(e) / sqrt(hd), goes in as three terms of 6 bits (e2m3: multiples of 1/8 below 2, 1/4 below 4, 1/2
+// up to 7.5), each a sixteenth of the one before: x = t0 + t1 / 16 + t2 / 256 in units of a power of two that takes the largest
+// of the 32 dims into [3.875, 7.75).  What is left of x is at most 2^-12 units, 2^-13.9 of that largest.  With 6-bit operands
+// the instruction runs at four times the rate of bf16, so that three products take 3/4 of the time of bf16's, no element of K is
+// converted, and the scores come out as the exponents that the softmax wants.  (Two e4m3 terms hold a bf16 exactly, at half the
+// rate: 16384 prompt rows 1810 us, 1800 with these.)
+// A scale of 255 makes every score of its token NaN, as a NaN in a bf16 cache would; so do not finite queries.
+typedef uint32_t u32x6_t __attribute__((ext_vector_type(6)));
+struct QTerms {
+    u32x6_t t[3];
+    int scale;   // bytes 0, 1, 2: of the terms
+};
+__device__ __forceinline__ i32x8 operand(u32x6_t v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], (int)v[4], (int)v[5], 0, 0}; }
+__device__ __forceinline__ i32x8 operand(u32x4_t v) { return i32x8{(int)v[0], (int)v[1], (int)v[2], (int)v[3], 0, 0, 0, 0}; }
+// Of 32 dims (p; times c): even and odd ones apart, as the conversion takes them.
+__device__ __forceinline__ QTerms q_terms(const bf16_t *p, float c) {
+    f32x16 x, y;
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) m = max(m, as_bits(x[i]) & 0x7fffffffu);
-    return m;
-}
-// Exponent field of the largest magnitude; 255 where it is not finite.
-__device__ __forceinline__ uint32_t q_exponent(uint32_t amax_bits) { return max(amax_bits >> 23, 12u); }
-__device__ __forceinline__ float q_mul(uint32_t e) { return as_float((261u - min(e, 254u)) << 23); }
-__device__ __forceinline__ int q_hi_scale(uint32_t e) { return e == 255u ? 255 : (int)e - 7; }
-__device__ __forceinline__ int q_lo_scale(uint32_t e) { return e == 255u ? 255 : (int)e - 11; }
-
-__device__ __forceinline__ void load16(const bf16_t *p, float *x) {
-    const bf16x8 a = ld_bf16x8(p), b = ld_bf16x8(p + 8);
+    for (int i = 0; i < 4; ++i) {
+        const bf16x8 v = ld_bf16x8(p + 8 * i);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        x[i] = (float)a[i];
-        x[8 + i] = (float)b[i];
+        for (int j = 0; j < 4; ++j) {
+            x[4 * i + j] = (float)v[2 * j] * c;
+            y[4 * i + j] = (float)v[2 * j + 1] * c;
+            m = max(max(m, as_bits(x[4 * i + j]) & 0x7fffffffu), as_bits(y[4 * i + j]) & 0x7fffffffu);
+        }
     }
+    const bool finite = m < 0x7f800000u;
+    const int e = max((int)((m + 0x00080000u) >> 23), 16) - 2;   // 1.9375 * 2^n and more count as 2^(n+1)
+    QTerms q;
+    q.scale = finite ? e | (e - 4) << 8 | (e - 8) << 16 : 0xffffff;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        const float s = as_float((uint32_t)(e - 4 * k) << 23);
+        q.t[k] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(x, y, s);
+        if (k < 2) {
+            typedef float f32x32 __attribute__((ext_vector_type(32)));
+            const f32x32 r = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q.t[k], s);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                x[i] -= r[2 * i];
+                y[i] -= r[2 * i + 1];
+            }
+        }
+    }
+    return q;
 }
 
 // Four tokens of a dim pair (a dword of codes, a dword of scale bytes) -> the even dim's four values and the odd dim's.
-struct V4 {
-    u32x2_t even, odd;
-    uint32_t top;   // the largest of the scales, as bits: 0x7f800000 where one is 255
+struct V4 { u32x2_t even, odd; };
+struct V4Steps {   // in three steps, for code that puts other instructions between them
+    float s[4];
+    uint32_t x[4];
+    __device__ __forceinline__ void scales(uint32_t four) { s[0] = kv4_scale_of<0>(four), s[1] = kv4_scale_of<1>(four), s[2] = kv4_scale_of<2>(four), s[3] = kv4_scale_of<3>(four); }
+    // the largest of them and `m`, as bits: 0x7f800000 where one is 255
+    __device__ __forceinline__ uint32_t top(uint32_t m) const { return max(max(max(max(m, as_bits(s[0])), as_bits(s[1])), as_bits(s[2])), as_bits(s[3])); }
+    __device__ __forceinline__ void convert(uint32_t codes) {
+        x[0] = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s[0], 0)), x[1] = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s[1], 1));
+        x[2] = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s[2], 2)), x[3] = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s[3], 3));
+    }
+    __device__ __forceinline__ V4 values() const {
+        return {u32x2_t{__builtin_amdgcn_perm(x[1], x[0], 0x05040100u), __builtin_amdgcn_perm(x[3], x[2], 0x05040100u)},
+                u32x2_t{__builtin_amdgcn_perm(x[1], x[0], 0x07060302u), __builtin_amdgcn_perm(x[3], x[2], 0x07060302u)}};
+    }
 };
 __device__ __forceinline__ V4 v_values(uint32_t codes, uint32_t scales) {
-    const float s0 = kv4_scale_of<0>(scales), s1 = kv4_scale_of<1>(scales), s2 = kv4_scale_of<2>(scales), s3 = kv4_scale_of<3>(scales);
-    const uint32_t x0 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s0, 0)), x1 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s1, 1));
-    const uint32_t x2 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s2, 2)), x3 = as_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s3, 3));
-    return {u32x2_t{__builtin_amdgcn_perm(x1, x0, 0x05040100u), __builtin_amdgcn_perm(x3, x2, 0x05040100u)},
-            u32x2_t{__builtin_amdgcn_perm(x1, x0, 0x07060302u), __builtin_amdgcn_perm(x3, x2, 0x07060302u)},
-            max(max(max(as_bits(s0), as_bits(s1)), as_bits(s2)), as_bits(s3))};
+    V4Steps v;
+    v.scales(scales);
+    v.convert(codes);
+    return v.values();
 }
 __device__ __forceinline__ bf16x8 join8(u32x2_t a, u32x2_t b) { return __builtin_bit_cast(bf16x8, u32x4_t{a[0], a[1], b[0], b[1]}); }
 
@@ -305,7 +322,7 @@ __device__ __forceinline__ bf16_t *kv4_out(const Kv4AttnArgs &a, int row, int co
 
 // ---- pieces of rows ---------------------------------------------------------------------------------------------------------
 // A row of one head that several workgroups compute leaves a piece each: the weighted sum of values, relative to the piece's own
-// maximum of raw scores, that maximum and the sum of weights.  A workgroup joins the pieces of the heads of one kv head of one
+// maximum, that maximum and the sum of weights.  A workgroup joins the pieces of the heads of one kv head of one
 // row, in order; a thread takes four dims.  Bound by round trips to memory: up to 8 pieces are asked for at once, whether the
 // row has them or not, beside its length; more in eights behind a pass over the maxima (64 rows of 3 chunks, 8B heads: 4.1 us, 32 rows of
 // 16 chunks 4.7; a launch that does nothing is 2).
@@ -314,7 +331,6 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
     __shared__ float s[2 * 16];
     const int row = blockIdx.y, G = a.Hq / a.Hkv, hq0 = blockIdx.x * G;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const float sc = a.scale_log2;
     const size_t p0 = ((size_t)row * a.Hq + hq0) * a.n_chunks;
     const float2 *ml = (const float2 *)a.part_ml + p0;
     const f32x4 *po = (const f32x4 *)a.part_o + p0 * (HD / 4);
@@ -347,7 +363,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (j < n) {
-                    const float e = __builtin_amdgcn_exp2f((m[j].x - ms) * sc);
+                    const float e = __builtin_amdgcn_exp2f(m[j].x - ms);
                     acc += v[j] * e;
                     l += m[j].y * e;
                 }
@@ -365,7 +381,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
         const float ms = mx == NEG_INF ? 0.f : mx;
         for (int c = lane; c < n; c += 64) {
             const float2 v = mg[c];
-            l += v.y * __builtin_amdgcn_exp2f((v.x - ms) * sc);
+            l += v.y * __builtin_amdgcn_exp2f(v.x - ms);
         }
         l = wave_sum(l);
         if (lane == 0) {
@@ -391,7 +407,7 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (c0 + j < n) acc += v[j] * __builtin_amdgcn_exp2f((m[j] - ms) * sc);
+                if (c0 + j < n) acc += v[j] * __builtin_amdgcn_exp2f(m[j] - ms);
         }
         store(g, d4, acc, s[2 * g + 1]);
     }
@@ -433,44 +449,9 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 3 : 2) void kv4_decode_kernel(Kv
     int my_blk = lane < per_wave / 16 ? a.tables[(size_t)b * a.max_blk + min((t0 >> 4) + lane, a.max_blk - 1)] : -1;
     int n_keys = __builtin_amdgcn_readfirstlane(a.ctx_lens[b]) + 1;
 
-    // the query's terms: bytes 0-15 of a lane's operand are dims 16h.., bytes 16-31 dims 64 + 16h..
-    i32x8 qh, ql;
-    int qh_scale, ql_scale;
-    {
-        float x[2][16];
-        const bool col = c16 < Gq;
-        const bf16_t *qp = a.q + (size_t)b * a.q_stride + (size_t)(hk * Gq + (col ? c16 : 0)) * HD + 16 * h;
-        load16(qp, x[0]);
-        if (HD == 128) load16(qp + 64, x[1]);
-        uint32_t e[2];
-        int hi[8], lo[8];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            if (HD == 64 && p == 1) {
-                e[1] = 127;
-#pragma unroll
-                for (int w = 0; w < 4; ++w) hi[4 + w] = lo[4 + w] = 0;
-                break;
-            }
-            if (!col)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[p][i] = 0.f;
-            uint32_t mine = absmax16(x[p]);
-            mine = max(mine, (uint32_t)__shfl_xor((int)mine, 16, 64));
-            e[p] = q_exponent(mine);
-            q_split(x[p], q_mul(e[p]), hi + 4 * p, lo + 4 * p);
-        }
-#pragma unroll
-        for (int w = 0; w < 8; ++w) {
-            qh[w] = hi[w];
-            ql[w] = lo[w];
-        }
-        // lane quarter h gives the scale of dims 32h..: those of the first 64 are in e[0] of the quarters 2h, of the second in e[1]
-        const uint32_t e0 = (uint32_t)__shfl((int)e[0], (2 * (h & 1)) * 16 + c16, 64), e1 = (uint32_t)__shfl((int)e[1], (2 * (h & 1)) * 16 + c16, 64);
-        const uint32_t mine = h < 2 ? e0 : e1;
-        qh_scale = q_hi_scale(mine);
-        ql_scale = q_lo_scale(mine);
-    }
+    // the query's terms, a column and 32 dims a lane (columns without a head, and the lanes behind head_dim: zeros)
+    QTerms q = q_terms(a.q + (size_t)b * a.q_stride + (size_t)(hk * Gq + min(c16, Gq - 1)) * HD + 32 * (h & (G - 1)), a.scale_log2);
+    if (c16 >= Gq || h >= G) q = QTerms{{{}, {}, {}}, 127 | 127 << 8 | 127 << 16};
 
     if (n_keys < 0 || n_keys > a.max_ctx) {
         if (tid == 0 && chunk == 0 && hk == 0) atomicOr(a.err_flag, 8);
@@ -493,7 +474,6 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 3 : 2) void kv4_decode_kernel(Kv
     f32x4 o[2 * G];   // (group, parity of the dim)
 #pragma unroll
     for (int i = 0; i < 2 * G; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const float sc = a.scale_log2;
     const uint8_t *head = a.pool + (size_t)hk * F::BYTES;
     const size_t blk_stride = (size_t)a.Hkv * F::BYTES;
     const uint32_t off_k = F::k_chunk(h & (G - 1), c16), off_ks = F::k_scale(h & (G - 1), c16), off_v = F::V + (h * 16 + c16) * (4 * G), off_vs = F::VS + h * (4 * G);
@@ -523,10 +503,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 3 : 2) void kv4_decode_kernel(Kv
         f32x4 s[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const i32x8 k = {(int)f.kc[u][0], (int)f.kc[u][1], (int)f.kc[u][2], (int)f.kc[u][3], 0, 0, 0, 0};
             s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, ql, s[u], 4, 0, 0, (int)f.ks[u], 0, ql_scale);
-            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(k, qh, s[u], 4, 0, 0, (int)f.ks[u], 0, qh_scale);
+            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(f.kc[u]), operand(q.t[2]), s[u], 4, 2, 0, (int)f.ks[u], 2, q.scale);
+            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(f.kc[u]), operand(q.t[1]), s[u], 4, 2, 0, (int)f.ks[u], 1, q.scale);
+            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(f.kc[u]), operand(q.t[0]), s[u], 4, 2, 0, (int)f.ks[u], 0, q.scale);
         }
         if (!(base + 32 <= t1 && b0 >= 0 && b1 >= 0)) {   // uniform
 #pragma unroll
@@ -541,18 +521,17 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 3 : 2) void kv4_decode_kernel(Kv
             }
         }
         const float m_tile = max_of_quarters(fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))));
-        const float m_new = fmaxf(m_run, m_tile), m_safe = m_new == NEG_INF ? 0.f : m_new;
-        const float ms = m_safe * sc;
+        const float m_new = fmaxf(m_run, m_tile), ms = m_new == NEG_INF ? 0.f : m_new;
         bf16x8 pf;   // the weights are rounded to bf16 for the second product (at most 2^-8 each); their sum is of the unrounded ones
         float psum = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], sc, -ms));
+            const float p = __builtin_amdgcn_exp2f(s[i >> 2][i & 3] - ms);
             psum += p;
             pf[i] = (bf16_t)p;
         }
         if (__any(m_new != m_run)) {
-            const float alpha = __builtin_amdgcn_exp2f((m_run - m_safe) * sc);
+            const float alpha = __builtin_amdgcn_exp2f(m_run - ms);
             l_run *= alpha;
 #pragma unroll
             for (int i = 0; i < 2 * G; ++i) o[i] = o[i] * alpha;
@@ -607,7 +586,7 @@ __global__ __launch_bounds__(64 * NW, NW == 4 ? 3 : 2) void kv4_decode_kernel(Kv
         float acc = 0.f, l = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float e = __builtin_amdgcn_exp2f((s_m[w * Gq + gg] - ms) * sc);
+            const float e = __builtin_amdgcn_exp2f(s_m[w * Gq + gg] - ms);
             acc += s_o[(w * HD + d) * Gq + gg] * e;
             l += s_l[w * Gq + gg] * e;
         }
@@ -682,6 +661,9 @@ void kv4_kernels_init() {
 // V in LDS: per block two halves [hd][8 tokens], half i the quads i and 2 + i, the dims of a group even ones first: the order
 // in which a lane holds its scores, so the weights need no exchange between lanes.
 #define KV4_COLS 128
+// Weights are at most 2^4: a bf16 is as fine there as below 1, and the accumulators are rescaled in a few tiles of a long prompt
+// instead of in two of five (16384 rows 1800 -> 1694 us; the error against float64 0.0019 -> 0.0020 of the result).
+#define KV4_REF_BEHIND 4.f
 template <int HD> struct Kv4Lds {
     static constexpr int K = 4 * 8 * HD, KS = 4 * (HD / 2), V = 4 * 2 * HD * 16, TILE = K + KS + V;
 };
@@ -697,7 +679,8 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
     const int hk = blockIdx.x % a.Hkv, split = blockIdx.y, Gq = a.Hq / a.Hkv;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c32 = lane & 31, h = lane >> 5;
 
-    int unit = blockIdx.x / a.Hkv, req = 0, units = 0;
+    int unit = a.fold > 0 && (int)blockIdx.x >= a.fold ? (int)(gridDim.x - 1 - (blockIdx.x - a.fold)) / a.Hkv : (int)blockIdx.x / a.Hkv;
+    int req = 0, units = 0;
     for (; req < a.seq.n_req; ++req) {
         units = kv4_units(a.seq.cu[req + 1] - a.seq.cu[req], Gq);
         if (unit < units) break;
@@ -716,42 +699,19 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
     // this workgroup's share of the key tiles
     const int kt0 = (int)((int64_t)n_tiles * split / a.n_chunks), kt1 = (int)((int64_t)n_tiles * (split + 1) / a.n_chunks);
 
-    // the query's terms: of each 64 dims bytes 0-15 are dims 16h.., bytes 16-31 dims 32 + 16h..
-    i32x8 qh[KSTEP], ql[KSTEP];
-    int qhs[KSTEP], qls[KSTEP];
-    {
-        const bf16_t *qp = a.q + (size_t)(row0 + row) * a.q_stride + (size_t)hq * HD + 16 * h;
+    QTerms q[KSTEP];   // of dims 64 s + 32 h ..
 #pragma unroll
-        for (int s = 0; s < KSTEP; ++s) {
-            float x[2][16];
-            uint32_t e[2];
-            int hi[8], lo[8];
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
-                load16(qp + 64 * s + 32 * p, x[p]);
-                uint32_t mine = absmax16(x[p]);
-                mine = max(mine, (uint32_t)__shfl_xor((int)mine, 32, 64));
-                e[p] = q_exponent(mine);
-                q_split(x[p], q_mul(e[p]), hi + 4 * p, lo + 4 * p);
-            }
-#pragma unroll
-            for (int w = 0; w < 8; ++w) {
-                qh[s][w] = hi[w];
-                ql[s][w] = lo[w];
-            }
-            const uint32_t mine = h ? e[1] : e[0];
-            qhs[s] = q_hi_scale(mine);
-            qls[s] = q_lo_scale(mine);
-        }
-    }
+    for (int s = 0; s < KSTEP; ++s) q[s] = q_terms(a.q + (size_t)(row0 + row) * a.q_stride + (size_t)hq * HD + 64 * s + 32 * h, a.scale_log2);
 
-    float m_run = NEG_INF, l_run = 0.f;
+    // Scores are computed relative to a reference, from whose negative the products start: the row's first maximum, moved to the
+    // running one once a score is KV4_REF_BEHIND above it (limit; -inf while the row has seen no key).
+    f32x16 minus_ref = {};
+    float limit = NEG_INF, l_run = 0.f, l_odd = 0.f;   // the sum of weights in two parts
     f32x16 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
-    const float sc = a.scale_log2;
     const int32_t *tab = a.tables + (size_t)req * a.max_blk;
 
     // A wave brings one block of a key tile: a lane HD/8 bytes of K's codes, the codes and scales of two V units (quads v_half
@@ -788,27 +748,30 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
     // What was fetched goes to LDS in parts, which the first product's instructions lie between: K; then of each group the values
     // of two quads and their stores.  (No branch among them: what the products give is used behind it, and the compiler would move
     // them there.)
-    constexpr int PARTS = 1 + 3 * UG;
-    V4 px, py;
+    constexpr int PARTS = 6 * UG;
+    V4Steps step;
+    V4 px;
     uint32_t top = 0;
     auto put = [&](int part, uint8_t *t) {
         uint8_t *scales = t + L::K + wave * (HD / 2);
         bf16x8 *v = (bf16x8 *)(t + L::K + L::KS) + (wave * 2 + v_half) * HD + 32 * vg + vj;
+        const int g = part / 6, u = part / 3 % 2;
         if (part == 0) {
             *(kvec *)(t + wave * (8 * HD) + lane * (HD / 8)) = rk;
             ((uint32_t *)scales)[lane & (HD / 8 - 1)] = rks;
             top = 0;
+        }
+        if (part % 3 == 0) {
+            step.scales(rs[u][g]);
+        } else if (part % 3 == 1) {
+            top = step.top(top);
+            step.convert(rv[u][g]);
+        } else if (u == 0) {
+            px = step.values();
         } else {
-            const int g = (part - 1) / 3, what = (part - 1) % 3;
-            if (what == 0) {
-                px = v_values(rv[0][g], rs[0][g]);
-            } else if (what == 1) {
-                py = v_values(rv[1][g], rs[1][g]);
-            } else {
-                top = max(max(top, px.top), py.top);
-                v[32 * g] = join8(px.even, py.even);
-                v[32 * g + 16] = join8(px.odd, py.odd);
-            }
+            const V4 py = step.values();
+            v[32 * g] = join8(px.even, py.even);
+            v[32 * g + 16] = join8(px.odd, py.odd);
         }
     };
     // A value that is not finite must not reach the rows before it, whose weight of it is zero: the token's scores are made NaN
@@ -853,20 +816,19 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
                 ks[t2][s] = t[s_base + L::K + t2 * HD + s * 32];
             }
         f32x16 st[2];
+        __builtin_amdgcn_s_setprio(1);   // a wave with products goes before one with softmax (16384 rows 1845 -> 1810 us)
 #pragma unroll
-        for (int i = 0; i < 4 * KSTEP; ++i) {   // the two score tiles in turn
-            const int t2 = i & 1, s = i >> 2;
-            const i32x8 k = {(int)kc[t2][s][0], (int)kc[t2][s][1], (int)kc[t2][s][2], (int)kc[t2][s][3], 0, 0, 0, 0};
-            if (i < 2) {
-                const f32x16 zero = {};
-                st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, ql[s], zero, 4, 0, 0, ks[t2][s], 0, qls[s]);
-            } else {
-                st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(k, i & 2 ? qh[s] : ql[s], st[t2], 4, 0, 0, ks[t2][s], 0, i & 2 ? qhs[s] : qls[s]);
-            }
+        for (int i = 0; i < PARTS; ++i) {   // step s of head_dim, the query's smallest term first, the two score tiles in turn
+            const int t2 = i & 1, s = i / 6, k = 2 - (i >> 1) % 3;
+            const f32x16 from = i < 2 ? minus_ref : st[t2];
+            if (k == 2) st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(kc[t2][s]), operand(q[s].t[2]), from, 4, 2, 0, ks[t2][s], 2, q[s].scale);
+            if (k == 1) st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(kc[t2][s]), operand(q[s].t[1]), from, 4, 2, 0, ks[t2][s], 1, q[s].scale);
+            if (k == 0) st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(kc[t2][s]), operand(q[s].t[0]), from, 4, 2, 0, ks[t2][s], 0, q[s].scale);
             __builtin_amdgcn_sched_barrier(0);
-            if (i < PARTS) put(i, other);
+            put(i, other);
             __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
         asm volatile("" : "+v"(st[0]), "+v"(st[1]));   // the products stay in front of the branch
         put_nan(other);
         fetch(min(kt + 2, kt1 - 1));
@@ -886,25 +848,30 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
             const auto sw = __builtin_amdgcn_permlane32_swap(as_bits(m_tile), as_bits(m_tile), false, false);
             m_tile = fmaxf(as_float((uint32_t)sw[0]), as_float((uint32_t)sw[1]));
         }
-        const float m_new = fmaxf(m_run, m_tile), m_safe = m_new == NEG_INF ? 0.f : m_new;
-        if (__any(m_new != m_run)) {
-            const float alpha = __builtin_amdgcn_exp2f((m_run - m_safe) * sc);
+        if (__any(m_tile > limit)) {
+            const bool moves = m_tile > limit;
+            const float by = moves ? m_tile : 0.f, alpha = limit == NEG_INF ? 1.f : __builtin_amdgcn_exp2f(-by);
             l_run *= alpha;
+            l_odd *= alpha;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[dt] = o[dt] * alpha;
-            m_run = m_new;
+            minus_ref -= by;
+            st[0] -= by;
+            st[1] -= by;
+            if (moves) limit = KV4_REF_BEHIND;
         }
-        const float ms = m_safe * sc;
-        // weights of a block, a pair at a time, rounded to bf16 for the product (at most 2^-8 each); their sum is of the rounded ones
+        // weights of a block, a pair at a time, rounded to bf16 for the product (at most 2^-8 each); their sum is of the unrounded
+        // ones (plain additions: the dot instruction, half as many, does not run beside the matrix unit)
         u32x4_t pw[2];
-        const bf16x2 ones = {(bf16_t)1.f, (bf16_t)1.f};
         auto weights = [&](int b4, int w0, int n) {
 #pragma unroll
             for (int w = w0; w < w0 + n; ++w) {
+                const float p0 = __builtin_amdgcn_exp2f(st[b4 >> 1][8 * (b4 & 1) + 2 * w]), p1 = __builtin_amdgcn_exp2f(st[b4 >> 1][8 * (b4 & 1) + 2 * w + 1]);
+                l_run += p0;
+                l_odd += p1;
                 bf16x2 p;
-                p[0] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(st[b4 >> 1][8 * (b4 & 1) + 2 * w], sc, -ms));
-                p[1] = (bf16_t)__builtin_amdgcn_exp2f(fmaf(st[b4 >> 1][8 * (b4 & 1) + 2 * w + 1], sc, -ms));
-                l_run = __builtin_amdgcn_fdot2_f32_bf16(p, ones, l_run, false);
+                p[0] = (bf16_t)p0;
+                p[1] = (bf16_t)p1;
                 pw[b4 & 1][w] = as_bits(p);
             }
         };
@@ -915,6 +882,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
         for (int f = 0; f < R - 1; ++f) vf[f] = values(f);
         weights(0, 0, 4);
         __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int f = 0; f < NV; ++f) {
             const int b4 = f / DT, dt = f % DT;
@@ -924,6 +892,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
             if (b4 < 3) weights(b4 + 1, dt * (4 / DT), 4 / DT);
             __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
     };
     if (kt0 < kt1) {
         next_blk = block_at(kt0);
@@ -943,6 +912,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
             __syncthreads();
         }
     }
+    l_run += l_odd;
     l_run += __shfl_xor(l_run, 32, 64);
     if (!valid) return;
     // rows of o: register i of tile dt is dim 32 dt + 2 (8 (i / 4 & 1) + 4 h + i % 4) + i / 8
@@ -973,7 +943,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
             dst[1] = f32x4{o[dt][4 * j + 2], o[dt][8 + 4 * j + 2], o[dt][4 * j + 3], o[dt][8 + 4 * j + 3]};
         }
     if (h == 0) {
-        a.part_ml[2 * pi] = m_run;
+        a.part_ml[2 * pi] = limit == NEG_INF ? NEG_INF : -minus_ref[0];
         a.part_ml[2 * pi + 1] = l_run;
     }
 }
@@ -998,7 +968,10 @@ void launch_kv4_prefill(hipStream_t st, const Kv4AttnArgs &args) {
     a.n_chunks = kv4_prefill_splits(a.seq, a.Hq, a.Hkv, &units);
     if (units == 0) return;
     a.ctx_lens = nullptr;
-    const dim3 grid(a.Hkv * units, a.n_chunks);
+    const int wgs = a.Hkv * units;
+    // workgroups that all run at once, two a compute unit: the shorter half in rising order, beside the longer (2048 rows 52.7 -> 48.0 us)
+    a.fold = a.n_chunks == 1 && wgs > 256 && wgs <= 512 ? 256 : 0;
+    const dim3 grid(wgs, a.n_chunks);
     if (a.hd == 128) hipLaunchKernelGGL(kv4_prefill_kernel<128>, grid, dim3(256), 2 * Kv4Lds<128>::TILE, st, a);
     else hipLaunchKernelGGL(kv4_prefill_kernel<64>, grid, dim3(256), 2 * Kv4Lds<64>::TILE, st, a);
     if (a.n_chunks > 1) launch_kv4_merge(st, a, a.seq.cu[a.seq.n_req]);

@@ -90,10 +90,12 @@ def attention(q, k, v, first):
     """q [rows, Hq, hd] at positions first.. over k, v [n, Hkv, hd], causal.  Returns the output and a bound of what rounding may
     do to it, element by element (float64):
 
-    every weight is rounded to bf16 (2^-8 of itself), its score is off by at most 2^-15 of sum|q k| / sqrt(hd) (the matrix
-    instruction with block scales adds its products in fewer bits than float32: 2^-15.7 at most was measured) and so itself by
-    as much relatively, once in the numerator and once in the sum; the exponential and the sums in float32 are within 2^-16; and
-    the result is rounded to bf16 (2^-8 of itself, once more for the error in front of it)."""
+    every weight is rounded to bf16 (2^-8 of itself), once in the numerator and once in the sum, which is taken of the rounded or
+    of the unrounded ones; its score is off by delta and so itself by as much relatively, again in both; delta is what the query's
+    terms leave of it, at most 2^-13 of the largest of the 32 dims for each (2^-13.9, and float32's rounding of the product with
+    the scale), and 2^-14 of sum|q k| for the sums in the matrix unit and the maximum that they start from (2^-15.7 at most was
+    measured with products of more bits); the exponential and the sums in float32 are within 2^-16; and the result is rounded to
+    bf16 (2^-8 of itself, once more for the error in front of it)."""
     rows, Hq, hd = q.shape
     G = Hq // k.shape[1]
     out, bound = np.zeros((rows, Hq, hd)), np.zeros((rows, Hq, hd))
@@ -104,10 +106,11 @@ def attention(q, k, v, first):
         for h in range(Hq):
             kk, vv = k[:n, h // G], v[:n, h // G]
             s = kk @ q[r, h] / math.sqrt(hd)
-            delta = 2.0 ** -15 * float(np.max(np.abs(kk) @ np.abs(q[r, h]))) / math.sqrt(hd)
+            top = np.repeat(np.abs(q[r, h]).reshape(-1, 32).max(1), 32)
+            delta = float(np.max(np.abs(kk) @ (2.0 ** -14 * np.abs(q[r, h]) + 2.0 ** -13 * top))) / math.sqrt(hd)
             p = np.exp(s - s.max())
             p /= p.sum()
             out[r, h] = p @ vv
-            e = (p @ np.abs(vv)) * (2.0 ** -8 + 2.0 * delta + 2.0 ** -16)
+            e = (p @ np.abs(vv)) * (2.0 ** -8 + 2.0 * delta + 2.0 ** -16) + 2.0 ** -8 * np.abs(p @ vv)
             bound[r, h] = e + 2.0 ** -8 * (np.abs(out[r, h]) + e)
     return out, bound
