@@ -96,20 +96,28 @@ struct Kv4AttnArgs {
     const int32_t *tables;
     const int32_t *ctx_lens;  // decode: row b sees ctx_lens[b] + 1 tokens
     int32_t *err_flag;
-    float *part_o, *part_ml;  // [rows][Hq][n_chunks][hd], [..][2]: pieces of rows that more than one workgroup computes
+    float *part_o, *part_ml;  // pieces of rows that more than one workgroup computes: [..][hd], and [..][2]
     int B, Hq, Hkv, hd, max_blk, n_blocks, max_ctx;
     float scale_log2;         // log2(e) / sqrt(hd)
-    SeqInfo seq;              // prompts
     int out_row0 = 0, out_Mt = 0;   // first row and row tiles of the packed output matrix
-    int chunk = 0, n_chunks = 0, fold = 0;    // set by the launchers
+    int chunk = 0, n_chunks = 0;    // decode, set by the launcher; its pieces are [B][Hq][n_chunks]
 };
-#define KV4_SPLIT_WGS 512      // most workgroups of a launch whose rows are cut into key ranges
+// Prompts.  Set by the launcher: of each request the units (128 columns of one kv head) times the pieces that their keys are cut
+// into, and where those begin: first (in units and pieces), base (in pieces, [rows][Hq][cut]), row (in rows that are cut).
+struct Kv4PromptArgs : Kv4AttnArgs {
+    SeqInfo seq;
+    int fold;
+    // (All of 32 bits: beside a byte array, indexed alike, the compiler loaded these from an odd base and an odd offset that only
+    // together are a multiple of 4, and scalar loads drop the low bits of each.)
+    int32_t first[RS_MAX_RUNS], base[RS_MAX_RUNS], row[RS_MAX_RUNS], cut[RS_MAX_RUNS];
+};
+#define KV4_PIECES 1024        // most (unit, kv head, key range) pieces of cut rows in a launch
 struct Kv4Cut { int chunk, waves; };
 Kv4Cut kv4_cut(int64_t pairs, int max_ctx);
 int64_t kv4_most_pieces(int64_t pairs, int max_ctx);
 void kv4_kernels_init();
 void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &a);
-void launch_kv4_prefill(hipStream_t st, const Kv4AttnArgs &a);
+void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &a);
 
 enum GemmEpilogue { EPI_STORE = 0, EPI_RESIDUAL = 1, EPI_SWIGLU = 2 };
 

@@ -81,11 +81,15 @@ template <int HD> struct Kv4 {
 // A workgroup of 2 hd threads takes one (block, kv head) of one request: a thread 16 dims of one token's key (first half of the
 // threads) or value.  Bound by memory: 4 hd bytes of bf16 and 17/16 hd of cache a (token, head).
 struct RunBlock { int req, bi; };
-// The u-th block of the run of blocks that the requests' tokens touch (u less than their number): every lane looks at one request.
-__device__ __forceinline__ RunBlock run_block(const Kv4RowsArgs &a, int u) {
+// The last of n (1 to 64) ascending numbers, the first of them 0, that is at most u: every lane looks at one.  (The last: an empty
+// run begins where the next one does.)
+__device__ __forceinline__ int last_at_most(const int32_t *first, int n, int u) {
     const int lane = threadIdx.x & 63;
-    const unsigned long long before = __ballot(lane < a.seq.n_req && a.first[min(lane, RS_MAX_RUNS - 1)] <= u);
-    const int r = 63 - __builtin_clzll(before);   // (the last: empty runs begin where the next one does; first[0] is 0)
+    return 63 - __builtin_clzll(__ballot(lane < n && first[lane] <= u));
+}
+// The u-th block of the run of blocks that the requests' tokens touch (u less than their number).
+__device__ __forceinline__ RunBlock run_block(const Kv4RowsArgs &a, int u) {
+    const int r = last_at_most(a.first, a.seq.n_req, u);
     return {r, (a.seq.start[r] >> 4) + u - a.first[r]};
 }
 static int run_blocks(Kv4RowsArgs &a) {
@@ -326,35 +330,32 @@ __device__ __forceinline__ bf16_t *kv4_out(const Kv4AttnArgs &a, int row, int co
 // row, in order; a thread takes four dims.  Bound by round trips to memory: up to 8 pieces are asked for at once, whether the
 // row has them or not, beside its length; more in eights behind a pass over the maxima (64 rows of 3 chunks, 8B heads: 4.1 us, 32 rows of
 // 16 chunks 4.7; a launch that does nothing is 2).
-template <int HD>
-__global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
+// Of row `row`: at most `most` pieces, from piece p0 on, n() of them in use.
+template <int HD, class N>
+__device__ __forceinline__ void kv4_join(const Kv4AttnArgs &a, int row, size_t p0, int most, N n_of) {
     __shared__ float s[2 * 16];
-    const int row = blockIdx.y, G = a.Hq / a.Hkv, hq0 = blockIdx.x * G;
+    const int G = a.Hq / a.Hkv, hq0 = blockIdx.x * G;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const size_t p0 = ((size_t)row * a.Hq + hq0) * a.n_chunks;
     const float2 *ml = (const float2 *)a.part_ml + p0;
     const f32x4 *po = (const f32x4 *)a.part_o + p0 * (HD / 4);
-    auto pieces = [&]() {   // of this row
-        return a.ctx_lens ? (min(max(__builtin_amdgcn_readfirstlane(a.ctx_lens[row]) + 1, 0), a.max_ctx) + a.chunk - 1) / a.chunk : a.n_chunks;
-    };
     auto store = [&](int g, int d4, f32x4 acc, float l) {
         bf16x4 w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = (bf16_t)(l == 0.f ? 0.f : acc[j] / l);   // (0: an empty row, or every block of it refused)
         *(bf16x4 *)kv4_out(a, row, (hq0 + g) * HD + 4 * d4) = w;
     };
-    if (a.n_chunks <= 8) {
+    if (most <= 8) {
         for (int i = tid; i < G * (HD / 4); i += 256) {
             const int g = i / (HD / 4), d4 = i % (HD / 4);
             f32x4 v[8];
             float2 m[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const size_t c = (size_t)g * a.n_chunks + min(j, a.n_chunks - 1);
+                const size_t c = (size_t)g * most + min(j, most - 1);
                 v[j] = po[c * (HD / 4) + d4];
                 m[j] = ml[c];
             }
-            const int n = pieces();
+            const int n = n_of();
             float mx = NEG_INF, l = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) mx = fmaxf(mx, j < n ? m[j].x : NEG_INF);
@@ -371,9 +372,9 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
         }
         return;
     }
-    const int n = pieces();
+    const int n = n_of();
     for (int g = wave; g < G; g += 4) {
-        const float2 *mg = ml + (size_t)g * a.n_chunks;
+        const float2 *mg = ml + (size_t)g * most;
         float mx = NEG_INF, l = 0.f;
         for (int c = lane; c < n; c += 64) mx = fmaxf(mx, mg[c].x);
 #pragma unroll
@@ -393,8 +394,8 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
     for (int i = tid; i < G * (HD / 4); i += 256) {
         const int g = i / (HD / 4), d4 = i % (HD / 4);
         const float ms = s[2 * g];
-        const f32x4 *pg = po + (size_t)g * a.n_chunks * (HD / 4) + d4;
-        const float2 *mg = ml + (size_t)g * a.n_chunks;
+        const f32x4 *pg = po + (size_t)g * most * (HD / 4) + d4;
+        const float2 *mg = ml + (size_t)g * most;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         for (int c0 = 0; c0 < n; c0 += 8) {
             f32x4 v[8];
@@ -413,9 +414,11 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
     }
 }
 
-static void launch_kv4_merge(hipStream_t st, const Kv4AttnArgs &a, int rows) {
-    if (a.hd == 128) hipLaunchKernelGGL(kv4_merge_kernel<128>, dim3(a.Hkv, rows), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(kv4_merge_kernel<64>, dim3(a.Hkv, rows), dim3(256), 0, st, a);
+template <int HD>
+__global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
+    const int row = blockIdx.y;
+    kv4_join<HD>(a, row, ((size_t)row * a.Hq + blockIdx.x * (a.Hq / a.Hkv)) * a.n_chunks, a.n_chunks,
+                 [&]() { return (min(max(__builtin_amdgcn_readfirstlane(a.ctx_lens[row]) + 1, 0), a.max_ctx) + a.chunk - 1) / a.chunk; });
 }
 
 // ---- attention: one row per request -----------------------------------------------------------------------------------------
@@ -647,7 +650,10 @@ void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &args) {
         if (a.hd == 128) launch_kv4_decode_form<128, 4>(st, a);
         else launch_kv4_decode_form<64, 4>(st, a);
     }
-    if (a.n_chunks > 1) launch_kv4_merge(st, a, a.B);
+    if (a.n_chunks > 1) {
+        if (a.hd == 128) hipLaunchKernelGGL(kv4_merge_kernel<128>, dim3(a.Hkv, a.B), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL(kv4_merge_kernel<64>, dim3(a.Hkv, a.B), dim3(256), 0, st, a);
+    }
 }
 
 void kv4_kernels_init() {
@@ -661,6 +667,7 @@ void kv4_kernels_init() {
 // V in LDS: per block two halves [hd][8 tokens], half i the quads i and 2 + i, the dims of a group even ones first: the order
 // in which a lane holds its scores, so the weights need no exchange between lanes.
 #define KV4_COLS 128
+#define KV4_MIN_TILES 4   // key tiles of a piece at least
 // Weights are at most 2^4: a bf16 is as fine there as below 1, and the accumulators are rescaled in a few tiles of a long prompt
 // instead of in two of five (16384 rows 1800 -> 1694 us; the error against float64 0.0019 -> 0.0020 of the result).
 #define KV4_REF_BEHIND 4.f
@@ -668,27 +675,20 @@ template <int HD> struct Kv4Lds {
     static constexpr int K = 4 * 8 * HD, KS = 4 * (HD / 2), V = 4 * 2 * HD * 16, TILE = K + KS + V;
 };
 
-__device__ __forceinline__ int kv4_units(int rows, int G) { return (rows * G + KV4_COLS - 1) / KV4_COLS; }
-
 template <int HD>
-__global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
+__global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4PromptArgs a) {
     using F = Kv4<HD>;
     using L = Kv4Lds<HD>;
     constexpr int G = F::G, KSTEP = HD / 64, DT = HD / 32;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem_kv4p[];
-    const int hk = blockIdx.x % a.Hkv, split = blockIdx.y, Gq = a.Hq / a.Hkv;
+    const int hk = blockIdx.x % a.Hkv, Gq = a.Hq / a.Hkv;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c32 = lane & 31, h = lane >> 5;
 
-    int unit = a.fold > 0 && (int)blockIdx.x >= a.fold ? (int)(gridDim.x - 1 - (blockIdx.x - a.fold)) / a.Hkv : (int)blockIdx.x / a.Hkv;
-    int req = 0, units = 0;
-    for (; req < a.seq.n_req; ++req) {
-        units = kv4_units(a.seq.cu[req + 1] - a.seq.cu[req], Gq);
-        if (unit < units) break;
-        unit -= units;
-    }
-    if (req >= a.seq.n_req) return;
+    const int at = (a.fold > 0 && (int)blockIdx.x >= a.fold ? (int)(gridDim.x - 1 - (blockIdx.x - a.fold)) : (int)blockIdx.x) / a.Hkv;
+    const int req = last_at_most(a.first, a.seq.n_req, at);
+    const int cut = a.cut[req], unit = (at - a.first[req]) / cut, split = (at - a.first[req]) % cut;
     const int row0 = a.seq.cu[req], len = a.seq.cu[req + 1] - row0, prior = a.seq.start[req];
-    const int col0 = (units - 1 - unit) * KV4_COLS, n_cols = len * Gq;   // the longest first
+    const int n_cols = len * Gq, col0 = ((n_cols + KV4_COLS - 1) / KV4_COLS - 1 - unit) * KV4_COLS;   // the longest first
     const int col = col0 + 32 * wave + c32;
     const bool valid = col < n_cols;
     const int colc = min(col, n_cols - 1), row = colc / Gq, hq = hk * Gq + colc % Gq;
@@ -697,7 +697,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
     const int kv_end = prior + min(col0 + KV4_COLS - 1, n_cols - 1) / Gq + 1;
     const int n_tiles = (kv_end + 63) >> 6;
     // this workgroup's share of the key tiles
-    const int kt0 = (int)((int64_t)n_tiles * split / a.n_chunks), kt1 = (int)((int64_t)n_tiles * (split + 1) / a.n_chunks);
+    const int kt0 = (int)((int64_t)n_tiles * split / cut), kt1 = (int)((int64_t)n_tiles * (split + 1) / cut);
 
     QTerms q[KSTEP];   // of dims 64 s + 32 h ..
 #pragma unroll
@@ -917,7 +917,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
     if (!valid) return;
     // rows of o: register i of tile dt is dim 32 dt + 2 (8 (i / 4 & 1) + 4 h + i % 4) + i / 8
     const int out_row = row0 + row;
-    if (a.n_chunks == 1) {
+    if (cut == 1) {
         const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -933,7 +933,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
             }
         return;
     }
-    const size_t pi = ((size_t)out_row * a.Hq + hq) * a.n_chunks + split;
+    const size_t pi = a.base[req] + ((size_t)row * a.Hq + hq) * cut + split;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
@@ -948,31 +948,83 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4AttnArgs a) {
     }
 }
 
-// Key ranges that a launch's rows are cut into, from the sizes alone: as many as give two workgroups to every compute unit, of 256 keys at least.
-int kv4_prefill_splits(const SeqInfo &seq, int Hq, int Hkv, int *units_out) {
-    int units = 0, longest = 0;
-    for (int r = 0; r < seq.n_req; ++r) {
-        const int len = seq.cu[r + 1] - seq.cu[r];
-        if (len <= 0) continue;
-        units += (len * (Hq / Hkv) + KV4_COLS - 1) / KV4_COLS;
-        longest = std::max(longest, seq.start[r] + len);
-    }
-    *units_out = units;
-    if (units == 0) return 1;
-    return std::max(1, std::min(KV4_SPLIT_WGS / (units * Hkv), longest / 256));
+// The rows that were cut.
+template <int HD>
+__global__ __launch_bounds__(256) void kv4_prompt_merge_kernel(Kv4PromptArgs a) {
+    const int req = last_at_most(a.row, a.seq.n_req, blockIdx.y), row = blockIdx.y - a.row[req], cut = a.cut[req];
+    kv4_join<HD>(a, a.seq.cu[req] + row, a.base[req] + ((size_t)row * a.Hq + blockIdx.x * (a.Hq / a.Hkv)) * cut, cut, [&]() { return cut; });
 }
 
-void launch_kv4_prefill(hipStream_t st, const Kv4AttnArgs &args) {
-    Kv4AttnArgs a = args;
-    int units = 0;
-    a.n_chunks = kv4_prefill_splits(a.seq, a.Hq, a.Hkv, &units);
-    if (units == 0) return;
-    a.ctx_lens = nullptr;
-    const int wgs = a.Hkv * units;
+// How many pieces the keys of each request's units are cut into, from the sizes alone: the number of key tiles of a piece that
+// makes the launch shortest by this account, in us.  A compute unit takes 0.85 us a tile (head_dim 128) with two workgroups,
+// 0.95 with one; the longest piece is the tail.  Pieces are joined by a launch of their own, 5 us, and pass through memory as
+// float32, 0.2 us a MB written and read.  8B heads, us, uncut / the longest unit in 2, 4, 8, 24 pieces (chosen):
+//   19 rows behind 6005 tokens 96 / 56, 34, 23, 18 (24);  512 behind 8000 133 / 86, 78, 85, 84 (2);  512 behind 1024 31.5 (1) / 33, 33, 45, 40
+//   512 rows 16.1 (1) / 25, 27, 40, 40;  1024 rows 24.8 (1) / 41, 47, 47, 47;  2000 rows beside 100 behind 8000 145 / 93, 71, 71, 77 (3: 77)
+// Returns the workgroups for each kv head, *rows_cut the rows to join.
+static int kv4_prompt_cuts(Kv4PromptArgs &a, int *rows_cut) {
+    const int G = a.Hq / a.Hkv;
+    const double tile_us = a.hd == 128 ? 0.85 : 0.5;
+    int units = 0, most = 0;
+    double tiles = 0;
+    auto n_units = [&](int r) { return ((a.seq.cu[r + 1] - a.seq.cu[r]) * G + KV4_COLS - 1) / KV4_COLS; };
+    auto longest = [&](int r) { return (a.seq.start[r] + a.seq.cu[r + 1] - a.seq.cu[r] + 63) / 64; };   // key tiles of its last unit
+    for (int r = 0; r < a.seq.n_req; ++r)
+        if (const int u = n_units(r)) {
+            units += u;
+            tiles += 0.5 * u * ((a.seq.start[r] + 63) / 64 + longest(r) + 1);
+            most = std::max(most, longest(r));
+        }
+    if (units == 0) return 0;
+    const double even = tiles * a.Hkv / 256 * tile_us;
+    const bool folds = units * a.Hkv > 256 && units * a.Hkv <= 512;
+    int best = most;   // key tiles of a piece at most
+    double best_us = 0;
+    for (int c = 1; c <= 64; c += std::max(1, c / 2)) {   // pieces of the longest unit
+        const int share = (most + c - 1) / c;
+        if (c > 1 && share < KV4_MIN_TILES) break;
+        int n = 0, pieces = 0;
+        double mb = 0;
+        for (int r = 0; r < a.seq.n_req; ++r) {
+            const int u = n_units(r), cut = u ? (longest(r) + share - 1) / share : 1;
+            n += u * cut;
+            if (cut > 1) {
+                pieces += u * a.Hkv * cut;
+                mb += 1e-6 * (a.seq.cu[r + 1] - a.seq.cu[r]) * a.Hq * cut * a.hd * 4;
+            }
+        }
+        if (pieces > KV4_PIECES) break;
+        const double tail = share * tile_us * (n * a.Hkv <= 256 ? 1.12 : folds && c == 1 ? 1.3 : 1.95);
+        const double us = std::max(even, tail) + (pieces ? 5 + 0.4 * mb : 0);
+        if (c == 1 || us < best_us) best = share, best_us = us;
+    }
+    int n = 0, rows = 0, pieces = 0;
+    for (int r = 0; r < a.seq.n_req; ++r) {
+        const int u = n_units(r), cut = u ? (longest(r) + best - 1) / best : 1;
+        a.first[r] = n;
+        a.base[r] = pieces * KV4_COLS;
+        a.row[r] = rows;
+        a.cut[r] = cut;
+        n += u * cut;
+        if (cut > 1) {
+            pieces += u * a.Hkv * cut;
+            rows += a.seq.cu[r + 1] - a.seq.cu[r];
+        }
+    }
     // workgroups that all run at once, two a compute unit: the shorter half in rising order, beside the longer (2048 rows 52.7 -> 48.0 us)
-    a.fold = a.n_chunks == 1 && wgs > 256 && wgs <= 512 ? 256 : 0;
-    const dim3 grid(wgs, a.n_chunks);
-    if (a.hd == 128) hipLaunchKernelGGL(kv4_prefill_kernel<128>, grid, dim3(256), 2 * Kv4Lds<128>::TILE, st, a);
-    else hipLaunchKernelGGL(kv4_prefill_kernel<64>, grid, dim3(256), 2 * Kv4Lds<64>::TILE, st, a);
-    if (a.n_chunks > 1) launch_kv4_merge(st, a, a.seq.cu[a.seq.n_req]);
+    a.fold = folds && n == units ? 256 : 0;
+    *rows_cut = rows;
+    return n;
+}
+
+void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &args) {
+    Kv4PromptArgs a = args;
+    int rows = 0;
+    const int n = kv4_prompt_cuts(a, &rows);
+    if (n == 0) return;
+    if (a.hd == 128) hipLaunchKernelGGL(kv4_prefill_kernel<128>, dim3(a.Hkv * n), dim3(256), 2 * Kv4Lds<128>::TILE, st, a);
+    else hipLaunchKernelGGL(kv4_prefill_kernel<64>, dim3(a.Hkv * n), dim3(256), 2 * Kv4Lds<64>::TILE, st, a);
+    if (rows == 0) return;
+    if (a.hd == 128) hipLaunchKernelGGL(kv4_prompt_merge_kernel<128>, dim3(a.Hkv, rows), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(kv4_prompt_merge_kernel<64>, dim3(a.Hkv, rows), dim3(256), 0, st, a);
 }

@@ -1004,7 +1004,7 @@ struct OnDevice {
 // (row, query head) pieces that a side's attention can leave: the split launches of prompts, and those of `rows` decode rows.
 size_t kv4_pieces(const rs_ctx *c, bool prefill, int rows) {
     const rs_model_desc &m = c->m;
-    size_t n = prefill ? (size_t)KV4_SPLIT_WGS * 128 : 0;
+    size_t n = prefill ? (size_t)KV4_PIECES * 128 : 0;
     if (rows > 0) n = std::max(n, (size_t)kv4_most_pieces((int64_t)rows * m.n_kv_heads, c->lim.max_context) * (m.n_q_heads / m.n_kv_heads));
     return n;
 }
@@ -1646,7 +1646,8 @@ int32_t rs_kv4_prefill_attention(rs_ctx *c, int32_t layer, const void *q, int64_
     if (rc) return rc;
     const int width = c->m.n_q_heads * c->m.head_dim;
     if ((rc = check_kv4_rows("q", q, q_stride, width)) || (rc = check_kv4_rows("out", out, out_stride, width))) return rc;
-    Kv4AttnArgs a = kv4_attn_args(c, RS_SIDE_PREFILL, layer, q, q_stride, out, out_stride, tables, max_blk);
+    Kv4PromptArgs a{};
+    (Kv4AttnArgs &)a = kv4_attn_args(c, RS_SIDE_PREFILL, layer, q, q_stride, out, out_stride, tables, max_blk);
     if ((rc = kv4_runs(cu_seqlens, start_pos, n_req, max_blk, &a.seq))) return rc;
     if (a.seq.cu[n_req] > c->lim.max_prefill_tokens)
         return fail(RS_ERR_BAD_ARG, "%d rows, the limit is %d", a.seq.cu[n_req], c->lim.max_prefill_tokens);
