@@ -7,6 +7,7 @@ ImportError-like failure at first use.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from typing import Optional, Sequence
@@ -119,6 +120,8 @@ def load() -> ctypes.CDLL:
         for name in EXPORTS:
             if name != "rs_last_error":
                 getattr(lib, name).restype = ctypes.c_int32
+        for name, kinds in _KV4_ARGS.items():
+            getattr(lib, name).argtypes = [_ARG[k] for k in kinds]
         _lib = lib
     return _lib
 
@@ -133,13 +136,26 @@ def _i32(a) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.int32)
 
 
+# argument types of the calls on the 4-bit cache (c: context, i: int32, l: int64, p: pointer); with them ctypes takes plain integers,
+# which is half of what a call of one row costs on the host
+_ARG = {"c": ctypes.c_void_p, "i": ctypes.c_int32, "l": ctypes.c_int64, "p": ctypes.c_void_p}
+_KV4_ARGS = {"rs_kv4_write": "ciipplppipi", "rs_kv4_read": "ciipplppipi", "rs_kv4_append": "ciipplppii", "rs_kv4_decode_attention": "ciplplppiii",
+             "rs_kv4_prefill_attention": "ciplplppipi"}
+
+
 def _runs(cu_seqlens, start_pos):
-    """cu_seqlens, their number of runs and start_pos (None: null) as ctypes arguments."""
+    """cu_seqlens and start_pos (None: null) as int32 arrays, and the number of runs."""
     n = len(cu_seqlens) - 1
     if start_pos is not None and len(start_pos) != n:
         raise ValueError(f"{len(start_pos)} first positions for {n} requests")
-    sp = (ctypes.c_int32 * max(n, 1))(*map(int, start_pos)) if start_pos is not None else None
-    return (ctypes.c_int32 * (n + 1))(*map(int, cu_seqlens)), ctypes.c_int32(n), sp
+    return array.array("i", cu_seqlens), n, array.array("i", start_pos) if start_pos is not None else None
+
+
+def _addr(x) -> Optional[int]:
+    """Address of a torch tensor's or an array's first element (an int is one already, None is null)."""
+    if x is None or isinstance(x, int):
+        return x
+    return x.buffer_info()[0] if isinstance(x, array.array) else x.data_ptr()
 
 
 def _ptr(x) -> ctypes.c_void_p:
@@ -300,28 +316,25 @@ class Context:
     # -- the cache held in 4 bits
     def kv4_write(self, side: int, layer: int, k, v, row_stride: int, cu_seqlens: Sequence[int], start_pos, block_tables, max_blk: int):
         cu, n, sp = _runs(cu_seqlens, start_pos)
-        _check(self._lib.rs_kv4_write(self._h, ctypes.c_int32(side), ctypes.c_int32(layer), _ptr(k), _ptr(v), ctypes.c_int64(row_stride),
-                                      cu, sp, n, _ptr(block_tables), ctypes.c_int32(max_blk)))
+        _check(self._lib.rs_kv4_write(self._h, side, layer, _addr(k), _addr(v), row_stride, _addr(cu), _addr(sp), n, _addr(block_tables), max_blk))
 
     def kv4_append(self, side: int, layer: int, k, v, row_stride: int, ctx_lens, block_tables, max_blk: int, B: int):
-        _check(self._lib.rs_kv4_append(self._h, ctypes.c_int32(side), ctypes.c_int32(layer), _ptr(k), _ptr(v), ctypes.c_int64(row_stride),
-                                       _ptr(ctx_lens), _ptr(block_tables), ctypes.c_int32(max_blk), ctypes.c_int32(B)))
+        _check(self._lib.rs_kv4_append(self._h, side, layer, _addr(k), _addr(v), row_stride, _addr(ctx_lens), _addr(block_tables), max_blk, B))
 
     def kv4_read(self, side: int, layer: int, k_out, v_out, row_stride: int, cu_seqlens: Sequence[int], start_pos, block_tables, max_blk: int):
         cu, n, sp = _runs(cu_seqlens, start_pos)
-        _check(self._lib.rs_kv4_read(self._h, ctypes.c_int32(side), ctypes.c_int32(layer), _ptr(k_out), _ptr(v_out), ctypes.c_int64(row_stride),
-                                     cu, sp, n, _ptr(block_tables), ctypes.c_int32(max_blk)))
+        _check(self._lib.rs_kv4_read(self._h, side, layer, _addr(k_out), _addr(v_out), row_stride, _addr(cu), _addr(sp), n, _addr(block_tables),
+                                     max_blk))
 
     def kv4_decode_attention(self, layer: int, q, q_stride: int, out, out_stride: int, ctx_lens, block_tables, max_blk: int, B: int, max_ctx: int):
-        _check(self._lib.rs_kv4_decode_attention(self._h, ctypes.c_int32(layer), _ptr(q), ctypes.c_int64(q_stride), _ptr(out),
-                                                 ctypes.c_int64(out_stride), _ptr(ctx_lens), _ptr(block_tables), ctypes.c_int32(max_blk),
-                                                 ctypes.c_int32(B), ctypes.c_int32(max_ctx)))
+        _check(self._lib.rs_kv4_decode_attention(self._h, layer, _addr(q), q_stride, _addr(out), out_stride, _addr(ctx_lens), _addr(block_tables),
+                                                 max_blk, B, max_ctx))
 
     def kv4_prefill_attention(self, layer: int, q, q_stride: int, out, out_stride: int, cu_seqlens: Sequence[int], start_pos, block_tables,
                               max_blk: int):
         cu, n, sp = _runs(cu_seqlens, start_pos)
-        _check(self._lib.rs_kv4_prefill_attention(self._h, ctypes.c_int32(layer), _ptr(q), ctypes.c_int64(q_stride), _ptr(out),
-                                                  ctypes.c_int64(out_stride), cu, sp, n, _ptr(block_tables), ctypes.c_int32(max_blk)))
+        _check(self._lib.rs_kv4_prefill_attention(self._h, layer, _addr(q), q_stride, _addr(out), out_stride, _addr(cu), _addr(sp), n,
+                                                  _addr(block_tables), max_blk))
 
     # -- CU split / manager
     def set_cu_split(self, prefill_cus: int, decode_cus: int):
