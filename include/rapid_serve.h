@@ -134,9 +134,11 @@ typedef struct {
  * split (256,256).  pool may have null pointers only for RS_HOST_ONLY.  prof may be NULL. */
 int32_t rs_init(const rs_model_desc *model, const rs_pool_desc *pool, const rs_limits *limits,
                 const rs_profile *prof, int32_t device, rs_ctx **out);
-/* rs_init for a context whose cache is held in 4 bits.  Allocates two more workspaces, for attention whose rows more than
- * one workgroup computes (34 MB and what the decode rows' 512-token chunks need, as for the bf16 cache, on each side that
- * runs such attention). */
+/* rs_init for a context whose cache is held in 4 bits.  Every call that serves a bf16 cache serves it too, layer passes
+ * (dense and sparse feed-forward blocks), captured and hybrid ones, rs_step_tokens and the engine, but for
+ * rs_decode_layer_noalloc (RS_ERR_STATE).  Allocates two more workspaces, for attention whose rows more than one workgroup
+ * computes: 131072 partial rows of head_dim + 2 floats on the prefill side (68 MB at head_dim 128), and on each side that
+ * serves decode rows as many as max_decode_batch and max_context may need (at least 512 for each query head of a KV head). */
 int32_t rs_init_kv4(const rs_model_desc *model, const rs_kv4_desc *pool, const rs_limits *limits,
                     const rs_profile *prof, int32_t device, rs_ctx **out);
 /* Waits for both sides, frees everything the library owns. */
@@ -231,6 +233,7 @@ int32_t rs_decode_layer(rs_ctx *ctx, int32_t layer, const void *x_in, void *x_ou
  * ... of request r (host arrays; start_pos may be null: all 0; any position may start a run, a run may be empty, n_req is 1 to
  * RS_MAX_PREFILL_REQS).  Tokens outside the runs keep what they hold.
  * rs_kv4_append: one token of each of B requests, row i at position ctx_lens[i] (device), -1: no request, nothing is done.
+ *   No two rows may be the same position of the same request.
  * rs_kv4_read: the inverse of rs_kv4_write, exactly what the cache holds as bf16.
  * RS_ERR_BAD_ARG for a null or misaligned pointer or a bad size, RS_ERR_BAD_BLOCK for a table too short for a run. */
 int32_t rs_kv4_write(rs_ctx *ctx, int32_t side, int32_t layer, const void *k, const void *v, int64_t row_stride,
@@ -244,8 +247,12 @@ int32_t rs_kv4_read(rs_ctx *ctx, int32_t side, int32_t layer, void *k_out, void 
 /* Attention over the cache, softmax(q K^T / sqrt(head_dim)) V of every query head, on the DECODE side: row i of q (rotated;
  * n_q_heads * head_dim elements) attends to ctx_lens[i] + 1 cached tokens (the newest one included, as rs_kv4_append leaves it).
  * ctx_lens[i] = -1: a row without a request, its output is zero.  B <= max_decode_batch, max_ctx (host) bounds
- * ctx_lens[i] + 1 as for rs_decode_layer.  Results depend on the sizes alone, not on the CU split.
- * A score whose key or value group is not finite is NaN, and so is its row's output for that head. */
+ * ctx_lens[i] + 1 as for rs_decode_layer (a bound near the longest context serves best).  Results depend on the sizes alone,
+ * max_ctx among them (it decides how contexts are cut), not on the CU split.
+ * A key's group that is not finite makes the rows that see it NaN in the heads of its KV head, a value's group at least the
+ * 32 dims of it (all of them where several rows are computed together, as rs_kv4_prefill_attention does).
+ * The calls may be recorded into a caller's graph from the side's stream (rs_get_stream).  Attention uses the side's
+ * workspaces: replay such a graph on that stream, or in order with it. */
 int32_t rs_kv4_decode_attention(rs_ctx *ctx, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
                                 const int32_t *ctx_lens, const int32_t *block_tables, int32_t max_blk, int32_t B,
                                 int32_t max_ctx);
@@ -268,7 +275,8 @@ int32_t rs_kv4_prefill_attention(rs_ctx *ctx, int32_t layer, const void *q, int6
  * long as the graph is reused, and block_tables rows must be long enough for it
  * (RS_ERR_BAD_BLOCK otherwise).  After rs_set_cu_split the decode stream differs and a new graph
  * is captured under the new mask.  At most 256 graphs are cached per context (RS_ERR_STATE);
- * rs_destroy frees them.  Results are bit-identical to rs_decode_layer's. */
+ * rs_destroy frees them.  Results are bit-identical to rs_decode_layer's (over a cache held in 4 bits: with
+ * max_ctx = max_ctx_bucket, which decides there how contexts are cut). */
 int32_t rs_decode_layer_graph(rs_ctx *ctx, int32_t layer, const void *x_in, void *x_out,
                               const int32_t *ctx_lens, const int32_t *block_tables, int32_t max_blk,
                               int32_t B, int32_t max_ctx_bucket);
@@ -299,7 +307,7 @@ int32_t rs_hybrid_layer(rs_ctx *ctx, int32_t layer, const void *x_in, void *x_ou
  * 32 MiB per GPU, held until the process ends; the call allocates nothing and calls nothing that
  * allocates.  A step that needs more (it grows with B, d_model, ffn_dim and max_ctx: the
  * Llama-3-8B-shaped layer at B = 64 and contexts up to 4096 needs 29 MB) is refused with RS_ERR_BAD_ARG and
- * nothing is enqueued; a layer with a sparse feed-forward block is refused with RS_ERR_STATE.  Every
+ * nothing is enqueued; a layer with a sparse feed-forward block, or a cache held in 4 bits, is refused with RS_ERR_STATE.  Every
  * context of the process on one GPU shares that GPU's array: calls that overlap on one GPU (two contexts,
  * or a captured graph replayed while another call runs) race on it; calls on one context's decode stream
  * are ordered and safe.  The array keeps the previous call's contents; the call clears what must start

@@ -598,7 +598,7 @@ __device__ __forceinline__ void qkv_finish(const QkvEpiArgs &a, const QkvPlace &
     bf16_t *row = a.qkv + (size_t)m * (n_heads * HD) + head * HD;
     *(bf16x4 *)(row + i0) = olo;
     *(bf16x4 *)(row + half + i0) = ohi;
-    if (head < a.Hq || !p.pos_ok) return;
+    if (head < a.Hq || !p.pos_ok || !a.k_pool) return;   // (no pool: a cache held in 4 bits, written by its own kernel)
     if ((unsigned)p.blk >= (unsigned)a.n_blocks) {
         if (of_head && head == a.Hq) atomicOr(a.err_flag, 2);
         return;

@@ -178,8 +178,8 @@ __global__ __launch_bounds__(256) void rope_kvwrite_kernel(RopeKvArgs a, int v_b
     const int bi = pos / RS_BLOCK_TOKENS, slot = pos % RS_BLOCK_TOKENS;
     int blk = -1;
     if (bi < a.max_blk) blk = a.tables[(size_t)req * a.max_blk + bi];
-    const bool blk_ok = (unsigned)blk < (unsigned)a.n_blocks;
-    if (!blk_ok && tid == 0) atomicOr(a.err_flag, 2);
+    const bool blk_ok = a.k_pool && (unsigned)blk < (unsigned)a.n_blocks;   // (no pool: the rotated k stays in its row for another kernel)
+    if (!blk_ok && a.k_pool && tid == 0) atomicOr(a.err_flag, 2);
 
     const int hd = a.hd, half = hd >> 1;
     const int cph = half >> 3;  // 8-element chunks per half head
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(256) void rope_kvwrite_kernel(RopeKvArgs a, int v_b
             olo[i] = (bf16_t)(x0 * cs.c - x1 * cs.s);
             ohi[i] = (bf16_t)(x1 * cs.c + x0 * cs.s);
         }
-        if (head < a.Hq) {
+        if (head < a.Hq || !a.k_pool) {
             st_bf16x8(hp + c * 8, olo);
             st_bf16x8(hp + half + c * 8, ohi);
         } else if (blk_ok) {
@@ -227,7 +227,7 @@ __global__ __launch_bounds__(256) void rope_kvwrite_kernel(RopeKvArgs a, int v_b
 void launch_rope_kvwrite(hipStream_t st, const RopeKvArgs &a) {
     if (a.M <= 0) return;
     int v_blocks = 0;   // prefill: one more workgroup per 16-token block of each prompt
-    if (!a.ctx_lens)
+    if (!a.ctx_lens && a.k_pool)
         for (int r = 0; r < a.seq.n_req; ++r)
             v_blocks += (a.seq.cu[r + 1] - a.seq.cu[r] + RS_BLOCK_TOKENS - 1) / RS_BLOCK_TOKENS;
     hipLaunchKernelGGL(rope_kvwrite_kernel, dim3(row_grid(a.M) + v_blocks), dim3(256), 0, st, a, v_blocks);

@@ -17,7 +17,7 @@ static int row_grid(int M) { return M < 128 ? M : (M + 127) / 128 * 128; }
 struct RopeKvArgs {
     bf16_t *qkv;            // [M][nqkv]; q part rotated in place
     const CosSin *table;    // [max_pos][hd/2]
-    bf16_t *k_pool;         // this layer: [n_blocks][Hkv][16][hd]
+    bf16_t *k_pool;         // this layer: [n_blocks][Hkv][16][hd], or nullptr: rotate only, k in place as well
     bf16_t *v_pool;         // this layer: [n_blocks][Hkv][hd][16]
     const int32_t *tables;  // [n_req][max_blk]
     const int32_t *ctx_lens;  // decode: position of row m (and request = m); prefill: nullptr
@@ -80,6 +80,7 @@ struct Kv4RowsArgs {
     const int32_t *ctx_lens;  // append: position of row m's token, -1: none
     int32_t *err_flag;
     int B, Hkv, hd, max_blk, n_blocks;
+    int max_pos;              // append: positions from here on are not written
     SeqInfo seq;              // write, read: request r's rows are its tokens start[r] ..
     int32_t first[RS_MAX_RUNS];   // set by the launchers: blocks that the requests before touch
 };
@@ -236,7 +237,7 @@ struct QkvEpiArgs {
     float eps;
     bf16_t *qkv;              // out: [M][(Hq+2Hkv)*hd] with q and k rotated
     const CosSin *table;
-    bf16_t *k_pool, *v_pool;  // this layer
+    bf16_t *k_pool, *v_pool;  // this layer, or nullptr: no cache write
     const int32_t *tables, *ctx_lens;   // of the decode rows [T, M)
     int32_t *err_flag;
     int M, Hq, Hkv, hd, max_blk, n_blocks, max_pos;

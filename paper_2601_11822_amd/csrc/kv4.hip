@@ -222,7 +222,7 @@ __global__ __launch_bounds__(HD) void kv4_append_kernel(Kv4RowsArgs a) {
     const int j = threadIdx.x & (HD / 2 - 1), g = j >> 4;
     const uint32_t x = *(const uint32_t *)((is_v ? a.v : a.k) + (size_t)row * a.row_stride + hk * HD + 2 * j);
     const int pos = a.ctx_lens[row];
-    if (pos == -1) return;   // a row without a request
+    if (pos == -1 || pos >= a.max_pos) return;   // a row without a request, or one without a rotary position (reported by the rotation)
     int blk = -1;
     if (pos >= 0 && (pos >> 4) < a.max_blk) blk = a.tables[(size_t)row * a.max_blk + (pos >> 4)];
     if ((unsigned)blk >= (unsigned)a.n_blocks) {

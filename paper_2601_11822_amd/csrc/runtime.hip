@@ -545,7 +545,6 @@ int32_t check_layer_call(rs_ctx *c, int side, int32_t layer, const void *x_in, v
     if (!c) return fail(RS_ERR_BAD_ARG, "null context");
     if (!c->gpu) return fail(RS_ERR_STATE, "host-only context cannot run layers");
     if (layer < 0 || layer >= c->m.n_layers) return fail(RS_ERR_BAD_ARG, "layer %d out of range", layer);
-    if (c->is_kv4) return fail(RS_ERR_STATE, "layer passes need the bf16 cache");
     if (!c->have_weights[layer]) return fail(RS_ERR_STATE, "weights of layer %d not set", layer);
     if (!x_in || !x_out || !tables) return fail(RS_ERR_BAD_ARG, "null pointer");
     if (c->side[side].cus <= 0) return fail(RS_ERR_STATE, "side %d has no compute units in the current split", side);
@@ -624,6 +623,85 @@ void lend_partials(PrefillAttnArgs &pa, const Workspace &w, int cus) {
     pa.park_cap = w.partial_cap;
 }
 
+// ---- a layer's cache held in 4 bits: its two steps between the QKV projection and the output projection ----
+Kv4RowsArgs kv4_rows_args(rs_ctx *c, int side, int32_t layer, int64_t row_stride, const int32_t *tables, int32_t max_blk) {
+    Kv4RowsArgs a{};
+    a.row_stride = (size_t)row_stride;
+    a.pool = c->kv4 + (size_t)layer * c->kv4_stride;
+    a.tables = tables;
+    a.err_flag = c->err_flag + side;
+    a.Hkv = c->m.n_kv_heads;
+    a.hd = c->m.head_dim;
+    a.max_blk = max_blk;
+    a.n_blocks = c->pool.n_blocks;
+    a.max_pos = INT32_MAX;
+    return a;
+}
+
+Kv4AttnArgs kv4_attn_args(rs_ctx *c, int side, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                          const int32_t *tables, int32_t max_blk) {
+    Kv4AttnArgs a{};
+    a.q = (const bf16_t *)q;
+    a.q_stride = (size_t)q_stride;
+    a.out = (bf16_t *)out;
+    a.out_stride = (size_t)out_stride;
+    a.pool = c->kv4 + (size_t)layer * c->kv4_stride;
+    a.tables = tables;
+    a.err_flag = c->err_flag + side;
+    a.part_o = c->kv4_part_o[side];
+    a.part_ml = c->kv4_part_ml[side];
+    a.Hq = c->m.n_q_heads;
+    a.Hkv = c->m.n_kv_heads;
+    a.hd = c->m.head_dim;
+    a.max_blk = max_blk;
+    a.n_blocks = c->pool.n_blocks;
+    a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c->m.head_dim));
+    return a;
+}
+
+// T prompt rows placed by seq, then B decode rows, of q | k | v rows with rotated q and k.
+struct Kv4Rows {
+    int T;
+    const SeqInfo &seq;
+    const int32_t *ptables;
+    int32_t max_blk_p;
+    int B;
+    const int32_t *ctx_lens, *dtables;
+    int32_t max_blk_d, max_ctx;
+};
+
+void kv4_store(rs_ctx *c, int side, Workspace &w, int32_t layer, const Kv4Rows &r) {
+    const rs_model_desc &m = c->m;
+    const size_t nqkv = (size_t)(m.n_q_heads + 2 * m.n_kv_heads) * m.head_dim;
+    const bf16_t *k = w.qkv + (size_t)m.n_q_heads * m.head_dim, *v = k + (size_t)m.n_kv_heads * m.head_dim;
+    if (r.T > 0) {
+        Kv4RowsArgs a = kv4_rows_args(c, side, layer, nqkv, r.ptables, r.max_blk_p);
+        a.k = k, a.v = v, a.seq = r.seq;
+        launch_kv4_write(c->side[side].stream, a);
+    }
+    if (r.B > 0) {
+        Kv4RowsArgs a = kv4_rows_args(c, side, layer, nqkv, r.dtables, r.max_blk_d);
+        a.k = k + r.T * nqkv, a.v = v + r.T * nqkv, a.ctx_lens = r.ctx_lens, a.B = r.B, a.max_pos = m.max_pos;
+        launch_kv4_append(c->side[side].stream, a);
+    }
+}
+
+void kv4_attend(rs_ctx *c, int side, Workspace &w, int32_t layer, const Kv4Rows &r) {
+    const rs_model_desc &m = c->m;
+    const size_t nqkv = (size_t)(m.n_q_heads + 2 * m.n_kv_heads) * m.head_dim;
+    if (r.T > 0) {
+        Kv4PromptArgs a{};
+        (Kv4AttnArgs &)a = kv4_attn_args(c, side, layer, w.qkv, nqkv, w.attn, 0, r.ptables, r.max_blk_p);
+        a.out_Mt = packed_mt(r.T + r.B), a.seq = r.seq;
+        launch_kv4_prefill(c->side[side].stream, a);
+    }
+    if (r.B > 0) {
+        Kv4AttnArgs a = kv4_attn_args(c, side, layer, w.qkv + r.T * nqkv, nqkv, w.attn, 0, r.dtables, r.max_blk_d);
+        a.out_Mt = packed_mt(r.T + r.B), a.out_row0 = r.T, a.ctx_lens = r.ctx_lens, a.B = r.B, a.max_ctx = r.max_ctx;
+        launch_kv4_decode(c->side[side].stream, a);
+    }
+}
+
 // A pass of at most RS_STREAM_ROWS rows through a dense layer: T prompt rows (prompts or later chunks of them, placed by
 // seq), then B decode rows.  Every projection is a stream of its weights with the RMSNorm of its input folded in
 // (decode_gemm.hip), and the kernels in between belong to their producers: QKV stream, its epilogue (row scale, rotary,
@@ -673,6 +751,8 @@ int32_t stream_layer(rs_ctx *c, int side, Workspace &w, int32_t layer, const voi
     }
     qe.S_ssq = S_ssq;
     if (!few_q) launch_qkv_rope_epilogue(st, qe);
+    const Kv4Rows rows4{T, seq, ptables, max_blk_p, B, ctx_lens, dtables, max_blk_d, max_ctx};
+    if (c->is_kv4) kv4_store(c, side, w, layer, rows4);
     tick(c, side, 2);
     tick(c, side, 3);
     PrefillAttnArgs pa{w.qkv, nqkv, w.attn, kp, vp, ptables, err, m.n_q_heads, m.n_kv_heads, hd, max_blk_p, c->pool.n_blocks, sl2, seq};
@@ -684,7 +764,8 @@ int32_t stream_layer(rs_ctx *c, int side, Workspace &w, int32_t layer, const voi
     da.out_row0 = T;
     da.out_Mt = packed_mt(M);
     da.n_keys = n_keys;
-    if (T > 0 && B > 0) launch_hybrid_attention(st, pa, da);
+    if (c->is_kv4) kv4_attend(c, side, w, layer, rows4);
+    else if (T > 0 && B > 0) launch_hybrid_attention(st, pa, da);
     else if (T > 0) launch_prefill_attention(st, pa);
     else launch_decode_attention(st, da);
     tick(c, side, 4);
@@ -737,6 +818,7 @@ bool qkv_project(rs_ctx *c, int side, Workspace &w, int32_t layer, bool skinny, 
     if (const int S = skinny ? 0 : launch_gemm_tiled_partials(st, g)) {
         launch_qkv_rope_epilogue(st, QkvEpiArgs{w.partials, nullptr, S, 0, nqkv, d, m.rms_eps, w.qkv, c->rope, kp, vp, dtables, ctx_lens, err, M,
                                                 m.n_q_heads, m.n_kv_heads, hd, max_blk_d, c->pool.n_blocks, m.max_pos, T, ptables, max_blk_p, seq});
+        if (c->is_kv4) kv4_store(c, side, w, layer, Kv4Rows{T, seq, ptables, max_blk_p, B, ctx_lens, dtables, max_blk_d, 0});
         tick(c, side, 2);
         tick(c, side, 3);
         return true;
@@ -751,6 +833,7 @@ bool qkv_project(rs_ctx *c, int side, Workspace &w, int32_t layer, bool skinny, 
     if (B > 0)
         launch_rope_kvwrite(st, RopeKvArgs{w.qkv + (size_t)T * nqkv, c->rope, kp, vp, dtables, ctx_lens, err, B, m.n_q_heads,
                                            m.n_kv_heads, hd, max_blk_d, c->pool.n_blocks, m.max_pos, SeqInfo{}});
+    if (c->is_kv4) kv4_store(c, side, w, layer, Kv4Rows{T, seq, ptables, max_blk_p, B, ctx_lens, dtables, max_blk_d, 0});
     tick(c, side, 3);
     return ok;
 }
@@ -794,7 +877,8 @@ int32_t prefill_layer(rs_ctx *c, int32_t layer, const void *x_in, void *x_out, c
     PrefillAttnArgs pa{w.qkv, nqkv, w.attn, kp, vp, tables, c->err_flag + RS_SIDE_PREFILL, m.n_q_heads, m.n_kv_heads, hd,
                        max_blk, c->pool.n_blocks, (float)(1.4426950408889634 / std::sqrt((double)hd)), seq};
     lend_partials(pa, w, c->side[RS_SIDE_PREFILL].cus);
-    launch_prefill_attention(st, pa);
+    if (c->is_kv4) kv4_attend(c, RS_SIDE_PREFILL, w, layer, Kv4Rows{T, seq, tables, max_blk, 0, nullptr, nullptr, 0, 0});
+    else launch_prefill_attention(st, pa);
     tick(c, RS_SIDE_PREFILL, 4);
     ok = run_post_attention(c, RS_SIDE_PREFILL, st, w, lw, c->packed[layer], c->moe[layer], (const bf16_t *)x_in, (bf16_t *)x_out, T, skinny) && ok;
     HIP_TRY(hipGetLastError());
@@ -860,7 +944,9 @@ int32_t hybrid_layer(rs_ctx *c, int32_t layer, const void *x_in, void *x_out, co
                        max_blk_p, c->pool.n_blocks, sl2, seq};
     pa.Mt_out = packed_mt(M);
     lend_partials(pa, w, c->side[RS_SIDE_PREFILL].cus);
-    if (B > 0) {
+    if (c->is_kv4) {
+        kv4_attend(c, RS_SIDE_PREFILL, w, layer, Kv4Rows{T, seq, ptables, max_blk_p, B, ctx_lens, dtables, max_blk_d, max_ctx});
+    } else if (B > 0) {
         DecodeAttnArgs da{w.qkv + (size_t)T * nqkv, nqkv, w.attn, kp, vp, dtables, ctx_lens, err, w.part_o, w.part_ml,
                           B, m.n_q_heads, m.n_kv_heads, hd, max_blk_d, c->pool.n_blocks, max_ctx,
                           (max_ctx + RS_DECODE_CHUNK - 1) / RS_DECODE_CHUNK, sl2, c->side[RS_SIDE_PREFILL].cus < RS_TOTAL_CUS};
@@ -910,7 +996,8 @@ int32_t decode_layer(rs_ctx *c, Workspace &w, int32_t layer, const void *x_in, v
                       B, m.n_q_heads, m.n_kv_heads, hd, max_blk, c->pool.n_blocks, max_ctx,
                       (max_ctx + RS_DECODE_CHUNK - 1) / RS_DECODE_CHUNK,
                       (float)(1.4426950408889634 / std::sqrt((double)hd)), c->side[RS_SIDE_DECODE].cus < RS_TOTAL_CUS};
-    launch_decode_attention(st, da);
+    if (c->is_kv4) kv4_attend(c, RS_SIDE_DECODE, w, layer, Kv4Rows{0, none, nullptr, 0, B, ctx_lens, tables, max_blk, max_ctx});
+    else launch_decode_attention(st, da);
     tick(c, RS_SIDE_DECODE, 4);
     ok = run_post_attention(c, RS_SIDE_DECODE, st, w, lw, c->packed[layer], c->moe[layer], (const bf16_t *)x_in, (bf16_t *)x_out, B, skinny) && ok;
     HIP_TRY(hipGetLastError());
@@ -1059,40 +1146,6 @@ int32_t kv4_runs(const int32_t *cu, const int32_t *start, int32_t n_req, int32_t
         seq->start[r] = first;
     }
     return RS_OK;
-}
-
-Kv4RowsArgs kv4_rows_args(rs_ctx *c, int side, int32_t layer, int64_t row_stride, const int32_t *tables, int32_t max_blk) {
-    Kv4RowsArgs a{};
-    a.row_stride = (size_t)row_stride;
-    a.pool = c->kv4 + (size_t)layer * c->kv4_stride;
-    a.tables = tables;
-    a.err_flag = c->err_flag + side;
-    a.Hkv = c->m.n_kv_heads;
-    a.hd = c->m.head_dim;
-    a.max_blk = max_blk;
-    a.n_blocks = c->pool.n_blocks;
-    return a;
-}
-
-Kv4AttnArgs kv4_attn_args(rs_ctx *c, int side, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
-                          const int32_t *tables, int32_t max_blk) {
-    Kv4AttnArgs a{};
-    a.q = (const bf16_t *)q;
-    a.q_stride = (size_t)q_stride;
-    a.out = (bf16_t *)out;
-    a.out_stride = (size_t)out_stride;
-    a.pool = c->kv4 + (size_t)layer * c->kv4_stride;
-    a.tables = tables;
-    a.err_flag = c->err_flag + side;
-    a.part_o = c->kv4_part_o[side];
-    a.part_ml = c->kv4_part_ml[side];
-    a.Hq = c->m.n_q_heads;
-    a.Hkv = c->m.n_kv_heads;
-    a.hd = c->m.head_dim;
-    a.max_blk = max_blk;
-    a.n_blocks = c->pool.n_blocks;
-    a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c->m.head_dim));
-    return a;
 }
 
 int32_t check_head_call(rs_ctx *c, int side, int n) {
@@ -1664,6 +1717,7 @@ int32_t rs_decode_layer_noalloc(rs_ctx *c, int32_t layer, const void *x_in, void
     int32_t rc = check_layer_call(c, RS_SIDE_DECODE, layer, x_in, x_out, block_tables);
     if (rc) return rc;
     if (c->moe[layer].E > 0) return fail(RS_ERR_STATE, "layer %d has a sparse feed-forward block: not served from the static scratch", layer);
+    if (c->is_kv4) return fail(RS_ERR_STATE, "a cache held in 4 bits is not served from the static scratch");
     if (B < 1 || max_ctx < 1) return fail(RS_ERR_BAD_ARG, "decode batch %d, max_ctx %d", B, max_ctx);
     unsigned char *base = (unsigned char *)g_static_scratch[c->device];
     if (!base) return fail(RS_ERR_STATE, "the static scratch array of device %d was not resolved", c->device);

@@ -31,7 +31,7 @@ import time
 
 import numpy as np
 
-from . import Context, RS_SIDE_DECODE, RS_SIDE_PREFILL
+from . import Context, RS_SIDE_DECODE, RS_SIDE_PREFILL, kv4_bytes
 
 
 def _log(*a):
@@ -55,19 +55,21 @@ def make_workload(n: int, rate: float, prompt_mean: float, prompt_sd: float, out
 
 
 def build_model(shape, n_layers: int, vocab: int, n_blocks: int, max_prefill: int, max_batch: int, max_context: int,
-                profile, device: int = 0, release: bool = False, experts: int = 0):
+                profile, device: int = 0, release: bool = False, experts: int = 0, kv4: bool = False):
     import torch
     dev = torch.device(f"cuda:{device}")
     g = torch.Generator(device=dev)
     g.manual_seed(0)
     Hkv, hd, d, f = shape.n_kv_heads, shape.head_dim, shape.d_model, shape.ffn_dim
-    k_pool = torch.zeros((n_layers, n_blocks, Hkv, 16, hd), dtype=torch.bfloat16, device=dev)
-    v_pool = torch.zeros((n_layers, n_blocks, Hkv, hd, 16), dtype=torch.bfloat16, device=dev)
-    c = Context.from_shape(shape, n_layers=n_layers, max_pos=max_context, n_blocks=n_blocks, k_pool=k_pool, v_pool=v_pool,
-                           max_prefill_tokens=max_prefill, max_decode_batch=max_batch, max_context=max_context,
+    if kv4:
+        pools = {"kv4_pool": torch.zeros((n_layers, n_blocks, Hkv, kv4_bytes(hd)), dtype=torch.uint8, device=dev)}
+    else:
+        pools = {"k_pool": torch.zeros((n_layers, n_blocks, Hkv, 16, hd), dtype=torch.bfloat16, device=dev),
+                 "v_pool": torch.zeros((n_layers, n_blocks, Hkv, hd, 16), dtype=torch.bfloat16, device=dev)}
+    c = Context.from_shape(shape, n_layers=n_layers, max_pos=max_context, n_blocks=n_blocks, **pools, max_prefill_tokens=max_prefill, max_decode_batch=max_batch, max_context=max_context,
                            profile=profile, device=device)
     rnd = lambda *s, std=0.02, mean=0.0: (torch.randn(s, generator=g, device=dev, dtype=torch.float32) * std + mean).to(torch.bfloat16)
-    keep = [k_pool, v_pool]
+    keep = list(pools.values())
     for l in range(n_layers):
         if experts:   # sparse feed-forward block: the experts' matrices are packed during the call and dropped here
             w = (rnd(d, mean=1.0), rnd(shape.qkv_dim, d), rnd(d, shape.q_dim), rnd(d, mean=1.0), None, None, None)
@@ -248,6 +250,7 @@ def main(argv=None):
                     help="with --profile measure: size of the prefill pass that runs beside the measured decode steps")
     ap.add_argument("--wait-decode", action="store_true", help="wait for each decode step (exact per-step GPU times)")
     ap.add_argument("--experts", type=int, default=0, help="sparse feed-forward block with this many experts (two per token)")
+    ap.add_argument("--kv4", action="store_true", help="hold the KV cache in 4 bits (rs_init_kv4): 3.76 times the tokens in the same memory")
     ap.add_argument("--release-weights", action="store_true", help="free each layer's row-major matrices after packing")
     ap.add_argument("--no-step-graphs", action="store_true", help="launch each decode step's kernels one by one (rs_set_step_graphs(0))")
     ap.add_argument("--engine", action="store_true", help="let the library's two threads drive (rs_engine_start)")
@@ -276,7 +279,7 @@ def main(argv=None):
                          (16, a.max_out), a.vocab, a.seed)
     t0 = time.time()
     c, keep = build_model(shape, a.layers, a.vocab, a.kv_tokens // 16, a.max_prompt, a.max_batch, a.max_prompt + a.max_out, prof,
-                          release=a.release_weights, experts=a.experts)
+                          release=a.release_weights, experts=a.experts, kv4=a.kv4)
     _log(f"[serve] model of {a.layers} layers built in {time.time() - t0:.1f}s; {a.requests} requests over "
          f"{work[-1][1]:.1f}s, {sum(len(w[2]) for w in work)} prompt tokens, {sum(w[3] for w in work)} to generate")
     if a.no_step_graphs:
@@ -300,7 +303,7 @@ def main(argv=None):
         rec = summarise(c, work, steps, wall)
     rec.update({"policy": a.policy, "shape": shape.name, "layers": a.layers, "rate_per_s": a.rate, "slo_ms": a.slo_ms,
                 "wait_decode": bool(a.wait_decode), "driver": "engine threads" if a.engine else "host step loop", "max_batch_cap": a.max_batch, "experts": a.experts, "data": "synthetic",
-                "chunk": a.chunk if a.policy == "hybrid" else None,
+                "kv_cache": "4-bit" if a.kv4 else "bf16", "chunk": a.chunk if a.policy == "hybrid" else None,
                 "step_graphs": rec.get("step_graphs") if not a.no_step_graphs else "off"})
     line = json.dumps(rec)
     print(line, flush=True)
