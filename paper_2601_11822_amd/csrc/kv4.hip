@@ -661,12 +661,11 @@ void kv4_kernels_init() {
 }
 
 // ---- attention: prompts and chunks of them ----------------------------------------------------------------------------------
-// Workgroup = (kv head, 128 columns, key range): a column is a (row, query head) pair, the G heads of the kv head beside each
-// other, so that 128 columns are 128 / G neighbouring rows and a chunk of few rows still fills the tiles.  Wave w owns 32
-// columns.  Keys come 64 (four blocks) at a time through two LDS buffers: K as its codes, V converted once for the four waves.
+// Workgroup = (kv head, 128 or 256 columns, key range): a column is a (row, query head) pair, the G heads of the kv head beside
+// each other, so that 128 columns are 128 / G neighbouring rows and a chunk of few rows still fills the tiles.  Wave w owns 32
+// columns.  Keys come 64 (four blocks) at a time through two LDS buffers: K as its codes, V converted once for all the waves.
 // V in LDS: per block two halves [hd][8 tokens], half i the quads i and 2 + i, the dims of a group even ones first: the order
 // in which a lane holds its scores, so the weights need no exchange between lanes.
-#define KV4_COLS 128
 #define KV4_MIN_TILES 4   // key tiles of a piece at least
 // Weights are at most 2^4: a bf16 is as fine there as below 1, and the accumulators are rescaled in a few tiles of a long prompt
 // instead of in two of five (16384 rows 1800 -> 1694 us; the error against float64 0.0019 -> 0.0020 of the result).
@@ -675,10 +674,12 @@ template <int HD> struct Kv4Lds {
     static constexpr int K = 4 * 8 * HD, KS = 4 * (HD / 2), V = 4 * 2 * HD * 16, TILE = K + KS + V;
 };
 
-template <int HD>
-__global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4PromptArgs a) {
+template <int HD, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void kv4_prefill_kernel(Kv4PromptArgs a) {
     using F = Kv4<HD>;
     using L = Kv4Lds<HD>;
+    constexpr int COLS = 32 * NW, WPB = NW / 4;   // waves that bring a block
+    static_assert(WPB == 1 || HD == 128, "a lane's share of a block");
     constexpr int G = F::G, KSTEP = HD / 64, DT = HD / 32;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem_kv4p[];
     const int hk = blockIdx.x % a.Hkv, Gq = a.Hq / a.Hkv;
@@ -688,13 +689,13 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4PromptArgs a) {
     const int req = last_at_most(a.first, a.seq.n_req, at);
     const int cut = a.cut[req], unit = (at - a.first[req]) / cut, split = (at - a.first[req]) % cut;
     const int row0 = a.seq.cu[req], len = a.seq.cu[req + 1] - row0, prior = a.seq.start[req];
-    const int n_cols = len * Gq, col0 = ((n_cols + KV4_COLS - 1) / KV4_COLS - 1 - unit) * KV4_COLS;   // the longest first
+    const int n_cols = len * Gq, col0 = ((n_cols + COLS - 1) / COLS - 1 - unit) * COLS;   // the longest first
     const int col = col0 + 32 * wave + c32;
     const bool valid = col < n_cols;
     const int colc = min(col, n_cols - 1), row = colc / Gq, hq = hk * Gq + colc % Gq;
     const int q_pos = prior + row;
     const int w_min = prior + min(col0 + 32 * wave, n_cols - 1) / Gq;
-    const int kv_end = prior + min(col0 + KV4_COLS - 1, n_cols - 1) / Gq + 1;
+    const int kv_end = prior + min(col0 + COLS - 1, n_cols - 1) / Gq + 1;
     const int n_tiles = (kv_end + 63) >> 6;
     // this workgroup's share of the key tiles
     const int kt0 = (int)((int64_t)n_tiles * split / cut), kt1 = (int)((int64_t)n_tiles * (split + 1) / cut);
@@ -714,24 +715,26 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4PromptArgs a) {
         for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
     const int32_t *tab = a.tables + (size_t)req * a.max_blk;
 
-    // A wave brings one block of a key tile: a lane HD/8 bytes of K's codes, the codes and scales of two V units (quads v_half
-    // and 2 + v_half, dim pair vj, UG groups from vg on), and the lanes of the first HD/8 bytes of K's scales.
-    constexpr int UG = G / 2;   // groups of a lane's V unit
-    const int vj = lane & 15, vg = ((lane >> 4) & 1) * UG, v_half = lane >> 5;
-    typedef uint32_t kvec __attribute__((ext_vector_type(HD / 32)));
+    // A wave (of eight: two) brings one block of a key tile: a lane its part of K's codes, the codes and scales of two V units (quads v_half
+    // and 2 + v_half, dim pair vj, UG groups from vg on) and a dword of K's scales.
+    constexpr int UG = G / (2 * WPB);   // groups of a lane's V unit
+    const int wb = wave / WPB, wp = wave % WPB;   // the wave's block, and which share of it
+    const int vj = lane & 15, vg = (2 * wp + ((lane >> 4) & 1)) * UG, v_half = lane >> 5;
+    const int k_scales = WPB == 1 ? lane & (HD / 8 - 1) : 4 * (wp + 2 * ((lane >> 2) & 1)) + (lane & 3);
+    typedef uint32_t kvec __attribute__((ext_vector_type(HD / 32 / WPB)));
     typedef uint32_t vvec __attribute__((ext_vector_type(UG)));
     kvec rk;
     uint32_t rks;
     vvec rv[2], rs[2];
     bool r_ok = true;      // whether the block of what was fetched is one of the pool
     int next_blk = 0;      // block of the tile to fetch next, asked for a tile ahead
-    auto block_at = [&](int kt) { return tab[min(kt * 4 + wave, (kv_end - 1) >> 4)]; };   // (behind the context: its last one, which nobody looks at)
+    auto block_at = [&](int kt) { return tab[min(kt * 4 + wb, (kv_end - 1) >> 4)]; };   // (behind the context: its last one, which nobody looks at)
     auto fetch = [&](int kt) {   // and asks for the block id of the tile after it
         const int blk = __builtin_amdgcn_readfirstlane(next_blk);
         r_ok = (unsigned)blk < (unsigned)a.n_blocks;
         const uint8_t *p = a.pool + ((size_t)(r_ok ? blk : 0) * a.Hkv + hk) * F::BYTES;
-        rk = *(const kvec *)(p + (uint32_t)(lane * (HD / 8)));
-        rks = *(const uint32_t *)(p + (uint32_t)(F::KS + 4 * (lane & (HD / 8 - 1))));
+        rk = *(const kvec *)(p + (uint32_t)((64 * wp + lane) * (HD / 8 / WPB)));
+        rks = *(const uint32_t *)(p + (uint32_t)(F::KS + 4 * k_scales));
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             rv[u] = *(const vvec *)(p + (uint32_t)(F::V + (((v_half + 2 * u) * 16 + vj) * G + vg) * 4));
@@ -748,17 +751,17 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4PromptArgs a) {
     // What was fetched goes to LDS in parts, which the first product's instructions lie between: K; then of each group the values
     // of two quads and their stores.  (No branch among them: what the products give is used behind it, and the compiler would move
     // them there.)
-    constexpr int PARTS = 6 * UG;
+    constexpr int PARTS = 6 * UG, SLOTS = 6 * KSTEP;
     V4Steps step;
     V4 px;
     uint32_t top = 0;
     auto put = [&](int part, uint8_t *t) {
-        uint8_t *scales = t + L::K + wave * (HD / 2);
-        bf16x8 *v = (bf16x8 *)(t + L::K + L::KS) + (wave * 2 + v_half) * HD + 32 * vg + vj;
+        uint8_t *scales = t + L::K + wb * (HD / 2);
+        bf16x8 *v = (bf16x8 *)(t + L::K + L::KS) + (wb * 2 + v_half) * HD + 32 * vg + vj;
         const int g = part / 6, u = part / 3 % 2;
         if (part == 0) {
-            *(kvec *)(t + wave * (8 * HD) + lane * (HD / 8)) = rk;
-            ((uint32_t *)scales)[lane & (HD / 8 - 1)] = rks;
+            *(kvec *)(t + wb * (8 * HD) + (64 * wp + lane) * (HD / 8 / WPB)) = rk;
+            ((uint32_t *)scales)[k_scales] = rks;
             top = 0;
         }
         if (part % 3 == 0) {
@@ -778,8 +781,8 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4PromptArgs a) {
     // instead, which only the rows that see it take.
     auto put_nan = [&](uint8_t *t) {
         if (!__any(top >= 0x7f800000u)) return;
-        uint8_t *scales = t + L::K + wave * (HD / 2);
-        bf16x8 *v = (bf16x8 *)(t + L::K + L::KS) + (wave * 2 + v_half) * HD + 32 * vg + vj;
+        uint8_t *scales = t + L::K + wb * (HD / 2);
+        bf16x8 *v = (bf16x8 *)(t + L::K + L::KS) + (wb * 2 + v_half) * HD + 32 * vg + vj;
         for (int u = 0; u < 2; ++u) {
             uint32_t ff = 0;   // bytes of 255
 #pragma unroll
@@ -787,7 +790,7 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4PromptArgs a) {
             ff = (ff >> 7) * 255u;
             rs[u] &= ~ff;
             for (int i = 0; i < 4; ++i)
-                if ((ff >> (8 * i)) & 1) scales[4 * (v_half + 2 * u) + i] = 255;   // of group 0, behind the wave's own store above
+                if ((ff >> (8 * i)) & 1) scales[16 * wp + 4 * (v_half + 2 * u) + i] = 255;   // of a group whose scales the wave itself stored above
         }
 #pragma unroll
         for (int g = 0; g < UG; ++g) {
@@ -818,14 +821,14 @@ __global__ __launch_bounds__(256, 2) void kv4_prefill_kernel(Kv4PromptArgs a) {
         f32x16 st[2];
         __builtin_amdgcn_s_setprio(1);   // a wave with products goes before one with softmax (16384 rows 1845 -> 1810 us)
 #pragma unroll
-        for (int i = 0; i < PARTS; ++i) {   // step s of head_dim, the query's smallest term first, the two score tiles in turn
+        for (int i = 0; i < SLOTS; ++i) {   // step s of head_dim, the query's smallest term first, the two score tiles in turn
             const int t2 = i & 1, s = i / 6, k = 2 - (i >> 1) % 3;
             const f32x16 from = i < 2 ? minus_ref : st[t2];
             if (k == 2) st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(kc[t2][s]), operand(q[s].t[2]), from, 4, 2, 0, ks[t2][s], 2, q[s].scale);
             if (k == 1) st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(kc[t2][s]), operand(q[s].t[1]), from, 4, 2, 0, ks[t2][s], 1, q[s].scale);
             if (k == 0) st[t2] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(operand(kc[t2][s]), operand(q[s].t[0]), from, 4, 2, 0, ks[t2][s], 0, q[s].scale);
             __builtin_amdgcn_sched_barrier(0);
-            put(i, other);
+            if (i % (SLOTS / PARTS) == 0) put(i / (SLOTS / PARTS), other);
             __builtin_amdgcn_sched_barrier(0);
         }
         __builtin_amdgcn_s_setprio(0);
@@ -956,18 +959,18 @@ __global__ __launch_bounds__(256) void kv4_prompt_merge_kernel(Kv4PromptArgs a) 
 }
 
 // How many pieces the keys of each request's units are cut into, from the sizes alone: the number of key tiles of a piece that
-// makes the launch shortest by this account, in us.  A compute unit takes 0.85 us a tile (head_dim 128) with two workgroups,
-// 0.95 with one; the longest piece is the tail.  Pieces are joined by a launch of their own, 5 us, and pass through memory as
+// makes the launch shortest by this account, in us.  A compute unit takes 0.85 us a tile (head_dim 128) with two workgroups of four
+// waves, 0.95 with one, 1.65 with one of eight; the longest piece is the tail.  Pieces are joined by a launch of their own, 5 us, and pass through memory as
 // float32, 0.2 us a MB written and read.  8B heads, us, uncut / the longest unit in 2, 4, 8, 24 pieces (chosen):
 //   19 rows behind 6005 tokens 96 / 56, 34, 23, 18 (24);  512 behind 8000 133 / 86, 78, 85, 84 (2);  512 behind 1024 31.5 (1) / 33, 33, 45, 40
 //   512 rows 16.1 (1) / 25, 27, 40, 40;  1024 rows 24.8 (1) / 41, 47, 47, 47;  2000 rows beside 100 behind 8000 145 / 93, 71, 71, 77 (3: 77)
 // Returns the workgroups for each kv head, *rows_cut the rows to join.
-static int kv4_prompt_cuts(Kv4PromptArgs &a, int *rows_cut) {
+static int kv4_prompt_cuts(Kv4PromptArgs &a, int cols, int *rows_cut) {
     const int G = a.Hq / a.Hkv;
-    const double tile_us = a.hd == 128 ? 0.85 : 0.5;
+    const double tile_us = a.hd != 128 ? 0.5 : cols == 128 ? 0.85 : 1.65;
     int units = 0, most = 0;
     double tiles = 0;
-    auto n_units = [&](int r) { return ((a.seq.cu[r + 1] - a.seq.cu[r]) * G + KV4_COLS - 1) / KV4_COLS; };
+    auto n_units = [&](int r) { return ((a.seq.cu[r + 1] - a.seq.cu[r]) * G + cols - 1) / cols; };
     auto longest = [&](int r) { return (a.seq.start[r] + a.seq.cu[r + 1] - a.seq.cu[r] + 63) / 64; };   // key tiles of its last unit
     for (int r = 0; r < a.seq.n_req; ++r)
         if (const int u = n_units(r)) {
@@ -993,8 +996,8 @@ static int kv4_prompt_cuts(Kv4PromptArgs &a, int *rows_cut) {
                 mb += 1e-6 * (a.seq.cu[r + 1] - a.seq.cu[r]) * a.Hq * cut * a.hd * 4;
             }
         }
-        if (pieces > KV4_PIECES) break;
-        const double tail = share * tile_us * (n * a.Hkv <= 256 ? 1.12 : folds && c == 1 ? 1.3 : 1.95);
+        if (pieces * cols > KV4_PIECES * 128) break;
+        const double tail = share * tile_us * (cols == 256 ? 1.0 : n * a.Hkv <= 256 ? 1.12 : folds && c == 1 ? 1.3 : 1.95);
         const double us = std::max(even, tail) + (pieces ? 5 + 0.4 * mb : 0);
         if (c == 1 || us < best_us) best = share, best_us = us;
     }
@@ -1002,7 +1005,7 @@ static int kv4_prompt_cuts(Kv4PromptArgs &a, int *rows_cut) {
     for (int r = 0; r < a.seq.n_req; ++r) {
         const int u = n_units(r), cut = u ? (longest(r) + best - 1) / best : 1;
         a.first[r] = n;
-        a.base[r] = pieces * KV4_COLS;
+        a.base[r] = pieces * cols;
         a.row[r] = rows;
         a.cut[r] = cut;
         n += u * cut;
@@ -1020,10 +1023,17 @@ static int kv4_prompt_cuts(Kv4PromptArgs &a, int *rows_cut) {
 void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &args) {
     Kv4PromptArgs a = args;
     int rows = 0;
-    const int n = kv4_prompt_cuts(a, &rows);
+    // Eight waves of 32 columns convert a value once for 256 columns instead of 128, but have their compute unit to themselves: where
+    // there are enough of them for the last round not to matter.  8B heads, us, four / eight waves (workgroups of eight):
+    //   2048 rows (256) 44.5 / 53.3;  4096 (512) 127 / 140;  6000 (752) 249 / 254;  8192 (1024) 446 / 428;  12000 (1504) 925 / 895;  16384 1700 / 1637
+    int units = 0;
+    for (int r = 0; r < a.seq.n_req; ++r) units += ((a.seq.cu[r + 1] - a.seq.cu[r]) * (a.Hq / a.Hkv) + 255) / 256;
+    const int cols = a.hd == 128 && units * a.Hkv >= 1024 ? 256 : 128;
+    const int n = kv4_prompt_cuts(a, cols, &rows);
     if (n == 0) return;
-    if (a.hd == 128) hipLaunchKernelGGL(kv4_prefill_kernel<128>, dim3(a.Hkv * n), dim3(256), 2 * Kv4Lds<128>::TILE, st, a);
-    else hipLaunchKernelGGL(kv4_prefill_kernel<64>, dim3(a.Hkv * n), dim3(256), 2 * Kv4Lds<64>::TILE, st, a);
+    if (cols == 256) hipLaunchKernelGGL((kv4_prefill_kernel<128, 8>), dim3(a.Hkv * n), dim3(512), 2 * Kv4Lds<128>::TILE, st, a);
+    else if (a.hd == 128) hipLaunchKernelGGL((kv4_prefill_kernel<128, 4>), dim3(a.Hkv * n), dim3(256), 2 * Kv4Lds<128>::TILE, st, a);
+    else hipLaunchKernelGGL((kv4_prefill_kernel<64, 4>), dim3(a.Hkv * n), dim3(256), 2 * Kv4Lds<64>::TILE, st, a);
     if (rows == 0) return;
     if (a.hd == 128) hipLaunchKernelGGL(kv4_prompt_merge_kernel<128>, dim3(a.Hkv, rows), dim3(256), 0, st, a);
     else hipLaunchKernelGGL(kv4_prompt_merge_kernel<64>, dim3(a.Hkv, rows), dim3(256), 0, st, a);

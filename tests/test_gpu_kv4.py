@@ -237,6 +237,43 @@ def test_prefill_attention(heads, lens, starts):
     c.c.destroy()
 
 
+@pytest.mark.parametrize("spoilt", [False, True])
+def test_prefill_attention_of_many_rows(spoilt):
+    """Enough rows for workgroups of eight waves: three requests, the columns of each of which end inside a workgroup; a key and a
+    value that are not finite make the rows behind them NaN in their kv head and no others."""
+    heads, lens, starts = (128, 8, 128), [2041, 1, 130], [0, 70, 333]
+    held = [s + n for s, n in zip(starts, lens)]
+    c = Cache(heads, 200, max_prefill=sum(lens), seed=5)
+    tab, dtab = c.tables(held)
+    c.fill(tab, held)
+    bad_k, bad_v = 1500, 1723   # of request 0, in kv heads 1 and 6
+    there = c.ref.copy()
+    if spoilt:
+        for pos, head, which in ((bad_k, 1, 2), (bad_v, 6, 3)):
+            for g in (1, 3):   # of the dims' groups two
+                there[0, tab[0, pos // 16], head, R.places(128, pos % 16)[which][g]] = 255
+        c.pool.copy_(torch.from_numpy(there))
+    cu = np.concatenate([[0], np.cumsum(lens)])
+    q = c.queries(int(cu[-1]))
+    got = run_prefill(c, q, cu, starts, dtab, tab.shape[1])
+    head = np.arange(128) // 16
+    nan = np.zeros((int(cu[-1]), 128), bool)
+    if spoilt:
+        pos = np.arange(lens[0])[:, None]
+        nan[:lens[0]] = ((head == 1) & (pos >= bad_k)) | ((head == 6) & (pos >= bad_v))
+    assert np.array_equal(np.isnan(got).all(-1), nan) and np.array_equal(np.isnan(got).any(-1), nan)
+    some = {0: [0, 1, 15, 16, 63, 64, 500, 1023, 1024, 1499, 1500, 1700, 1722, 1723, 2039, 2040], 1: [0], 2: [0, 17, 128, 129]}
+    for r, rows in some.items():
+        k, v = R.gather(c.ref[0], c.hd, tab[r], held[r])
+        for i in rows:
+            want, bound = R.attention(R.f64(q[cu[r] + i:cu[r] + i + 1]), k, v, starts[r] + i)
+            ok = ~nan[cu[r] + i]
+            g = got[cu[r] + i:cu[r] + i + 1]
+            fine = bool((np.abs(g - want) <= bound)[:, ok].all())
+            assert fine, (r, i, float(np.max((np.abs(g - want) / bound)[:, ok])))
+    c.c.destroy()
+
+
 @pytest.mark.parametrize("heads", [(8, 2, 128), (4, 4, 64)])
 def test_what_is_not_finite_reaches_the_rows_that_see_it_only(heads):
     """A NaN in a key, an infinity in a value: the rows in front of them are as they were, to the bit; the rows behind are NaN in
