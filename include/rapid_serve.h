@@ -138,7 +138,7 @@ int32_t rs_init(const rs_model_desc *model, const rs_pool_desc *pool, const rs_l
  * (dense and sparse feed-forward blocks), captured and hybrid ones, rs_step_tokens and the engine, but for
  * rs_decode_layer_noalloc (RS_ERR_STATE).  Allocates two more workspaces, for attention whose rows more than one workgroup
  * computes: 131072 partial rows of head_dim + 2 floats on the prefill side (68 MB at head_dim 128), and on each side that
- * serves decode rows as many as max_decode_batch and max_context may need (at least 512 for each query head of a KV head). */
+ * serves decode rows 1024 for each query head of a KV head (2 * n_q_heads where there are more than 512 KV heads). */
 int32_t rs_init_kv4(const rs_model_desc *model, const rs_kv4_desc *pool, const rs_limits *limits,
                     const rs_profile *prof, int32_t device, rs_ctx **out);
 /* Waits for both sides, frees everything the library owns. */
@@ -248,7 +248,7 @@ int32_t rs_kv4_read(rs_ctx *ctx, int32_t side, int32_t layer, void *k_out, void 
  * n_q_heads * head_dim elements) attends to ctx_lens[i] + 1 cached tokens (the newest one included, as rs_kv4_append leaves it).
  * ctx_lens[i] = -1: a row without a request, its output is zero.  B <= max_decode_batch, max_ctx (host) bounds
  * ctx_lens[i] + 1 as for rs_decode_layer (a bound near the longest context serves best).  Results depend on the sizes alone,
- * max_ctx among them (it decides how contexts are cut), not on the CU split.
+ * on max_ctx and the other rows' lengths too (they decide where contexts are cut), not on the CU split.
  * A key's group that is not finite makes the rows that see it NaN in the heads of its KV head, a value's group at least the
  * 32 dims of it (all of them where several rows are computed together, as rs_kv4_prefill_attention does).
  * The calls may be recorded into a caller's graph from the side's stream (rs_get_stream).  Attention uses the side's
@@ -276,7 +276,7 @@ int32_t rs_kv4_prefill_attention(rs_ctx *ctx, int32_t layer, const void *q, int6
  * (RS_ERR_BAD_BLOCK otherwise).  After rs_set_cu_split the decode stream differs and a new graph
  * is captured under the new mask.  At most 256 graphs are cached per context (RS_ERR_STATE);
  * rs_destroy frees them.  Results are bit-identical to rs_decode_layer's (over a cache held in 4 bits: with
- * max_ctx = max_ctx_bucket, which decides there how contexts are cut). */
+ * max_ctx = max_ctx_bucket, which has a say there in how contexts are cut). */
 int32_t rs_decode_layer_graph(rs_ctx *ctx, int32_t layer, const void *x_in, void *x_out,
                               const int32_t *ctx_lens, const int32_t *block_tables, int32_t max_blk,
                               int32_t B, int32_t max_ctx_bucket);

@@ -101,7 +101,8 @@ struct Kv4AttnArgs {
     int B, Hq, Hkv, hd, max_blk, n_blocks, max_ctx;
     float scale_log2;         // log2(e) / sqrt(hd)
     int out_row0 = 0, out_Mt = 0;   // first row and row tiles of the packed output matrix
-    int chunk = 0, n_chunks = 0;    // decode, set by the launcher; its pieces are [B][Hq][n_chunks]
+    int32_t *part_row = nullptr;    // decode: [B][2] the first and the last workgroup of a row
+    int wgs = 0, least = 0;         // decode, set by the launcher: workgroups a kv head (0: each takes a row) and units of one at least
 };
 // Prompts.  Set by the launcher: of each request the units (128 columns of one kv head) times the pieces that their keys are cut
 // into, and where those begin: first (in units and pieces), base (in pieces, [rows][Hq][cut]), row (in rows that are cut).
@@ -113,9 +114,7 @@ struct Kv4PromptArgs : Kv4AttnArgs {
     int32_t first[RS_MAX_RUNS], base[RS_MAX_RUNS], row[RS_MAX_RUNS], cut[RS_MAX_RUNS];
 };
 #define KV4_PIECES 1024        // most (unit, kv head, key range) pieces of cut rows in a launch
-struct Kv4Cut { int chunk, waves; };
-Kv4Cut kv4_cut(int64_t pairs, int max_ctx);
-int64_t kv4_most_pieces(int64_t pairs, int max_ctx);
+int64_t kv4_decode_pieces(int Hkv);   // pieces of a decode launch, for each query head of a kv head
 void kv4_kernels_init();
 void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &a);
 void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &a);

@@ -13,6 +13,7 @@
 // lane's share of V (4 tokens of a dim pair in every group) is another.  Both halves of a byte belong to one token, so tokens
 // can be appended one by one by anybody without reading what is there.
 #include <algorithm>
+#include <climits>
 #include <type_traits>
 
 #include "kernels.h"
@@ -327,35 +328,34 @@ __device__ __forceinline__ bf16_t *kv4_out(const Kv4AttnArgs &a, int row, int co
 // ---- pieces of rows ---------------------------------------------------------------------------------------------------------
 // A row of one head that several workgroups compute leaves a piece each: the weighted sum of values, relative to the piece's own
 // maximum, that maximum and the sum of weights.  A workgroup joins the pieces of the heads of one kv head of one
-// row, in order; a thread takes four dims.  Bound by round trips to memory: up to 8 pieces are asked for at once, whether the
-// row has them or not, beside its length; more in eights behind a pass over the maxima (64 rows of 3 chunks, 8B heads: 4.1 us, 32 rows of
-// 16 chunks 4.7; a launch that does nothing is 2).
-// Of row `row`: at most `most` pieces, from piece p0 on, n() of them in use.
-template <int HD, class N>
-__device__ __forceinline__ void kv4_join(const Kv4AttnArgs &a, int row, size_t p0, int most, N n_of) {
+// row, in order; a thread takes four dims.  Bound by round trips to memory: up to 8 pieces are asked for at once, more in eights
+// behind a pass over the maxima (8B heads, 64 rows of up to 4096 tokens 4.6 us, a row in 32 pieces 4.8; a launch that does nothing
+// is 2).
+// Of row `row`: n pieces, the j-th of head g of the kv head's is piece at(g, j).
+template <int HD, class At>
+__device__ __forceinline__ void kv4_join(const Kv4AttnArgs &a, int row, int n, At at) {
     __shared__ float s[2 * 16];
     const int G = a.Hq / a.Hkv, hq0 = blockIdx.x * G;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const float2 *ml = (const float2 *)a.part_ml + p0;
-    const f32x4 *po = (const f32x4 *)a.part_o + p0 * (HD / 4);
+    const float2 *ml = (const float2 *)a.part_ml;
+    const f32x4 *po = (const f32x4 *)a.part_o;
     auto store = [&](int g, int d4, f32x4 acc, float l) {
         bf16x4 w;
 #pragma unroll
         for (int j = 0; j < 4; ++j) w[j] = (bf16_t)(l == 0.f ? 0.f : acc[j] / l);   // (0: an empty row, or every block of it refused)
         *(bf16x4 *)kv4_out(a, row, (hq0 + g) * HD + 4 * d4) = w;
     };
-    if (most <= 8) {
+    if (n <= 8) {
         for (int i = tid; i < G * (HD / 4); i += 256) {
             const int g = i / (HD / 4), d4 = i % (HD / 4);
             f32x4 v[8];
             float2 m[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const size_t c = (size_t)g * most + min(j, most - 1);
+                const size_t c = at(g, max(min(j, n - 1), 0));
                 v[j] = po[c * (HD / 4) + d4];
                 m[j] = ml[c];
             }
-            const int n = n_of();
             float mx = NEG_INF, l = 0.f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) mx = fmaxf(mx, j < n ? m[j].x : NEG_INF);
@@ -372,16 +372,14 @@ __device__ __forceinline__ void kv4_join(const Kv4AttnArgs &a, int row, size_t p
         }
         return;
     }
-    const int n = n_of();
     for (int g = wave; g < G; g += 4) {
-        const float2 *mg = ml + (size_t)g * most;
         float mx = NEG_INF, l = 0.f;
-        for (int c = lane; c < n; c += 64) mx = fmaxf(mx, mg[c].x);
+        for (int c = lane; c < n; c += 64) mx = fmaxf(mx, ml[at(g, c)].x);
 #pragma unroll
         for (int o = 32; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, 64));
         const float ms = mx == NEG_INF ? 0.f : mx;
         for (int c = lane; c < n; c += 64) {
-            const float2 v = mg[c];
+            const float2 v = ml[at(g, c)];
             l += v.y * __builtin_amdgcn_exp2f(v.x - ms);
         }
         l = wave_sum(l);
@@ -394,8 +392,6 @@ __device__ __forceinline__ void kv4_join(const Kv4AttnArgs &a, int row, size_t p
     for (int i = tid; i < G * (HD / 4); i += 256) {
         const int g = i / (HD / 4), d4 = i % (HD / 4);
         const float ms = s[2 * g];
-        const f32x4 *pg = po + (size_t)g * most * (HD / 4) + d4;
-        const float2 *mg = ml + (size_t)g * most;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         for (int c0 = 0; c0 < n; c0 += 8) {
             f32x4 v[8];
@@ -403,8 +399,9 @@ __device__ __forceinline__ void kv4_join(const Kv4AttnArgs &a, int row, size_t p
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int c = min(c0 + j, n - 1);
-                v[j] = pg[(size_t)c * (HD / 4)];
-                m[j] = mg[c].x;
+                const size_t pc = at(g, c);
+                v[j] = po[pc * (HD / 4) + d4];
+                m[j] = ml[pc].x;
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -414,18 +411,14 @@ __device__ __forceinline__ void kv4_join(const Kv4AttnArgs &a, int row, size_t p
     }
 }
 
-template <int HD>
-__global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
-    const int row = blockIdx.y;
-    kv4_join<HD>(a, row, ((size_t)row * a.Hq + blockIdx.x * (a.Hq / a.Hkv)) * a.n_chunks, a.n_chunks,
-                 [&]() { return (min(max(__builtin_amdgcn_readfirstlane(a.ctx_lens[row]) + 1, 0), a.max_ctx) + a.chunk - 1) / a.chunk; });
-}
-
 // ---- attention: one row per request -----------------------------------------------------------------------------------------
-// Workgroup = (kv head, request, chunk of the context); its four waves take a quarter of the chunk's tokens each, 32 (two
-// blocks) at a time; the G query heads of the kv head are the columns of 16 x 16 tiles.  S^T = K Q^T, then O^T = V^T P^T: a
-// lane's eight scores (tokens 4h..4h+3 of both blocks) are the contraction slice that it supplies to the second product.
-// The 4.25 KB of the next 32 tokens are asked for before the present ones are computed, from block ids that the wave holds.
+// The G query heads of a kv head are the columns of 16 x 16 tiles, the keys come 32 (two blocks) at a time, which a workgroup's
+// waves take in turn.  S^T = K Q^T, then O^T = V^T P^T: a lane's eight scores (tokens 4h..4h+3 of both blocks) are the contraction
+// slice that it supplies to the second product.  The 4.25 KB of the wave's next 32 tokens are asked for before the present ones are
+// computed, from block ids that the wave holds (more of them in flight were slower: 64 rows of up to 8000 tokens 55, two further
+// tiles 62 us).
+// Workgroup = (kv head, row) or, CUT, (kv head, an equal share of the tokens of all rows): in units of UT tokens, counted by every
+// wave for itself, row after row from wherever the share begins.  What of a row is not all of it leaves a piece.
 __device__ __forceinline__ float max_of_quarters(float v) {   // over the four lanes of a column
     const auto x = __builtin_amdgcn_permlane16_swap(as_bits(v), as_bits(v), false, false);
     v = fmaxf(as_float((uint32_t)x[0]), as_float((uint32_t)x[1]));
@@ -433,231 +426,288 @@ __device__ __forceinline__ float max_of_quarters(float v) {   // over the four l
     return fmaxf(as_float((uint32_t)y[0]), as_float((uint32_t)y[1]));
 }
 
-template <int HD, int NW>
-__global__ __launch_bounds__(64 * NW, NW == 4 ? 3 : 2) void kv4_decode_kernel(Kv4AttnArgs a) {
+// units of UT tokens of a row of n
+template <int UT> __device__ __forceinline__ int units_of(const Kv4AttnArgs &a, int n) { return (min(max(n, 0), a.max_ctx) + UT - 1) / UT; }
+
+// The piece of a row that begins (or else ends, or is all) in workgroup wg.
+__device__ __forceinline__ size_t kv4_piece(const Kv4AttnArgs &a, int hk, int wg, bool begins, int g) {
+    return (((size_t)hk * a.wgs + wg) * 2 + begins) * (a.Hq / a.Hkv) + g;
+}
+
+template <int HD, int NW, bool CUT>
+__global__ __launch_bounds__(64 * NW, NW == 4 && !CUT ? 4 : 2) void kv4_decode_kernel(Kv4AttnArgs a) {
     using F = Kv4<HD>;
-    constexpr int G = F::G, NT = 64 * NW;
+    constexpr int G = F::G, NT = 64 * NW, UT = 32 * NW;
     typedef uint32_t gvec __attribute__((ext_vector_type(G)));
     extern __shared__ float smem_kv4[];
-    const int hk = blockIdx.x, b = blockIdx.z, chunk = blockIdx.y;
+    const int hk = blockIdx.x, wg = blockIdx.y;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, c16 = lane & 15, h = lane >> 4;
     const int Gq = a.Hq / a.Hkv;
-    float *s_o = smem_kv4;                // [NW][HD][Gq]
-    float *s_m = smem_kv4 + NW * HD * Gq; // [NW][Gq] maxima, [NW][Gq] sums
-    float *s_l = s_m + NW * Gq;
 
-    const int per_wave = a.chunk / NW;    // at most 1024 tokens: a lane holds a block id
-    const int t0 = chunk * a.chunk + wave * per_wave;
-    // asked for beside the length, not after it (within the table: it may end before the chunk does)
-    int my_blk = lane < per_wave / 16 ? a.tables[(size_t)b * a.max_blk + min((t0 >> 4) + lane, a.max_blk - 1)] : -1;
-    int n_keys = __builtin_amdgcn_readfirstlane(a.ctx_lens[b]) + 1;
-
-    // the query's terms, a column and 32 dims a lane (columns without a head, and the lanes behind head_dim: zeros)
-    QTerms q = q_terms(a.q + (size_t)b * a.q_stride + (size_t)(hk * Gq + min(c16, Gq - 1)) * HD + 32 * (h & (G - 1)), a.scale_log2);
-    if (c16 >= Gq || h >= G) q = QTerms{{{}, {}, {}}, 127 | 127 << 8 | 127 << 16};
-
-    if (n_keys < 0 || n_keys > a.max_ctx) {
-        if (tid == 0 && chunk == 0 && hk == 0) atomicOr(a.err_flag, 8);
-        n_keys = min(max(n_keys, 0), a.max_ctx);
-    }
-    if (n_keys == 0) {   // a row without a request
-        if (a.n_chunks == 1)
-            for (int c = tid * 8; c < Gq * HD; c += 8 * NT) *(u32x4_t *)kv4_out(a, b, hk * Gq * HD + c) = u32x4_t{0, 0, 0, 0};
-        return;
-    }
-    if (chunk * a.chunk >= n_keys) return;
-    const int t1 = min(t0 + per_wave, n_keys);
-    if (t0 + 16 * lane >= t1) my_blk = -1;
-    else if ((unsigned)my_blk >= (unsigned)a.n_blocks) {
-        atomicOr(a.err_flag, 2);
-        my_blk = -1;
-    }
-
-    float m_run = NEG_INF, l_run = 0.f;
-    f32x4 o[2 * G];   // (group, parity of the dim)
+    int row = wg, u0 = 0, left = INT_MAX;   // the first row, its first unit, and how many units the workgroup takes
+    if constexpr (CUT) {
+        // every wave by itself: a lane counts the units of `per` neighbouring rows, those of the lanes up to it are added up
+        const int per = (a.B + 63) / 64, r0 = min(lane * per, a.B), r1 = min(r0 + per, a.B);
+        int mine = 0;
+        for (int r = r0; r < r1; ++r) {
+            const int n = a.ctx_lens[r] + 1;
+            if ((n < 0 || n > a.max_ctx) && hk == 0 && wg == 0 && wave == 0) atomicOr(a.err_flag, 8);
+            mine += units_of<UT>(a, n);
+        }
+        int upto = mine;
 #pragma unroll
-    for (int i = 0; i < 2 * G; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int o = 1; o < 64; o *= 2) {
+            const int v = __shfl_up(upto, o, 64);
+            if (lane >= o) upto += v;
+        }
+        const int total = __builtin_amdgcn_readlane(upto, 63), n_wg = min(a.wgs, max(total / a.least, 1)), share = total / n_wg, more = total % n_wg;
+        left = share + (wg < more);
+        if (wg >= n_wg || left == 0) return;
+        const int first = wg * share + min(wg, more), owner = __builtin_ctzll(__ballot(upto > first));
+        int at = upto - mine;
+        if (lane == owner) {
+            row = r0;
+            for (int u; first >= at + (u = units_of<UT>(a, a.ctx_lens[row] + 1)); ++row) at += u;
+            u0 = first - at;
+        }
+        row = __builtin_amdgcn_readlane(row, owner);
+        u0 = __builtin_amdgcn_readlane(u0, owner);
+    }
     const uint8_t *head = a.pool + (size_t)hk * F::BYTES;
     const size_t blk_stride = (size_t)a.Hkv * F::BYTES;
     const uint32_t off_k = F::k_chunk(h & (G - 1), c16), off_ks = F::k_scale(h & (G - 1), c16), off_v = F::V + (h * 16 + c16) * (4 * G), off_vs = F::VS + h * (4 * G);
 
-    struct Buf {
-        u32x4_t kc[2];
-        uint32_t ks[2];
-        gvec vc[2], vs[2];
-    };
-    const int nit = t1 > t0 ? (t1 - t0 + 31) >> 5 : 0;   // the wave's
-    // (always loads, the last tokens again at the end: after a load under a branch, or a way out of the loop between its two halves,
-    // the compiler waits for all loads in flight, not for the older ones)
-    auto issue = [&](int it, Buf &f) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int blk = __builtin_amdgcn_readlane(my_blk, 2 * it + u);
-            const uint8_t *p = head + (size_t)max(blk, 0) * blk_stride;   // a missing block: memory of the pool, masked out
-            f.kc[u] = __builtin_nontemporal_load((const u32x4_t *)(p + off_k));
-            f.vc[u] = __builtin_nontemporal_load((const gvec *)(p + off_v));
-            f.ks[u] = p[off_ks];
-            f.vs[u] = *(const gvec *)(p + off_vs);
+    for (; row < a.B; ++row, u0 = 0) {
+        // the block ids of the wave's first 32 tiles (a lane's id: tile lane / 2 of the wave's, the lower or upper half of it), asked for
+        // beside the length, not after it
+        const int32_t *tab = a.tables + (size_t)row * a.max_blk;
+        const int my_place = 2 * ((lane >> 1) * NW + wave) + (lane & 1);
+        int place = u0 * (UT / 16) + my_place;
+        int my_blk = tab[min(place, a.max_blk - 1)];
+        const int n_given = __builtin_amdgcn_readfirstlane(a.ctx_lens[row]) + 1, n_keys = min(max(n_given, 0), a.max_ctx);
+
+        // the query's terms, a column and 32 dims a lane (columns without a head, and the lanes behind head_dim: zeros)
+        QTerms q = q_terms(a.q + (size_t)row * a.q_stride + (size_t)(hk * Gq + min(c16, Gq - 1)) * HD + 32 * (h & (G - 1)), a.scale_log2);
+        if (c16 >= Gq || h >= G) q = QTerms{{{}, {}, {}}, 127 | 127 << 8 | 127 << 16};
+
+        if (!CUT && n_given != n_keys && tid == 0 && hk == 0) atomicOr(a.err_flag, 8);
+        if (n_keys == 0) {   // a row without a request (of those in a cut launch, the kernel that joins the pieces writes the zeros)
+            if (CUT) continue;
+            for (int c = tid * 8; c < Gq * HD; c += 8 * NT) *(u32x4_t *)kv4_out(a, row, hk * Gq * HD + c) = u32x4_t{0, 0, 0, 0};
+            return;
         }
-    };
-    auto compute = [&](int it, Buf &f) {
-        const int base = t0 + 32 * it;
-        const int b0 = __builtin_amdgcn_readlane(my_blk, 2 * it), b1 = __builtin_amdgcn_readlane(my_blk, 2 * it + 1);
-        f32x4 s[2];
+        const int units = (n_keys + UT - 1) / UT, take = CUT ? min(left, units - u0) : units;
+        const int tok0 = u0 * UT, t1 = min((u0 + take) * UT, n_keys), n_tiles = (t1 - tok0 + 31) >> 5;   // of all waves, who take them in turn
+
+        float m_run = NEG_INF, l_run = 0.f;
+        f32x4 o[2 * G];   // (group, parity of the dim)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
-            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(f.kc[u]), operand(q.t[2]), s[u], 4, 2, 0, (int)f.ks[u], 2, q.scale);
-            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(f.kc[u]), operand(q.t[1]), s[u], 4, 2, 0, (int)f.ks[u], 1, q.scale);
-            s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(f.kc[u]), operand(q.t[0]), s[u], 4, 2, 0, (int)f.ks[u], 0, q.scale);
-        }
-        if (!(base + 32 <= t1 && b0 >= 0 && b1 >= 0)) {   // uniform
+        for (int i = 0; i < 2 * G; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        struct Buf {
+            u32x4_t kc[2];
+            uint32_t ks[2];
+            gvec vc[2], vs[2];
+        };
+        int pass = 0;   // first tile of the present ones
+        // (always loads, the last tokens again at the end: after a load under a branch, or a way out of the loop between its two halves,
+        // the compiler waits for all loads in flight, not for the older ones)
+        auto issue = [&](int it, Buf &f) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int nv = (u ? b1 : b0) >= 0 ? min(max(t1 - (base + 16 * u + 4 * h), 0), 4) : 0;   // valid tokens of this lane's four
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i >= nv) s[u][i] = NEG_INF;
-                const uint32_t keep = nv == 0 ? 0u : 0xffffffffu >> (32 - 8 * nv);
-#pragma unroll
-                for (int g = 0; g < G; ++g) f.vs[u][g] &= keep;   // what is behind the context may read as NaN
+                const int blk = __builtin_amdgcn_readlane(my_blk, 2 * it + u);
+                const uint8_t *p = head + (size_t)max(blk, 0) * blk_stride;   // a missing block: memory of the pool, masked out
+                f.kc[u] = __builtin_nontemporal_load((const u32x4_t *)(p + off_k));
+                f.vc[u] = __builtin_nontemporal_load((const gvec *)(p + off_v));
+                f.ks[u] = p[off_ks];
+                f.vs[u] = *(const gvec *)(p + off_vs);
             }
-        }
-        const float m_tile = max_of_quarters(fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))));
-        const float m_new = fmaxf(m_run, m_tile), ms = m_new == NEG_INF ? 0.f : m_new;
-        bf16x8 pf;   // the weights are rounded to bf16 for the second product (at most 2^-8 each); their sum is of the unrounded ones
-        float psum = 0.f;
+        };
+        auto compute = [&](int it, Buf &f) {
+            const int base = tok0 + 32 * (pass + it * NW + wave);
+            const int b0 = __builtin_amdgcn_readlane(my_blk, 2 * it), b1 = __builtin_amdgcn_readlane(my_blk, 2 * it + 1);
+            f32x4 s[2];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float p = __builtin_amdgcn_exp2f(s[i >> 2][i & 3] - ms);
-            psum += p;
-            pf[i] = (bf16_t)p;
-        }
-        if (__any(m_new != m_run)) {
-            const float alpha = __builtin_amdgcn_exp2f(m_run - ms);
-            l_run *= alpha;
+            for (int u = 0; u < 2; ++u) {
+                s[u] = f32x4{0.f, 0.f, 0.f, 0.f};
+                s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(f.kc[u]), operand(q.t[2]), s[u], 4, 2, 0, (int)f.ks[u], 2, q.scale);
+                s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(f.kc[u]), operand(q.t[1]), s[u], 4, 2, 0, (int)f.ks[u], 1, q.scale);
+                s[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(operand(f.kc[u]), operand(q.t[0]), s[u], 4, 2, 0, (int)f.ks[u], 0, q.scale);
+            }
+            if (!(base + 32 <= t1 && b0 >= 0 && b1 >= 0)) {   // uniform
 #pragma unroll
-            for (int i = 0; i < 2 * G; ++i) o[i] = o[i] * alpha;
-            m_run = m_new;
-        }
-        l_run += psum;
+                for (int u = 0; u < 2; ++u) {
+                    const int nv = (u ? b1 : b0) >= 0 ? min(max(t1 - (base + 16 * u + 4 * h), 0), 4) : 0;   // valid tokens of this lane's four
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const V4 va = v_values(f.vc[0][g], f.vs[0][g]), vb = v_values(f.vc[1][g], f.vs[1][g]);
-            o[2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join8(va.even, vb.even), pf, o[2 * g], 0, 0, 0);
-            o[2 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join8(va.odd, vb.odd), pf, o[2 * g + 1], 0, 0, 0);
+                    for (int i = 0; i < 4; ++i)
+                        if (i >= nv) s[u][i] = NEG_INF;
+                    const uint32_t keep = nv == 0 ? 0u : 0xffffffffu >> (32 - 8 * nv);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) f.vs[u][g] &= keep;   // what is behind the context may read as NaN
+                }
+            }
+            const float m_tile = max_of_quarters(fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))));
+            const float m_new = fmaxf(m_run, m_tile), ms = m_new == NEG_INF ? 0.f : m_new;
+            bf16x8 pf;   // the weights are rounded to bf16 for the second product (at most 2^-8 each); their sum is of the unrounded ones
+            float psum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float p = __builtin_amdgcn_exp2f(s[i >> 2][i & 3] - ms);
+                psum += p;
+                pf[i] = (bf16_t)p;
+            }
+            if (__any(m_new != m_run)) {
+                const float alpha = __builtin_amdgcn_exp2f(m_run - ms);
+                l_run *= alpha;
+#pragma unroll
+                for (int i = 0; i < 2 * G; ++i) o[i] = o[i] * alpha;
+                m_run = m_new;
+            }
+            l_run += psum;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const V4 va = v_values(f.vc[0][g], f.vs[0][g]), vb = v_values(f.vc[1][g], f.vs[1][g]);
+                o[2 * g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join8(va.even, vb.even), pf, o[2 * g], 0, 0, 0);
+                o[2 * g + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(join8(va.odd, vb.odd), pf, o[2 * g + 1], 0, 0, 0);
+            }
+        };
+        for (;;) {
+            if (16 * place >= t1) my_blk = -1;
+            else if ((unsigned)my_blk >= (unsigned)a.n_blocks) {
+                atomicOr(a.err_flag, 2);
+                my_blk = -1;
+            }
+            const int nit = min((n_tiles - pass - wave + NW - 1) / NW, 32);   // the wave's (0 or less: none)
+            if (nit > 0) {
+                Buf x, y;
+                issue(0, x);
+                for (int it = 0; it < nit; it += 2) {
+                    issue(min(it + 1, nit - 1), y);
+                    __builtin_amdgcn_sched_barrier(0);
+                    compute(it, x);
+                    __builtin_amdgcn_sched_barrier(0);
+                    issue(min(it + 2, nit - 1), x);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (it + 1 < nit) compute(it + 1, y);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            pass += 32 * NW;
+            if (pass >= n_tiles) break;
+            place += 64 * NW;
+            my_blk = tab[min(place, a.max_blk - 1)];
         }
-    };
-    if (nit > 0) {
-        Buf x, y;
-        issue(0, x);
-        for (int it = 0; it < nit; it += 2) {
-            issue(min(it + 1, nit - 1), y);
-            __builtin_amdgcn_sched_barrier(0);
-            compute(it, x);
-            __builtin_amdgcn_sched_barrier(0);
-            issue(min(it + 2, nit - 1), x);
-            __builtin_amdgcn_sched_barrier(0);
-            if (it + 1 < nit) compute(it + 1, y);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    }
-    l_run += __shfl_xor(l_run, 16, 64);
-    l_run += __shfl_xor(l_run, 32, 64);
+        l_run += __shfl_xor(l_run, 16, 64);
+        l_run += __shfl_xor(l_run, 32, 64);
 
-    // the waves, in order
-    if (c16 < Gq) {
+        // the waves, in order
+        int Gr = Gq;
+        if (CUT) asm volatile("" : "+s"(Gr));   // (or the addresses below, the same for every row, are held in registers all along)
+        float *s_o = smem_kv4, *s_m = smem_kv4 + NW * HD * Gr, *s_l = s_m + NW * Gr;   // [NW][HD][Gq], [NW][Gq] maxima, [NW][Gq] sums
+        if (c16 < Gr) {
 #pragma unroll
-        for (int g = 0; g < G; ++g)
+            for (int g = 0; g < G; ++g)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s_o[(wave * HD + 32 * g + 2 * (4 * h + i)) * Gq + c16] = o[2 * g][i];
-                s_o[(wave * HD + 32 * g + 2 * (4 * h + i) + 1) * Gq + c16] = o[2 * g + 1][i];
-            }
-        if (h == 0) {
-            s_m[wave * Gq + c16] = m_run;
-            s_l[wave * Gq + c16] = l_run;
-        }
-    }
-    __syncthreads();
-    for (int idx = tid; idx < Gq * HD; idx += NT) {
-        const int gg = idx / HD, d = idx % HD;
-        float mx = NEG_INF;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) mx = fmaxf(mx, s_m[w * Gq + gg]);
-        const float ms = mx == NEG_INF ? 0.f : mx;
-        float acc = 0.f, l = 0.f;
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            const float e = __builtin_amdgcn_exp2f(s_m[w * Gq + gg] - ms);
-            acc += s_o[(w * HD + d) * Gq + gg] * e;
-            l += s_l[w * Gq + gg] * e;
-        }
-        if (a.n_chunks == 1) {
-            *kv4_out(a, b, (hk * Gq + gg) * HD + d) = (bf16_t)(l == 0.f ? 0.f : acc / l);   // (0: every block of the row was refused)
-        } else {
-            const size_t pi = ((size_t)b * a.Hq + hk * Gq + gg) * a.n_chunks + chunk;
-            a.part_o[pi * HD + d] = acc;
-            if (d == 0) {
-                a.part_ml[pi * 2] = mx;
-                a.part_ml[pi * 2 + 1] = l;
+                for (int i = 0; i < 4; ++i) {
+                    s_o[(wave * HD + 32 * g + 2 * (4 * h + i)) * Gr + c16] = o[2 * g][i];
+                    s_o[(wave * HD + 32 * g + 2 * (4 * h + i) + 1) * Gr + c16] = o[2 * g + 1][i];
+                }
+            if (h == 0) {
+                s_m[wave * Gr + c16] = m_run;
+                s_l[wave * Gr + c16] = l_run;
             }
         }
+        __syncthreads();
+        for (int idx = tid; idx < Gr * HD; idx += NT) {
+            const int gg = idx / HD, d = idx % HD;
+            float mx = NEG_INF;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) mx = fmaxf(mx, s_m[w * Gr + gg]);
+            const float ms = mx == NEG_INF ? 0.f : mx;
+            float acc = 0.f, l = 0.f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float e = __builtin_amdgcn_exp2f(s_m[w * Gr + gg] - ms);
+                acc += s_o[(w * HD + d) * Gr + gg] * e;
+                l += s_l[w * Gr + gg] * e;
+            }
+            if (!CUT || take == units) {
+                *kv4_out(a, row, (hk * Gr + gg) * HD + d) = (bf16_t)(l == 0.f ? 0.f : acc / l);   // (0: every block of the row was refused)
+            } else {
+                const size_t pi = kv4_piece(a, hk, wg, u0 == 0, gg);
+                a.part_o[pi * HD + d] = acc;
+                if (d == 0) {
+                    a.part_ml[pi * 2] = mx;
+                    a.part_ml[pi * 2 + 1] = l;
+                }
+            }
+        }
+        if (!CUT) return;
+        if (hk == 0 && tid == 0) {
+            if (u0 == 0) a.part_row[2 * row] = wg;
+            if (u0 + take == units) a.part_row[2 * row + 1] = wg;
+        }
+        left -= take;
+        if (left == 0) return;
+        __syncthreads();   // before the next row's waves write theirs
     }
 }
 
-// How the rows of a decode launch are cut, from the sizes alone (pairs: rows times kv heads): tokens of a chunk and waves of its
-// workgroup.  A compute unit loads 57 GB/s, 2.4 us for 1024 tokens of 128 dims; pieces cost a launch of their own, 3 us and more:
-// whole contexts in one workgroup while that is the lesser, or while the pairs fill the chip by themselves.  Of eight waves where
-// they are no more than one a unit.  us a pass, 8B heads:
-//   1 row of 900 tokens: whole, 8 waves / 4 waves 8.1 / 8.7, in chunks of 256 8.9;  of 2000: 11.8 / 13.3, 9.0
-//   32 rows of 500 to 2000: 12.4 / 14.0, chunks of 1024 16.3;  32 of 1000 to 4000: 19.6 / 23.5, chunks of 2048 23.8
-//   128 rows of 250 to 1000: 29.9 / 21.9, chunks of 512 29.8;  203 rows of 1 to 1500, 4 heads of 64: whole 17.0, chunks of 1024 26.0
-// Chunks: the shortest of 256 .. that make 512 workgroups at most and 32 pieces a row, up to 1024 tokens, 2048 of contexts beyond 4096.
-//   1 row of 4000 / 32000 tokens in chunks of 256, 512, 1024, 2048: 9.5, 10.2, 12.5, 15.9 / 25, 16.3, 14.4, 18.0
-//   16 rows of 2000 to 8000: 512 26.1, 1024 25.4, 2048 23.6, 4096 27.5;  128 of 750 to 3000: 512 68.0, 1024 57.5, 2048 69.1, whole 62.8
-//   32 rows of 8192 to 32767: 1024 141, 2048 128, 4096 128
-Kv4Cut kv4_cut(int64_t pairs, int max_ctx) {
-    const int whole = pairs < 128 ? 1024 : pairs <= 256 ? 4096 : 2048;
-    if (max_ctx <= whole) {
-        const int waves = pairs <= 256 ? 8 : 4;
-        return {(max_ctx + 32 * waves - 1) / (32 * waves) * (32 * waves), waves};
-    }
-    const int cap = max_ctx <= 4096 ? 1024 : 2048;
-    int c = 256;
-    while (c < cap && (pairs * ((max_ctx + c - 1) / c) > 512 || (max_ctx + c - 1) / c > 32)) c *= 2;
-    return {c, 4};
+template <int HD>
+__global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
+    const int row = blockIdx.y, hk = blockIdx.x;
+    const int first = a.part_row[2 * row], last = a.part_row[2 * row + 1];
+    const int n = min(max(a.ctx_lens[row] + 1, 0), a.max_ctx) == 0 ? 0 : last - first + 1;   // (empty rows: nobody wrote first and last)
+    if (n == 1) return;
+    kv4_join<HD>(a, row, n, [&](int g, int j) { return n == 0 ? 0 : kv4_piece(a, hk, first + j, j == 0, g); });
 }
-// Most pieces, over all contexts up to max_ctx.
-int64_t kv4_most_pieces(int64_t pairs, int max_ctx) { return std::max<int64_t>(512, pairs * std::max(4, (max_ctx + 2047) / 2048)); }
 
-template <int HD, int NW>
+// Which form a decode launch takes, from the sizes alone (pairs: rows times kv heads).  Equal shares cost some 10 us, counting and
+// a launch that joins pieces; a workgroup with a whole row takes 3 us and 3.6 ns (eight waves) or 4.9 (four) a token, and the longest
+// row may run alone at the end.  So whole rows where contexts are short, longer ones the more pairs there are to hide one; of eight
+// waves where there is at most a workgroup for each compute unit.  8B heads, us, whole rows of 8 waves / of 4 / equal shares:
+//   1 row of 900 tokens 8.1 / 8.7 / 8.9;  of 1900 11.8 / 13.1 / 10.1;  of 4000 19.3 / 22.5 / 10.6;  of 32000 112 / 147 / 17
+//   8 rows of 200 to 2000 12.4 / 13.6 / 11.0;  16 of 500 to 2000 12.3 / 13.7 / 15.6;  16 of 0 to 3500 17.6 / 20.3 / 16.6
+//   32 rows of 500 to 3500 18.4 / 21.2 / 21.5;  of 0 to 6000 26.9 / 33.2 / 27.5;  of 8191 to 32766 138 / 163 / 116
+//   48 rows of 1000 to 2000 21.9 / 19.6 / 22.9;  of 500 to 6000 39.4 / 43.8 / 37.0;  64 of 4095 50.9 / 46.0 / 48.6
+//   64 rows of 0 to 4095 36.5 / 33.6 / 35.4;  of 0 to 8000 62 / 61 / 54;  128 of 100 to 2500 46.3 / 39.4 / 44.2;  of 0 to 4600 70 / 67 / 65
+//   256 rows of 0 to 2300 80 / 63 / 80;  200 rows of 0 to 1500, 4 heads of 64 19.6 / 17.8 / 26.0
+// Equal shares: of 512 workgroups (64 rows of 4095: 48.6; of 768 55.6, of 1024 51.4), of 2 units at least and as many as make 8 pieces
+// of the longest row, or of 8 and more that make 32 (shares of 2 / 4 / 8 units: 8 rows of 200 to 2000 11.0 / 13.3 / 15.4, 4 of 1000 to 4000
+// 12.2 / 10.9 / 12.8).
+static int kv4_wgs(int Hkv) { return std::max(1, 512 / Hkv); }
+int64_t kv4_decode_pieces(int Hkv) { return 2ll * Hkv * kv4_wgs(Hkv); }
+
+template <int HD, int NW, bool CUT>
 static void launch_kv4_decode_form(hipStream_t st, const Kv4AttnArgs &a) {
     const int Gq = a.Hq / a.Hkv;
-    hipLaunchKernelGGL((kv4_decode_kernel<HD, NW>), dim3(a.Hkv, a.n_chunks, a.B), dim3(64 * NW), (size_t)(NW * HD * Gq + 2 * NW * Gq) * sizeof(float), st, a);
+    hipLaunchKernelGGL((kv4_decode_kernel<HD, NW, CUT>), dim3(a.Hkv, CUT ? a.wgs : a.B), dim3(64 * NW), (size_t)(NW * HD * Gq + 2 * NW * Gq) * sizeof(float), st, a);
 }
 
 void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &args) {
     Kv4AttnArgs a = args;
     if (a.B <= 0) return;
-    const Kv4Cut cut = kv4_cut((int64_t)a.B * a.Hkv, a.max_ctx);
-    a.chunk = cut.chunk;
-    a.n_chunks = (a.max_ctx + a.chunk - 1) / a.chunk;
-    if (cut.waves == 8) {
-        if (a.hd == 128) launch_kv4_decode_form<128, 8>(st, a);
-        else launch_kv4_decode_form<64, 8>(st, a);
+    const int64_t pairs = (int64_t)a.B * a.Hkv;
+    const int64_t whole = pairs <= 256 ? std::max<int64_t>(1280, 24 * pairs) : 4608, units = (a.max_ctx + 127) / 128;
+    a.wgs = a.max_ctx <= whole ? 0 : kv4_wgs(a.Hkv);
+    a.least = (int)std::max({(int64_t)2, std::min<int64_t>(8, (units + 7) / 8), (units + 31) / 32});
+    if (a.wgs) {
+        if (a.hd == 128) launch_kv4_decode_form<128, 4, true>(st, a);
+        else launch_kv4_decode_form<64, 4, true>(st, a);
+    } else if (pairs <= 256) {
+        if (a.hd == 128) launch_kv4_decode_form<128, 8, false>(st, a);
+        else launch_kv4_decode_form<64, 8, false>(st, a);
     } else {
-        if (a.hd == 128) launch_kv4_decode_form<128, 4>(st, a);
-        else launch_kv4_decode_form<64, 4>(st, a);
+        if (a.hd == 128) launch_kv4_decode_form<128, 4, false>(st, a);
+        else launch_kv4_decode_form<64, 4, false>(st, a);
     }
-    if (a.n_chunks > 1) {
+    if (a.wgs) {
         if (a.hd == 128) hipLaunchKernelGGL(kv4_merge_kernel<128>, dim3(a.Hkv, a.B), dim3(256), 0, st, a);
         else hipLaunchKernelGGL(kv4_merge_kernel<64>, dim3(a.Hkv, a.B), dim3(256), 0, st, a);
     }
 }
 
 void kv4_kernels_init() {
-    (void)hipFuncSetAttribute((const void *)kv4_decode_kernel<128, 8>, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * (128 + 2) * 16 * 4);
+    (void)hipFuncSetAttribute((const void *)kv4_decode_kernel<128, 8, false>, hipFuncAttributeMaxDynamicSharedMemorySize, 8 * (128 + 2) * 16 * 4);
 }
 
 // ---- attention: prompts and chunks of them ----------------------------------------------------------------------------------
@@ -955,7 +1005,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_prefill_kernel(Kv4PromptArgs a
 template <int HD>
 __global__ __launch_bounds__(256) void kv4_prompt_merge_kernel(Kv4PromptArgs a) {
     const int req = last_at_most(a.row, a.seq.n_req, blockIdx.y), row = blockIdx.y - a.row[req], cut = a.cut[req];
-    kv4_join<HD>(a, a.seq.cu[req] + row, a.base[req] + ((size_t)row * a.Hq + blockIdx.x * (a.Hq / a.Hkv)) * cut, cut, [&]() { return cut; });
+    const size_t p0 = a.base[req] + ((size_t)row * a.Hq + blockIdx.x * (a.Hq / a.Hkv)) * cut;
+    kv4_join<HD>(a, a.seq.cu[req] + row, cut, [&](int g, int j) { return p0 + g * cut + j; });
 }
 
 // How many pieces the keys of each request's units are cut into, from the sizes alone: the number of key tiles of a piece that

@@ -173,6 +173,7 @@ struct rs_ctx {
     int64_t kv4_stride = 0;
     bool is_kv4 = false;
     float *kv4_part_o[2] = {nullptr, nullptr}, *kv4_part_ml[2] = {nullptr, nullptr};
+    int32_t *kv4_part_row[2] = {nullptr, nullptr};
     CosSin *rope = nullptr;
     // One error word per side (kernels OR bits into it: 1 position outside the rotary table, 2 block id outside
     // the pool, 4 token outside the vocabulary, 8 context length outside [1, max_ctx]) and its pinned host
@@ -650,6 +651,7 @@ Kv4AttnArgs kv4_attn_args(rs_ctx *c, int side, int32_t layer, const void *q, int
     a.err_flag = c->err_flag + side;
     a.part_o = c->kv4_part_o[side];
     a.part_ml = c->kv4_part_ml[side];
+    a.part_row = c->kv4_part_row[side];
     a.Hq = c->m.n_q_heads;
     a.Hkv = c->m.n_kv_heads;
     a.hd = c->m.head_dim;
@@ -1092,7 +1094,7 @@ struct OnDevice {
 size_t kv4_pieces(const rs_ctx *c, bool prefill, int rows) {
     const rs_model_desc &m = c->m;
     size_t n = prefill ? (size_t)KV4_PIECES * 128 : 0;
-    if (rows > 0) n = std::max(n, (size_t)kv4_most_pieces((int64_t)rows * m.n_kv_heads, c->lim.max_context) * (m.n_q_heads / m.n_kv_heads));
+    if (rows > 0) n = std::max(n, (size_t)kv4_decode_pieces(m.n_kv_heads) * (m.n_q_heads / m.n_kv_heads));
     return n;
 }
 
@@ -1103,6 +1105,7 @@ int32_t alloc_kv4(rs_ctx *c) {
         if (n == 0) continue;
         HIP_TRY(hipMalloc(&c->kv4_part_o[s], n * c->m.head_dim * sizeof(float)));
         HIP_TRY(hipMalloc(&c->kv4_part_ml[s], n * 2 * sizeof(float)));
+        HIP_TRY(hipMalloc(&c->kv4_part_row[s], (size_t)std::max(decode_rows, 1) * 2 * sizeof(int32_t)));
     }
     return RS_OK;
 }
@@ -1325,6 +1328,7 @@ int32_t rs_destroy(rs_ctx *c) {
             free_ws(c->ws[s]);
             if (c->kv4_part_o[s]) (void)hipFree(c->kv4_part_o[s]);
             if (c->kv4_part_ml[s]) (void)hipFree(c->kv4_part_ml[s]);
+            if (c->kv4_part_row[s]) (void)hipFree(c->kv4_part_row[s]);
         }
         for (auto &kv : c->graphs) (void)hipGraphExecDestroy(kv.second);
         drop_step_graphs(c);

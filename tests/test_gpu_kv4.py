@@ -203,6 +203,34 @@ def test_decode_attention_is_the_same_however_it_is_cut(batch):
     c.c.destroy()
 
 
+MANY = [int(x) for x in np.random.default_rng(8).integers(-1, 40, 150)]
+MANY[0] = MANY[1] = MANY[149] = -1
+MANY[77], MANY[80] = 4800, 600
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 128), (4, 4, 64), (16, 1, 128)])
+@pytest.mark.parametrize("ctx", [[5000, -1, 3, 700, -1, 1300], [127, 128, 255, 256, 383, 0, 126], [-1, -1, -1], [-1] * 70 + [1500], MANY, [4999]], ids=lambda x: f"{len(x)}-{max(x)}")
+def test_decode_attention_in_equal_shares(heads, ctx):
+    """A bound on the contexts that lets whole rows be cut anywhere: rows that are a share, a part of one and several, empty ones in
+    front, between and behind, more rows than a wave has lanes."""
+    c = Cache(heads, 700, max_batch=len(ctx), max_context=9000, seed=len(ctx))
+    tab, _ = c.tables([n + 1 for n in ctx])
+    tab = np.concatenate([tab, np.full((len(ctx), 563 - tab.shape[1]), -1, np.int32)], 1)
+    dtab = torch.from_numpy(tab).cuda()
+    c.fill(tab, [n + 1 for n in ctx])
+    q = c.queries(len(ctx))
+    got = run_decode(c, q, ctx, dtab, tab.shape[1], 9000)
+    assert np.array_equal(run_decode(c, q, ctx, dtab, tab.shape[1], 9000), got)
+    for r, n in enumerate(ctx):
+        if n < 0:
+            assert (got[r] == 0).all()
+            continue
+        k, v = R.gather(c.ref[0], c.hd, tab[r], n + 1)
+        want, bound = R.attention(R.f64(q[r:r + 1]), k, v, n)
+        held_to(got[r:r + 1], want, bound, f"row {r}, ctx {n}")
+    c.c.destroy()
+
+
 def run_prefill(c, q, cu, starts, dtab, width, stride=0, layer=0):
     W, T = c.Hq * c.hd, int(cu[-1])
     dq = wide(q, W, W + stride)
