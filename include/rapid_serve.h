@@ -233,9 +233,10 @@ int32_t rs_decode_layer(rs_ctx *ctx, int32_t layer, const void *x_in, void *x_ou
  * ... of request r (host arrays; start_pos may be null: all 0; any position may start a run, a run may be empty, n_req is 1 to
  * RS_MAX_PREFILL_REQS).  Tokens outside the runs keep what they hold.
  * rs_kv4_append: one token of each of B requests, row i at position ctx_lens[i] (device), -1: no request, nothing is done.
- *   No two rows may be the same position of the same request.
  * rs_kv4_read: the inverse of rs_kv4_write, exactly what the cache holds as bf16.
- * RS_ERR_BAD_ARG for a null or misaligned pointer or a bad size, RS_ERR_BAD_BLOCK for a table too short for a run. */
+ * No two tokens that one call writes may have the same place in the cache; reading calls may name a block any number of times.
+ * RS_ERR_BAD_ARG for a null or misaligned pointer or a bad size (among them runs of more tokens than one launch has threads
+ * for, 2^31 * 16 / (n_kv_heads * head_dim), 33 million at 8 heads of 128), RS_ERR_BAD_BLOCK for a table too short for a run. */
 int32_t rs_kv4_write(rs_ctx *ctx, int32_t side, int32_t layer, const void *k, const void *v, int64_t row_stride,
                      const int32_t *cu_seqlens, const int32_t *start_pos, int32_t n_req, const int32_t *block_tables,
                      int32_t max_blk);

@@ -148,7 +148,8 @@ def _runs(cu_seqlens, start_pos):
     n = len(cu_seqlens) - 1
     if start_pos is not None and len(start_pos) != n:
         raise ValueError(f"{len(start_pos)} first positions for {n} requests")
-    return array.array("i", cu_seqlens), n, array.array("i", start_pos) if start_pos is not None else None
+    ints = lambda x: array.array("i", x if isinstance(x, list) else np.asarray(x).tolist())
+    return ints(cu_seqlens), n, ints(start_pos) if start_pos is not None else None
 
 
 def _addr(x) -> Optional[int]:

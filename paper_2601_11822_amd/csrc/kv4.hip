@@ -333,9 +333,9 @@ __device__ __forceinline__ bf16_t *kv4_out(const Kv4AttnArgs &a, int row, int co
 // is 2).
 // Of row `row`: n pieces, the j-th of head g of the kv head's is piece at(g, j).
 template <int HD, class At>
-__device__ __forceinline__ void kv4_join(const Kv4AttnArgs &a, int row, int n, At at) {
+__device__ __forceinline__ void kv4_join(const Kv4AttnArgs &a, int hk, int row, int n, At at) {
     __shared__ float s[2 * 16];
-    const int G = a.Hq / a.Hkv, hq0 = blockIdx.x * G;
+    const int G = a.Hq / a.Hkv, hq0 = hk * G;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const float2 *ml = (const float2 *)a.part_ml;
     const f32x4 *po = (const f32x4 *)a.part_o;
@@ -654,11 +654,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && !CUT ? 4 : 2) void kv4_decode_k
 
 template <int HD>
 __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
-    const int row = blockIdx.y, hk = blockIdx.x;
+    const int row = blockIdx.x / a.Hkv, hk = blockIdx.x % a.Hkv;
     const int first = a.part_row[2 * row], last = a.part_row[2 * row + 1];
     const int n = min(max(a.ctx_lens[row] + 1, 0), a.max_ctx) == 0 ? 0 : last - first + 1;   // (empty rows: nobody wrote first and last)
     if (n == 1) return;
-    kv4_join<HD>(a, row, n, [&](int g, int j) { return n == 0 ? 0 : kv4_piece(a, hk, first + j, j == 0, g); });
+    kv4_join<HD>(a, hk, row, n, [&](int g, int j) { return n == 0 ? 0 : kv4_piece(a, hk, first + j, j == 0, g); });
 }
 
 // Which form a decode launch takes, from the sizes alone (pairs: rows times kv heads).  Equal shares cost some 10 us, counting and
@@ -701,8 +701,8 @@ void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &args) {
         else launch_kv4_decode_form<64, 4, false>(st, a);
     }
     if (a.wgs) {
-        if (a.hd == 128) hipLaunchKernelGGL(kv4_merge_kernel<128>, dim3(a.Hkv, a.B), dim3(256), 0, st, a);
-        else hipLaunchKernelGGL(kv4_merge_kernel<64>, dim3(a.Hkv, a.B), dim3(256), 0, st, a);
+        if (a.hd == 128) hipLaunchKernelGGL(kv4_merge_kernel<128>, dim3(a.Hkv * a.B), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL(kv4_merge_kernel<64>, dim3(a.Hkv * a.B), dim3(256), 0, st, a);
     }
 }
 
@@ -1004,9 +1004,9 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_prefill_kernel(Kv4PromptArgs a
 // The rows that were cut.
 template <int HD>
 __global__ __launch_bounds__(256) void kv4_prompt_merge_kernel(Kv4PromptArgs a) {
-    const int req = last_at_most(a.row, a.seq.n_req, blockIdx.y), row = blockIdx.y - a.row[req], cut = a.cut[req];
-    const size_t p0 = a.base[req] + ((size_t)row * a.Hq + blockIdx.x * (a.Hq / a.Hkv)) * cut;
-    kv4_join<HD>(a, a.seq.cu[req] + row, cut, [&](int g, int j) { return p0 + g * cut + j; });
+    const int hk = blockIdx.x % a.Hkv, at = blockIdx.x / a.Hkv, req = last_at_most(a.row, a.seq.n_req, at), row = at - a.row[req], cut = a.cut[req];
+    const size_t p0 = a.base[req] + ((size_t)row * a.Hq + hk * (a.Hq / a.Hkv)) * cut;
+    kv4_join<HD>(a, hk, a.seq.cu[req] + row, cut, [&](int g, int j) { return p0 + g * cut + j; });
 }
 
 // How many pieces the keys of each request's units are cut into, from the sizes alone: the number of key tiles of a piece that
@@ -1086,6 +1086,6 @@ void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &args) {
     else if (a.hd == 128) hipLaunchKernelGGL((kv4_prefill_kernel<128, 4>), dim3(a.Hkv * n), dim3(256), 2 * Kv4Lds<128>::TILE, st, a);
     else hipLaunchKernelGGL((kv4_prefill_kernel<64, 4>), dim3(a.Hkv * n), dim3(256), 2 * Kv4Lds<64>::TILE, st, a);
     if (rows == 0) return;
-    if (a.hd == 128) hipLaunchKernelGGL(kv4_prompt_merge_kernel<128>, dim3(a.Hkv, rows), dim3(256), 0, st, a);
-    else hipLaunchKernelGGL(kv4_prompt_merge_kernel<64>, dim3(a.Hkv, rows), dim3(256), 0, st, a);
+    if (a.hd == 128) hipLaunchKernelGGL(kv4_prompt_merge_kernel<128>, dim3(a.Hkv * rows), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(kv4_prompt_merge_kernel<64>, dim3(a.Hkv * rows), dim3(256), 0, st, a);
 }

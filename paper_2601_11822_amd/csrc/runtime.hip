@@ -1134,7 +1134,7 @@ int32_t check_kv4_rows(const char *what, const void *p, int64_t stride, int64_t 
 }
 
 // Runs of tokens by request -> their description for the kernels.
-int32_t kv4_runs(const int32_t *cu, const int32_t *start, int32_t n_req, int32_t max_blk, SeqInfo *seq) {
+int32_t kv4_runs(const rs_ctx *c, const int32_t *cu, const int32_t *start, int32_t n_req, int32_t max_blk, SeqInfo *seq) {
     if (!cu || n_req < 1 || n_req > RS_MAX_PREFILL_REQS) return fail(RS_ERR_BAD_ARG, "n_req %d out of range, or null cu_seqlens", n_req);
     if (cu[0] != 0) return fail(RS_ERR_BAD_ARG, "cu_seqlens must start at 0");
     seq->n_req = n_req;
@@ -1148,6 +1148,9 @@ int32_t kv4_runs(const int32_t *cu, const int32_t *start, int32_t n_req, int32_t
         seq->cu[r + 1] = cu[r + 1];
         seq->start[r] = first;
     }
+    // a launch holds fewer than 2^32 threads: 2 hd for each (block, kv head) that the runs touch
+    if (((int64_t)cu[n_req] / RS_KV_BLOCK + 2 * n_req) * c->m.n_kv_heads * 2 * c->m.head_dim > UINT32_MAX)
+        return fail(RS_ERR_BAD_ARG, "%d tokens in one call", cu[n_req]);
     return RS_OK;
 }
 
@@ -1624,7 +1627,7 @@ int32_t rs_kv4_write(rs_ctx *c, int32_t side, int32_t layer, const void *k, cons
     const int width = c->m.n_kv_heads * c->m.head_dim;
     if ((rc = check_kv4_rows("k", k, row_stride, width)) || (rc = check_kv4_rows("v", v, row_stride, width))) return rc;
     Kv4RowsArgs a = kv4_rows_args(c, side, layer, row_stride, tables, max_blk);
-    if ((rc = kv4_runs(cu_seqlens, start_pos, n_req, max_blk, &a.seq))) return rc;
+    if ((rc = kv4_runs(c, cu_seqlens, start_pos, n_req, max_blk, &a.seq))) return rc;
     a.k = (const bf16_t *)k;
     a.v = (const bf16_t *)v;
     if ((rc = check_kv4_side(c, side))) return rc;
@@ -1663,7 +1666,7 @@ int32_t rs_kv4_read(rs_ctx *c, int32_t side, int32_t layer, void *k_out, void *v
     const int width = c->m.n_kv_heads * c->m.head_dim;
     if ((rc = check_kv4_rows("k_out", k_out, row_stride, width)) || (rc = check_kv4_rows("v_out", v_out, row_stride, width))) return rc;
     Kv4RowsArgs a = kv4_rows_args(c, side, layer, row_stride, tables, max_blk);
-    if ((rc = kv4_runs(cu_seqlens, start_pos, n_req, max_blk, &a.seq))) return rc;
+    if ((rc = kv4_runs(c, cu_seqlens, start_pos, n_req, max_blk, &a.seq))) return rc;
     a.k_out = (bf16_t *)k_out;
     a.v_out = (bf16_t *)v_out;
     if ((rc = check_kv4_side(c, side))) return rc;
@@ -1705,7 +1708,7 @@ int32_t rs_kv4_prefill_attention(rs_ctx *c, int32_t layer, const void *q, int64_
     if ((rc = check_kv4_rows("q", q, q_stride, width)) || (rc = check_kv4_rows("out", out, out_stride, width))) return rc;
     Kv4PromptArgs a{};
     (Kv4AttnArgs &)a = kv4_attn_args(c, RS_SIDE_PREFILL, layer, q, q_stride, out, out_stride, tables, max_blk);
-    if ((rc = kv4_runs(cu_seqlens, start_pos, n_req, max_blk, &a.seq))) return rc;
+    if ((rc = kv4_runs(c, cu_seqlens, start_pos, n_req, max_blk, &a.seq))) return rc;
     if (a.seq.cu[n_req] > c->lim.max_prefill_tokens)
         return fail(RS_ERR_BAD_ARG, "%d rows, the limit is %d", a.seq.cu[n_req], c->lim.max_prefill_tokens);
     if ((rc = check_kv4_side(c, RS_SIDE_PREFILL))) return rc;

@@ -9,7 +9,8 @@ LEVELS = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
 
 def f64(bits):
     """bf16 patterns (uint16) -> float64."""
-    return (np.ascontiguousarray(bits, np.uint16).astype(np.uint32) << 16).view(np.float32).astype(np.float64)
+    with np.errstate(invalid="ignore"):
+        return (np.ascontiguousarray(bits, np.uint16).astype(np.uint32) << 16).view(np.float32).astype(np.float64)
 
 
 def to_bf16_bits(x):
@@ -25,9 +26,7 @@ def quantise(x):
     finite = np.isfinite(x).all(-1)
     y = np.where(finite[..., None], x, 0.0)
     amax = np.abs(y).max(-1)
-    b = np.full(amax.shape, 2)
-    for e in range(2, 252):   # the smallest scale of which 7 are more than amax
-        b = np.where((b == e) & (amax >= 7.0 * 2.0 ** (e - 127)), e + 1, b)
+    b = 2 + np.searchsorted(7.0 * 2.0 ** (np.arange(2, 252) - 127.0), amax, side="right")   # the smallest scale of which 7 are more than amax
     r = np.abs(y) / (2.0 ** (b - 127.0))[..., None]
     d = np.abs(r[..., None] - LEVELS)
     near = d.min(-1, keepdims=True)

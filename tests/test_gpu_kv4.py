@@ -336,6 +336,47 @@ def test_what_is_not_finite_reaches_the_rows_that_see_it_only(heads):
     c.c.destroy()
 
 
+@pytest.mark.parametrize("bad", [0x7FC0, 0xFF80])
+def test_a_query_that_is_not_finite_stays_in_its_row_and_head(bad):
+    """A NaN or an infinity in one head of one row: that head of that row is NaN, everything else is as it was, to the bit; whole
+    rows and shares of them, prompts uncut and cut."""
+    n = 2000
+    c = Cache((8, 2, 128), 300, max_prefill=40, max_batch=3, max_context=9000)
+    tab, dtab = c.tables([n, n])
+    c.fill(tab, [n, n])
+    wide_tab = torch.from_numpy(np.concatenate([tab, np.full((2, 563 - tab.shape[1]), -1, np.int32)], 1)).cuda()
+    clean = c.queries(40)
+    spoilt = clean.copy()
+    spoilt[1, 5, 77] = bad
+    outs = []
+    for q in (clean, spoilt):
+        outs.append([run_decode(c, q[:2], [900, 1000], dtab, tab.shape[1], 1001), run_decode(c, q[:2], [1999, 1990], wide_tab, 563, 9000),
+                     run_prefill(c, q, [0, 40, 40], None, dtab, tab.shape[1]), run_prefill(c, q[:20], [0, 20, 20], [1900, 0], dtab, tab.shape[1])])
+    for x, y in zip(*outs):
+        nan = np.zeros(y.shape[:2], bool)
+        nan[1, 5] = True
+        assert np.isnan(y[nan]).all() and np.array_equal(y[~nan], x[~nan]) and np.isfinite(x).all()
+    c.c.destroy()
+
+
+def test_a_prompt_of_65536_rows_of_one_head_cut_in_two():
+    """More rows to join than one dimension of a launch has room for."""
+    n, hd = 65536, 64
+    c = Cache((1, 1, hd), n // 16, max_prefill=n, max_context=n)
+    c.ref[:] = c.g.integers(0, 256, c.ref.shape, dtype=np.uint8)
+    c.ref[..., 16 * hd:] = c.ref[..., 16 * hd:] % 8 + 120
+    c.pool.copy_(torch.from_numpy(c.ref))
+    tab, dtab = c.tables([n], extra=0)
+    q = c.queries(n)
+    got = run_prefill(c, q, [0, n], None, dtab, tab.shape[1])
+    blocks = c.ref[0, tab[0]].reshape(1, n // 16, 17 * hd)   # a block as a head
+    k, v = (np.stack(x, 1).reshape(n, 1, hd) for x in zip(*[R.get(blocks, hd, 0, t) for t in range(16)]))
+    for i in (0, 1, 127, 128, 8191, 40000, n - 1):
+        want, bound = R.attention(R.f64(q[i:i + 1]), k[:i + 1], v[:i + 1], i)
+        held_to(got[i:i + 1], want, bound, f"row {i}")
+    c.c.destroy()
+
+
 def test_bad_blocks_and_lengths_are_reported_and_nothing_is_touched():
     """Ids outside the pool in every call, lengths outside the bound: nothing is read or written there, the next sync says so, and the
     other requests' results stay the same to the bit."""

@@ -183,10 +183,11 @@ def test_captured_step_is_the_eager_one_over_replays():
     assert np.isfinite(S.bf16_bits_to_f32(eager[0])).all() and not np.array_equal(eager[0], eager[3])
 
 
-def test_calls_captured_by_the_caller_and_replayed():
+@pytest.mark.parametrize("width", [64, 160])   # whole rows, and shares of them
+def test_calls_captured_by_the_caller_and_replayed(width):
     """Append, attention and reading back recorded from the decode side's stream into one graph; two graphs, of different batch
     sizes, that share the side's workspace.  Replays with other queries, tokens and lengths are the eager calls' results to the bit."""
-    Hq, Hkv, hd, n_blocks, width = 8, 2, 128, 400, 64
+    Hq, Hkv, hd, n_blocks = 8, 2, 128, 1000
     g = np.random.default_rng(2)
     pool = torch.zeros((1, n_blocks, Hkv, 17 * hd), dtype=torch.uint8, device="cuda")
     c = rs.Context(d_model=256, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=hd, ffn_dim=256, n_layers=1, rms_eps=1e-5, rope_base=1e4, max_pos=64,

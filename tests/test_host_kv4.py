@@ -3,6 +3,7 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2601_11822_amd as rs
 from tests import kv4_ref as R
@@ -86,7 +87,8 @@ RUNS = [(dict(cu_seqlens=[1, 5]), -1), (dict(cu_seqlens=[0]), -1), (dict(cu_seql
         (dict(cu_seqlens=[0, 5, 4]), -1), (dict(cu_seqlens=[0, 65]), -4)]
 K = [(dict(k=None), -1), (dict(v=None), -1), (dict(k=P + 8), -1), (dict(v=P + 2), -1), (dict(row_stride=120), -1), (dict(row_stride=132), -1)]
 STARTS = [(dict(cu_seqlens=[0, 5], start_pos=[60]), -4), (dict(cu_seqlens=[0, 5], start_pos=[-1]), -1),
-          (dict(cu_seqlens=[0, 5], start_pos=[2**31 - 2]), -1), (dict(cu_seqlens=[0, 64], start_pos=[0]), -6)]
+          (dict(cu_seqlens=[0, 5], start_pos=[2**31 - 2]), -1), (dict(cu_seqlens=[0, 64], start_pos=[0]), -6),
+          (dict(cu_seqlens=[0, 268435456], max_blk=1 << 25), -1), (dict(cu_seqlens=[0, 268434000], max_blk=1 << 25), -6)]
 CALLS = (
     [("kv4_write", WRITE, ch, code) for ch, code in COMMON + SIDE + RUNS[:4] + K + STARTS + [({}, -6)]]
     + [("kv4_read", WRITE, ch, code) for ch, code in COMMON + SIDE + RUNS[:4] + K + STARTS + [({}, -6)]]
@@ -117,6 +119,8 @@ def test_a_bf16_context_refuses_them_and_a_wrong_count_of_positions_is_seen():
         _refused(rs.RS_ERR_STATE, getattr(c, name), **kw)
     c.destroy()
     c = _ctx()
+    for cu in (np.array([0, 5, 5, 30]), torch.tensor([0, 5, 5, 30]), (0, 5, 5, 30)):
+        _refused(rs.RS_ERR_STATE, c.kv4_write, **dict(WRITE, cu_seqlens=cu, start_pos=np.array([3, 64, 39], np.int32)))
     with pytest.raises(ValueError):
         c.kv4_write(**dict(WRITE, start_pos=[0]))
     c.destroy()
