@@ -136,7 +136,8 @@ int32_t rs_init(const rs_model_desc *model, const rs_pool_desc *pool, const rs_l
                 const rs_profile *prof, int32_t device, rs_ctx **out);
 /* rs_init for a context whose cache is held in 4 bits.  Every call that serves a bf16 cache serves it too, layer passes
  * (dense and sparse feed-forward blocks), captured and hybrid ones, rs_step_tokens and the engine, but for
- * rs_decode_layer_noalloc (RS_ERR_STATE).  Allocates two more workspaces, for attention whose rows more than one workgroup
+ * rs_decode_layer_noalloc (RS_ERR_STATE); a decode row's last bits may then depend on the lengths of the other rows'
+ * contexts (rs_kv4_decode_attention).  Allocates two more workspaces, for attention whose rows more than one workgroup
  * computes: 131072 partial rows of head_dim + 2 floats on the prefill side (68 MB at head_dim 128), and on each side that
  * serves decode rows 1024 for each query head of a KV head (2 * n_q_heads where there are more than 512 KV heads). */
 int32_t rs_init_kv4(const rs_model_desc *model, const rs_kv4_desc *pool, const rs_limits *limits,
