@@ -671,6 +671,8 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
 //   48 rows of 1000 to 2000 21.9 / 19.6 / 22.9;  of 500 to 6000 39.4 / 43.8 / 37.0;  64 of 4095 50.9 / 46.0 / 48.6
 //   64 rows of 0 to 4095 36.5 / 33.6 / 35.4;  of 0 to 8000 62 / 61 / 54;  128 of 100 to 2500 46.3 / 39.4 / 44.2;  of 0 to 4600 70 / 67 / 65
 //   256 rows of 0 to 2300 80 / 63 / 80;  200 rows of 0 to 1500, 4 heads of 64 19.6 / 17.8 / 26.0
+// Few rows of up to 2048 are whole for another reason: where several contexts, on hardware queues of their own, are active in turn, no
+// kernel takes less than 9.6 us (three contexts, 8 rows of 200 to 2000: whole 10.7, shares and their join 20.0).
 // Equal shares: of 512 workgroups (64 rows of 4095: 48.6; of 768 55.6, of 1024 51.4), of 2 units at least and as many as make 8 pieces
 // of the longest row, or of 8 and more that make 32 (shares of 2 / 4 / 8 units: 8 rows of 200 to 2000 11.0 / 13.3 / 15.4, 4 of 1000 to 4000
 // 12.2 / 10.9 / 12.8).
@@ -687,7 +689,7 @@ void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &args) {
     Kv4AttnArgs a = args;
     if (a.B <= 0) return;
     const int64_t pairs = (int64_t)a.B * a.Hkv;
-    const int64_t whole = pairs <= 256 ? std::max<int64_t>(1280, 24 * pairs) : 4608, units = (a.max_ctx + 127) / 128;
+    const int64_t whole = pairs <= 256 ? std::max<int64_t>(2048, 24 * pairs) : 4608, units = (a.max_ctx + 127) / 128;
     a.wgs = a.max_ctx <= whole ? 0 : kv4_wgs(a.Hkv);
     a.least = (int)std::max({(int64_t)2, std::min<int64_t>(8, (units + 7) / 8), (units + 31) / 32});
     if (a.wgs) {
