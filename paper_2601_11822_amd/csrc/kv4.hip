@@ -325,6 +325,11 @@ __device__ __forceinline__ bf16_t *kv4_out(const Kv4AttnArgs &a, int row, int co
     return a.out_Mt ? a.out + packed_offset(a.out_row0 + row, col, a.out_Mt) + (col & 7) : a.out + (size_t)row * a.out_stride + col;
 }
 
+// Weights are relative to a reference that is moved to the running maximum once a score is this far above it, so they are at most
+// 2^4: a bf16 is as fine there as below 1, and the accumulators are rescaled in a few tiles of a long context instead of in two of
+// five (16384 prompt rows 1800 -> 1694 us; the error against float64 0.0019 -> 0.0020 of the result).
+#define KV4_REF_BEHIND 4.f
+
 // ---- pieces of rows ---------------------------------------------------------------------------------------------------------
 // A row of one head that several workgroups compute leaves a piece each: the weighted sum of values, relative to the piece's own
 // maximum, that maximum and the sum of weights.  A workgroup joins the pieces of the heads of one kv head of one
@@ -545,8 +550,11 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && !CUT ? 4 : 2) void kv4_decode_k
                     for (int g = 0; g < G; ++g) f.vs[u][g] &= keep;   // what is behind the context may read as NaN
                 }
             }
-            const float m_tile = max_of_quarters(fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3]))));
-            const float m_new = fmaxf(m_run, m_tile), ms = m_new == NEG_INF ? 0.f : m_new;
+            float m_tile = NEG_INF;   // (one by one: three at a time, and no instructions that only quiet a NaN)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m_tile = fmaxf(m_tile, s[i >> 2][i & 3]);
+            m_tile = max_of_quarters(m_tile);
+            const float m_new = m_tile > m_run + KV4_REF_BEHIND ? m_tile : m_run, ms = m_new == NEG_INF ? 0.f : m_new;
             bf16x8 pf;   // the weights are rounded to bf16 for the second product (at most 2^-8 each); their sum is of the unrounded ones
             float psum = 0.f;
 #pragma unroll
@@ -719,9 +727,6 @@ void kv4_kernels_init() {
 // V in LDS: per block two halves [hd][8 tokens], half i the quads i and 2 + i, the dims of a group even ones first: the order
 // in which a lane holds its scores, so the weights need no exchange between lanes.
 #define KV4_MIN_TILES 4   // key tiles of a piece at least
-// Weights are at most 2^4: a bf16 is as fine there as below 1, and the accumulators are rescaled in a few tiles of a long prompt
-// instead of in two of five (16384 rows 1800 -> 1694 us; the error against float64 0.0019 -> 0.0020 of the result).
-#define KV4_REF_BEHIND 4.f
 template <int HD> struct Kv4Lds {
     static constexpr int K = 4 * 8 * HD, KS = 4 * (HD / 2), V = 4 * 2 * HD * 16, TILE = K + KS + V;
 };
