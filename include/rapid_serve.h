@@ -227,7 +227,7 @@ int32_t rs_decode_layer(rs_ctx *ctx, int32_t layer, const void *x_in, void *x_ou
  * current stream and returns; calls on one side are ordered, between the sides the caller orders them.  Block ids come from
  * rs_kv_alloc.  Rows are bf16, `row_stride` elements apart (a multiple of 8, and 16-byte aligned; at least the row's own
  * length).  A block id outside the pool is never dereferenced: what it would have held is skipped (rows that would be read
- * from it are zero), and rs_sync reports RS_ERR_BAD_BLOCK.
+ * from it are zero; attention is over the other tokens, and zero where there are none), and rs_sync reports RS_ERR_BAD_BLOCK.
  *
  * rs_kv4_write: quantises keys (after the rotary embedding) and values of runs of tokens.  Rows [cu_seqlens[r],
  * cu_seqlens[r+1]) of k and v, n_kv_heads * head_dim elements each, are the tokens at positions start_pos[r], start_pos[r] + 1,

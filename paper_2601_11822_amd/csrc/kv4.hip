@@ -783,13 +783,15 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_prefill_kernel(Kv4PromptArgs a
     kvec rk;
     uint32_t rks;
     vvec rv[2], rs[2];
-    bool r_ok = true;      // whether the block of what was fetched is one of the pool
-    int next_blk = 0;      // block of the tile to fetch next, asked for a tile ahead
-    auto block_at = [&](int kt) { return tab[min(kt * 4 + wb, (kv_end - 1) >> 4)]; };   // (behind the context: its last one, which nobody looks at)
-    auto fetch = [&](int kt) {   // and asks for the block id of the tile after it
-        const int blk = __builtin_amdgcn_readfirstlane(next_blk);
-        r_ok = (unsigned)blk < (unsigned)a.n_blocks;
-        const uint8_t *p = a.pool + ((size_t)(r_ok ? blk : 0) * a.Hkv + hk) * F::BYTES;
+    // A lane's block of the tile to fetch next (the lane & 3-th), asked for a tile ahead (behind the context: its last one, which nobody
+    // looks at).  So every wave knows which of all four are none of the pool: their tokens are masked.
+    int next_blk = 0;
+    uint32_t r_none = 0, none = 0;   // those, a bit each, of what was fetched and of the tile that comes next
+    auto block_at = [&](int kt) { return tab[min(kt * 4 + (lane & 3), (kv_end - 1) >> 4)]; };
+    auto fetch = [&](int kt) {   // and asks for the block ids of the tile after it
+        r_none = (uint32_t)__ballot((unsigned)next_blk >= (unsigned)a.n_blocks) & 15;
+        const int blk = __builtin_amdgcn_readlane(next_blk, wb);
+        const uint8_t *p = a.pool + ((size_t)((r_none >> wb) & 1 ? 0 : blk) * a.Hkv + hk) * F::BYTES;
         rk = *(const kvec *)(p + (uint32_t)((64 * wp + lane) * (HD / 8 / WPB)));
         rks = *(const uint32_t *)(p + (uint32_t)(F::KS + 4 * k_scales));
 #pragma unroll
@@ -799,8 +801,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_prefill_kernel(Kv4PromptArgs a
         }
         next_blk = block_at(min(kt + 1, kt1 - 1));
     };
-    auto refuse = [&]() {   // a block that is none: small scores, no values
-        if (r_ok) return;
+    auto refuse = [&]() {   // a block that is none: nothing that reads as NaN
+        if (!((r_none >> wb) & 1)) return;
         if (lane == 0) atomicOr(a.err_flag, 2);
         rks = 0;
         rs[0] = rs[1] = 0;
@@ -865,7 +867,9 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_prefill_kernel(Kv4PromptArgs a
         constexpr int B = decltype(btag)::value;
         uint8_t *t = smem_kv4p + B * L::TILE, *other = smem_kv4p + (1 - B) * L::TILE;
         const int kv0 = kt * 64;
+        const uint32_t hidden = none;
         refuse();
+        none = r_none;
         u32x4_t kc[2][KSTEP];
         int ks[2][KSTEP];
 #pragma unroll
@@ -892,12 +896,16 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_prefill_kernel(Kv4PromptArgs a
         asm volatile("" : "+v"(st[0]), "+v"(st[1]));   // the products stay in front of the branch
         put_nan(other);
         fetch(min(kt + 2, kt1 - 1));
-        if (kv0 + 63 > w_min) {   // only tiles that touch the diagonal need the mask
+        // Only tiles that touch the diagonal, or lack a block, need the mask (one for both: with a branch of its own for a missing block
+        // 16384 rows took 1659 us, so 1645, without it 1633).
+        if (kv0 + 63 > w_min || hidden) {
 #pragma unroll
-            for (int t2 = 0; t2 < 2; ++t2)
+            for (int b4 = 0; b4 < 4; ++b4) {
+                const int last = (hidden >> b4) & 1 ? -1 : q_pos;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (kv0 + 32 * t2 + (i >> 2) * 8 + 4 * h + (i & 3) > q_pos) st[t2][i] = NEG_INF;
+                for (int i = 8 * (b4 & 1); i < 8 * (b4 & 1) + 8; ++i)
+                    if (kv0 + 32 * (b4 >> 1) + (i >> 2) * 8 + 4 * h + (i & 3) > last) st[b4 >> 1][i] = NEG_INF;
+            }
         }
         float m_tile = NEG_INF;
 #pragma unroll
@@ -958,6 +966,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_prefill_kernel(Kv4PromptArgs a
         next_blk = block_at(kt0);
         fetch(kt0);
         refuse();
+        none = r_none;
 #pragma unroll
         for (int i = 0; i < PARTS; ++i) put(i, smem_kv4p);
         put_nan(smem_kv4p);
