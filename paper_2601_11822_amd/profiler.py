@@ -21,7 +21,9 @@ layer times `n_layers` (every layer of a Llama-style stack has the same shape).
 Decode loads are keyed like the manager keys them: decode batch size and total cached tokens.
 A load (B, S) is profiled with B requests of S / B cached tokens each, shuffled block tables.
 
-    python -m paper_2601_11822_amd.profiler --out profile.json --md profile.md
+A table holds for the kind of cache it was measured over: with `--kv4` that is the cache held in 4 bits.
+
+    python -m paper_2601_11822_amd.profiler --out profile.json --md profile.md [--kv4]
     python -m paper_2601_11822_amd.profiler --rows-curve [--shape ..] [--cus 256,128] [--rows ..] [--md out.md]
 """
 from __future__ import annotations
@@ -30,11 +32,11 @@ import argparse
 import json
 import sys
 import time
-from typing import Dict, List, Sequence
+from typing import Dict, List, Optional, Sequence
 
 import numpy as np
 
-from . import KERNEL_SLOT_NAMES, Context, Profile, timing
+from . import KERNEL_SLOT_NAMES, Context, Profile, kv4_bytes, timing
 
 TOTAL_CUS = 256
 
@@ -44,10 +46,10 @@ def _log(*a):
 
 
 class Rig:
-    """Weights, KV pools and activations of one layer, sized for the largest profiled load."""
+    """Weights, KV pools (kv4: one in 4 bits) and activations of one layer, sized for the largest profiled load."""
 
     def __init__(self, shape, batch_edges: Sequence[int], ctx_edges: Sequence[int], prefill_tokens: int,
-                 max_context: int, device: int = 0, experts: int = 0):
+                 max_context: int, device: int = 0, experts: int = 0, kv4: bool = False):
         import torch
         import rs_synth as S
         self.S, self.torch, self.shape = S, torch, shape
@@ -68,12 +70,17 @@ class Rig:
         g = torch.Generator(device=dev)
         g.manual_seed(S.SEED_CACHE)
         Hkv, hd = shape.n_kv_heads, shape.head_dim
-        self.k_pool = torch.randn((self.n_blocks, Hkv, 16, hd), generator=g, device=dev, dtype=torch.float32).to(torch.bfloat16)
-        self.v_pool = torch.randn((self.n_blocks, Hkv, hd, 16), generator=g, device=dev, dtype=torch.float32).to(torch.bfloat16)
+        self.kv_cache = "4-bit" if kv4 else "bf16"
+        if kv4:   # any codes, scales of 2^-3 to 1
+            pool = torch.randint(0, 256, (self.n_blocks, Hkv, kv4_bytes(hd)), generator=g, device=dev, dtype=torch.uint8)
+            pool[..., 16 * hd:] = pool[..., 16 * hd:] % 4 + 124
+            self.pools = {"kv4_pool": pool}
+        else:
+            normal = lambda *sh: torch.randn(sh, generator=g, device=dev, dtype=torch.float32).to(torch.bfloat16)
+            self.pools = {"k_pool": normal(self.n_blocks, Hkv, 16, hd), "v_pool": normal(self.n_blocks, Hkv, hd, 16)}
         self.max_batch = max(batch_edges)
         self.c = Context.from_shape(shape, max_pos=max(max_context, prefill_tokens), n_blocks=self.n_blocks,
-                                    k_pool=self.k_pool, v_pool=self.v_pool, max_prefill_tokens=prefill_tokens,
-                                    max_decode_batch=self.max_batch, max_context=max_context, device=device)
+                                    **self.pools, max_prefill_tokens=prefill_tokens, max_decode_batch=self.max_batch, max_context=max_context, device=device)
         self.c.set_weights(0, w["g1"], w["wqkv"], w["wo"], w["g2"], w["wg"], w["wu"], w["wd"])
         self._w = w
         if experts:   # sparse feed-forward block (random weights: only the timing matters here)
@@ -153,20 +160,26 @@ def profile(rig: Rig, batch_edges: Sequence[int], ctx_edges: Sequence[int], deco
         "batch_edges": list(map(int, batch_edges)), "ctx_edges": list(map(int, ctx_edges)),
         "decode_cus": list(map(int, decode_cus)), "lat_distinct_us": lat_distinct.tolist(),
         "lat_over_us": lat_over.tolist(),
-        "meta": {"shape": rig.shape.name, "n_layers": n_layers, "prefill_tokens": rig.T, "steps": steps,
+        "meta": {"shape": rig.shape.name, "kv_cache": rig.kv_cache, "n_layers": n_layers, "prefill_tokens": rig.T, "steps": steps,
                  "unit": "microseconds per decode step of the whole model (one layer x n_layers), p50 under co-run"},
         "curves": curves,
     }
 
 
-def load_profile(path_or_dict, slo_us: int) -> Profile:
+def load_profile(path_or_dict, slo_us: int, kv_cache: Optional[str] = None) -> Profile:
+    """The table as rs_init takes it.  kv_cache ("bf16" or "4-bit"): refuse one that was measured over the other kind (a table that does
+    not say is of the bf16 cache)."""
     d = path_or_dict if isinstance(path_or_dict, dict) else json.load(open(path_or_dict))
+    of = d.get("meta", {}).get("kv_cache", "bf16")
+    if kv_cache is not None and of != kv_cache:
+        raise ValueError(f"the profile was measured over a {of} KV cache, not over a {kv_cache} one")
     return Profile(d["batch_edges"], d["ctx_edges"], d["decode_cus"], d["lat_distinct_us"], d["lat_over_us"], slo_us)
 
 
 def to_markdown(d: Dict) -> str:
     m = d["meta"]
-    out = [f"# Offline profile of the decode step against the CU split ({m['shape']}, prefill of {m['prefill_tokens']} tokens beside it)\n",
+    cache = ", KV cache in 4 bits" if m.get("kv_cache") == "4-bit" else ""
+    out = [f"# Offline profile of the decode step against the CU split ({m['shape']}{cache}, prefill of {m['prefill_tokens']} tokens beside it)\n",
            "Written by `python -m paper_2601_11822_amd.profiler` (command at the end).  Milliseconds for ONE layer; the",
            f"manager's table holds the same co-run latencies x {m['n_layers']} layers in microseconds.\n"]
     for rec in d["curves"]:
@@ -195,12 +208,13 @@ def main(argv=None):
     ap.add_argument("--prefill-tokens", type=int, default=2048)
     ap.add_argument("--max-context", type=int, default=16385)
     ap.add_argument("--steps", type=int, default=10)
+    ap.add_argument("--kv4", action="store_true", help="over a KV cache held in 4 bits")
     ap.add_argument("--out", default="profile.json")
     ap.add_argument("--md", default=None)
     a = ap.parse_args(argv)
     ints = lambda s: [int(v) for v in s.split(",")]
     be, ce, dc = ints(a.batch_edges), ints(a.ctx_edges), ints(a.decode_cus)
-    rig = Rig(S.SHAPES[a.shape], be, ce, a.prefill_tokens, a.max_context)
+    rig = Rig(S.SHAPES[a.shape], be, ce, a.prefill_tokens, a.max_context, kv4=a.kv4)
     d = profile(rig, be, ce, dc, a.n_layers, steps=a.steps)
     d["meta"]["command"] = "python -m paper_2601_11822_amd.profiler " + " ".join(sys.argv[1:] if argv is None else argv)
     with open(a.out, "w") as f:

@@ -268,13 +268,16 @@ def main(argv=None):
             be = sorted({b for b in (16, 32, 64, 128, 256) if b < a.max_batch} | {a.max_batch})
             ce, dc = sorted(int(x) for x in a.profile_ctx_edges.split(",")), [32, 64, 96, 128, 160, 192]
             rig = profiler.Rig(shape, be, ce, prefill_tokens=a.profile_prefill_tokens, max_context=a.max_prompt + a.max_out,
-                               experts=a.experts)
+                               experts=a.experts, kv4=a.kv4)
             d = profiler.profile(rig, be, ce, dc, a.layers, steps=6, warmup=2)
             rig.c.destroy()
             del rig
         else:
             d = json.load(open(a.profile))
-        prof = profiler.load_profile(d, int(a.slo_ms * 1000))
+        try:
+            prof = profiler.load_profile(d, int(a.slo_ms * 1000), kv_cache="4-bit" if a.kv4 else "bf16")
+        except ValueError as e:
+            ap.error(f"--profile {a.profile}: {e}")
     work = make_workload(a.requests, a.rate, a.prompt_mean, a.prompt_sd, a.out_mean, a.out_sd, (a.min_prompt, a.max_prompt),
                          (16, a.max_out), a.vocab, a.seed)
     t0 = time.time()
