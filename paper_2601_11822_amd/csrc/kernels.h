@@ -115,6 +115,9 @@ struct Kv4PromptArgs : Kv4AttnArgs {
 };
 #define KV4_PIECES 1024        // most (unit, kv head, key range) pieces of cut rows in a launch
 int64_t kv4_decode_pieces(int Hkv);   // pieces of a decode launch, for each query head of a kv head
+// A decode launch: a workgroup of eight or of four waves for each (row, kv head), or equal shares of the tokens of all rows.
+enum Kv4DecodeForm { KV4_SHARES, KV4_WHOLE8, KV4_WHOLE4 };
+Kv4DecodeForm kv4_decode_form(int B, int Hkv, int max_ctx);
 void kv4_kernels_init();
 void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &a);
 void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &a);

@@ -669,23 +669,33 @@ __global__ __launch_bounds__(256) void kv4_merge_kernel(Kv4AttnArgs a) {
     kv4_join<HD>(a, hk, row, n, [&](int g, int j) { return n == 0 ? 0 : kv4_piece(a, hk, first + j, j == 0, g); });
 }
 
-// Which form a decode launch takes, from the sizes alone (pairs: rows times kv heads).  Equal shares cost some 10 us, counting and
-// a launch that joins pieces; a workgroup with a whole row takes 3 us and 3.6 ns (eight waves) or 4.9 (four) a token, and the longest
-// row may run alone at the end.  So whole rows where contexts are short, longer ones the more pairs there are to hide one; of eight
-// waves where there is at most a workgroup for each compute unit.  8B heads, us, whole rows of 8 waves / of 4 / equal shares:
-//   1 row of 900 tokens 8.1 / 8.7 / 8.9;  of 1900 11.8 / 13.1 / 10.1;  of 4000 19.3 / 22.5 / 10.6;  of 32000 112 / 147 / 17
-//   8 rows of 200 to 2000 12.4 / 13.6 / 11.0;  16 of 500 to 2000 12.3 / 13.7 / 15.6;  16 of 0 to 3500 17.6 / 20.3 / 16.6
-//   32 rows of 500 to 3500 18.4 / 21.2 / 21.5;  of 0 to 6000 26.9 / 33.2 / 27.5;  of 8191 to 32766 138 / 163 / 116
-//   48 rows of 1000 to 2000 21.9 / 19.6 / 22.9;  of 500 to 6000 39.4 / 43.8 / 37.0;  64 of 4095 50.9 / 46.0 / 48.6
-//   64 rows of 0 to 4095 36.5 / 33.6 / 35.4;  of 0 to 8000 62 / 61 / 54;  128 of 100 to 2500 46.3 / 39.4 / 44.2;  of 0 to 4600 70 / 67 / 65
-//   256 rows of 0 to 2300 80 / 63 / 80;  200 rows of 0 to 1500, 4 heads of 64 19.6 / 17.8 / 26.0
-// Few rows of up to 2048 are whole for another reason: where several contexts, on hardware queues of their own, are active in turn, no
-// kernel takes less than 9.6 us (three contexts, 8 rows of 200 to 2000: whole 10.7, shares and their join 20.0).
+// Which form a decode launch takes, from the sizes alone (pairs: rows times kv heads).  Equal shares cost a launch that joins pieces, and
+// where contexts are of unequal lengths a share lies over the border of two of them; a workgroup with a whole row takes 3 us and 3.6 ns
+// (eight waves) or 4.9 (four) a token, and the longest row may run alone at the end.  So whole rows where contexts are short, longer
+// ones the more pairs there are to hide one; of eight waves where there is at most a workgroup for each compute unit.  One context, its
+// calls one behind another; 8B heads, us, whole rows of 8 waves / of 4 / equal shares:
+//   1 row of 900 tokens 8.3 / 8.7 / 9.4;  of 1279 9.4 / 10.1 / 9.5;  of 1536 10.5 / 11.8 / 10.2;  of 1664 11.1 / 12.2 / 9.6;  of 2047 11.7 / 13.3 / 9.8
+//   1 row of 4000 18.4 / 22.0 / 10.7;  of 32000 110 / 147 / 17;  heads of 64: 1536 9.0 / 10.2 / 9.6;  1664 9.5 / 10.5 / 9.0
+//   2 rows of 0 to 1700 11.1 / 12.2 / 12.7;  both of 1700 11.1 / 12.3 / 9.6;  0 to 2600 13.7 / 16.2 / 13.3;  both of 2600 13.7 / 16.2 / 10.5
+//   8 rows of 0 to 1700 11.0 / 12.2 / 13.0;  of 200 to 2000 11.8 / 13.4 / 10.8;  of 1000 to 2047 11.8 / 13.4 / 14.5;  of 0 to 2600 13.8 / 16.2 / 13.6
+//   16 of 500 to 2000 12.0 / 13.6 / 16.2;  16 of 0 to 3500 17.1 / 20.2 / 18.5;  of 0 to 6000 25.0 / 31.9 / 20.5
+//   32 rows (256 pairs) of 0 to 4608 21.8 / 27.0 / 25.4;  all of 4608 29.4 / 30.5 / 34.8;  of 0 to 6144 27.5 / 34.0 / 27.6;  all of 6144 37.2 / 38.2 / 43.2
+//   33 rows (264) of 0 to 4096 23.9 / 26.7 / 24.9;  of 0 to 4608 25.8 / 29.7 / 25.0;  all of 4608 46.4 / 39.3 / 35.7;  of 0 to 6144 31.8 / 37.9 / 29.3
+//   48 rows of 0 to 4608 31.5 / 34.1 / 32.4;  all of 4608 47.9 / 44.9 / 47.0;  64 of 0 to 4096 35.9 / 33.3 / 36.3;  all of 4096 50.6 / 48.4 / 51.0
+//   64 rows of 0 to 6144 49.1 / 48.6 / 46.1;  all of 6144 72.2 / 68.8 / 71.7;  65 rows of heads of 64 of 0 to 4608 18.5 / 23.1 / 22.5
+// (Up to 256 pairs every workgroup has a compute unit to itself: rows of up to 6144 are whole there, behind it of up to 4608.  One row
+// ends with its last share, so it is cut from 1536 on, several from 2048.)
 // Equal shares: of 512 workgroups (64 rows of 4095: 48.6; of 768 55.6, of 1024 51.4), of 2 units at least and as many as make 8 pieces
 // of the longest row, or of 8 and more that make 32 (shares of 2 / 4 / 8 units: 8 rows of 200 to 2000 11.0 / 13.3 / 15.4, 4 of 1000 to 4000
 // 12.2 / 10.9 / 12.8).
 static int kv4_wgs(int Hkv) { return std::max(1, 512 / Hkv); }
 int64_t kv4_decode_pieces(int Hkv) { return 2ll * Hkv * kv4_wgs(Hkv); }
+
+Kv4DecodeForm kv4_decode_form(int B, int Hkv, int max_ctx) {
+    const int64_t pairs = (int64_t)B * Hkv;
+    if (pairs > 256) return max_ctx <= 4608 ? KV4_WHOLE4 : KV4_SHARES;
+    return max_ctx <= std::max<int64_t>(B == 1 ? 1536 : 2048, 24 * pairs) ? KV4_WHOLE8 : KV4_SHARES;
+}
 
 template <int HD, int NW, bool CUT>
 static void launch_kv4_decode_form(hipStream_t st, const Kv4AttnArgs &a) {
@@ -696,14 +706,14 @@ static void launch_kv4_decode_form(hipStream_t st, const Kv4AttnArgs &a) {
 void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &args) {
     Kv4AttnArgs a = args;
     if (a.B <= 0) return;
-    const int64_t pairs = (int64_t)a.B * a.Hkv;
-    const int64_t whole = pairs <= 256 ? std::max<int64_t>(2048, 24 * pairs) : 4608, units = (a.max_ctx + 127) / 128;
-    a.wgs = a.max_ctx <= whole ? 0 : kv4_wgs(a.Hkv);
+    const Kv4DecodeForm form = kv4_decode_form(a.B, a.Hkv, a.max_ctx);
+    const int64_t units = (a.max_ctx + 127) / 128;
+    a.wgs = form == KV4_SHARES ? kv4_wgs(a.Hkv) : 0;
     a.least = (int)std::max({(int64_t)2, std::min<int64_t>(8, (units + 7) / 8), (units + 31) / 32});
     if (a.wgs) {
         if (a.hd == 128) launch_kv4_decode_form<128, 4, true>(st, a);
         else launch_kv4_decode_form<64, 4, true>(st, a);
-    } else if (pairs <= 256) {
+    } else if (form == KV4_WHOLE8) {
         if (a.hd == 128) launch_kv4_decode_form<128, 8, false>(st, a);
         else launch_kv4_decode_form<64, 8, false>(st, a);
     } else {
