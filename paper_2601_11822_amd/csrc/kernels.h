@@ -118,6 +118,11 @@ int64_t kv4_decode_pieces(int Hkv);   // pieces of a decode launch, for each que
 // A decode launch: a workgroup of eight or of four waves for each (row, kv head), or equal shares of the tokens of all rows.
 enum Kv4DecodeForm { KV4_SHARES, KV4_WHOLE8, KV4_WHOLE4 };
 Kv4DecodeForm kv4_decode_form(int B, int Hkv, int max_ctx);
+int kv4_least_share(int max_ctx);   // units of 128 tokens of a share at least
+// A prompt launch: columns of a workgroup (128: of four waves, 256: of eight), workgroups for each kv head, rows whose keys are cut.
+// Sets fold, first, base, row and cut of a.
+struct Kv4PromptPlan { int cols, n, rows; };
+Kv4PromptPlan kv4_prompt_plan(Kv4PromptArgs &a);
 void kv4_kernels_init();
 void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &a);
 void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &a);

@@ -696,6 +696,10 @@ Kv4DecodeForm kv4_decode_form(int B, int Hkv, int max_ctx) {
     if (pairs > 256) return max_ctx <= 4608 ? KV4_WHOLE4 : KV4_SHARES;
     return max_ctx <= std::max<int64_t>(B == 1 ? 1536 : 2048, 24 * pairs) ? KV4_WHOLE8 : KV4_SHARES;
 }
+int kv4_least_share(int max_ctx) {
+    const int units = (max_ctx + 127) / 128;
+    return std::max({2, std::min(8, (units + 7) / 8), (units + 31) / 32});
+}
 
 template <int HD, int NW, bool CUT>
 static void launch_kv4_decode_form(hipStream_t st, const Kv4AttnArgs &a) {
@@ -707,9 +711,8 @@ void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &args) {
     Kv4AttnArgs a = args;
     if (a.B <= 0) return;
     const Kv4DecodeForm form = kv4_decode_form(a.B, a.Hkv, a.max_ctx);
-    const int64_t units = (a.max_ctx + 127) / 128;
     a.wgs = form == KV4_SHARES ? kv4_wgs(a.Hkv) : 0;
-    a.least = (int)std::max({(int64_t)2, std::min<int64_t>(8, (units + 7) / 8), (units + 31) / 32});
+    a.least = kv4_least_share(a.max_ctx);
     if (a.wgs) {
         if (a.hd == 128) launch_kv4_decode_form<128, 4, true>(st, a);
         else launch_kv4_decode_form<64, 4, true>(st, a);
@@ -1097,16 +1100,21 @@ static int kv4_prompt_cuts(Kv4PromptArgs &a, int cols, int *rows_cut) {
     return n;
 }
 
-void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &args) {
-    Kv4PromptArgs a = args;
-    int rows = 0;
+Kv4PromptPlan kv4_prompt_plan(Kv4PromptArgs &a) {
     // Eight waves of 32 columns convert a value once for 256 columns instead of 128, but have their compute unit to themselves: where
     // there are enough of them for the last round not to matter.  8B heads, us, four / eight waves (workgroups of eight):
     //   2048 rows (256) 44.5 / 53.3;  4096 (512) 127 / 140;  6000 (752) 249 / 254;  8192 (1024) 446 / 428;  12000 (1504) 925 / 895;  16384 1700 / 1637
     int units = 0;
     for (int r = 0; r < a.seq.n_req; ++r) units += ((a.seq.cu[r + 1] - a.seq.cu[r]) * (a.Hq / a.Hkv) + 255) / 256;
     const int cols = a.hd == 128 && units * a.Hkv >= 1024 ? 256 : 128;
+    int rows = 0;
     const int n = kv4_prompt_cuts(a, cols, &rows);
+    return {cols, n, rows};
+}
+
+void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &args) {
+    Kv4PromptArgs a = args;
+    const auto [cols, n, rows] = kv4_prompt_plan(a);
     if (n == 0) return;
     if (cols == 256) hipLaunchKernelGGL((kv4_prefill_kernel<128, 8>), dim3(a.Hkv * n), dim3(512), 2 * Kv4Lds<128>::TILE, st, a);
     else if (a.hd == 128) hipLaunchKernelGGL((kv4_prefill_kernel<128, 4>), dim3(a.Hkv * n), dim3(256), 2 * Kv4Lds<128>::TILE, st, a);
