@@ -251,6 +251,8 @@ int32_t rs_kv4_read(rs_ctx *ctx, int32_t side, int32_t layer, void *k_out, void 
  * ctx_lens[i] = -1: a row without a request, its output is zero.  B <= max_decode_batch, max_ctx (host) bounds
  * ctx_lens[i] + 1 as for rs_decode_layer (a bound near the longest context serves best).  Results depend on the sizes alone,
  * on max_ctx and the other rows' lengths too (they decide where contexts are cut), not on the CU split.
+ * Rounding: of each 32 dims of a query what is above 2^-13.9 of their largest counts, softmax weights go into the product with V as
+ * bf16, sums are float32; with the result's own rounding 0.0020 to 0.0023 of it (2-norm) against float64 over the same cache.
  * A key's group that is not finite makes the rows that see it NaN in the heads of its KV head, a value's group at least the
  * 32 dims of it (all of them where several rows are computed together, as rs_kv4_prefill_attention does).
  * The calls may be recorded into a caller's graph from the side's stream (rs_get_stream).  Attention uses the side's

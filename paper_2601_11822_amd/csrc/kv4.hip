@@ -248,7 +248,9 @@ void launch_kv4_append(hipStream_t st, const Kv4RowsArgs &a) {
 // Scores.  K stays as it is in the cache: the matrix instruction with block scales takes 4-bit rows, 32 dims and their scale a
 // lane.  The query, times log2(e) / sqrt(hd), goes in as three terms of 6 bits (e2m3: multiples of 1/8 below 2, 1/4 below 4, 1/2
 // up to 7.5), each a sixteenth of the one before: x = t0 + t1 / 16 + t2 / 256 in units of a power of two that takes the largest
-// of the 32 dims into [3.875, 7.75).  What is left of x is at most 2^-12 units, 2^-13.9 of that largest.  With 6-bit operands
+// of the 32 dims into [3.875, 7.75).  What is left of x is at most 2^-12 units, 2^-13.9 of that largest: a dim 2^j below the largest keeps
+// 13 - j bits, where a bf16 has 8.  The keys that it meets are themselves off by up to a seventh of the largest of their 32 dims; with
+// channels as loud as keys have, the result moves by 1.4e-4 of itself (2-norm), a twelfth of its own rounding to bf16.  With 6-bit operands
 // the instruction runs at four times the rate of bf16, so that three products take 3/4 of the time of bf16's, no element of K is
 // converted, and the scores come out as the exponents that the softmax wants.  (Two e4m3 terms hold a bf16 exactly, at half the
 // rate: 16384 prompt rows 1810 us, 1800 with these.)
@@ -555,7 +557,10 @@ __global__ __launch_bounds__(64 * NW, NW == 4 && !CUT ? 4 : 2) void kv4_decode_k
             for (int i = 0; i < 8; ++i) m_tile = fmaxf(m_tile, s[i >> 2][i & 3]);
             m_tile = max_of_quarters(m_tile);
             const float m_new = m_tile > m_run + KV4_REF_BEHIND ? m_tile : m_run, ms = m_new == NEG_INF ? 0.f : m_new;
-            bf16x8 pf;   // the weights are rounded to bf16 for the second product (at most 2^-8 each); their sum is of the unrounded ones
+            // The weights are rounded to bf16 for the second product (at most 2^-8 each, as in attention over a bf16 cache: two terms would
+            // double the products and their operands); their sum is of the unrounded ones.  With the result's own rounding the
+            // deviation from float64 is 0.0020 to 0.0023 (2-norm) instead of 0.0016.
+            bf16x8 pf;
             float psum = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -941,8 +946,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kv4_prefill_kernel(Kv4PromptArgs a
             st[1] -= by;
             if (moves) limit = KV4_REF_BEHIND;
         }
-        // weights of a block, a pair at a time, rounded to bf16 for the product (at most 2^-8 each); their sum is of the unrounded
-        // ones (plain additions: the dot instruction, half as many, does not run beside the matrix unit)
+        // weights of a block, a pair at a time, rounded to bf16 for the product (at most 2^-8 each, as in decode); their sum is of the
+        // unrounded ones (plain additions: the dot instruction, half as many, does not run beside the matrix unit)
         u32x4_t pw[2];
         auto weights = [&](int b4, int w0, int n) {
 #pragma unroll
@@ -1039,11 +1044,14 @@ __global__ __launch_bounds__(256) void kv4_prompt_merge_kernel(Kv4PromptArgs a) 
 }
 
 // How many pieces the keys of each request's units are cut into, from the sizes alone: the number of key tiles of a piece that
-// makes the launch shortest by this account, in us.  A compute unit takes 0.85 us a tile (head_dim 128) with two workgroups of four
-// waves, 0.95 with one, 1.65 with one of eight; the longest piece is the tail.  Pieces are joined by a launch of their own, 5 us, and pass through memory as
-// float32, 0.2 us a MB written and read.  8B heads, us, uncut / the longest unit in 2, 4, 8, 24 pieces (chosen):
-//   19 rows behind 6005 tokens 96 / 56, 34, 23, 18 (24);  512 behind 8000 133 / 86, 78, 85, 84 (2);  512 behind 1024 31.5 (1) / 33, 33, 45, 40
-//   512 rows 16.1 (1) / 25, 27, 40, 40;  1024 rows 24.8 (1) / 41, 47, 47, 47;  2000 rows beside 100 behind 8000 145 / 93, 71, 71, 77 (3: 77)
+// makes the launch shortest by this account, in us.  A compute unit is taken to need 0.85 a tile (head_dim 128) with two workgroups of
+// four waves, 0.95 with one, 1.65 with one of eight; the longest piece is the tail.  Pieces are joined by a launch of their own, 5 us, and pass
+// through memory as float32, 0.2 us a MB written and read.  These are numbers that put the forms in the measured order, not the times of a
+// tile (a wave that has a SIMD to itself takes 1.3 us): 2048 rows are 35 by the account and 46 as measured.  8B heads, us, uncut / the
+// longest unit in 2, 4 pieces / in more (chosen):
+//   19 rows behind 6005 tokens 97 / 57, 35 / 9: 24, 24: 19 (24);  512 behind 8000 135 / 84, 78 (4);  2000 rows beside 100 behind 8000 146 / 95, 72 (4)
+//   512 behind 1024 31 (1) / 32;  512 rows 16 (1) / 24;  1024 rows 25 (1) / 36, 44;  2048 rows 46 (1) / 74
+//   70B heads, 700 rows behind 1024, 33 behind 4000 and 1391: 93 / 81 (2);  heads of 64, 19 behind 6005 76 / 46, 29 / 9: 21, 24: 18 (24)
 // Returns the workgroups for each kv head, *rows_cut the rows to join.
 static int kv4_prompt_cuts(Kv4PromptArgs &a, int cols, int *rows_cut) {
     const int G = a.Hq / a.Hkv;
@@ -1103,7 +1111,7 @@ static int kv4_prompt_cuts(Kv4PromptArgs &a, int cols, int *rows_cut) {
 Kv4PromptPlan kv4_prompt_plan(Kv4PromptArgs &a) {
     // Eight waves of 32 columns convert a value once for 256 columns instead of 128, but have their compute unit to themselves: where
     // there are enough of them for the last round not to matter.  8B heads, us, four / eight waves (workgroups of eight):
-    //   2048 rows (256) 44.5 / 53.3;  4096 (512) 127 / 140;  6000 (752) 249 / 254;  8192 (1024) 446 / 428;  12000 (1504) 925 / 895;  16384 1700 / 1637
+    //   2048 rows (256) 47 / 57;  4096 (512) 133 / 146;  6000 (752) 263 / 264;  8192 (1024) 471 / 450;  12000 (1504) 978 / 936;  16384 1785 / 1707
     int units = 0;
     for (int r = 0; r < a.seq.n_req; ++r) units += ((a.seq.cu[r + 1] - a.seq.cu[r]) * (a.Hq / a.Hkv) + 255) / 256;
     const int cols = a.hd == 128 && units * a.Hkv >= 1024 ? 256 : 128;
