@@ -249,7 +249,7 @@ void launch_kv4_append(hipStream_t st, const Kv4RowsArgs &a) {
 // lane.  The query, times log2(e) / sqrt(hd), goes in as three terms of 6 bits (e2m3: multiples of 1/8 below 2, 1/4 below 4, 1/2
 // up to 7.5), each a sixteenth of the one before: x = t0 + t1 / 16 + t2 / 256 in units of a power of two that takes the largest
 // of the 32 dims into [3.875, 7.75).  What is left of x is at most 2^-12 units, 2^-13.9 of that largest: a dim 2^j below the largest keeps
-// 13 - j bits, where a bf16 has 8.  The keys that it meets are themselves off by up to a seventh of the largest of their 32 dims; with
+// 13 - j bits, where a bf16 has 8.  The keys that it meets are themselves off by up to a fifth of the largest of their 32 dims; with
 // channels as loud as keys have, the result moves by 1.4e-4 of itself (2-norm), a twelfth of its own rounding to bf16.  With 6-bit operands
 // the instruction runs at four times the rate of bf16, so that three products take 3/4 of the time of bf16's, no element of K is
 // converted, and the scores come out as the exponents that the softmax wants.  (Two e4m3 terms hold a bf16 exactly, at half the
