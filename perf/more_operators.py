@@ -1,0 +1,598 @@
+"""Operators over the bf16 paged KV cache for steps that are no whole layer pass: windowed attention, drafted trees, and the cache's upkeep
+on the GPU.
+
+kind "plan":    block tables, slots, positions and the trees' ancestor masks of a step's new tokens, from the requests' lengths.
+kind "store":   queries and keys of new tokens rotated (positions on one axis, or on three), keys and values written to their slots.
+kind "decode":  attention of one row per request to a window of its latest tokens and to its first few (sinks).
+kind "prefill": the same for several rows per request, each causal.
+kind "tree":    attention of the tokens of a drafted tree to the cached tokens and to their ancestors.
+kind "compact": the tokens of the accepted path moved behind the cached ones, in every layer.
+
+The cache (one layer): blocks of 16 tokens, K [n_blocks][kv heads][head_dim/32][4][16][8], where token slot t of a block is row p(t), t
+with bits 2 and 3 swapped, and V [n_blocks][kv heads][head_dim][16].
+
+Lengths follow from the case alone, so that every seed is the same amount of work; the seed draws the values, the order of the
+requests, the shapes of the trees and the blocks.
+"""
+import math
+
+import numpy as np
+import torch
+
+own = False
+
+ROPE_BASE = 500000.0
+
+
+def _case(kind, name=None, hq=32, hkv=8, hd=128, prompts="", starts="", batch=0, ctx_lo=0, ctx_hi=0, empty=0, window=0, sinks=0, draft=0,
+          chain=False, axes=1, layers=1):
+    c = dict(kind=kind, hq=hq, hkv=hkv, hd=hd, prompts=prompts, starts=starts, batch=batch, ctx_lo=ctx_lo, ctx_hi=ctx_hi, empty=empty,
+             window=window, sinks=sinks, draft=draft, chain=chain, axes=axes, layers=layers)
+    if name:
+        c["name"] = name
+    return c
+
+
+def listed():
+    return [
+        # a decode batch that verifies drafted trees: 64 requests, up to 16 tokens each (latency counts)
+        _case("plan", "plan_trees_64", hq=1, hkv=1, hd=64, batch=64, ctx_lo=512, ctx_hi=4096, draft=16),
+        # many requests at once, runs of tokens of uneven lengths, some of them none
+        _case("plan", "plan_runs_1000", hq=1, hkv=1, hd=64, batch=1000, ctx_lo=0, ctx_hi=2000, draft=63, chain=True, empty=37),
+        # the drafted tokens of one step
+        _case("store", "store_64x8", batch=64, ctx_lo=512, ctx_hi=4096, draft=8),
+        # prompts of text and images, positions on three axes, two of them behind cached prefixes that end inside a block
+        _case("store", "store_axes_ragged", prompts="4391,1518,6730,3805", starts="0,1037,0,250", axes=3),
+        # one user's chat turn: a row that sees 1024 tokens and four sinks (latency and the number of launches count)
+        _case("decode", "decode_1", batch=1, ctx_lo=6000, ctx_hi=6000, window=1024, sinks=4),
+        # the benchmark's batch, behind longer conversations than its window
+        _case("decode", "decode_64", batch=64, ctx_lo=512, ctx_hi=16383, window=4096, sinks=16),
+        # the 70B-shaped configuration's heads: chunks of prompts behind cached ones, of uneven lengths
+        _case("prefill", "prefill_ragged_70b", hq=64, prompts="700,33,1391", starts="1024,4000,0", window=512, sinks=4),
+        # the long-context configuration's whole prompt
+        _case("prefill", "prefill_16384", prompts="16384", window=4096, sinks=16),
+        # one user's chat turn: eight drafted tokens
+        _case("tree", "tree_1x8", batch=1, ctx_lo=900, ctx_hi=900, draft=8),
+        # a batch of wide trees
+        _case("tree", "tree_32x32", batch=32, ctx_lo=512, ctx_hi=4096, draft=32),
+        # one request's accepted path in every layer of a stack
+        _case("compact", "compact_1", batch=1, ctx_lo=900, ctx_hi=900, draft=8, layers=32),
+        # a batch's, through heads of 64 too short to fill a line
+        _case("compact", "compact_64", hkv=4, hd=64, batch=64, ctx_lo=16, ctx_hi=600, draft=32, layers=16),
+    ]
+
+
+def _log_uniform(rng, lo, hi):
+    return int(round(lo * (hi / lo) ** rng.random()))
+
+
+def draw(rng):
+    kind = rng.choice(("plan", "plan", "store", "store", "decode", "decode", "prefill", "prefill", "tree", "tree", "tree", "compact"))
+    hq, hkv, hd = rng.choice(((32, 8, 128), (64, 8, 128), (8, 2, 128), (32, 4, 64), (9, 3, 128), (16, 16, 64), (16, 1, 128)))
+    heads = dict(hq=hq, hkv=hkv, hd=hd)
+    join = lambda v: ",".join(str(x) for x in v)
+    chain = rng.random() < 0.3
+    if kind == "plan":
+        batch = _log_uniform(rng, 1, 1000)
+        hi = _log_uniform(rng, 16, 8000)
+        # (a plan does not depend on the heads)
+        return _case(kind, hq=1, hkv=1, hd=64, batch=batch, ctx_lo=rng.randint(0, hi), ctx_hi=hi, draft=_log_uniform(rng, 1, 63), chain=chain,
+                     empty=rng.randint(0, batch // 4))
+    if kind in ("tree", "compact"):
+        batch = _log_uniform(rng, 1, 64)
+        hi = _log_uniform(rng, 16, 4096 if kind == "tree" else 600)
+        draft = _log_uniform(rng, 1 if kind == "tree" else 2, min(63, 1024 // batch))
+        return _case(kind, batch=batch, ctx_lo=rng.randint(0, hi), ctx_hi=hi, draft=draft, chain=chain,
+                     empty=rng.randint(0, batch // 4), layers=_log_uniform(rng, 1, 16) if kind == "compact" else 1, **heads)
+    if kind == "decode":
+        batch = _log_uniform(rng, 1, 256)
+        window = _log_uniform(rng, 16, max(64, min(4096, 250000 // batch)))
+        hi = _log_uniform(rng, 16, min(16383, max(64, 1000000 // batch)))
+        return _case(kind, batch=batch, ctx_lo=rng.randint(0, hi), ctx_hi=hi, empty=rng.randint(0, batch // 4), window=window,
+                     sinks=rng.choice((0, 1, 4, 16, 33, 128)), **heads)
+    if kind == "store" and rng.random() < 0.5:
+        batch = _log_uniform(rng, 1, 64)
+        hi = _log_uniform(rng, 16, 2000)
+        return _case(kind, batch=batch, ctx_lo=rng.randint(0, hi), ctx_hi=hi, draft=_log_uniform(rng, 1, 63), chain=chain, axes=rng.choice((1, 3)), **heads)
+    n = rng.randint(1, 5)
+    total = _log_uniform(rng, 1, 5000 if kind == "prefill" else 16000)
+    weights = [0.2 + rng.random() for _ in range(n)]
+    lens = [max(1, int(total * w / sum(weights))) for w in weights]
+    starts = [0 if rng.random() < 0.5 else _log_uniform(rng, 1, 6000 if kind == "prefill" else 2000) for _ in lens]
+    if kind == "prefill":
+        return _case(kind, prompts=join(lens), starts=join(starts), window=_log_uniform(rng, 16, 4096), sinks=rng.choice((0, 1, 4, 16, 33, 128)), **heads)
+    return _case(kind, prompts=join(lens), starts=join(starts), axes=rng.choice((1, 3)), **heads)
+
+
+def _ints(text):
+    return [int(v) for v in text.split(",")] if text else []
+
+
+def _lengths(case):
+    """(cached tokens, new tokens) of each request; of a row without a request (-1, 0)."""
+    if case["batch"]:
+        n = case["batch"] - case["empty"]
+        ctx = [int(round(c)) for c in np.linspace(case["ctx_lo"], case["ctx_hi"], n)]
+        # one request in three drafts fewer tokens, one in nine none (a batch of one all of them)
+        new = [case["draft"] if i % 3 != 1 else (case["draft"] * 5 + 4) // 9 if i % 9 != 4 else 0 for i in range(n)]
+        return list(zip(ctx, new)) + [(-1, 0)] * case["empty"]
+    lens = _ints(case["prompts"])
+    return list(zip(_ints(case["starts"]) or [0] * len(lens), lens))
+
+
+def _decode_lengths(case):
+    """Of a decode row the cached tokens before the row's own, which is cached too."""
+    return [c for c, _ in _lengths(case)]
+
+
+# ---- the cache, as the plain forms read and write it -------------------------------------------------------------------
+
+def _slot_rows(device):
+    t = torch.arange(16, device=device)
+    return (t & 3) | ((t & 8) >> 1) | ((t & 4) << 1)
+
+
+def _put(kp, vp, k, v, blocks, slots):
+    """Rows k, v [n, kv heads, head_dim] into (blocks[i], slots[i]) of pools K [blocks, heads, hd/32, 4, 16, 8] and V [blocks, heads, hd, 16]."""
+    n, h, hd = k.shape
+    kp[blocks, :, :, :, _slot_rows(k.device)[slots]] = k.view(n, h, hd // 32, 4, 8).to(kp.dtype)
+    vp[blocks, :, :, slots] = v.to(vp.dtype)
+
+
+def _get(kp, vp, blocks, slots):
+    """Keys and values of (blocks[i], slots[i]), float32 [n, kv heads, head_dim]."""
+    k = kp[blocks, :, :, :, _slot_rows(kp.device)[slots]].flatten(2).float()
+    return k, vp[blocks, :, :, slots].float()
+
+
+def _softmax_product(s, v):
+    """Scores s [..., rows, keys] (-inf: masked) and values [..., keys, hd] -> weighted means, zero where nothing is visible."""
+    p = torch.exp(s - s.amax(-1, keepdim=True).clamp(min=torch.finfo(torch.float32).min))
+    return torch.matmul(p, v) / p.sum(-1, keepdim=True).clamp(min=1e-30)
+
+
+# ---- the plain forms -------------------------------------------------------------------------------------------------
+
+def _plan_plain(st):
+    lens, new, held, tables = st["lens"], st["new"], st["held"], st["tables"]
+    B, width, rows = lens.numel(), st["width"], st["rows"]
+    n = torch.where(lens >= 0, new, 0)
+    need = ((lens + n + 15) // 16 - held).clamp(min=0) * (lens >= 0)
+    cu = torch.zeros(B + 1, dtype=torch.int32, device=lens.device)
+    cu[1:] = torch.cumsum(n, 0)
+    first = torch.cumsum(need, 0) - need
+    # block j of request b beyond the held ones is the (first[b] + j - held[b])-th from the top of the free ids
+    col = torch.arange(width, device=lens.device)[None]
+    take = first[:, None] + col - held[:, None]
+    fresh = (col >= held[:, None]) & (col < (held + need)[:, None])
+    at = (st["n_free"] - 1 - take).clamp(min=0, max=st["free"].numel() - 1)
+    tables.copy_(torch.where(fresh, st["free"][at], tables))
+    row = torch.arange(rows, device=lens.device)
+    req = torch.searchsorted(cu.long(), row, right=True) - 1
+    i = row - cu[req]
+    token = lens[req] + i
+    st["slots"].copy_(tables[req, token // 16] * 16 + token % 16)
+    out = {"tables": tables, "held": (held + need).int(), "n_free": (st["n_free"] - need.sum()).int(), "cu": cu, "slots": st["slots"]}
+    if st["parents"] is None:
+        st["positions"].copy_(token)
+    else:
+        par = st["parents"]
+        depth = torch.zeros(par.shape, dtype=torch.int64, device=par.device)
+        mask = torch.zeros(par.shape, dtype=torch.int64, device=par.device)
+        for j in range(par.shape[1]):
+            p = par[:, j:j + 1].long()
+            depth[:, j:j + 1] = torch.where(p >= 0, depth.gather(1, p.clamp(min=0)) + 1, 0)
+            mask[:, j:j + 1] = torch.where(p >= 0, mask.gather(1, p.clamp(min=0)), 0) | (1 << j if j < 63 else -(1 << 63))
+        st["positions"].copy_(lens[req] + depth[req, i])
+        st["masks"].copy_(mask[req, i])
+        out["masks"] = st["masks"]
+    out["positions"] = st["positions"]
+    return out
+
+
+def _store_plain(st):
+    hq, h, hd = st["hq"], st["hkv"], st["hd"]
+    x = st["qkv"].float().view(-1, hq + 2 * h, hd)
+    pair = torch.arange(hd // 2, device=x.device)
+    axis = torch.tensor(st["pair_axis"], device=x.device)
+    angle = st["positions"][axis].t().double() * ROPE_BASE ** (-2.0 * pair.double() / hd)
+    cos, sin = torch.cos(angle).float()[:, None], torch.sin(angle).float()[:, None]
+    a, b = x[:, :hq + h, :hd // 2], x[:, :hq + h, hd // 2:]
+    turned = torch.cat((a * cos - b * sin, b * cos + a * sin), -1)
+    _put(st["kp"][0], st["vp"][0], turned[:, hq:], x[:, hq + h:], st["slots"].long() // 16, st["slots"].long() % 16)
+    st["q_out"].copy_(turned[:, :hq].flatten(1))
+    return {"q": st["q_out"], "k": st["kp"][0], "v": st["vp"][0]}
+
+
+def _decode_plain(st):
+    B, hq, h, hd, window, sinks = st["B"], st["hq"], st["hkv"], st["hd"], st["window"], st["sinks"]
+    ctx = st["ctx"].long()[:, None]
+    recent = ctx - torch.arange(min(window, st["max_ctx"]), device=ctx.device)
+    early = torch.arange(min(sinks, st["max_ctx"]), device=ctx.device).expand(B, -1)
+    at = torch.cat((early, recent), 1)
+    seen = torch.cat(((early <= ctx), (recent >= min(sinks, st["max_ctx"]))), 1)  # a sink inside the window counts once
+    at = torch.where(seen, at, 0)
+    blocks = st["tables"].long().gather(1, at // 16)
+    k, v = _get(st["kp"][0], st["vp"][0], torch.where(seen, blocks, 0).flatten(), (at % 16).flatten())
+    k, v = (x.view(B, -1, h, hd).transpose(1, 2) for x in (k, v))
+    s = torch.matmul(st["q"].float().view(B, h, hq // h, hd), k.transpose(2, 3).contiguous()) / math.sqrt(hd)
+    s = s.masked_fill(~seen[:, None, None], -math.inf)
+    return _softmax_product(s, v.masked_fill(~seen[:, None, :, None], 0.0).contiguous()).reshape(B, hq * hd).bfloat16()
+
+
+def _prefill_plain(st):
+    hq, h, hd, window, sinks = st["hq"], st["hkv"], st["hd"], st["window"], st["sinks"]
+    q = st["q"].float().view(-1, h, hq // h, hd)
+    out = torch.empty_like(st["q"]).view(-1, h, hq // h, hd)
+    for r, (start, rows) in enumerate(st["lengths"]):
+        tok = torch.arange(start + rows, device=q.device)
+        for first in range(0, rows, 1024):
+            n = min(1024, rows - first)
+            pos = start + first + torch.arange(n, device=q.device)
+            lo = max(min(sinks, start + first), start + first - window + 1)
+            key = torch.cat((tok[:min(sinks, lo)], tok[lo:start + first + n]))
+            k, v = _get(st["kp"][0], st["vp"][0], st["tables"][r].long()[key // 16], key % 16)
+            seen = (key <= pos[:, None]) & ((key > pos[:, None] - window) | (key < sinks))
+            some = slice(st["cu_host"][r] + first, st["cu_host"][r] + first + n)
+            s = torch.matmul(q[some].permute(1, 2, 0, 3).reshape(h, -1, hd), k.permute(1, 2, 0).contiguous()) / math.sqrt(hd)
+            s = s.view(h, hq // h, n, -1).masked_fill(~seen, -math.inf)
+            o = _softmax_product(s.view(h, -1, key.numel()), v.transpose(0, 1).contiguous())
+            out[some] = o.view(h, hq // h, n, hd).permute(2, 0, 1, 3).bfloat16()
+    return out.view(-1, hq * hd)
+
+
+def _bits(masks, n):
+    """[rows] ancestor masks -> [rows, n] truth values."""
+    return (masks[:, None] >> torch.arange(n, device=masks.device)) & 1 == 1
+
+
+def _tree_plain(st):
+    hq, h, hd = st["hq"], st["hkv"], st["hd"]
+    q = st["q"].float().view(-1, h, hq // h, hd)
+    out = torch.empty_like(st["q"]).view(-1, h, hq // h, hd)
+    for r, (ctx, n) in enumerate(st["lengths"]):
+        if n <= 0:
+            continue
+        tok = torch.arange(ctx + n, device=q.device)
+        k, v = _get(st["kp"][0], st["vp"][0], st["tables"][r].long()[tok // 16], tok % 16)
+        some = slice(st["cu_host"][r], st["cu_host"][r] + n)
+        seen = torch.cat((torch.ones(n, ctx, dtype=torch.bool, device=q.device), _bits(st["masks"][some], n)), 1)
+        s = torch.matmul(q[some].permute(1, 2, 0, 3).reshape(h, -1, hd), k.permute(1, 2, 0).contiguous()) / math.sqrt(hd)
+        s = s.view(h, hq // h, n, -1).masked_fill(~seen, -math.inf)
+        o = _softmax_product(s.view(h, -1, ctx + n), v.transpose(0, 1).contiguous())
+        out[some] = o.view(h, hq // h, n, hd).permute(2, 0, 1, 3).bfloat16()
+    return out.view(-1, hq * hd)
+
+
+def _compact_plain(st):
+    n = st["keep_lens"].long()[:, None]
+    i = torch.arange(st["keep"].shape[1], device=n.device).expand(n.numel(), -1)
+    some = i < n
+    ctx = st["ctx"].long()[:, None].expand_as(i)[some]
+    src, dst = ctx + st["keep"].long()[some], ctx + i[some]
+    table = st["tables"].long().repeat_interleave(some.sum(1), 0, output_size=st["kept"])
+    pick = lambda t: table.gather(1, (t // 16)[:, None])[:, 0]
+    rows = _slot_rows(n.device)
+    for kp, vp in zip(st["kp"], st["vp"]):
+        k, v = kp[pick(src), :, :, :, rows[src % 16]], vp[pick(src), :, :, src % 16]
+        kp[pick(dst), :, :, :, rows[dst % 16]] = k
+        vp[pick(dst), :, :, dst % 16] = v
+    return {"k": st["kp"], "v": st["vp"]}
+
+
+# ---- what a program holds, and its calls ---------------------------------------------------------------------------------
+
+def _tree(host, n, chain):
+    """Parents of n drafted tokens in the order of a walk that follows each path to its end, so that a path's later tokens stand together."""
+    parents = []
+    for i in range(n):
+        if chain or i == 0:
+            parents.append(i - 1)
+        else:
+            # mostly the token before; else one further up, or another first token
+            parents.append(i - 1 if host.random() < 0.6 else int(host.integers(-1, i)))
+    return parents
+
+
+def prepare(case, seed):
+    hq, h, hd, kind = case["hq"], case["hkv"], case["hd"], case["kind"]
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    host = np.random.Generator(np.random.Philox(key=[seed, 0]))
+    lengths = _lengths(case)
+    if kind == "decode":
+        lengths = [(c, 1 if c >= 0 else 0) for c in _decode_lengths(case)]
+    if case["batch"]:
+        lengths = [lengths[i] for i in host.permutation(len(lengths))]
+    B = len(lengths)
+    total = [max(c, 0) + n for c, n in lengths]
+    width = max(max(-(-t // 16) for t in total), 1)
+    n_blocks = sum(-(-t // 16) for t in total) + 16
+    perm, at = host.permutation(n_blocks).astype(np.int32), 0
+    # of a plan the blocks of the cached tokens are held and the rest is free; else all are held
+    held = [-(-max(c, 0) // 16) if kind == "plan" else -(-t // 16) for (c, _), t in zip(lengths, total)]
+    tables = np.full((B, width), -1, np.int32)
+    for r, n in enumerate(held):
+        tables[r, :n] = perm[at:at + n]
+        at += n
+    cu = [0]
+    for _, n in lengths:
+        cu.append(cu[-1] + n)
+    dev = lambda x, t=torch.int32: torch.tensor(x, dtype=t).cuda()
+    st = dict(kind=kind, hq=hq, hkv=h, hd=hd, B=B, lengths=lengths, starts=[max(c, 0) for c, _ in lengths], cu_host=cu, rows=cu[-1], width=width,
+              max_ctx=max(total), window=case["window"], sinks=case["sinks"], draft=max(case["draft"], 1),
+              tables=torch.from_numpy(tables).cuda(), ctx=dev([c for c, _ in lengths]), cu=dev(cu))
+
+    if kind in ("plan", "tree"):
+        most = max([n for _, n in lengths] + [1])
+        parents = np.full((B, most), -1, np.int32)
+        for r, (_, n) in enumerate(lengths):
+            parents[r, :n] = _tree(host, n, case["chain"])
+        if kind == "tree":
+            masks = []
+            for r, (_, n) in enumerate(lengths):
+                own_path = []
+                for i in range(n):
+                    p = int(parents[r, i])
+                    own_path.append((own_path[p] if p >= 0 else 0) | 1 << i)
+                masks += own_path
+            st["masks"] = dev(masks, torch.int64)  # at most 63 tokens of a request
+    if kind == "plan":
+        st.update(lens=st["ctx"], new=dev([n for _, n in lengths]), held=dev(held), free=torch.from_numpy(perm[at:].copy()).cuda(), n_free=dev([n_blocks - at]),
+                  parents=None if case["chain"] else torch.from_numpy(parents).cuda(), held_out=dev(held), n_free_out=dev([0]), cu_out=dev([0] * (B + 1)))
+        for name, t in (("slots", torch.int32), ("positions", torch.int32), ("masks", torch.int64)):
+            st[name] = torch.zeros(st["rows"], dtype=t, device="cuda")
+        if own:
+            _enter(case, st, n_blocks)
+        return st
+
+    # keys have a few channels much larger than the rest, as keys do
+    loud = torch.exp(0.7 * torch.randn(h, hd, generator=gen, device="cuda"))
+    normal = lambda *shape: torch.randn(*shape, generator=gen, device="cuda")
+    L = case["layers"]
+    st["kp"] = torch.empty(L, n_blocks, h, hd // 32, 4, 16, 8, dtype=torch.bfloat16, device="cuda")
+    st["vp"] = torch.empty(L, n_blocks, h, hd, 16, dtype=torch.bfloat16, device="cuda")
+    for layer in range(L):
+        for first in range(0, n_blocks, 4096):
+            n = min(4096, n_blocks - first)
+            st["kp"][layer, first:first + n] = normal(n, h, hd // 32, 4, 16, 8) * loud.view(h, hd // 32, 4, 1, 8)
+            st["vp"][layer, first:first + n] = normal(n, h, hd, 16)
+
+    if kind == "store":
+        req = np.repeat(np.arange(B), [n for _, n in lengths])
+        token = np.concatenate([max(c, 0) + np.arange(n) for c, n in lengths])
+        st["slots"] = torch.from_numpy((tables[req, token // 16] * 16 + token % 16).astype(np.int32)).cuda()
+        positions = [token]
+        if case["axes"] == 3:
+            # images of 24 x 24 patches between runs of text: the patches share a time, rows and columns count from it
+            inside = token % 600 < 576
+            base = token - token % 600
+            positions = [np.where(inside, base, token), np.where(inside, base + token % 600 // 24, token), np.where(inside, base + token % 24, token)]
+        st["positions"] = torch.from_numpy(np.stack(positions).astype(np.int32)).cuda()
+        # a quarter of the pairs turns with the time, three eighths with the row, the rest with the column
+        st["pair_axis"] = [0] * (hd // 2) if case["axes"] == 1 else [0] * (hd // 8) + [1] * (3 * hd // 16) + [2] * (hd // 2 - hd // 8 - 3 * hd // 16)
+        qkv = normal(st["rows"], (hq + 2 * h) * hd)
+        qkv[:, hq * hd:(hq + h) * hd] *= loud.flatten()
+        st["qkv"] = qkv.bfloat16()
+        st["q_out"] = torch.empty(st["rows"], hq * hd, dtype=torch.bfloat16, device="cuda")
+    elif kind == "compact":
+        # the first tokens of the draft as they stand, then the later ones of another path, which move
+        keep = np.zeros((B, st["draft"]), np.int32)
+        keep_lens = [0] * B
+        for r, (_, n) in enumerate(lengths):
+            kept, stay = n // 2, n // 4
+            keep[r, :kept] = list(range(stay)) + list(range(n - (kept - stay), n))
+            keep_lens[r] = kept
+        st.update(keep=torch.from_numpy(keep).cuda(), keep_lens=dev(keep_lens), kept=sum(keep_lens))
+    else:
+        rows = B if kind == "decode" else st["rows"]
+        st["q"] = (normal(rows, h, hq // h, hd) / loud[:, None]).bfloat16().view(rows, hq * hd)
+        st["out"] = torch.empty_like(st["q"])
+    if own:
+        _enter(case, st, n_blocks)
+    return st
+
+
+class _Program:
+    """What a serving program makes when it starts: one context, and the pools of its layers' caches.  Every call goes to the streams of
+    that context, one behind another."""
+
+    def __init__(self, case, st, n_blocks):
+        import paper_2601_11822_amd as rs
+        self.case = case
+        L = case["layers"]
+        self.free = [L * i for i in range(4)]  # first layers
+        h, hd = case["hkv"], case["hd"]
+        self.kp = torch.empty(4 * L, n_blocks, h, hd // 32, 4, 16, 8, dtype=torch.bfloat16, device="cuda")
+        self.vp = torch.empty(4 * L, n_blocks, h, hd, 16, dtype=torch.bfloat16, device="cuda")
+        self.c = rs.Context(d_model=case["hq"] * case["hd"], n_q_heads=case["hq"], n_kv_heads=case["hkv"], head_dim=case["hd"],
+                            ffn_dim=case["hq"] * case["hd"], n_layers=4 * L, rms_eps=1e-5, rope_base=ROPE_BASE, max_pos=st["max_ctx"],
+                            n_blocks=n_blocks, k_pool=self.kp, v_pool=self.vp,
+                            max_prefill_tokens=0 if case["batch"] else st["rows"], max_decode_batch=case["batch"], max_context=st["max_ctx"])
+
+    def __del__(self):
+        if hasattr(self, "c"):
+            self.c.destroy()
+
+
+class _Layers:
+    """Layers of a program's cache, until nobody holds them any more."""
+
+    def __init__(self, program):
+        self.program, self.at = program, program.free.pop()
+
+    def __del__(self):
+        self.program.free.append(self.at)
+
+
+def _enter(case, st, n_blocks):
+    """Puts the cache that `st` begins with into layers of the program for the case's sizes (the one that runs, if it is for them and has
+    layers free).  Nothing that a call computes is done here; the copied bytes are those that the plain form reads."""
+    sizes = {k: v for k, v in case.items() if k != "name"}
+    program = getattr(_enter, "program", None)
+    if program is None or program.case != sizes or not program.free:
+        program = _enter.program = _Program(sizes, st, n_blocks)
+    torch.cuda.synchronize()  # layers given back may still be read
+    layers = _Layers(program)
+    st["held_by"], st["c"], st["layer"] = layers, program.c, layers.at
+    if "kp" in st:
+        for name, pool in (("kp", program.kp), ("vp", program.vp)):
+            mine = pool[layers.at:layers.at + case["layers"]]
+            mine.copy_(st[name])
+            st[name] = mine
+
+
+def _plan_own(st):
+    c, trees = st["c"], st["parents"] is not None
+    c.kv_plan(1, st["lens"], st["new"], st["held"], st["tables"], st["width"], st["B"], st["free"], st["n_free"], st["rows"], st["cu_out"],
+              st["positions"], st["slots"], st["held_out"], st["n_free_out"], parents=st["parents"], parent_stride=st["parents"].shape[1] if trees else 0,
+              masks=st["masks"] if trees else None)
+    out = {"tables": st["tables"], "held": st["held_out"], "n_free": st["n_free_out"], "cu": st["cu_out"], "slots": st["slots"], "positions": st["positions"]}
+    if trees:
+        out["masks"] = st["masks"]
+    return out
+
+
+def _store_own(st):
+    row = (st["hq"] + 2 * st["hkv"]) * st["hd"]
+    st["c"].kv_store(1, st["layer"], st["qkv"], row, st["q_out"], st["hq"] * st["hd"], st["positions"], st["slots"], st["rows"],
+                     n_axes=st["positions"].shape[0], pair_axis=st["pair_axis"])
+    return {"q": st["q_out"], "k": st["kp"][0], "v": st["vp"][0]}
+
+
+def _decode_own(st):
+    row = st["hq"] * st["hd"]
+    st["c"].window_decode_attention(st["layer"], st["q"], row, st["out"], row, st["ctx"], st["tables"], st["width"], st["B"], st["max_ctx"],
+                                    st["window"], st["sinks"])
+    return st["out"]
+
+
+def _prefill_own(st):
+    row = st["hq"] * st["hd"]
+    st["c"].window_prefill_attention(st["layer"], st["q"], row, st["out"], row, st["cu_host"], st["starts"], st["tables"], st["width"],
+                                     st["window"], st["sinks"])
+    return st["out"]
+
+
+def _tree_own(st):
+    row = st["hq"] * st["hd"]
+    st["c"].tree_attention(st["layer"], st["q"], row, st["out"], row, st["ctx"], st["cu"], st["masks"], st["tables"], st["width"], st["B"], st["rows"],
+                           st["draft"], st["max_ctx"])
+    return st["out"]
+
+
+def _compact_own(st):
+    st["c"].kv_compact(1, st["layer"], st["kp"].shape[0], st["ctx"], st["keep"], st["keep"].shape[1], st["keep_lens"], st["tables"], st["width"], st["B"])
+    return {"k": st["kp"], "v": st["vp"]}
+
+
+def run(state):
+    forms = {"plan": (_plan_plain, _plan_own), "store": (_store_plain, _store_own), "decode": (_decode_plain, _decode_own),
+             "prefill": (_prefill_plain, _prefill_own), "tree": (_tree_plain, _tree_own), "compact": (_compact_plain, _compact_own)}
+    return forms[state["kind"]][1 if own else 0](state)
+
+
+def _seen(first, rows, window, sinks):
+    """Pairs of (row, visible token) and tokens that any row sees, rows at positions first .."""
+    pos = np.arange(first, first + rows, dtype=np.int64)
+    lo = np.maximum(pos + 1 - window, 0)
+    pairs = int((pos + 1 - lo + np.minimum(lo, sinks)).sum())
+    oldest = max(first + 1 - window, 0)
+    return pairs, first + rows - oldest + min(oldest, sinks)
+
+
+def work(case):
+    """Tokens of the cache that a pass uses read or written once, bf16 rows and integers read or written once."""
+    hq, h, hd, kind = case["hq"], case["hkv"], case["hd"], case["kind"]
+    token = 4 * h * hd  # bytes of a token's keys and values
+    lengths = _lengths(case)
+    if kind == "plan":
+        rows = sum(n for _, n in lengths)
+        taken = sum(max(0, -(-(c + n) // 16) - -(-c // 16)) for c, n in lengths if c >= 0)
+        per_row = 8 if case["chain"] else 4 + 8 + 8
+        return {"bytes": float(16 * len(lengths) + 8 * taken + per_row * rows + 4 * (len(lengths) + 3)), "flops": 0.0}
+    if kind == "store":
+        rows = sum(n for _, n in lengths)
+        return {"bytes": float(rows * (4 * hq * hd + 2 * token + 4 + 4 * case["axes"])), "flops": float(rows * (hq + h) * hd * 3)}
+    if kind == "compact":
+        moved = sum(n // 2 - n // 4 for _, n in lengths)
+        return {"bytes": float(max(moved, 1) * case["layers"] * 2 * token), "flops": 0.0}
+    if kind == "tree":
+        rows = sum(n for _, n in lengths)
+        held = sum(c + n for c, n in lengths if n > 0)
+        pairs = sum(n * c + n * (n + 1) / 2 for c, n in lengths if n > 0)
+        return {"bytes": float(held * token + rows * (4 * hq * hd + 8)), "flops": float(4 * hq * hd * pairs)}
+    if kind == "decode":
+        lengths = [(c, 1) for c in _decode_lengths(case) if c >= 0]
+    seen = [_seen(c, n, case["window"], case["sinks"]) for c, n in lengths]
+    rows = case["batch"] or sum(n for _, n in lengths)
+    return {"bytes": float(sum(t for _, t in seen) * token + 4 * rows * hq * hd), "flops": float(4 * hq * hd * sum(p for p, _ in seen))}
+
+
+# ---- the definition in 64 bits --------------------------------------------------------------------------------------------
+
+def _at(kp, vp, table, tokens):
+    """Keys and values [tokens, kv heads, head_dim] in float64: dim d of token t, element by element of the pools' layout."""
+    h, g = kp.shape[1], kp.shape[2]
+    d = torch.arange(32 * g, device=kp.device)
+    block, t = table.long()[tokens // 16], tokens % 16
+    row = 4 * (2 * (t // 4 % 2) + t // 8) + t % 4
+    kk = kp.reshape(kp.shape[0], h, -1)[block]
+    where = ((d // 32 * 4 + d % 32 // 8) * 16 + row[:, None]) * 8 + d % 8
+    k = kk.gather(2, where[:, None].expand(-1, h, -1))
+    v = vp.reshape(vp.shape[0], h, -1)[block].gather(2, (16 * d + t[:, None])[:, None].expand(-1, h, -1))
+    return k.double(), v.double()
+
+
+def exact(case, seed):
+    st = prepare(case, seed)
+    hq, h, hd, kind = st["hq"], st["hkv"], st["hd"], st["kind"]
+    if kind == "plan":
+        return None  # whole numbers
+    if kind == "compact":
+        kp, vp = st["kp"].double(), st["vp"].double()
+        tables, keep, keep_lens = st["tables"].tolist(), st["keep"].tolist(), st["keep_lens"].tolist()
+        place = lambda r, t: (tables[r][t // 16], t % 16, 4 * (2 * (t // 4 % 2) + t // 8 % 2) + t % 4)
+        for r, (ctx, _) in enumerate(st["lengths"]):
+            for i in range(keep_lens[r]):  # in order: a token moves to places that are free by then
+                (b0, t0, row0), (b1, t1, row1) = place(r, ctx + keep[r][i]), place(r, ctx + i)
+                kp[:, b1, :, :, :, row1], vp[:, b1, :, :, t1] = kp[:, b0, :, :, :, row0], vp[:, b0, :, :, t0]
+        return {"k": kp, "v": vp}
+    if kind == "store":
+        x = st["qkv"].double().view(-1, hq + 2 * h, 2, hd // 2)
+        i = torch.arange(hd // 2, device=x.device)
+        position = torch.stack([st["positions"][a] for a in st["pair_axis"]], 1).double()
+        turn = torch.polar(torch.ones_like(position), position * torch.exp(-2.0 * i.double() / hd * math.log(ROPE_BASE)))[:, None]
+        z = torch.complex(x[:, :hq + h, 0].contiguous(), x[:, :hq + h, 1].contiguous()) * turn
+        z = torch.cat((z.real, z.imag), -1)
+        kp, vp = st["kp"][0].double(), st["vp"][0].double()
+        block, t = st["slots"].long() // 16, st["slots"].long() % 16
+        row = 4 * (2 * (t // 4 % 2) + t // 8) + t % 4
+        for d in range(hd):
+            kp[block, :, d // 32, d % 32 // 8, row, d % 8] = z[:, hq:, d]
+            vp[block, :, d, t] = x[:, hq + h:].flatten(2)[:, :, d]
+        return {"q": z[:, :hq].flatten(1), "k": kp, "v": vp}
+    q = st["q"].double().view(-1, h, hq // h, hd)
+    out = torch.zeros_like(q)
+    for r, (ctx, n) in enumerate(st["lengths"]):
+        first = max(ctx, 0)
+        at = r if kind == "decode" else st["cu_host"][r]
+        for i0 in range(0, n, 512):
+            rows = torch.arange(i0, min(n, i0 + 512), device=q.device)
+            pos = first + rows
+            if kind == "tree":
+                key = torch.arange(first + n, device=q.device)
+                paths = st["masks"][at + rows]
+                ancestors = [paths // 2 ** j % 2 == 1 for j in range(n)]
+                seen = torch.cat((torch.ones(rows.numel(), first, device=q.device) > 0, torch.stack(ancestors, 1)), 1)
+            else:
+                oldest = max(first + i0 + 1 - st["window"], 0)
+                key = torch.arange(first + i0 + rows.numel(), device=q.device)
+                key = key[(key >= oldest) | (key < st["sinks"])]
+                back = pos[:, None] - key
+                seen = (back >= 0) & ((back < st["window"]) | (key < st["sinks"]))
+            k, v = _at(st["kp"][0], st["vp"][0], st["tables"][r], key)
+            for head in range(h):
+                s = torch.einsum("rgd,td->grt", q[at + rows, head], k[:, head]) / math.sqrt(hd)
+                out[at + rows, head] = torch.einsum("grt,td->rgd", torch.softmax(torch.where(seen, s, -math.inf), -1), v[:, head])
+    return out.view(-1, hq * hd)
