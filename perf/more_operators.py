@@ -444,7 +444,7 @@ def _enter(case, st, n_blocks):
 
 def _plan_own(st):
     c, trees = st["c"], st["parents"] is not None
-    c.kv_plan(1, st["lens"], st["new"], st["held"], st["tables"], st["width"], st["B"], st["free"], st["n_free"], st["rows"], st["cu_out"],
+    c.kv_plan(1, st["lens"], st["new"], st["held"], st["tables"], st["width"], st["B"], st["free"], st["free"].numel(), st["n_free"], st["rows"], st["cu_out"],
               st["positions"], st["slots"], st["held_out"], st["n_free_out"], parents=st["parents"], parent_stride=st["parents"].shape[1] if trees else 0,
               masks=st["masks"] if trees else None)
     out = {"tables": st["tables"], "held": st["held_out"], "n_free": st["n_free_out"], "cu": st["cu_out"], "slots": st["slots"], "positions": st["positions"]}
