@@ -267,6 +267,90 @@ int32_t rs_kv4_prefill_attention(rs_ctx *ctx, int32_t layer, const void *q, int6
                                  const int32_t *cu_seqlens, const int32_t *start_pos, int32_t n_req,
                                  const int32_t *block_tables, int32_t max_blk);
 
+/* ---- windows, drafted trees, and the cache's upkeep on the GPU ----------------------------------------
+ * Calls over the bf16 pools of a context of rs_init (RS_ERR_STATE for a cache held in 4 bits, but for rs_kv_plan, which touches no
+ * cache) for steps that are no whole layer pass: long conversations whose rows see a window and the first few tokens, and
+ * speculative decoding, where a step's lengths are known on the GPU alone.  One step over drafted trees:
+ *   rs_kv_plan -> in every layer, between its projections: rs_kv_store, rs_tree_attention -> (the caller chooses a path)
+ *   -> rs_kv_compact.
+ * Each call enqueues on the named side's current stream and returns; calls on one side are ordered, between the sides the caller
+ * orders them.  Pointers are device memory unless they are said to be host arrays.  Rows are bf16, `stride` elements apart (a
+ * multiple of 8, 16-byte aligned, at least the row's own length).  Nothing is allocated, and every call may be recorded into a
+ * caller's graph from the side's stream (rs_get_stream); attention and plans use the side's workspaces: replay such a graph on
+ * that stream, or in order with it.  Errors found on the GPU are reported by rs_sync and named with each call.  Otherwise RS_ERR_BAD_ARG for a
+ * null or misaligned pointer or a bad size, RS_ERR_BAD_BLOCK for a table too short, RS_ERR_STATE on a host-only context.
+ * rs_init allocates 17 MB a side for attention whose keys several workgroups share (head_dim 128; half of that at 64).
+ *
+ * Attention, softmax(q K^T / sqrt(head_dim)) V of every query head over the keys that a row sees; q is rotated.  Softmax weights go into
+ * the product with V as bf16, sums are float32.  What a key or value holds that a row does not see, NaN included, does not reach the
+ * row.  A block id outside the pool is never dereferenced: its tokens are seen by no row, and rs_sync reports RS_ERR_BAD_BLOCK.  Results
+ * depend on the sizes alone (max_ctx among them), not on the CU split.  out may not overlap q. */
+
+/* Row i of q (DECODE side), the token at position ctx_lens[i] (cached already), sees the latest `window` tokens up to its own, and the first
+ * `sinks` tokens of its request: positions j <= ctx_lens[i] with j > ctx_lens[i] - window or j < sinks.  window >= 1, sinks >= 0; a window
+ * of max_ctx or more is causal attention.  Blocks that no row sees are not looked at, and their entries of block_tables may hold anything.
+ * ctx_lens[i] = -1: a row without a request, its output is zero; so it is for a length outside [-1, max_ctx - 1], reported as
+ * RS_ERR_BAD_BLOCK.  B <= max_decode_batch; max_ctx (host) bounds ctx_lens[i] + 1. */
+int32_t rs_window_decode_attention(rs_ctx *ctx, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                                   const int32_t *ctx_lens, const int32_t *block_tables, int32_t max_blk, int32_t B,
+                                   int32_t max_ctx, int32_t window, int32_t sinks);
+/* The same for several rows a request, on the PREFILL side: rows [cu_seqlens[r], cu_seqlens[r+1]) are positions start_pos[r] .. of
+ * request r (host arrays; start_pos null: all 0; any position may start a run, a run may be empty, n_req is 1 to
+ * RS_MAX_PREFILL_REQS), their tokens cached already.  At most max_prefill_tokens rows. */
+int32_t rs_window_prefill_attention(rs_ctx *ctx, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                                    const int32_t *cu_seqlens, const int32_t *start_pos, int32_t n_req,
+                                    const int32_t *block_tables, int32_t max_blk, int32_t window, int32_t sinks);
+/* Drafted tokens (DECODE side): rows [cu_rows[b], cu_rows[b+1]) of q are the drafted tokens of request b, cached already in the places
+ * ctx_lens[b], ctx_lens[b] + 1, ... behind its ctx_lens[b] tokens.  A row sees those, and of the request's drafted tokens the t-th where
+ * bit t of the row's mask is set (rs_kv_plan makes masks of ancestors; the row's own bit is not implied; bits behind the request's
+ * rows are ignored).  masks null: the tokens up to the row's own, a chain.  A row that sees nothing gets zero.
+ * B <= max_decode_batch; max_rows, max_draft (1 to RS_MAX_DRAFT) and max_ctx (host) bound cu_rows[B], a request's rows, and
+ * ctx_lens[b] plus its rows.  A request whose cu_rows contradict these bounds is skipped (RS_ERR_BAD_ARG), one whose length does gets
+ * zeros (RS_ERR_BAD_BLOCK); so does one with ctx_lens[b] = -1 that has rows.  Rows of out outside [cu_rows[0], cu_rows[B]) are left as
+ * they were. */
+#define RS_MAX_DRAFT 64
+int32_t rs_tree_attention(rs_ctx *ctx, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                          const int32_t *ctx_lens, const int32_t *cu_rows, const uint64_t *masks, const int32_t *block_tables,
+                          int32_t max_blk, int32_t B, int32_t max_rows, int32_t max_draft, int32_t max_ctx);
+
+/* A step's plan.  Request b (of B, 1 to 65535) has lens[b] cached tokens (-1: no request, nothing is done), n_held[b] entries in its row
+ * of block_tables, and gets n_new[b] tokens behind the cached ones.  Where its blocks do not hold them it gets the missing
+ * ones: ids are taken from the top of the stack free_ids (free_ids[*n_free - 1] first; at most free_cap ids), in the order of the requests,
+ * and written behind its table entries.  The ids are the caller's, who took them with rs_kv_alloc.
+ *   cu_rows [B+1]          first row of each request: exclusive sums of n_new
+ *   positions [max_rows]   of the row's token for the rotary embedding: lens[b] + i, of trees lens[b] + the token's depth
+ *   slots [max_rows]       where it goes: 16 * block + place, the place of position lens[b] + i (trees too: tokens in the draft's order)
+ *   n_held_out [B], n_free_out [1]   entries and free ids afterwards; may be n_held and n_free themselves
+ *   parents [B][parent_stride]       trees (null: chains of any length): the request's row that the row's token follows, less than its own
+ *                          index, or -1: it follows the cached tokens.  n_new[b] <= parent_stride <= RS_MAX_DRAFT
+ *   masks [max_rows]       of trees, may be null: bit t is set for the row itself and for each of its ancestors t
+ * Rows from cu_rows[B] on are left as they were.  Where the call cannot be done it changes nothing but cu_rows, which is all zero (so that calls
+ * behind it find no rows): RS_ERR_NO_BLOCKS if too few ids are free, RS_ERR_BAD_BLOCK if a table of max_blk entries is too short
+ * or n_held[b] blocks do not hold lens[b] tokens, RS_ERR_BAD_ARG for a negative count or more than max_rows rows.  A block id
+ * outside the pool gives slots of -1 (RS_ERR_BAD_BLOCK), a parent that does not come before its row counts as -1 (RS_ERR_BAD_ARG). */
+int32_t rs_kv_plan(rs_ctx *ctx, int32_t side, const int32_t *lens, const int32_t *n_new, const int32_t *n_held,
+                   int32_t *block_tables, int32_t max_blk, int32_t B, const int32_t *free_ids, int32_t free_cap,
+                   const int32_t *n_free, const int32_t *parents, int32_t parent_stride, int32_t max_rows, int32_t *cu_rows,
+                   int32_t *positions, int32_t *slots, uint64_t *masks, int32_t *n_held_out, int32_t *n_free_out);
+/* Rotates the queries and keys of rows q | k | v (as the QKV projection leaves them) and writes keys and values to the cache.  Pair i of
+ * a head (dims i and i + head_dim/2) turns by positions[a][row] * rope_base^(-2i/head_dim) with a = pair_axis[i] (host array of
+ * head_dim/2; null with one axis): one axis for text, several (at most RS_MAX_AXES) for images and video, in any arrangement.
+ * positions is [n_axes][max_rows].  q_out: rotated queries, null: not wanted, or the queries in qkv themselves.  slots as rs_kv_plan makes
+ * them, -1: the row is rotated but not stored; no two rows may have the same slot.  n_rows (device, null: max_rows): the rows
+ * there are, those behind are left alone (cu_rows + B of a plan).  A row with a position outside [0, max_pos) on any of the axes
+ * is skipped, one with a slot outside the pool is not stored; both RS_ERR_BAD_BLOCK. */
+#define RS_MAX_AXES 4
+int32_t rs_kv_store(rs_ctx *ctx, int32_t side, int32_t layer, const void *qkv, int64_t row_stride, void *q_out, int64_t q_stride,
+                    const int32_t *positions, int32_t n_axes, const uint8_t *pair_axis, const int32_t *slots,
+                    const int32_t *n_rows, int32_t max_rows);
+/* Behind an accepted path: in each of n_layers layers from `layer` on, the token of request b in place ctx_lens[b] + keep[b][i] moves
+ * to place ctx_lens[b] + i, for i < keep_lens[b].  keep is [B][keep_stride], ascending, less than RS_MAX_DRAFT; keep_stride <=
+ * RS_MAX_DRAFT.  ctx_lens[b] = -1: nothing.  Other tokens keep what they hold, but those between that were moved over.  A request with
+ * indices that do not ascend, or a bad length, is left alone in all layers (RS_ERR_BAD_ARG), and one whose table is too short or
+ * names a block outside the pool (RS_ERR_BAD_BLOCK). */
+int32_t rs_kv_compact(rs_ctx *ctx, int32_t side, int32_t layer, int32_t n_layers, const int32_t *ctx_lens, const int32_t *keep,
+                      int32_t keep_stride, const int32_t *keep_lens, const int32_t *block_tables, int32_t max_blk, int32_t B);
+
 /* The same decode step, replayed from a captured HIP graph (section 4.5.2: decode steps are
  * captured as graphs per batch size; section 4.5.3: the CU mask a graph was captured under stays
  * with it).  The first call with a given (layer, pointers, max_blk, B, max_ctx_bucket, current

@@ -35,6 +35,7 @@ EXPORTS = [
     "rs_set_head", "rs_embed", "rs_lm_head_greedy", "rs_submit_tokens", "rs_step_tokens", "rs_request_output",
     "rs_debug_push_sampled", "rs_request_times", "rs_request_release", "rs_set_step_graphs", "rs_step_graph_stats", "rs_engine_start", "rs_engine_stop", "rs_engine_stats", "rs_release_source_weights", "rs_set_moe_weights", "rs_debug_read_moe_routing",
     "rs_init_kv4", "rs_kv4_write", "rs_kv4_append", "rs_kv4_read", "rs_kv4_decode_attention", "rs_kv4_prefill_attention",
+    "rs_window_decode_attention", "rs_window_prefill_attention", "rs_tree_attention", "rs_kv_plan", "rs_kv_store", "rs_kv_compact",
 ]
 
 
@@ -120,7 +121,7 @@ def load() -> ctypes.CDLL:
         for name in EXPORTS:
             if name != "rs_last_error":
                 getattr(lib, name).restype = ctypes.c_int32
-        for name, kinds in _KV4_ARGS.items():
+        for name, kinds in {**_KV4_ARGS, **_STEP_ARGS}.items():
             getattr(lib, name).argtypes = [_ARG[k] for k in kinds]
         _lib = lib
     return _lib
@@ -136,11 +137,13 @@ def _i32(a) -> np.ndarray:
     return np.ascontiguousarray(a, dtype=np.int32)
 
 
-# argument types of the calls on the 4-bit cache (c: context, i: int32, l: int64, p: pointer); with them ctypes takes plain integers,
+# argument types of the calls on parts of a step (c: context, i: int32, l: int64, p: pointer); with them ctypes takes plain integers,
 # which is half of what a call of one row costs on the host
 _ARG = {"c": ctypes.c_void_p, "i": ctypes.c_int32, "l": ctypes.c_int64, "p": ctypes.c_void_p}
 _KV4_ARGS = {"rs_kv4_write": "ciipplppipi", "rs_kv4_read": "ciipplppipi", "rs_kv4_append": "ciipplppii", "rs_kv4_decode_attention": "ciplplppiii",
              "rs_kv4_prefill_attention": "ciplplppipi"}
+_STEP_ARGS = {"rs_window_decode_attention": "ciplplppiiiii", "rs_window_prefill_attention": "ciplplppipiii", "rs_tree_attention": "ciplplppppiiiii",
+              "rs_kv_plan": "cippppiipippiipppppp", "rs_kv_store": "ciiplplpipppi", "rs_kv_compact": "ciiippippii"}
 
 
 def _runs(cu_seqlens, start_pos):
@@ -208,6 +211,7 @@ class Context:
         self._keep_layers = []
         self.n_layers = n_layers
         self.max_context = max_context
+        self.head_dim = head_dim
         init = self._lib.rs_init_kv4 if kv4 else self._lib.rs_init
         _check(init(ctypes.byref(m), ctypes.byref(p), ctypes.byref(lim), ctypes.byref(pd) if pd is not None else None,
                     ctypes.c_int32(device), ctypes.byref(self._h)))
@@ -336,6 +340,41 @@ class Context:
         cu, n, sp = _runs(cu_seqlens, start_pos)
         _check(self._lib.rs_kv4_prefill_attention(self._h, layer, _addr(q), q_stride, _addr(out), out_stride, _addr(cu), _addr(sp), n,
                                                   _addr(block_tables), max_blk))
+
+    # -- windows, drafted trees, and the cache's upkeep on the GPU
+    def window_decode_attention(self, layer: int, q, q_stride: int, out, out_stride: int, ctx_lens, block_tables, max_blk: int, B: int, max_ctx: int,
+                                window: int, sinks: int):
+        _check(self._lib.rs_window_decode_attention(self._h, layer, _addr(q), q_stride, _addr(out), out_stride, _addr(ctx_lens), _addr(block_tables),
+                                                    max_blk, B, max_ctx, window, sinks))
+
+    def window_prefill_attention(self, layer: int, q, q_stride: int, out, out_stride: int, cu_seqlens: Sequence[int], start_pos, block_tables,
+                                 max_blk: int, window: int, sinks: int):
+        cu, n, sp = _runs(cu_seqlens, start_pos)
+        _check(self._lib.rs_window_prefill_attention(self._h, layer, _addr(q), q_stride, _addr(out), out_stride, _addr(cu), _addr(sp), n,
+                                                     _addr(block_tables), max_blk, window, sinks))
+
+    def tree_attention(self, layer: int, q, q_stride: int, out, out_stride: int, ctx_lens, cu_rows, masks, block_tables, max_blk: int, B: int,
+                       max_rows: int, max_draft: int, max_ctx: int):
+        _check(self._lib.rs_tree_attention(self._h, layer, _addr(q), q_stride, _addr(out), out_stride, _addr(ctx_lens), _addr(cu_rows), _addr(masks),
+                                           _addr(block_tables), max_blk, B, max_rows, max_draft, max_ctx))
+
+    def kv_plan(self, side: int, lens, n_new, n_held, block_tables, max_blk: int, B: int, free_ids, free_cap: int, n_free, max_rows: int, cu_rows,
+                positions, slots, n_held_out, n_free_out, parents=None, parent_stride: int = 0, masks=None):
+        _check(self._lib.rs_kv_plan(self._h, side, _addr(lens), _addr(n_new), _addr(n_held), _addr(block_tables), max_blk, B, _addr(free_ids), free_cap,
+                                    _addr(n_free), _addr(parents), parent_stride, max_rows, _addr(cu_rows), _addr(positions), _addr(slots), _addr(masks),
+                                    _addr(n_held_out), _addr(n_free_out)))
+
+    def kv_store(self, side: int, layer: int, qkv, row_stride: int, q_out, q_stride: int, positions, slots, max_rows: int, n_rows=None, n_axes: int = 1,
+                 pair_axis: Optional[Sequence[int]] = None):
+        if pair_axis is not None and len(pair_axis) != self.head_dim // 2:
+            raise ValueError(f"{len(pair_axis)} axes for {self.head_dim // 2} pairs of dims")
+        axes = bytes(pair_axis) if pair_axis is not None else None
+        _check(self._lib.rs_kv_store(self._h, side, layer, _addr(qkv), row_stride, _addr(q_out), q_stride, _addr(positions), n_axes, axes, _addr(slots),
+                                     _addr(n_rows), max_rows))
+
+    def kv_compact(self, side: int, layer: int, n_layers: int, ctx_lens, keep, keep_stride: int, keep_lens, block_tables, max_blk: int, B: int):
+        _check(self._lib.rs_kv_compact(self._h, side, layer, n_layers, _addr(ctx_lens), _addr(keep), keep_stride, _addr(keep_lens), _addr(block_tables),
+                                       max_blk, B))
 
     # -- CU split / manager
     def set_cu_split(self, prefill_cus: int, decode_cus: int):

@@ -127,6 +127,76 @@ void kv4_kernels_init();
 void launch_kv4_decode(hipStream_t st, const Kv4AttnArgs &a);
 void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &a);
 
+// ---- attention over the bf16 cache with other masks than the causal one (masked_attention.hip) ----
+// Bits of a side's error word, besides 1 (position), 2 (block id), 4 (token) and 8 (context length).
+#define RS_FLAG_NO_BLOCKS 16   // a plan needs more blocks than are free
+#define RS_FLAG_LENGTHS 32     // row counts, lengths or parents that contradict each other
+#define MASKED_COLS 128        // columns, (row, query head of a kv head), of a unit
+#define MASKED_PIECES 256      // most pieces of units whose keys are cut, in a launch
+struct MaskedAttnArgs {
+    const bf16_t *q;          // rows of Hq * hd, q_stride elements apart
+    size_t q_stride;
+    bf16_t *out;              // rows of Hq * hd, out_stride elements apart
+    size_t out_stride;
+    const bf16_t *k_pool, *v_pool;   // this layer
+    const int32_t *tables;
+    int32_t *err_flag;
+    float *part_o, *part_ml;  // pieces of cut units: [MASKED_PIECES][MASKED_COLS][hd], and [..][2] maximum and sum
+    int Hq, Hkv, hd, max_blk, n_blocks;
+    float scale_log2;         // log2(e) / sqrt(hd)
+    int window = 0, sinks = 0;
+    // one row per request (decode): the row's position; trees: cached tokens
+    const int32_t *ctx_lens = nullptr;
+    int B = 0, max_ctx = 0;
+    // trees: rows of request b are [cu_rows[b], cu_rows[b + 1]), bit t of a row's mask lets it see the request's t-th row; no masks: the
+    // rows up to its own
+    const int32_t *cu_rows = nullptr;
+    const uint64_t *masks = nullptr;
+    int max_rows = 0, max_draft = 0;
+    SeqInfo seq{};            // else prompts: request r's rows are its tokens start[r] ..
+    int n_units = 0, units_per_req = 0, cut = 1;   // set by the launcher
+};
+void launch_masked_attention(hipStream_t st, const MaskedAttnArgs &a);
+void masked_attention_init();
+
+// ---- the bf16 cache's upkeep on the GPU (kv_upkeep.hip) ----
+struct KvPlanArgs {
+    const int32_t *lens, *n_new, *held;   // [B] cached tokens (-1: no request), tokens to come, entries of the table
+    int32_t *tables;                      // [B][max_blk]
+    const int32_t *free_ids, *n_free;     // a stack of block ids, the top is [*n_free - 1]
+    const int32_t *parents;               // [B][parent_stride] or nullptr
+    int32_t *cu_rows, *positions, *slots; // [B + 1], [max_rows], [max_rows]
+    uint64_t *masks;                      // [max_rows] or nullptr
+    int32_t *held_out, *n_free_out;       // may be held and n_free
+    int32_t *ticket, *err_flag;           // the ticket is 0 between launches
+    int B, max_blk, n_blocks, free_cap, max_rows, parent_stride;
+};
+void launch_kv_plan(hipStream_t st, const KvPlanArgs &a);
+struct KvStoreArgs {
+    const bf16_t *qkv;        // rows of (Hq + 2 Hkv) * hd, row_stride elements apart
+    size_t row_stride;
+    bf16_t *q_out;            // rows of Hq * hd, q_stride elements apart, or nullptr; may be the queries in qkv themselves
+    size_t q_stride;
+    const int32_t *positions; // [n_axes][max_rows]
+    const int32_t *slots;     // [max_rows] 16 * block + place, -1: not stored
+    const int32_t *n_rows;    // rows there are, or nullptr: max_rows
+    const CosSin *table;      // [max_pos][hd / 2]
+    bf16_t *k_pool, *v_pool;  // this layer
+    int32_t *err_flag;
+    uint64_t axis[2];         // two bits a pair of dims
+    int n_axes, max_rows, Hq, Hkv, hd, n_blocks, max_pos;
+};
+void launch_kv_store(hipStream_t st, const KvStoreArgs &a);
+struct KvCompactArgs {
+    bf16_t *k_pool, *v_pool;  // the first of n_layers
+    int64_t layer_stride;
+    const int32_t *ctx_lens, *keep, *keep_lens;   // [B], [B][keep_stride], [B]
+    const int32_t *tables;
+    int32_t *err_flag;
+    int n_layers, keep_stride, B, Hkv, hd, max_blk, n_blocks;
+};
+void launch_kv_compact(hipStream_t st, const KvCompactArgs &a);
+
 enum GemmEpilogue { EPI_STORE = 0, EPI_RESIDUAL = 1, EPI_SWIGLU = 2 };
 
 // out[M,N] = epi(A[M,K] * W[N,K]^T).  EPI_RESIDUAL adds resid[M,N].  EPI_SWIGLU:

@@ -1,0 +1,497 @@
+// Attention over the bf16 paged cache for rows that do not see all that is before them: windows with sinks (decode rows and prompt
+// rows), and the tokens of a drafted tree.
+//
+//   o(row) = sum_j w_j v_j / sum_j w_j,   w_j = exp(q k_j / sqrt(hd) - max),   over the keys j that the row sees:
+//   window:  j <= p  and  (j > p - window  or  j < sinks),   p the row's position;
+//   tree:    j < ctx, and ctx + t for every bit t of the row's ancestor mask.
+// A row that sees nothing gets zero.  What a key holds that a row does not see, NaN included, does not reach that row.
+//
+// A UNIT is as many rows of one request and one kv head as fill 128 columns, a column being (row, query head of the group): the
+// keys of a block are read once for all of them.  The blocks that any row of a unit sees are counted through (`Span`): those of the
+// sinks, then those of the windows; blocks between are not looked at, nor are their table entries.
+#include <algorithm>
+
+#include "kernels.h"
+
+#define NEG_INF (-__builtin_huge_valf())
+
+namespace {
+
+__device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+
+constexpr int COLS = MASKED_COLS;
+
+// What a unit's rows see.
+struct Span {
+    int row0 = 0, rows = 0;      // rows of q and out
+    int req = 0;                 // row of the block tables
+    int first = 0;               // window: position of the unit's first row; tree: cached tokens
+    int i0 = 0, n = 0;           // tree: the unit's first row among the request's n
+    int sink_blocks = 0, skip = 0, blocks = 0;   // counted block j is table entry j, from sink_blocks on j + skip
+    bool dead = false;           // rows without a request, or with a length out of range: zero
+};
+
+template <bool TREE>
+__device__ __forceinline__ Span unit_span(const MaskedAttnArgs &a, int u) {
+    Span s;
+    const int G = a.Hq / a.Hkv, per = COLS / G;
+    int end;   // keys before this position
+    if (TREE) {
+        s.req = u / a.units_per_req;
+        s.i0 = u % a.units_per_req * per;
+        const int r0 = a.cu_rows[s.req], r1 = a.cu_rows[s.req + 1];
+        if (r0 < 0 || r1 < r0 || r1 > a.max_rows || r1 - r0 > a.max_draft) {   // not a row is touched
+            if (threadIdx.x == 0) atomicOr(a.err_flag, RS_FLAG_LENGTHS);
+            return s;
+        }
+        s.n = r1 - r0;
+        s.rows = min(per, s.n - s.i0);
+        if (s.rows <= 0) return s;
+        s.row0 = r0 + s.i0;
+        s.first = a.ctx_lens[s.req];
+        if (s.first < 0 || s.first > a.max_ctx - s.n) {
+            if (threadIdx.x == 0) atomicOr(a.err_flag, 8);
+            s.dead = true;
+            return s;
+        }
+        end = s.first + s.n;
+    } else {
+        if (a.ctx_lens) {
+            s.req = s.row0 = u;
+            s.rows = 1;
+            s.first = a.ctx_lens[u];
+            if (s.first < 0 || s.first >= a.max_ctx) {
+                if (s.first != -1 && threadIdx.x == 0) atomicOr(a.err_flag, 8);
+                s.dead = true;
+                return s;
+            }
+        } else {
+            u = a.n_units - 1 - u;   // the last rows of a prompt see most
+            int n = 0;
+            for (;; ++s.req) {
+                n = (a.seq.cu[s.req + 1] - a.seq.cu[s.req] + per - 1) / per;
+                if (u < n || s.req + 1 >= a.seq.n_req) break;
+                u -= n;
+            }
+            s.row0 = a.seq.cu[s.req] + u * per;
+            s.rows = min(per, a.seq.cu[s.req + 1] - s.row0);
+            s.first = a.seq.start[s.req] + u * per;
+        }
+        end = s.first + s.rows;
+        const int oldest = max(s.first - a.window + 1, 0), w0 = oldest >> 4;
+        s.sink_blocks = min((min(a.sinks, end) + 15) >> 4, w0);
+        s.skip = w0 - s.sink_blocks;
+    }
+    s.blocks = ((end + 15) >> 4) - s.skip;
+    return s;
+}
+
+// What one row sees.
+struct Sight {
+    int lo, hi, sinks;       // window: keys lo .. hi and those below sinks (of them none above hi)
+    int ctx;                 // tree: keys below, and the bits of
+    uint64_t bits;
+    // the 16 keys from pos on, a bit each.  (Without branches: of a chain of conditions on 16 score registers the compiler, clang 22 of ROCm 7.2,
+    // made control flow that lost the first register's.)
+    template <bool TREE>
+    __device__ __forceinline__ uint32_t sees16(int pos) const {
+        auto upto = [](int n) { return (1u << min(max(n, 0), 16)) - 1; };
+        if (TREE) {
+            const int d = ctx - pos;
+            const uint64_t drafted = d > 0 ? bits << min(d, 63) : bits >> min(-d, 63);
+            return upto(d) | ((d < 16 && d > -64 ? (uint32_t)drafted : 0u) & 0xffffu);
+        }
+        return upto(hi - pos + 1) & (~upto(lo - pos) | upto(sinks - pos));
+    }
+};
+template <bool TREE>
+__device__ __forceinline__ Sight row_sight(const MaskedAttnArgs &a, const Span &s, int r) {
+    Sight v{};
+    if (TREE) {
+        v.ctx = s.first;
+        const int i = s.i0 + r;
+        v.bits = a.masks ? a.masks[s.row0 + r] : (2ull << i) - 1;
+        if (s.n < 64) v.bits &= (1ull << s.n) - 1;   // places behind the request's rows hold nothing
+    } else {
+        v.hi = s.first + r;
+        v.lo = max(v.hi - a.window + 1, 0);
+        v.sinks = a.sinks;
+    }
+    return v;
+}
+
+__device__ __forceinline__ bf16_t *out_at(const MaskedAttnArgs &a, const Span &s, int col, int hk, int G) {
+    return a.out + (size_t)(s.row0 + col / G) * a.out_stride + (size_t)(hk * G + col % G) * a.hd;
+}
+
+// The same sums one key after the other in float32, without the matrix unit: for units whose result is not finite.  There a weight
+// of zero times a value that is infinite or NaN may have reached rows that do not see that value; here it cannot.  Slow (some ms for
+// 4096 keys), and only taken where a cache holds such values.
+template <int HD, bool TREE>
+__device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span &s, int hk, int b0, int b1, size_t slot, int threads) {
+    constexpr int D = 32;   // dims of a thread
+    const int G = a.Hq / a.Hkv, parts = HD / D;
+    const int32_t *tab = a.tables + (size_t)s.req * a.max_blk;
+    for (int item = threadIdx.x; item < s.rows * G * parts; item += threads) {
+        const int col = item / parts, d0 = item % parts * D;
+        const Sight see = row_sight<TREE>(a, s, col / G);
+        const bf16_t *q = a.q + (size_t)(s.row0 + col / G) * a.q_stride + (size_t)(hk * G + col % G) * HD;
+        float m = NEG_INF, l = 0.f, o[D];
+        for (int i = 0; i < D; ++i) o[i] = 0.f;
+        for (int j = b0; j < b1; ++j) {
+            const int e = j < s.sink_blocks ? j : j + s.skip, blk = tab[e];
+            if ((unsigned)blk >= (unsigned)a.n_blocks) continue;
+            const size_t head = ((size_t)blk * a.Hkv + hk) * 16 * HD;
+            const uint32_t seen = see.sees16<TREE>(16 * e);
+#pragma unroll 1
+            for (int t = 0; t < 16; ++t) {
+                if (!(seen >> t & 1)) continue;
+                float dot = 0.f;
+#pragma unroll 1
+                for (int d = 0; d < HD; d += 8) {
+                    const bf16x8 x = ld_bf16x8(q + d), y = ld_bf16x8(a.k_pool + head + kpool_chunk_offset(t, d));
+                    for (int i = 0; i < 8; ++i) dot = fmaf((float)x[i], (float)y[i], dot);
+                }
+                const float top = fmaxf(m, dot), ref = top == NEG_INF ? 0.f : top;
+                const float keep = exp2f((m - ref) * a.scale_log2), w = exp2f((dot - ref) * a.scale_log2);
+                l = l * keep + w;
+                for (int i = 0; i < D; ++i) o[i] = o[i] * keep + w * (float)a.v_pool[head + (size_t)(d0 + i) * 16 + t];
+                m = top;
+            }
+        }
+        if (a.cut > 1) {
+            for (int i = 0; i < D; ++i) a.part_o[(slot * COLS + col) * HD + d0 + i] = o[i];
+            if (d0 == 0) a.part_ml[2 * (slot * COLS + col)] = m, a.part_ml[2 * (slot * COLS + col) + 1] = l;
+        } else {
+            bf16_t *p = out_at(a, s, col, hk, G) + d0;
+            for (int i = 0; i < D; ++i) p[i] = (bf16_t)(l == 0.f ? 0.f : o[i] / l);
+        }
+    }
+}
+
+// A unit, or one of the `cut` pieces of its keys, by KW teams of four waves; team t takes every KW-th tile of 64 keys, from LDS buffers of its
+// own, and the teams' sums are brought together at the end.  S^T = K Q^T and O^T = V^T P^T, so that a lane owns one column.
+template <int HD, int KW, bool TREE>
+__global__ __launch_bounds__(256 * KW, 2) void masked_attn_kernel(MaskedAttnArgs a) {
+    constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD;
+    extern __shared__ __attribute__((aligned(1024))) bf16_t smem_masked[];
+    const int tid = threadIdx.x & 255, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int team = KW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
+    const int c32 = lane & 31, h = lane >> 5;
+    const int G = a.Hq / a.Hkv;
+    // kv heads go to the XCDs in turn, so that a head's keys are in one L2 where there are eight of them
+    const int hk = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, piece = rest % a.cut, unit = rest / a.cut;
+    const Span s = unit_span<TREE>(a, unit);
+    if (s.rows <= 0) return;
+    const size_t slot = (size_t)rest * a.Hkv + hk;
+    const int cols = s.rows * G;
+    if (s.dead) {
+        if (piece == 0)
+            for (int i = threadIdx.x; i < cols * HD; i += 256 * KW) out_at(a, s, i / HD, hk, G)[i % HD] = (bf16_t)0.f;
+        return;
+    }
+    const int n_tiles = (s.blocks + 3) >> 2;
+    const int t0 = (int)((int64_t)n_tiles * piece / a.cut), t1 = (int)((int64_t)n_tiles * (piece + 1) / a.cut);
+    const int32_t *tab = a.tables + (size_t)s.req * a.max_blk;
+    const float sc = a.scale_log2;
+
+    bf16_t *Ks = smem_masked + team * (4 * 64 * HD);   // [2][4 blocks][BLK] in the pool's order
+    bf16_t *Vs = Ks + 2 * 64 * HD;                     // [2][4 blocks][2 halves][HD][8 tokens]
+    float *x_ml = (float *)(smem_masked + KW * 4 * 64 * HD);   // [KW][4 waves][32][2]
+
+    const int col = wave * 32 + c32, row = min(col, cols - 1) / G;
+    const Sight see = row_sight<TREE>(a, s, row);
+    bf16x8 qf[KS];
+    {
+        const bf16_t *qp = a.q + (size_t)(s.row0 + row) * a.q_stride + (size_t)(hk * G + min(col, cols - 1) % G) * HD + 8 * h;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) qf[i] = ld_bf16x8(qp + 16 * i);
+    }
+    // of the wave's rows: positions of the first and of the last
+    const int w_first = s.first + min(wave * 32, cols - 1) / G, w_last = s.first + min(wave * 32 + 31, cols - 1) / G;
+    const bool wave_idle = wave * 32 >= cols;
+
+    // lane l < 4: table entry and block id of the l-th block of a tile; -1: none, or not one of the pool
+    auto entry = [&](int t) { const int j = 4 * t + (lane & 3); return j < s.sink_blocks ? j : j + s.skip; };
+    auto fetch_ids = [&](int t) { return t < t1 && 4 * t + (lane & 3) < s.blocks ? tab[entry(t)] : -1; };
+    auto checked = [&](int t, int id) {
+        if ((unsigned)id < (unsigned)a.n_blocks) return id;
+        if (t < t1 && 4 * t + (lane & 3) < s.blocks && tid < 4) atomicOr(a.err_flag, 2);
+        return -1;
+    };
+    // Brings a tile into LDS buffer buf by LDS-DMA (16 bytes a lane, lane l's at the window's base + 16 l): wave w copies block w.  K keeps
+    // the pool's order; V's chunk (dim, half of 8 tokens) goes to [half][dim].  A block that is missing is read as block 0, and masked.
+    auto load_tile = [&](int ids, int buf) {
+        const size_t head = ((size_t)max(__builtin_amdgcn_readlane(ids, wave), 0) * a.Hkv + hk) * BLK;
+        const auto kbuf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.k_pool + head), 0, 2 * BLK, 0x00020000);
+        const auto vbuf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.v_pool + head), 0, 2 * BLK, 0x00020000);
+        bf16_t *kd = Ks + buf * 64 * HD + wave * BLK, *vd = Vs + buf * 64 * HD + wave * BLK;
+        typedef __attribute__((address_space(3))) void lds_void;
+#define KV_PIECE(i) \
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(kbuf, (lds_void *)kd, 16, lane * 16, 0, 1024 * (i), 0); \
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(vbuf, (lds_void *)(vd + (i) * 512), 16, lane * 32, ((i) % (HD / 64)) * 2048 + ((i) / (HD / 64)) * 16, 0, 0);
+        KV_PIECE(0)
+        KV_PIECE(1)
+        if constexpr (HD == 128) {
+            KV_PIECE(2)
+            KV_PIECE(3)
+        }
+#undef KV_PIECE
+    };
+    auto klds = [](int r, int cc) { return (r >> 4) * BLK + kpool_chunk_offset(r & 15, cc * 8); };
+    auto vlds = [](int blk, int half, int d) { return blk * BLK + half * (8 * HD) + d * 8; };
+
+    float m_run = NEG_INF, l_run = 0.f;   // running maximum of raw scores, running sum
+    f32x16 o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+
+    const int n_it = (t1 - t0 + KW - 1) / KW;   // as many for every team: the barriers are the workgroup's
+    auto tile_at = [&](int it) { return t0 + KW * it + team; };
+    int ids = checked(tile_at(0), fetch_ids(tile_at(0))), next = fetch_ids(tile_at(1));
+    if (tile_at(0) < t1) load_tile(ids, 0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the LDS-DMA loads have landed
+    __syncthreads();
+    for (int it = 0; it < n_it; ++it) {
+        const int t = tile_at(it);
+        const int nids = checked(t + KW, next);
+        if (t + KW < t1) load_tile(nids, (it + 1) & 1);
+        next = fetch_ids(t + 2 * KW);
+        // the four blocks' first positions, whether the wave's rows see all of them, and any
+        int pos[4];
+        bool full = true, some = false;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int e = 4 * t + j;
+            pos[j] = 16 * (e < s.sink_blocks ? e : e + s.skip);
+            const bool there = __builtin_amdgcn_readlane(ids, j) >= 0;
+            const int p = pos[j];
+            if (TREE) {
+                full = full && there && p + 15 < s.first;
+                some = some || there;
+            } else {
+                full = full && there && p + 15 <= w_first && (p > w_last - a.window || p + 15 < a.sinks);
+                some = some || (there && p <= w_last && (p + 15 > w_first - a.window || p < a.sinks));
+            }
+        }
+        if (t < t1 && some && !wave_idle) {
+            const bf16_t *ks = Ks + (it & 1) * 64 * HD;
+            const bf16_t *vs = Vs + (it & 1) * 64 * HD;
+            f32x16 st[2];
+#pragma unroll
+            for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) st[t2][i] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 2 * KS; ++i) {
+                const bf16x8 kf = *(const bf16x8 *)&ks[klds(32 * (i & 1) + c32, 2 * (i >> 1) + h)];
+                st[i & 1] = mfma32(kf, qf[i >> 1], st[i & 1]);
+            }
+            if (!full) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t seen = __builtin_amdgcn_readlane(ids, j) >= 0 ? see.sees16<TREE>(pos[j]) >> (4 * h) : 0u;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float x = st[j >> 1][8 * (j & 1) + i];
+                        st[j >> 1][8 * (j & 1) + i] = seen & (1u << ((i >> 2) * 8 + (i & 3))) ? x : NEG_INF;
+                    }
+                }
+            }
+            float m_tile = NEG_INF;
+#pragma unroll
+            for (int t2 = 0; t2 < 2; ++t2)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) m_tile = fmaxf(m_tile, st[t2][i]);
+            m_tile = fmaxf(m_tile, __shfl_xor(m_tile, 32, 64));
+            const float m_new = fmaxf(m_run, m_tile);
+            const float m_safe = m_new == NEG_INF ? 0.f : m_new;
+            if (__any(m_new != m_run)) {
+                const float alpha = __builtin_amdgcn_exp2f((m_run - m_safe) * sc);
+                l_run *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[dt] = o[dt] * alpha;
+                m_run = m_new;
+            }
+            const float ms = m_safe * sc;
+#pragma unroll
+            for (int blk4 = 0; blk4 < 4; ++blk4) {   // one 16-token block per product step
+                bf16x8 pf;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float p = __builtin_amdgcn_exp2f(fmaf(st[blk4 >> 1][8 * (blk4 & 1) + i], sc, -ms));
+                    l_run += p;
+                    pf[i] = (bf16_t)p;
+                }
+                // The half-waves (same column) hold a block's tokens 4h..4h+3 and 8+4h..8+4h+3 and trade their middle pieces:
+                // h = 0 then has tokens 0-7, h = 1 tokens 8-15, the contraction slices of V's own layout.
+                typedef uint32_t u32x4p __attribute__((ext_vector_type(4)));
+                u32x4p pr4 = __builtin_bit_cast(u32x4p, pf);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const auto sw = __builtin_amdgcn_permlane32_swap(pr4[u], pr4[u + 2], false, false);
+                    pr4[u] = sw[0];
+                    pr4[u + 2] = sw[1];
+                }
+                pf = __builtin_bit_cast(bf16x8, pr4);
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32(*(const bf16x8 *)&vs[vlds(blk4, h, 32 * dt + c32)], pf, o[dt]);
+            }
+        }
+        ids = nids;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the LDS-DMA loads have landed
+        __syncthreads();
+    }
+    l_run += __shfl_xor(l_run, 32, 64);
+
+    bool odd = false;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd = odd || !(fabsf(o[dt][i]) < __builtin_huge_valf());
+    if (__syncthreads_or(odd && col < cols)) {
+        careful_unit<HD, TREE>(a, s, hk, 4 * t0, min(4 * t1, s.blocks), slot, 256 * KW);
+        return;
+    }
+
+    if (KW == 2) {
+        // both teams rescale to the common maximum; team 0 finishes the first half of head_dim, team 1 the second, each with the other's
+        // part through the K/V buffers (nobody reads those any more)
+        f32x4 *x_o = (f32x4 *)smem_masked;   // [KW][4 waves][2 DT][64]
+        float *mine = x_ml + (team * 4 + wave) * 64, *theirs = x_ml + ((1 - team) * 4 + wave) * 64;
+        if (h == 0) {
+            mine[2 * c32] = m_run;
+            mine[2 * c32 + 1] = l_run;
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT / 2; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                f32x4 v;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = team == 0 ? o[DT / 2 + dt][4 * j + i] : o[dt][4 * j + i];
+                x_o[((team * 4 + wave) * (2 * DT) + dt * 4 + j) * 64 + lane] = v;
+            }
+        __syncthreads();
+        const float m_o = theirs[2 * c32], l_o = theirs[2 * c32 + 1];
+        const float top = fmaxf(m_run, m_o), ref = top == NEG_INF ? 0.f : top;
+        const float e = __builtin_amdgcn_exp2f((m_run - ref) * sc), e_o = __builtin_amdgcn_exp2f((m_o - ref) * sc);
+        l_run = l_run * e + l_o * e_o;
+        m_run = top;
+#pragma unroll
+        for (int dt = 0; dt < DT / 2; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const f32x4 v = x_o[(((1 - team) * 4 + wave) * (2 * DT) + dt * 4 + j) * 64 + lane];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[dt][4 * j + i] = (team == 0 ? o[dt][4 * j + i] : o[DT / 2 + dt][4 * j + i]) * e + v[i] * e_o;
+            }
+    }
+    if (col >= cols) return;
+    const int d0 = team * (HD / KW) + 4 * h;   // this lane's dims: d0 + 32 dt + 8 j + i
+    if (a.cut > 1) {
+        float *po = a.part_o + (slot * COLS + col) * HD;
+#pragma unroll
+        for (int dt = 0; dt < DT / KW; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *(f32x4 *)(po + d0 + 32 * dt + 8 * j) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
+        if (h == 0 && team == 0) *(float2 *)(a.part_ml + 2 * (slot * COLS + col)) = float2{m_run, l_run};
+        return;
+    }
+    const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
+    bf16_t *p = out_at(a, s, col, hk, G);
+#pragma unroll
+    for (int dt = 0; dt < DT / KW; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            bf16x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(o[dt][4 * j + i] * inv);
+            *(bf16x4 *)(p + d0 + 32 * dt + 8 * j) = v;
+        }
+}
+
+// Brings the pieces of a unit's columns together: a thread per (column, four dims).
+template <int HD, bool TREE>
+__global__ __launch_bounds__(256) void masked_join_kernel(MaskedAttnArgs a) {
+    const int G = a.Hq / a.Hkv, hk = blockIdx.x % a.Hkv, unit = blockIdx.x / a.Hkv;
+    const Span s = unit_span<TREE>(a, unit);
+    const int item = blockIdx.y * 256 + threadIdx.x, col = item / (HD / 4), d = item % (HD / 4) * 4;
+    if (s.rows <= 0 || s.dead || col >= s.rows * G) return;
+    auto at = [&](int piece) { return ((((size_t)unit * a.cut + piece) * a.Hkv + hk) * COLS + col); };
+    float top = NEG_INF, l = 0.f;
+    for (int i = 0; i < a.cut; ++i) top = fmaxf(top, a.part_ml[2 * at(i)]);
+    const float ref = top == NEG_INF ? 0.f : top;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < a.cut; ++i) {
+        const float2 ml = *(const float2 *)(a.part_ml + 2 * at(i));
+        if (ml.y == 0.f) continue;   // a piece none of whose keys the row sees
+        const float e = exp2f((ml.x - ref) * a.scale_log2);
+        l += ml.y * e;
+        acc += *(const f32x4 *)(a.part_o + at(i) * HD + d) * e;
+    }
+    bf16x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(l == 0.f ? 0.f : acc[i] / l);
+    *(bf16x4 *)(out_at(a, s, col, hk, G) + d) = v;
+}
+
+constexpr int masked_lds(int hd, int kw) { return kw * 4 * 64 * hd * 2 + kw * 4 * 64 * 4; }
+
+template <int HD, bool TREE>
+void launch(hipStream_t st, const MaskedAttnArgs &a, bool teams) {
+    const dim3 grid(a.n_units * a.cut * a.Hkv);
+    if (teams) hipLaunchKernelGGL((masked_attn_kernel<HD, 2, TREE>), grid, dim3(512), masked_lds(HD, 2), st, a);
+    else hipLaunchKernelGGL((masked_attn_kernel<HD, 1, TREE>), grid, dim3(256), masked_lds(HD, 1), st, a);
+    if (a.cut > 1) {
+        const int rows = TREE ? std::min(a.max_draft, COLS / (a.Hq / a.Hkv)) : a.ctx_lens ? 1 : COLS / (a.Hq / a.Hkv);
+        hipLaunchKernelGGL((masked_join_kernel<HD, TREE>), dim3(a.n_units * a.Hkv, (rows * (a.Hq / a.Hkv) * HD / 4 + 255) / 256), dim3(256), 0, st, a);
+    }
+}
+
+}  // namespace
+
+void launch_masked_attention(hipStream_t st, const MaskedAttnArgs &args) {
+    MaskedAttnArgs a = args;
+    const int per = COLS / (a.Hq / a.Hkv);
+    const bool tree = a.cu_rows != nullptr;
+    int keys = 0;   // most keys of a unit
+    if (tree) {
+        a.units_per_req = (a.max_draft + per - 1) / per;
+        a.n_units = a.B * a.units_per_req;
+        keys = a.max_ctx;
+    } else if (a.ctx_lens) {
+        a.n_units = a.B;
+        keys = a.max_ctx;
+    } else {
+        a.n_units = 0;
+        for (int r = 0; r < a.seq.n_req; ++r) {
+            a.n_units += (a.seq.cu[r + 1] - a.seq.cu[r] + per - 1) / per;
+            keys = std::max(keys, a.seq.start[r] + a.seq.cu[r + 1] - a.seq.cu[r]);
+        }
+    }
+    if (a.n_units <= 0) return;
+    if (!tree) keys = (int)std::min<int64_t>(keys, (int64_t)a.window + a.sinks + per + 32);
+    const int wgs = a.n_units * a.Hkv, tiles = (keys + 63) / 64;
+    const bool teams = wgs <= 256;
+    a.cut = std::max(1, std::min({256 / wgs, MASKED_PIECES / wgs, (tiles + 7) / 8}));
+    if (a.hd == 128) {
+        if (tree) launch<128, true>(st, a, teams);
+        else launch<128, false>(st, a, teams);
+    } else {
+        if (tree) launch<64, true>(st, a, teams);
+        else launch<64, false>(st, a, teams);
+    }
+}
+
+void masked_attention_init() {
+    auto set = [](const void *f, int lds) { (void)hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, lds); };
+    set((const void *)masked_attn_kernel<128, 1, false>, masked_lds(128, 1));
+    set((const void *)masked_attn_kernel<128, 1, true>, masked_lds(128, 1));
+    set((const void *)masked_attn_kernel<128, 2, false>, masked_lds(128, 2));
+    set((const void *)masked_attn_kernel<128, 2, true>, masked_lds(128, 2));
+    set((const void *)masked_attn_kernel<64, 2, false>, masked_lds(64, 2));
+    set((const void *)masked_attn_kernel<64, 2, true>, masked_lds(64, 2));
+}

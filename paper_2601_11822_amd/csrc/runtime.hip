@@ -174,9 +174,13 @@ struct rs_ctx {
     bool is_kv4 = false;
     float *kv4_part_o[2] = {nullptr, nullptr}, *kv4_part_ml[2] = {nullptr, nullptr};
     int32_t *kv4_part_row[2] = {nullptr, nullptr};
+    // scratch of windowed and tree attention whose keys are cut, and the ticket of plans, per side
+    float *mask_part_o[2] = {nullptr, nullptr}, *mask_part_ml[2] = {nullptr, nullptr};
+    int32_t *plan_ticket = nullptr;
     CosSin *rope = nullptr;
     // One error word per side (kernels OR bits into it: 1 position outside the rotary table, 2 block id outside
-    // the pool, 4 token outside the vocabulary, 8 context length outside [1, max_ctx]) and its pinned host
+    // the pool, 4 token outside the vocabulary, 8 context length outside [1, max_ctx], 16 a plan found too few free blocks,
+    // 32 row counts, lengths or parents that contradict each other) and its pinned host
     // mirrors: h_err[side] is what rs_sync reads, h_err[2 + i] travels with decode step buffer i, h_err[4]
     // with a prefill pass of the serving loop.  Every copy and clear runs on the side's own stream: a
     // blocking copy on the null stream would make one side wait for the other.
@@ -1045,6 +1049,8 @@ int32_t head_greedy(rs_ctx *c, int side, const bf16_t *x, int n, float *logits, 
 // The status a set of error bits stands for (see rs_ctx::err_flag).
 int32_t report_flag(int32_t flag) {
     if (flag & 4) return fail(RS_ERR_BAD_ARG, "a kernel met a token outside the vocabulary (flag %d)", flag);
+    if (flag & RS_FLAG_LENGTHS) return fail(RS_ERR_BAD_ARG, "a kernel met row counts, lengths or parents that contradict each other (flag %d)", flag);
+    if (flag == RS_FLAG_NO_BLOCKS) return fail(RS_ERR_NO_BLOCKS, "a plan needs more blocks than are free; it changed nothing");
     return fail(RS_ERR_BAD_BLOCK, "a kernel skipped an illegal block id, rotary position or context length (flag %d)", flag);
 }
 
@@ -1154,6 +1160,105 @@ int32_t kv4_runs(const rs_ctx *c, const int32_t *cu, const int32_t *start, int32
     return RS_OK;
 }
 
+// ---- windowed and tree attention, and the cache's upkeep on the GPU ----
+
+int32_t alloc_masked(rs_ctx *c) {
+    const int rows[2] = {c->lim.max_prefill_tokens, c->lim.max_decode_batch};
+    for (int s = 0; s < 2 && !c->is_kv4; ++s) {
+        if (rows[s] <= 0) continue;
+        const size_t n = (size_t)MASKED_PIECES * MASKED_COLS;
+        HIP_TRY(hipMalloc(&c->mask_part_o[s], n * c->m.head_dim * sizeof(float)));
+        HIP_TRY(hipMalloc(&c->mask_part_ml[s], n * 2 * sizeof(float)));
+    }
+    HIP_TRY(hipMalloc(&c->plan_ticket, 2 * sizeof(int32_t)));
+    HIP_TRY(hipMemset(c->plan_ticket, 0, 2 * sizeof(int32_t)));
+    return RS_OK;
+}
+
+// Layers [layer, layer + n) of the bf16 pools; 16-byte pieces of them are read and written.
+int32_t check_bf16_call(rs_ctx *c, int32_t side, int32_t layer, int32_t n) {
+    if (!c) return fail(RS_ERR_BAD_ARG, "null context");
+    if (side < 0 || side > 1) return fail(RS_ERR_BAD_ARG, "side %d", side);
+    if (c->is_kv4) return fail(RS_ERR_STATE, "the context's cache is held in 4 bits");
+    if (layer < 0 || n < 1 || layer > c->m.n_layers - n) return fail(RS_ERR_BAD_ARG, "layers %d .. of %d out of range", layer, n);
+    if (((uintptr_t)c->pool.k_pool | (uintptr_t)c->pool.v_pool) % 16 || (c->m.n_layers > 1 && c->pool.layer_stride % 8))
+        return fail(RS_ERR_BAD_ARG, "the pools or their layer_stride are not a multiple of 16 bytes");
+    return RS_OK;
+}
+
+int32_t check_tables(const int32_t *tables, int32_t max_blk) {
+    if (!tables || (uintptr_t)tables % 4) return fail(RS_ERR_BAD_ARG, "null or misaligned block tables");
+    if (max_blk < 1 || max_blk >= 1 << 27) return fail(RS_ERR_BAD_BLOCK, "block tables of %d entries", max_blk);
+    return RS_OK;
+}
+
+int32_t check_words(const char *what, const void *p, size_t size) {
+    if (!p || (uintptr_t)p % size) return fail(RS_ERR_BAD_ARG, "%s: a null or misaligned pointer", what);
+    return RS_OK;
+}
+
+// A launch holds fewer than 2^32 threads.
+int32_t check_grid(int64_t wgs, int threads) {
+    if (wgs * threads > UINT32_MAX) return fail(RS_ERR_BAD_ARG, "more rows than a launch has threads for");
+    return RS_OK;
+}
+
+MaskedAttnArgs masked_args(rs_ctx *c, int side, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                           const int32_t *tables, int32_t max_blk) {
+    MaskedAttnArgs a{};
+    a.q = (const bf16_t *)q;
+    a.q_stride = (size_t)q_stride;
+    a.out = (bf16_t *)out;
+    a.out_stride = (size_t)out_stride;
+    a.k_pool = (const bf16_t *)c->pool.k_pool + (size_t)layer * c->pool.layer_stride;
+    a.v_pool = (const bf16_t *)c->pool.v_pool + (size_t)layer * c->pool.layer_stride;
+    a.tables = tables;
+    a.err_flag = c->err_flag + side;
+    a.part_o = c->mask_part_o[side];
+    a.part_ml = c->mask_part_ml[side];
+    a.Hq = c->m.n_q_heads;
+    a.Hkv = c->m.n_kv_heads;
+    a.hd = c->m.head_dim;
+    a.max_blk = max_blk;
+    a.n_blocks = c->pool.n_blocks;
+    a.scale_log2 = (float)(1.4426950408889634 / std::sqrt((double)c->m.head_dim));
+    return a;
+}
+
+int32_t check_masked_call(rs_ctx *c, int32_t side, int32_t layer, const void *q, int64_t q_stride, const void *out, int64_t out_stride,
+                          const int32_t *tables, int32_t max_blk) {
+    int32_t rc = check_bf16_call(c, side, layer, 1);
+    if (rc) return rc;
+    const int width = c->m.n_q_heads * c->m.head_dim;
+    if ((rc = check_kv4_rows("q", q, q_stride, width)) || (rc = check_kv4_rows("out", out, out_stride, width))) return rc;
+    return check_tables(tables, max_blk);
+}
+
+int32_t check_contexts(rs_ctx *c, const int32_t *ctx_lens, int32_t max_blk, int32_t B, int32_t max_ctx) {
+    int32_t rc = check_words("ctx_lens", ctx_lens, 4);
+    if (rc) return rc;
+    if (B < 1 || B > c->lim.max_decode_batch || B > 65535) return fail(RS_ERR_BAD_ARG, "decode batch %d, the limit is %d", B, c->lim.max_decode_batch);
+    if (max_ctx < 1 || max_ctx > c->lim.max_context) return fail(RS_ERR_BAD_ARG, "max_ctx %d outside [1, %d]", max_ctx, c->lim.max_context);
+    if ((max_ctx + (int64_t)RS_KV_BLOCK - 1) / RS_KV_BLOCK > max_blk)
+        return fail(RS_ERR_BAD_BLOCK, "block table of %d entries too short for context %d", max_blk, max_ctx);
+    return RS_OK;
+}
+
+int32_t check_window(int32_t window, int32_t sinks) {
+    if (window < 1 || sinks < 0) return fail(RS_ERR_BAD_ARG, "a window of %d tokens and %d sinks", window, sinks);
+    return RS_OK;
+}
+
+int32_t run_masked(rs_ctx *c, int32_t side, const MaskedAttnArgs &a) {
+    int32_t rc = check_kv4_side(c, side);
+    if (rc) return rc;
+    OnDevice on(c->device);
+    HIP_TRY(on.err);
+    launch_masked_attention(c->side[side].stream, a);
+    HIP_TRY(hipGetLastError());
+    return RS_OK;
+}
+
 int32_t check_head_call(rs_ctx *c, int side, int n) {
     if (!c) return fail(RS_ERR_BAD_ARG, "null context");
     if (side < 0 || side > 1) return fail(RS_ERR_BAD_ARG, "side %d", side);
@@ -1254,6 +1359,7 @@ static int32_t init_ctx(const rs_model_desc *model, const rs_pool_desc *pool, co
         decode_gemm_kernels_init();
         attention_kernels_init();
         kv4_kernels_init();
+        masked_attention_init();
         // rotary table, angles in float64
         const int half = m.head_dim / 2;
         std::vector<CosSin> tab((size_t)m.max_pos * half);
@@ -1275,6 +1381,7 @@ static int32_t init_ctx(const rs_model_desc *model, const rs_pool_desc *pool, co
         r = alloc_ws(c, c->ws[RS_SIDE_DECODE], limits->max_decode_batch, true);
         if (r) return r;
         if (kv4 && (r = alloc_kv4(c))) return r;
+        if ((r = alloc_masked(c))) return r;
         for (int s = 0; s < 2; ++s) {
             HIP_TRY(hipEventCreateWithFlags(&c->side[s].order, hipEventDisableTiming));
             c->side[s].marks.assign(RS_MAX_MARKS, nullptr);
@@ -1332,6 +1439,8 @@ int32_t rs_destroy(rs_ctx *c) {
             if (c->kv4_part_o[s]) (void)hipFree(c->kv4_part_o[s]);
             if (c->kv4_part_ml[s]) (void)hipFree(c->kv4_part_ml[s]);
             if (c->kv4_part_row[s]) (void)hipFree(c->kv4_part_row[s]);
+            if (c->mask_part_o[s]) (void)hipFree(c->mask_part_o[s]);
+            if (c->mask_part_ml[s]) (void)hipFree(c->mask_part_ml[s]);
         }
         for (auto &kv : c->graphs) (void)hipGraphExecDestroy(kv.second);
         drop_step_graphs(c);
@@ -1341,6 +1450,7 @@ int32_t rs_destroy(rs_ctx *c) {
         for (auto &ml : c->moe)
             for (bf16_t *q : {ml.wg, ml.wu, ml.wd})
                 if (q) (void)hipFree(q);
+        if (c->plan_ticket) (void)hipFree(c->plan_ticket);
         if (c->rope) (void)hipFree(c->rope);
         if (c->err_flag) (void)hipFree(c->err_flag);
         if (c->h_err) (void)hipHostFree(c->h_err);
@@ -1715,6 +1825,133 @@ int32_t rs_kv4_prefill_attention(rs_ctx *c, int32_t layer, const void *q, int64_
     OnDevice on(c->device);
     HIP_TRY(on.err);
     launch_kv4_prefill(c->side[RS_SIDE_PREFILL].stream, a);
+    HIP_TRY(hipGetLastError());
+    return RS_OK;
+}
+
+int32_t rs_window_decode_attention(rs_ctx *c, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                                   const int32_t *ctx_lens, const int32_t *tables, int32_t max_blk, int32_t B, int32_t max_ctx,
+                                   int32_t window, int32_t sinks) {
+    int32_t rc = check_masked_call(c, RS_SIDE_DECODE, layer, q, q_stride, out, out_stride, tables, max_blk);
+    if (rc || (rc = check_contexts(c, ctx_lens, max_blk, B, max_ctx)) || (rc = check_window(window, sinks))) return rc;
+    if ((rc = check_grid((int64_t)B * c->m.n_kv_heads, 512))) return rc;
+    MaskedAttnArgs a = masked_args(c, RS_SIDE_DECODE, layer, q, q_stride, out, out_stride, tables, max_blk);
+    a.ctx_lens = ctx_lens, a.B = B, a.max_ctx = max_ctx, a.window = window, a.sinks = sinks;
+    return run_masked(c, RS_SIDE_DECODE, a);
+}
+
+int32_t rs_window_prefill_attention(rs_ctx *c, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride,
+                                    const int32_t *cu_seqlens, const int32_t *start_pos, int32_t n_req, const int32_t *tables,
+                                    int32_t max_blk, int32_t window, int32_t sinks) {
+    int32_t rc = check_masked_call(c, RS_SIDE_PREFILL, layer, q, q_stride, out, out_stride, tables, max_blk);
+    if (rc || (rc = check_window(window, sinks))) return rc;
+    MaskedAttnArgs a = masked_args(c, RS_SIDE_PREFILL, layer, q, q_stride, out, out_stride, tables, max_blk);
+    if ((rc = kv4_runs(c, cu_seqlens, start_pos, n_req, max_blk, &a.seq))) return rc;
+    if (a.seq.cu[n_req] > c->lim.max_prefill_tokens)
+        return fail(RS_ERR_BAD_ARG, "%d rows, the limit is %d", a.seq.cu[n_req], c->lim.max_prefill_tokens);
+    if ((rc = check_grid(((int64_t)a.seq.cu[n_req] / (MASKED_COLS / (a.Hq / a.Hkv)) + n_req) * a.Hkv, 512))) return rc;
+    a.window = window, a.sinks = sinks;
+    return run_masked(c, RS_SIDE_PREFILL, a);
+}
+
+int32_t rs_tree_attention(rs_ctx *c, int32_t layer, const void *q, int64_t q_stride, void *out, int64_t out_stride, const int32_t *ctx_lens,
+                          const int32_t *cu_rows, const uint64_t *masks, const int32_t *tables, int32_t max_blk, int32_t B,
+                          int32_t max_rows, int32_t max_draft, int32_t max_ctx) {
+    int32_t rc = check_masked_call(c, RS_SIDE_DECODE, layer, q, q_stride, out, out_stride, tables, max_blk);
+    if (rc || (rc = check_contexts(c, ctx_lens, max_blk, B, max_ctx)) || (rc = check_words("cu_rows", cu_rows, 4))) return rc;
+    if (masks && (rc = check_words("masks", masks, 8))) return rc;
+    if (max_draft < 1 || max_draft > RS_MAX_DRAFT || max_rows < 0) return fail(RS_ERR_BAD_ARG, "%d drafted tokens of a request, %d in all", max_draft, max_rows);
+    const int per = MASKED_COLS / (c->m.n_q_heads / c->m.n_kv_heads);
+    if ((rc = check_grid((int64_t)B * ((max_draft + per - 1) / per) * c->m.n_kv_heads, 512))) return rc;
+    MaskedAttnArgs a = masked_args(c, RS_SIDE_DECODE, layer, q, q_stride, out, out_stride, tables, max_blk);
+    a.ctx_lens = ctx_lens, a.B = B, a.max_ctx = max_ctx;
+    a.cu_rows = cu_rows, a.masks = masks, a.max_rows = max_rows, a.max_draft = max_draft;
+    return run_masked(c, RS_SIDE_DECODE, a);
+}
+
+int32_t rs_kv_plan(rs_ctx *c, int32_t side, const int32_t *lens, const int32_t *n_new, const int32_t *n_held, int32_t *tables, int32_t max_blk,
+                   int32_t B, const int32_t *free_ids, int32_t free_cap, const int32_t *n_free, const int32_t *parents, int32_t parent_stride,
+                   int32_t max_rows, int32_t *cu_rows, int32_t *positions, int32_t *slots, uint64_t *masks, int32_t *n_held_out,
+                   int32_t *n_free_out) {
+    if (!c) return fail(RS_ERR_BAD_ARG, "null context");
+    if (side < 0 || side > 1) return fail(RS_ERR_BAD_ARG, "side %d", side);
+    int32_t rc = check_tables(tables, max_blk);
+    if (rc) return rc;
+    const struct { const char *what; const void *p; } in[] = {{"lens", lens}, {"n_new", n_new}, {"n_held", n_held}, {"free_ids", free_ids}, {"n_free", n_free},
+        {"cu_rows", cu_rows}, {"positions", positions}, {"slots", slots}, {"n_held_out", n_held_out}, {"n_free_out", n_free_out}};
+    for (const auto &x : in)
+        if ((rc = check_words(x.what, x.p, 4))) return rc;
+    if (B < 1 || B > 65535) return fail(RS_ERR_BAD_ARG, "%d requests", B);
+    if (free_cap < 0 || max_rows < 0) return fail(RS_ERR_BAD_ARG, "%d free ids, %d rows", free_cap, max_rows);
+    if (c->pool.n_blocks >= 1 << 27) return fail(RS_ERR_BAD_ARG, "a pool of %d blocks has no 32-bit slots", c->pool.n_blocks);
+    if (parents && ((rc = check_words("parents", parents, 4)) || parent_stride < 1 || parent_stride > RS_MAX_DRAFT))
+        return rc ? rc : fail(RS_ERR_BAD_ARG, "parents of %d tokens a request", parent_stride);
+    if (masks && (!parents || (rc = check_words("masks", masks, 8)))) return rc ? rc : fail(RS_ERR_BAD_ARG, "masks without parents");
+    if ((rc = check_kv4_side(c, side))) return rc;
+    OnDevice on(c->device);
+    HIP_TRY(on.err);
+    launch_kv_plan(c->side[side].stream, KvPlanArgs{lens, n_new, n_held, tables, free_ids, n_free, parents, cu_rows, positions, slots, masks, n_held_out,
+                                                    n_free_out, c->plan_ticket + side, c->err_flag + side, B, max_blk, c->pool.n_blocks, free_cap, max_rows,
+                                                    parent_stride});
+    HIP_TRY(hipGetLastError());
+    return RS_OK;
+}
+
+int32_t rs_kv_store(rs_ctx *c, int32_t side, int32_t layer, const void *qkv, int64_t row_stride, void *q_out, int64_t q_stride,
+                    const int32_t *positions, int32_t n_axes, const uint8_t *pair_axis, const int32_t *slots, const int32_t *n_rows,
+                    int32_t max_rows) {
+    int32_t rc = check_bf16_call(c, side, layer, 1);
+    if (rc) return rc;
+    const rs_model_desc &m = c->m;
+    if ((rc = check_kv4_rows("qkv", qkv, row_stride, (int64_t)(m.n_q_heads + 2 * m.n_kv_heads) * m.head_dim))) return rc;
+    if (q_out && (rc = check_kv4_rows("q_out", q_out, q_stride, (int64_t)m.n_q_heads * m.head_dim))) return rc;
+    if ((rc = check_words("positions", positions, 4)) || (rc = check_words("slots", slots, 4))) return rc;
+    if (n_rows && (rc = check_words("n_rows", n_rows, 4))) return rc;
+    if (n_axes < 1 || n_axes > RS_MAX_AXES) return fail(RS_ERR_BAD_ARG, "%d axes of positions, at most %d", n_axes, RS_MAX_AXES);
+    if (n_axes > 1 && !pair_axis) return fail(RS_ERR_BAD_ARG, "no axis of each pair");
+    if (max_rows < 1) return fail(RS_ERR_BAD_ARG, "%d rows", max_rows);
+    KvStoreArgs a{};
+    for (int i = 0; pair_axis && i < m.head_dim / 2; ++i) {
+        if (pair_axis[i] >= n_axes) return fail(RS_ERR_BAD_ARG, "pair %d turns with axis %d of %d", i, pair_axis[i], n_axes);
+        a.axis[i >> 5] |= (uint64_t)pair_axis[i] << (2 * (i & 31));
+    }
+    if ((rc = check_grid(((int64_t)max_rows / 16 + 1) * ((m.n_q_heads + 7) / 8 + (m.n_kv_heads + 3) / 4), 256))) return rc;
+    if ((rc = check_kv4_side(c, side))) return rc;
+    a.qkv = (const bf16_t *)qkv;
+    a.row_stride = (size_t)row_stride;
+    a.q_out = (bf16_t *)q_out;
+    a.q_stride = (size_t)q_stride;
+    a.positions = positions;
+    a.slots = slots;
+    a.n_rows = n_rows;
+    a.table = c->rope;
+    a.k_pool = (bf16_t *)c->pool.k_pool + (size_t)layer * c->pool.layer_stride;
+    a.v_pool = (bf16_t *)c->pool.v_pool + (size_t)layer * c->pool.layer_stride;
+    a.err_flag = c->err_flag + side;
+    a.n_axes = n_axes, a.max_rows = max_rows, a.Hq = m.n_q_heads, a.Hkv = m.n_kv_heads, a.hd = m.head_dim;
+    a.n_blocks = c->pool.n_blocks, a.max_pos = m.max_pos;
+    OnDevice on(c->device);
+    HIP_TRY(on.err);
+    launch_kv_store(c->side[side].stream, a);
+    HIP_TRY(hipGetLastError());
+    return RS_OK;
+}
+
+int32_t rs_kv_compact(rs_ctx *c, int32_t side, int32_t layer, int32_t n_layers, const int32_t *ctx_lens, const int32_t *keep, int32_t keep_stride,
+                      const int32_t *keep_lens, const int32_t *tables, int32_t max_blk, int32_t B) {
+    int32_t rc = check_bf16_call(c, side, layer, n_layers);
+    if (rc || (rc = check_tables(tables, max_blk))) return rc;
+    if ((rc = check_words("ctx_lens", ctx_lens, 4)) || (rc = check_words("keep", keep, 4)) || (rc = check_words("keep_lens", keep_lens, 4))) return rc;
+    if (B < 1 || B > 65535 || n_layers > 65535) return fail(RS_ERR_BAD_ARG, "%d requests, %d layers", B, n_layers);
+    if (keep_stride < 1 || keep_stride > RS_MAX_DRAFT) return fail(RS_ERR_BAD_ARG, "%d kept tokens a request, at most %d", keep_stride, RS_MAX_DRAFT);
+    if ((rc = check_grid((int64_t)c->m.n_kv_heads * B * n_layers, 256))) return rc;
+    if ((rc = check_kv4_side(c, side))) return rc;
+    OnDevice on(c->device);
+    HIP_TRY(on.err);
+    launch_kv_compact(c->side[side].stream, KvCompactArgs{(bf16_t *)c->pool.k_pool + (size_t)layer * c->pool.layer_stride,
+                                                          (bf16_t *)c->pool.v_pool + (size_t)layer * c->pool.layer_stride, c->pool.layer_stride,
+                                                          ctx_lens, keep, keep_lens, tables, c->err_flag + side, n_layers, keep_stride, B,
+                                                          c->m.n_kv_heads, c->m.head_dim, max_blk, c->pool.n_blocks});
     HIP_TRY(hipGetLastError());
     return RS_OK;
 }
