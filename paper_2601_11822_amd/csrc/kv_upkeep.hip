@@ -15,35 +15,34 @@ namespace {
 // everything writes: a ticket counts them and is zero again behind the launch.
 // Bound by latency: lengths, then the sums, then held blocks' ids.
 // ---------------------------------------------------------------------------------------------
-constexpr int PLAN_REQS = 64;   // requests of a workgroup
+constexpr int PLAN_REQS = 64, PLAN_WAVES = 16;   // requests and waves of a workgroup
 
-__global__ __launch_bounds__(256) void kv_plan_kernel(KvPlanArgs a) {
-    __shared__ uint32_t s_n[4], s_need[4];
+__global__ __launch_bounds__(64 * PLAN_WAVES) void kv_plan_kernel(KvPlanArgs a) {
+    constexpr int T = 64 * PLAN_WAVES, K = PLAN_REQS / PLAN_WAVES;
+    __shared__ uint32_t s_n[PLAN_WAVES], s_need[PLAN_WAVES];
     __shared__ int s_row[PLAN_REQS], s_first[PLAN_REQS], s_len[PLAN_REQS], s_new[PLAN_REQS], s_held[PLAN_REQS], s_more[PLAN_REQS];
-    __shared__ int64_t s_tot_n[4], s_tot_need[4];
+    __shared__ int64_t s_tot_n[PLAN_WAVES], s_tot_need[PLAN_WAVES];
     __shared__ int s_bad, s_last;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int r0 = blockIdx.x * PLAN_REQS, mine = min(PLAN_REQS, a.B - r0);
     const bool first_y = blockIdx.y == 0;
     if (tid == 0) s_bad = 0;
-    const int n_free = min(max(*a.n_free, 0), a.free_cap);
+    const int given = *a.n_free, n_free = min(max(given, 0), a.free_cap);
 
-    // sums over the requests, 256 at a time
+    // sums over the requests, T at a time
     uint32_t carry_n = 0, carry_need = 0;
     int bad = 0;
     int64_t tot_n = 0, tot_need = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 256) {
+    for (int b0 = 0; b0 < a.B; b0 += T) {
         const int b = b0 + tid;
         int n = 0, need = 0, len = -1, held = 0;
         if (b < a.B) {
-            len = a.lens[b], held = a.held[b];
-            if (len != -1) {
-                n = a.n_new[b];
-                const int64_t end = (int64_t)len + n;
-                if (len < 0 || n < 0 || held < 0 || (a.parents && n > a.parent_stride)) bad |= RS_FLAG_LENGTHS, n = 0;
-                else if (held > a.max_blk || (int64_t)len > 16ll * held || end > 16ll * a.max_blk) bad |= 2, n = 0;
-                else need = max((int)((end + 15) >> 4) - held, 0);
-            }
+            len = a.lens[b], held = a.held[b], n = a.n_new[b];
+            const int64_t end = (int64_t)len + n;
+            if (len == -1) n = 0;
+            else if (len < 0 || n < 0 || held < 0 || (a.parents && n > a.parent_stride)) bad |= RS_FLAG_LENGTHS, n = 0;
+            else if (held > a.max_blk || (int64_t)len > 16ll * held || end > 16ll * a.max_blk) bad |= 2, n = 0;
+            else need = max((int)((end + 15) >> 4) - held, 0);
         }
         tot_n += n, tot_need += need;
         uint32_t x = n, y = need;   // inclusive sums of the wave
@@ -52,12 +51,16 @@ __global__ __launch_bounds__(256) void kv_plan_kernel(KvPlanArgs a) {
             const uint32_t xo = __shfl_up(x, o, 64), yo = __shfl_up(y, o, 64);
             if (lane >= o) x += xo, y += yo;
         }
-        __syncthreads();   // the sums of the 256 before have been read
+        __syncthreads();   // the sums of those before have been read
         if (lane == 63) s_n[wave] = x, s_need[wave] = y;
         __syncthreads();
         uint32_t row = carry_n + x - n, first = carry_need + y - need;
-        for (int w = 0; w < wave; ++w) row += s_n[w], first += s_need[w];
-        for (int w = 0; w < 4; ++w) carry_n += s_n[w], carry_need += s_need[w];
+#pragma unroll
+        for (int w = 0; w < PLAN_WAVES; ++w) {
+            const uint32_t xw = s_n[w], yw = s_need[w];
+            if (w < wave) row += xw, first += yw;
+            carry_n += xw, carry_need += yw;
+        }
         const int i = b - r0;
         if (i >= 0 && i < mine) s_row[i] = row, s_first[i] = first, s_len[i] = len, s_new[i] = n, s_held[i] = held, s_more[i] = need;
     }
@@ -68,71 +71,96 @@ __global__ __launch_bounds__(256) void kv_plan_kernel(KvPlanArgs a) {
     }
     if (lane == 0) s_tot_n[wave] = tot_n, s_tot_need[wave] = tot_need;
     if (bad) atomicOr(&s_bad, bad);
+    asm volatile("" ::"v"(given));   // has been read
     __syncthreads();
-    tot_n = s_tot_n[0] + s_tot_n[1] + s_tot_n[2] + s_tot_n[3];
-    tot_need = s_tot_need[0] + s_tot_need[1] + s_tot_need[2] + s_tot_need[3];
+    // this workgroup's sums are formed: once all have theirs, nobody reads held and n_free any more
+    const int wgs = gridDim.x * gridDim.y;
+    int arrived = 0;
+    if (tid == 0 && wgs > 1) arrived = atomicAdd(a.ticket, 1);
+    tot_n = tot_need = 0;
+#pragma unroll
+    for (int w = 0; w < PLAN_WAVES; ++w) tot_n += s_tot_n[w], tot_need += s_tot_need[w];
     bad = s_bad;
     if (!bad && tot_n > a.max_rows) bad = RS_FLAG_LENGTHS;
     if (!bad && tot_need > n_free) bad = RS_FLAG_NO_BLOCKS;
-    if (tid == 0) {
-        // the sums of this call have been formed by this workgroup: once all have, nobody reads held and n_free any more
-        const int wgs = gridDim.x * gridDim.y;
-        s_last = wgs == 1 || atomicAdd(a.ticket, 1) == wgs - 1;
-    }
-    __syncthreads();
-    if (s_last) {
-        for (int b = tid; b < a.B; b += 256) {
-            const int len = a.lens[b], held = a.held[b];
-            a.held_out[b] = bad || len == -1 ? held : max((int)(((int64_t)len + a.n_new[b] + 15) >> 4), held);
-        }
-        if (tid == 0) {
-            *a.n_free_out = bad ? *a.n_free : n_free - (int)tot_need;
-            *a.ticket = 0;
-            if (bad) atomicOr(a.err_flag, bad);
-        }
-    }
     if (first_y) {
-        for (int i = tid; i < mine; i += 256) a.cu_rows[r0 + i] = bad ? 0 : s_row[i];
+        for (int i = tid; i < mine; i += T) a.cu_rows[r0 + i] = bad ? 0 : s_row[i];
         if (r0 + mine == a.B && tid == 0) a.cu_rows[a.B] = bad ? 0 : (int)tot_n;
     }
-    if (bad) return;
-    auto block_of = [&](int i, int j) { return j < s_held[i] ? a.tables[(size_t)(r0 + i) * a.max_blk + j] : a.free_ids[n_free - 1 - (s_first[i] + j - s_held[i])]; };
-    auto slot_of = [&](int i, int token) {
-        const int id = block_of(i, token >> 4);
-        if ((unsigned)id < (unsigned)a.n_blocks) return 16 * id + (token & 15);
-        atomicOr(a.err_flag, 2);
-        return -1;
-    };
-    for (int i = wave; i < mine; i += 4) {
-        if (first_y)
-            for (int j = lane; j < s_more[i]; j += 64) a.tables[(size_t)(r0 + i) * a.max_blk + s_held[i] + j] = a.free_ids[n_free - 1 - (s_first[i] + j)];
-        const int n = s_new[i], row = s_row[i], len = s_len[i];
-        if (a.parents) {
-            // a lane a token; ancestors by doubling: after k steps `mask` holds 2^k of them and `up` is the one behind
-            if (!first_y || n == 0) continue;
-            int up = lane < n ? a.parents[(size_t)(r0 + i) * a.parent_stride + lane] : -1;
-            if (up < -1 || up >= lane) {
-                atomicOr(a.err_flag, RS_FLAG_LENGTHS);
-                up = -1;
-            }
-            uint64_t mask = 1ull << lane;
+    if (!bad) {
+        auto source = [&](int i, int j) -> const int32_t * {   // where the id of a request's block j stands
+            return j < s_held[i] ? a.tables + (size_t)(r0 + i) * a.max_blk + j : a.free_ids + n_free - 1 - (s_first[i] + j - s_held[i]);
+        };
+        auto slot_of = [&](int id, int token) {
+            if ((unsigned)id < (unsigned)a.n_blocks) return 16 * id + (token & 15);
+            atomicOr(a.err_flag, 2);
+            return -1;
+        };
+        // A wave takes up to K requests, a lane a token of each, with everything asked for at once; where there are fewer requests than waves
+        // several waves share one.
+        const int sub = mine >= PLAN_WAVES ? 1 : PLAN_WAVES / mine, step = PLAN_WAVES / sub, part = wave % sub + sub * blockIdx.y, parts = sub * gridDim.y;
+        int id[K], fresh[K], up[K];
 #pragma unroll
-            for (int k = 0; k < 6; ++k) {
-                const uint64_t m = __shfl(mask, up & 63, 64);
-                const int u = __shfl(up, up & 63, 64);
-                if (up >= 0) mask |= m, up = u;
-            }
-            if (lane < n) {
-                a.positions[row + lane] = len + __popcll(mask) - 1;
-                a.slots[row + lane] = slot_of(i, len + lane);
-                if (a.masks) a.masks[row + lane] = mask;
-            }
-        } else {
-            for (int j = lane + 64 * blockIdx.y; j < n; j += 64 * gridDim.y) {
-                a.positions[row + j] = len + j;
-                a.slots[row + j] = slot_of(i, len + j);
+        for (int k = 0; k < K; ++k) {
+            const int i = wave / sub + k * step, j = lane + 64 * part;
+            id[k] = fresh[k] = 0, up[k] = -1;
+            if (i >= mine) continue;
+            if (j < s_new[i]) id[k] = *source(i, (s_len[i] + j) >> 4);
+            if (j < s_more[i]) fresh[k] = *source(i, s_held[i] + j);
+            if (a.parents && j < s_new[i]) up[k] = a.parents[(size_t)(r0 + i) * a.parent_stride + j];
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int i = wave / sub + k * step;
+            if (i >= mine) continue;   // (uniform)
+            const int n = s_new[i], row = s_row[i], len = s_len[i], held = s_held[i], more = s_more[i];
+            int32_t *tab = a.tables + (size_t)(r0 + i) * a.max_blk + held;
+            const int j0 = lane + 64 * part;
+            if (j0 < more) tab[j0] = fresh[k];
+            for (int j = j0 + 64 * parts; j < more; j += 64 * parts) tab[j] = *source(i, held + j);
+            if (a.parents) {
+                if (part > 0 || n == 0) continue;
+                // ancestors by doubling: after k steps `mask` holds 2^k of them and `u` is the one behind
+                int u = up[k];
+                if (u < -1 || u >= lane) {
+                    if (lane < n) atomicOr(a.err_flag, RS_FLAG_LENGTHS);
+                    u = -1;
+                }
+                uint64_t mask = 1ull << lane;
+#pragma unroll
+                for (int k2 = 0; k2 < 6; ++k2) {
+                    const uint64_t m = __shfl(mask, u & 63, 64);
+                    const int v = __shfl(u, u & 63, 64);
+                    if (u >= 0) mask |= m, u = v;
+                }
+                if (lane < n) {
+                    a.positions[row + lane] = len + __popcll(mask) - 1;
+                    a.slots[row + lane] = slot_of(id[k], len + lane);
+                    if (a.masks) a.masks[row + lane] = mask;
+                }
+            } else {
+                if (j0 < n) {
+                    a.positions[row + j0] = len + j0;
+                    a.slots[row + j0] = slot_of(id[k], len + j0);
+                }
+                for (int j = j0 + 64 * parts; j < n; j += 64 * parts) {
+                    a.positions[row + j] = len + j;
+                    a.slots[row + j] = slot_of(*source(i, (len + j) >> 4), len + j);
+                }
             }
         }
+    }
+    if (tid == 0) s_last = wgs == 1 || arrived == wgs - 1;
+    __syncthreads();
+    if (!s_last) return;
+    for (int b = tid; b < a.B; b += T) {
+        const int len = a.lens[b], held = a.held[b], n = a.n_new[b];
+        a.held_out[b] = bad || len == -1 ? held : max((int)(((int64_t)len + n + 15) >> 4), held);
+    }
+    if (tid == 0) {
+        *a.n_free_out = bad ? given : n_free - (int)tot_need;
+        *a.ticket = 0;
+        if (bad) atomicOr(a.err_flag, bad);
     }
 }
 
@@ -172,138 +200,210 @@ __device__ __forceinline__ void turn(const CosSin cs[8], bf16x8 &lo, bf16x8 &hi)
     }
 }
 
+typedef uint32_t u32x4_s __attribute__((ext_vector_type(4)));
+
+// Keys of n rows of a block (lane r: row r's slot) to their places: items (row, 8 pairs), a wave's two rounds of them asked for at once.
+template <int HD>
+__device__ __forceinline__ void turn_keys(const KvStoreArgs &a, const bf16_t *src, int first, int n, int my, int lane, bf16_t *kd) {
+    constexpr int C = HD / 16, ROUNDS = 16 * C / 64;
+    bf16x8 lo[ROUNDS], hi[ROUNDS];
+    CosSin cs[ROUNDS][8];
+    bool ok[ROUNDS];
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) {
+        const int it = 64 * k + lane, c = it % C, r = it / C;
+        ok[k] = false;
+        if (r < n) {
+            const bf16_t *p = src + (size_t)r * a.row_stride + 8 * c;
+            lo[k] = ld_bf16x8(p), hi[k] = ld_bf16x8(p + HD / 2);
+            ok[k] = angles(a, first + r, 8 * c, cs[k]);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < ROUNDS; ++k) {
+        const int it = 64 * k + lane, c = it % C, t = __shfl(my, it / C, 64) & 15;
+        if (!ok[k]) continue;
+        turn(cs[k], lo[k], hi[k]);
+        st_bf16x8(kd + kpool_chunk_offset(t, 8 * c), lo[k]);
+        st_bf16x8(kd + kpool_chunk_offset(t, HD / 2 + 8 * c), hi[k]);
+    }
+}
+
 template <int HD>
 __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int n_groups, int q_parts) {
     constexpr int C = HD / 16;   // 8-dim chunks of half a head
+    constexpr int BLK = 16 * HD, PL = HD / 8;   // PL: places of a lane's V
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int group = blockIdx.x % n_groups, part = blockIdx.x / n_groups;
     const int rows = a.n_rows ? min(max(*a.n_rows, 0), a.max_rows) : a.max_rows;
     const int row0 = 16 * group;
     if (row0 >= rows) return;
     if (part < q_parts) {
-        const int h0 = part * 8, h1 = min(a.Hq, h0 + 8);
-        for (int it = tid; it < 16 * C * 2; it += 256) {   // two threads a (row, chunk), every second head each
+        // a thread: 8 pairs of a row, in every second one of 8 heads
+        const int h0 = part * 8;
+        for (int it = tid; it < 16 * C * 2; it += 256) {
             const int c = it % C, row = row0 + it / C % 16, first = h0 + it / (16 * C);
-            CosSin cs[8];
             if (row >= rows) continue;
+            const bf16_t *p = a.qkv + (size_t)row * a.row_stride + 8 * c;
+            bf16x8 lo[4], hi[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)   // all asked for before one is written (queries in place are the thread's own)
+                if (first + 2 * k < a.Hq) lo[k] = ld_bf16x8(p + (first + 2 * k) * HD), hi[k] = ld_bf16x8(p + (first + 2 * k) * HD + HD / 2);
+            CosSin cs[8];
             if (!angles(a, row, 8 * c, cs)) {
                 atomicOr(a.err_flag, 1);
                 continue;
             }
             if (!a.q_out) continue;
-            for (int head = first; head < h1; head += 2) {
-                const bf16_t *p = a.qkv + (size_t)row * a.row_stride + head * HD + 8 * c;
-                bf16_t *q = a.q_out + (size_t)row * a.q_stride + head * HD + 8 * c;
-                bf16x8 lo = ld_bf16x8(p), hi = ld_bf16x8(p + HD / 2);
-                turn(cs, lo, hi);
-                st_bf16x8(q, lo);
-                st_bf16x8(q + HD / 2, hi);
-            }
+            bf16_t *q = a.q_out + (size_t)row * a.q_stride + 8 * c;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (first + 2 * k < a.Hq) {
+                    turn(cs, lo[k], hi[k]);
+                    st_bf16x8(q + (first + 2 * k) * HD, lo[k]);
+                    st_bf16x8(q + (first + 2 * k) * HD + HD / 2, hi[k]);
+                }
         }
         return;
     }
     const int kvh = (part - q_parts) * 4 + wave;
     if (kvh >= a.Hkv) return;
-    // lane l < 17: the block of row row0 - 1 + l (-1: not a row, or none)
-    auto slot_at = [&](int row) { return row >= 0 && row < rows ? a.slots[row] : -1; };
+    // lane l: the slot of row row0 - 1 + l and its block, -1: not a row, or none
     auto block_at = [&](int slot) { return slot < 0 || (slot >> 4) >= a.n_blocks ? -1 : slot >> 4; };
     const int r_l = row0 - 1 + lane;
-    const int sl = lane < 17 ? slot_at(r_l) : -1, bl = block_at(sl);
-    if (lane > 0 && lane < 17 && r_l < rows && bl < 0 && sl != -1) atomicOr(a.err_flag, 2);
+    const int sl = lane < 33 && r_l >= 0 && r_l < rows ? a.slots[r_l] : -1, bl = block_at(sl);
+    if (lane > 0 && lane < 17 && bl < 0 && sl != -1) atomicOr(a.err_flag, 2);
     const int prev = __shfl_up(bl, 1, 64);
     uint64_t starts = __ballot(lane > 0 && lane < 17 && bl >= 0 && bl != prev);
     while (starts) {
         const int l0 = __ffsll((unsigned long long)starts) - 1;
         starts &= starts - 1;
-        int first = row0 - 1 + l0;
         const int blk = __builtin_amdgcn_readlane(bl, l0);
+        int first = row0 - 1 + l0;
+        int my = __shfl(sl, (l0 + lane) & 63, 64);   // lane l < 16: the slot of row first + l
+        if (lane >= 16) my = -1;
         for (;;) {   // 16 rows at a time: a block has no more places, but slots may name one twice
-            const int my = lane < 16 ? slot_at(first + lane) : -1;
-            const uint64_t same = __ballot(lane < 16 && block_at(my) == blk);
+            const uint64_t same = __ballot(block_at(my) == blk);
             const int n = __ffsll((unsigned long long)~same) - 1;   // rows of this block from `first` on
             if (n == 0) break;
-            bf16_t *kd = a.k_pool + ((size_t)blk * a.Hkv + kvh) * 16 * HD, *vd = a.v_pool + ((size_t)blk * a.Hkv + kvh) * 16 * HD;
-            for (int i0 = 0; i0 < n * C; i0 += 64) {
-                const int it = i0 + lane, c = it % C, row = first + it / C, t = __shfl(my, it / C & 15, 64) & 15;
-                CosSin cs[8];
-                if (it >= n * C || !angles(a, row, 8 * c, cs)) continue;   // (a bad position is reported by the queries' workgroups)
-                const bf16_t *p = a.qkv + (size_t)row * a.row_stride + (size_t)(a.Hq + kvh) * HD + 8 * c;
-                bf16x8 lo = ld_bf16x8(p), hi = ld_bf16x8(p + HD / 2);
-                turn(cs, lo, hi);
-                st_bf16x8(kd + kpool_chunk_offset(t, 8 * c), lo);
-                st_bf16x8(kd + kpool_chunk_offset(t, HD / 2 + 8 * c), hi);
+            bf16_t *kd = a.k_pool + ((size_t)blk * a.Hkv + kvh) * BLK, *vd = a.v_pool + ((size_t)blk * a.Hkv + kvh) * BLK;
+            const bf16_t *src = a.qkv + (size_t)first * a.row_stride + (size_t)(a.Hq + kvh) * HD;
+            // whether the places are consecutive, and every position is in the table (a bad one is reported by the queries' workgroups)
+            bool fine = true;
+            if (lane < n) {
+                fine = (my & 15) == (__builtin_amdgcn_readfirstlane(my) & 15) + lane;
+                for (int x = 0; x < a.n_axes; ++x) fine = fine && (unsigned)a.positions[(size_t)x * a.max_rows + first + lane] < (unsigned)a.max_pos;
             }
-            for (int i0 = 0; i0 < n * HD; i0 += 64) {
-                const int it = i0 + lane, r = it % n, d = it / n, row = first + r, t = __shfl(my, r, 64) & 15;
-                bool ok = it < n * HD;
-                for (int x = 0; x < a.n_axes; ++x) ok = ok && (unsigned)a.positions[(size_t)x * a.max_rows + row] < (unsigned)a.max_pos;
-                if (ok) vd[d * 16 + t] = a.qkv[(size_t)row * a.row_stride + (size_t)(a.Hq + a.Hkv + kvh) * HD + d];
+            const bool plain = !__any(!fine);
+            const int t0 = __builtin_amdgcn_readfirstlane(my) & 15;
+            if (plain) {
+                // V: a lane two dims of all the rows; places t0 .. t0 + n - 1 of a dim are consecutive
+                const int dp = lane % (HD / 2), u0 = lane / (HD / 2) * 8;   // (head_dim 64: a half-wave eight places)
+                uint32_t w[PL];
+#pragma unroll
+                for (int u = 0; u < PL; ++u) {
+                    const int r = u0 + u - t0;
+                    w[u] = r >= 0 && r < n ? *(const uint32_t *)(src + (size_t)r * a.row_stride + a.Hkv * HD + 2 * dp) : 0u;
+                }
+                turn_keys<HD>(a, src, first, n, my, lane, kd);
+                uint32_t ev[PL / 2], od[PL / 2];
+#pragma unroll
+                for (int j = 0; j < PL / 2; ++j) {
+                    ev[j] = (w[2 * j] & 0xffffu) | (w[2 * j + 1] << 16);
+                    od[j] = (w[2 * j] >> 16) | (w[2 * j + 1] & 0xffff0000u);
+                }
+                bf16_t *dst = vd + 2 * dp * 16 + u0;
+                if (n == 16) {
+#pragma unroll
+                    for (int j = 0; j < PL / 8; ++j) {
+                        *(u32x4_s *)(dst + 8 * j) = u32x4_s{ev[4 * j], ev[4 * j + 1], ev[4 * j + 2], ev[4 * j + 3]};
+                        *(u32x4_s *)(dst + 16 + 8 * j) = u32x4_s{od[4 * j], od[4 * j + 1], od[4 * j + 2], od[4 * j + 3]};
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < PL / 2; ++j) {   // pairs of places; at the ends one alone, so that others are not touched
+                        const int lo = u0 + 2 * j - t0;
+                        const bool has_lo = lo >= 0 && lo < n, has_hi = lo + 1 >= 0 && lo + 1 < n;
+                        if (has_lo && has_hi) {
+                            *(uint32_t *)(dst + 2 * j) = ev[j];
+                            *(uint32_t *)(dst + 16 + 2 * j) = od[j];
+                        } else if (has_lo || has_hi) {
+                            const int at = 2 * j + (has_hi ? 1 : 0), shift = has_hi ? 16 : 0;
+                            *(uint16_t *)(dst + at) = (uint16_t)(ev[j] >> shift);
+                            *(uint16_t *)(dst + 16 + at) = (uint16_t)(od[j] >> shift);
+                        }
+                    }
+                }
+            } else {
+                turn_keys<HD>(a, src, first, n, my, lane, kd);
+                for (int i0 = 0; i0 < n * HD; i0 += 64) {
+                    const int it = i0 + lane, r = it % n, d = it / n, t = __shfl(my, r, 64) & 15;
+                    bool ok = it < n * HD;
+                    for (int x = 0; x < a.n_axes; ++x) ok = ok && (unsigned)a.positions[(size_t)x * a.max_rows + first + r] < (unsigned)a.max_pos;
+                    if (ok) vd[d * 16 + t] = src[(size_t)r * a.row_stride + a.Hkv * HD + d];
+                }
             }
             if (n < 16) break;
             first += 16;
+            my = lane < 16 && first + lane < rows ? a.slots[first + lane] : -1;
         }
     }
 }
 
 // ---------------------------------------------------------------------------------------------
-// Compact.  Token ctx + keep[i] of a request takes the place of token ctx + i, in every layer; keep ascends, so that a token moves to
-// a place before its own, and all that move are read before one is written.  A workgroup per (request, kv head, layer).
+// Compact.  Token ctx + keep[i] of a request takes the place of token ctx + i, in every layer.  keep ascends, so a token moves to a place
+// before its own and before those of all that come later: a wave takes a (request, layer, kv head) for itself, eight tokens at a time, and has
+// read all of them before it writes one.  Latency bound: lengths, indices, block ids, tokens.
 // ---------------------------------------------------------------------------------------------
 template <int HD>
 __global__ __launch_bounds__(256) void kv_compact_kernel(KvCompactArgs a) {
-    __shared__ bf16x8 s_k[64 * HD / 8];
-    __shared__ bf16_t s_v[64 * HD];
-    __shared__ int s_src[64], s_dst[64];   // 16 * block + place
-    __shared__ int s_bad;
-    const int tid = threadIdx.x, kvh = blockIdx.x, b = blockIdx.y, layer = blockIdx.z;
+    constexpr int N = 8, KR = N * HD / 8 / 64, VR = N * HD / 64;   // tokens at a time; 16-byte pieces and single elements of a lane
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, b = blockIdx.y, layer = blockIdx.z;
+    const int kvh = blockIdx.x * 4 + wave;
+    if (kvh >= a.Hkv) return;
     const int ctx = a.ctx_lens[b], n = a.keep_lens[b];
+    const int k = lane < a.keep_stride ? a.keep[(size_t)b * a.keep_stride + lane] : 0;
     if (ctx == -1 || n == 0) return;
-    if (tid == 0) s_bad = 0;
-    __syncthreads();
     if (ctx < 0 || n < 0 || n > a.keep_stride) {
-        if (tid == 0) atomicOr(a.err_flag, RS_FLAG_LENGTHS);
+        if (lane == 0) atomicOr(a.err_flag, RS_FLAG_LENGTHS);
         return;
     }
-    const int32_t *keep = a.keep + (size_t)b * a.keep_stride, *tab = a.tables + (size_t)b * a.max_blk;
-    if (tid < n) {
-        const int k = keep[tid], before = tid > 0 ? keep[tid - 1] : -1;
-        if (k <= before || k >= 64) atomicOr(&s_bad, RS_FLAG_LENGTHS);
-        else if ((int64_t)ctx + k >= 16ll * a.max_blk) atomicOr(&s_bad, 2);
-        else {
-            const int src = tab[(ctx + k) >> 4], dst = tab[(ctx + tid) >> 4];
-            if ((unsigned)src >= (unsigned)a.n_blocks || (unsigned)dst >= (unsigned)a.n_blocks) atomicOr(&s_bad, 2);
-            s_src[tid] = 16 * src + ((ctx + k) & 15);
-            s_dst[tid] = 16 * dst + ((ctx + tid) & 15);
+    const int32_t *tab = a.tables + (size_t)b * a.max_blk;
+    const int before = __shfl_up(k, 1, 64);
+    const bool mine = lane < n;
+    if (__any(mine && (k <= (lane > 0 ? before : -1) || k >= 64))) {
+        if (lane == 0) atomicOr(a.err_flag, RS_FLAG_LENGTHS);
+        return;
+    }
+    int src = -1, dst = -1;
+    if (mine && (int64_t)ctx + k < 16ll * a.max_blk) src = tab[(ctx + k) >> 4], dst = tab[(ctx + lane) >> 4];
+    if (__any(mine && ((unsigned)src >= (unsigned)a.n_blocks || (unsigned)dst >= (unsigned)a.n_blocks))) {
+        if (lane == 0) atomicOr(a.err_flag, 2);
+        return;
+    }
+    const int ps = (ctx + k) & 15, pd = (ctx + lane) & 15;
+    const int stay = __ffsll((unsigned long long)__ballot(mine && k != lane)) - 1;   // the first that moves
+    if (stay < 0) return;
+    bf16_t *kp = a.k_pool + layer * a.layer_stride + (size_t)kvh * 16 * HD, *vp = a.v_pool + layer * a.layer_stride + (size_t)kvh * 16 * HD;
+    const size_t blk = (size_t)a.Hkv * 16 * HD;
+    for (int i0 = stay; i0 < n; i0 += N) {
+        // item e of a lane: token i0 + e % N, so that neighbouring lanes have neighbouring places
+        const int i = min(i0 + lane % N, n - 1);
+        const bool there = i0 + lane % N < n;
+        const size_t s0 = __shfl(src, i, 64) * blk, d0 = __shfl(dst, i, 64) * blk;
+        const int s_at = __shfl(ps, i, 64), d_at = __shfl(pd, i, 64);
+        bf16x8 kk[KR];
+        bf16_t vv[VR];
+#pragma unroll
+        for (int e = 0; e < KR; ++e) kk[e] = ld_bf16x8(kp + s0 + kpool_chunk_offset(s_at, 8 * (8 * e + lane / N)));
+#pragma unroll
+        for (int e = 0; e < VR; ++e) vv[e] = vp[s0 + 16 * (8 * e + lane / N) + s_at];
+        if (there) {
+#pragma unroll
+            for (int e = 0; e < KR; ++e) st_bf16x8(kp + d0 + kpool_chunk_offset(d_at, 8 * (8 * e + lane / N)), kk[e]);
+#pragma unroll
+            for (int e = 0; e < VR; ++e) vp[d0 + 16 * (8 * e + lane / N) + d_at] = vv[e];
         }
-    }
-    __syncthreads();
-    if (s_bad) {
-        if (tid == 0) atomicOr(a.err_flag, s_bad);
-        return;
-    }
-    // the first tokens that stay where they are
-    int stay = 0;
-    while (stay < n && s_src[stay] == s_dst[stay]) ++stay;
-    const int m = n - stay;
-    if (m == 0) return;
-    bf16_t *kp = a.k_pool + layer * a.layer_stride, *vp = a.v_pool + layer * a.layer_stride;
-    auto head = [&](int slot) { return ((size_t)(slot >> 4) * a.Hkv + kvh) * 16 * HD; };
-    for (int it = tid; it < m * (HD / 8); it += 256) {
-        const int i = it % m, c = it / m, s = s_src[stay + i];
-        s_k[it] = ld_bf16x8(kp + head(s) + kpool_chunk_offset(s & 15, 8 * c));
-    }
-    for (int it = tid; it < m * HD; it += 256) {
-        const int i = it % m, d = it / m, s = s_src[stay + i];
-        s_v[it] = vp[head(s) + 16 * d + (s & 15)];
-    }
-    __syncthreads();
-    for (int it = tid; it < m * (HD / 8); it += 256) {
-        const int i = it % m, c = it / m, s = s_dst[stay + i];
-        st_bf16x8(kp + head(s) + kpool_chunk_offset(s & 15, 8 * c), s_k[it]);
-    }
-    for (int it = tid; it < m * HD; it += 256) {
-        const int i = it % m, d = it / m, s = s_dst[stay + i];
-        vp[head(s) + 16 * d + (s & 15)] = s_v[it];
     }
 }
 
@@ -311,9 +411,9 @@ __global__ __launch_bounds__(256) void kv_compact_kernel(KvCompactArgs a) {
 
 void launch_kv_plan(hipStream_t st, const KvPlanArgs &a) {
     const int x = (a.B + PLAN_REQS - 1) / PLAN_REQS;
-    // long runs: some 1024 rows for each workgroup
-    const int y = a.parents ? 1 : std::max(1, std::min((a.max_rows / x + 1023) / 1024, 256));
-    hipLaunchKernelGGL(kv_plan_kernel, dim3(x, y), dim3(256), 0, st, a);
+    // long runs: some 4096 rows for each workgroup
+    const int y = a.parents ? 1 : std::max(1, std::min((a.max_rows / x + 4095) / 4096, 64));
+    hipLaunchKernelGGL(kv_plan_kernel, dim3(x, y), dim3(64 * PLAN_WAVES), 0, st, a);
 }
 
 void launch_kv_store(hipStream_t st, const KvStoreArgs &a) {
@@ -324,7 +424,7 @@ void launch_kv_store(hipStream_t st, const KvStoreArgs &a) {
 }
 
 void launch_kv_compact(hipStream_t st, const KvCompactArgs &a) {
-    const dim3 grid(a.Hkv, a.B, a.n_layers);
+    const dim3 grid((a.Hkv + 3) / 4, a.B, a.n_layers);
     if (a.hd == 128) hipLaunchKernelGGL(kv_compact_kernel<128>, grid, dim3(256), 0, st, a);
     else hipLaunchKernelGGL(kv_compact_kernel<64>, grid, dim3(256), 0, st, a);
 }
