@@ -133,6 +133,7 @@ void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &a);
 #define RS_FLAG_LENGTHS 32     // row counts, lengths or parents that contradict each other
 #define MASKED_COLS 128        // columns, (row, query head of a kv head), of a unit
 #define MASKED_PIECES 256      // most pieces of units whose keys are cut, in a launch
+#define MASKED_MAX_CUT 8       // and most of one unit
 struct MaskedAttnArgs {
     const bf16_t *q;          // rows of Hq * hd, q_stride elements apart
     size_t q_stride;
@@ -141,7 +142,7 @@ struct MaskedAttnArgs {
     const bf16_t *k_pool, *v_pool;   // this layer
     const int32_t *tables;
     int32_t *err_flag;
-    float *part_o, *part_ml;  // pieces of cut units: [MASKED_PIECES][MASKED_COLS][hd], and [..][2] maximum and sum
+    float *part_o, *part_ml;  // pieces of cut units: [pieces][columns][hd], at most MASKED_PIECES * MASKED_COLS columns, and [..][2] maximum and sum
     int Hq, Hkv, hd, max_blk, n_blocks;
     float scale_log2;         // log2(e) / sqrt(hd)
     int window = 0, sinks = 0;
@@ -154,8 +155,13 @@ struct MaskedAttnArgs {
     const uint64_t *masks = nullptr;
     int max_rows = 0, max_draft = 0;
     SeqInfo seq{};            // else prompts: request r's rows are its tokens start[r] ..
-    int n_units = 0, units_per_req = 0, cut = 1;   // set by the launcher
+    int32_t *tickets = nullptr;   // [MASKED_PIECES], 0 between launches
+    int unit_rows = 0, n_units = 0, units_per_req = 0, cut = 1;   // set by masked_form
 };
+// Units of up to 32 columns by four or eight waves; of up to 128 by four waves, or two teams of four.
+enum MaskedKind { MASKED_FEW4, MASKED_FEW8, MASKED_WIDE, MASKED_TEAMS };
+struct MaskedForm { MaskedKind kind; };
+MaskedForm masked_form(MaskedAttnArgs &a);
 void launch_masked_attention(hipStream_t st, const MaskedAttnArgs &a);
 void masked_attention_init();
 

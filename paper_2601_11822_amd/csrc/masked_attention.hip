@@ -19,8 +19,6 @@ namespace {
 
 __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
-constexpr int COLS = MASKED_COLS;
-
 // What a unit's rows see.
 struct Span {
     int row0 = 0, rows = 0;      // rows of q and out
@@ -34,7 +32,7 @@ struct Span {
 template <bool TREE>
 __device__ __forceinline__ Span unit_span(const MaskedAttnArgs &a, int u) {
     Span s;
-    const int G = a.Hq / a.Hkv, per = COLS / G;
+    const int per = a.unit_rows;
     int end;   // keys before this position
     if (TREE) {
         s.req = u / a.units_per_req;
@@ -91,7 +89,7 @@ struct Sight {
     int lo, hi, sinks;       // window: keys lo .. hi and those below sinks (of them none above hi)
     int ctx;                 // tree: keys below, and the bits of
     uint64_t bits;
-    // the 16 keys from pos on, a bit each.  (Without branches: of a chain of conditions on 16 score registers the compiler, clang 22 of ROCm 7.2,
+    // The 16 keys from pos on, a bit each.  (Without branches: of a chain of conditions on 16 score registers the compiler, clang 22 of ROCm 7.2,
     // made control flow that lost the first register's.)
     template <bool TREE>
     __device__ __forceinline__ uint32_t sees16(int pos) const {
@@ -120,15 +118,90 @@ __device__ __forceinline__ Sight row_sight(const MaskedAttnArgs &a, const Span &
     return v;
 }
 
+// Weights of a block: the half-waves (same column) hold tokens 4h..4h+3 and 8+4h..8+4h+3 and trade their middle pieces; h = 0 then has tokens
+// 0-7, h = 1 tokens 8-15, the contraction slices of V's own layout.
+__device__ __forceinline__ bf16x8 by_tokens(bf16x8 p) {
+    typedef uint32_t u32x4p __attribute__((ext_vector_type(4)));
+    u32x4p w = __builtin_bit_cast(u32x4p, p);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const auto sw = __builtin_amdgcn_permlane32_swap(w[u], w[u + 2], false, false);
+        w[u] = sw[0];
+        w[u + 2] = sw[1];
+    }
+    return __builtin_bit_cast(bf16x8, w);
+}
+
 __device__ __forceinline__ bf16_t *out_at(const MaskedAttnArgs &a, const Span &s, int col, int hk, int G) {
     return a.out + (size_t)(s.row0 + col / G) * a.out_stride + (size_t)(hk * G + col % G) * a.hd;
+}
+
+// Pieces of a unit's keys leave their sums in part_o [piece][column][hd] and part_ml (maximum of raw scores, sum); the last workgroup of a
+// (unit, kv head) to arrive brings them together, in the pieces' order, so that results do not depend on which one that is.  The sums
+// are written and read as relaxed atomics of the device's scope, which pass the XCDs' own L2 caches by; a workgroup's have arrived when
+// its waves have waited for them, in front of the ticket.  (A fence at that scope writes back and invalidates whole caches instead.)
+__device__ __forceinline__ void put_far(float *p, float x, float y) {
+    const uint64_t v = (uint64_t)__builtin_bit_cast(uint32_t, y) << 32 | __builtin_bit_cast(uint32_t, x);
+    __hip_atomic_store((uint64_t *)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 get_far(const float *p) {
+    const uint64_t v = __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return float2{__builtin_bit_cast(float, (uint32_t)v), __builtin_bit_cast(float, (uint32_t)(v >> 32))};
+}
+struct Piece {
+    size_t base;   // of the unit's first piece, in columns
+    int piece, cols;   // columns of a piece's place
+    __device__ __forceinline__ size_t at(int p, int col) const { return base + (size_t)p * cols + col; }
+};
+
+template <int HD>
+__device__ __forceinline__ void join_pieces(const MaskedAttnArgs &a, const Span &s, int hk, int unit, const Piece &pc, int threads) {
+    __shared__ int last;
+    const int G = a.Hq / a.Hkv, cols = s.rows * G;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's sums have arrived
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        int32_t *ticket = a.tickets + unit * a.Hkv + hk;
+        last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.cut - 1;
+        if (last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!last) return;
+    for (int item = threadIdx.x; item < cols * (HD / 4); item += threads) {
+        const int col = item / (HD / 4), d = item % (HD / 4) * 4;
+        float top = NEG_INF, l = 0.f;
+        float2 ml[MASKED_MAX_CUT], x[MASKED_MAX_CUT], y[MASKED_MAX_CUT];
+#pragma unroll
+        for (int i = 0; i < MASKED_MAX_CUT; ++i) {   // everything asked for at once
+            const size_t at = pc.at(min(i, a.cut - 1), col);
+            ml[i] = get_far(a.part_ml + 2 * at);
+            x[i] = get_far(a.part_o + at * HD + d);
+            y[i] = get_far(a.part_o + at * HD + d + 2);
+        }
+#pragma unroll
+        for (int i = 0; i < MASKED_MAX_CUT; ++i)
+            if (i < a.cut) top = fmaxf(top, ml[i].x);
+        const float ref = top == NEG_INF ? 0.f : top;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < MASKED_MAX_CUT; ++i) {
+            if (i >= a.cut || ml[i].y == 0.f) continue;   // (a sum of nothing: a piece none of whose keys the row sees)
+            const float e = exp2f((ml[i].x - ref) * a.scale_log2);
+            l += ml[i].y * e;
+            acc += f32x4{x[i].x, x[i].y, y[i].x, y[i].y} * e;
+        }
+        bf16x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(l == 0.f ? 0.f : acc[i] / l);
+        *(bf16x4 *)(out_at(a, s, col, hk, G) + d) = v;
+    }
 }
 
 // The same sums one key after the other in float32, without the matrix unit: for units whose result is not finite.  There a weight
 // of zero times a value that is infinite or NaN may have reached rows that do not see that value; here it cannot.  Slow (some ms for
 // 4096 keys), and only taken where a cache holds such values.
 template <int HD, bool TREE>
-__device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span &s, int hk, int b0, int b1, size_t slot, int threads) {
+__device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span &s, int hk, int b0, int b1, const Piece &pc, int threads) {
     constexpr int D = 32;   // dims of a thread
     const int G = a.Hq / a.Hkv, parts = HD / D;
     const int32_t *tab = a.tables + (size_t)s.req * a.max_blk;
@@ -160,8 +233,9 @@ __device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span
             }
         }
         if (a.cut > 1) {
-            for (int i = 0; i < D; ++i) a.part_o[(slot * COLS + col) * HD + d0 + i] = o[i];
-            if (d0 == 0) a.part_ml[2 * (slot * COLS + col)] = m, a.part_ml[2 * (slot * COLS + col) + 1] = l;
+            const size_t at = pc.at(pc.piece, col);
+            for (int i = 0; i < D; i += 2) put_far(a.part_o + at * HD + d0 + i, o[i], o[i + 1]);
+            if (d0 == 0) put_far(a.part_ml + 2 * at, m, l);
         } else {
             bf16_t *p = out_at(a, s, col, hk, G) + d0;
             for (int i = 0; i < D; ++i) p[i] = (bf16_t)(l == 0.f ? 0.f : o[i] / l);
@@ -183,7 +257,7 @@ __global__ __launch_bounds__(256 * KW, 2) void masked_attn_kernel(MaskedAttnArgs
     const int hk = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, piece = rest % a.cut, unit = rest / a.cut;
     const Span s = unit_span<TREE>(a, unit);
     if (s.rows <= 0) return;
-    const size_t slot = (size_t)rest * a.Hkv + hk;
+    const Piece pc{((size_t)unit * a.Hkv + hk) * a.cut * MASKED_COLS, piece, MASKED_COLS};
     const int cols = s.rows * G;
     if (s.dead) {
         if (piece == 0)
@@ -325,17 +399,7 @@ __global__ __launch_bounds__(256 * KW, 2) void masked_attn_kernel(MaskedAttnArgs
                     l_run += p;
                     pf[i] = (bf16_t)p;
                 }
-                // The half-waves (same column) hold a block's tokens 4h..4h+3 and 8+4h..8+4h+3 and trade their middle pieces:
-                // h = 0 then has tokens 0-7, h = 1 tokens 8-15, the contraction slices of V's own layout.
-                typedef uint32_t u32x4p __attribute__((ext_vector_type(4)));
-                u32x4p pr4 = __builtin_bit_cast(u32x4p, pf);
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const auto sw = __builtin_amdgcn_permlane32_swap(pr4[u], pr4[u + 2], false, false);
-                    pr4[u] = sw[0];
-                    pr4[u + 2] = sw[1];
-                }
-                pf = __builtin_bit_cast(bf16x8, pr4);
+                pf = by_tokens(pf);
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32(*(const bf16x8 *)&vs[vlds(blk4, h, 32 * dt + c32)], pf, o[dt]);
             }
@@ -352,7 +416,8 @@ __global__ __launch_bounds__(256 * KW, 2) void masked_attn_kernel(MaskedAttnArgs
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = odd || !(fabsf(o[dt][i]) < __builtin_huge_valf());
     if (__syncthreads_or(odd && col < cols)) {
-        careful_unit<HD, TREE>(a, s, hk, 4 * t0, min(4 * t1, s.blocks), slot, 256 * KW);
+        careful_unit<HD, TREE>(a, s, hk, 4 * t0, min(4 * t1, s.blocks), pc, 256 * KW);
+        if (a.cut > 1) join_pieces<HD>(a, s, hk, unit, pc, 256 * KW);
         return;
     }
 
@@ -389,17 +454,20 @@ __global__ __launch_bounds__(256 * KW, 2) void masked_attn_kernel(MaskedAttnArgs
                 for (int i = 0; i < 4; ++i) o[dt][4 * j + i] = (team == 0 ? o[dt][4 * j + i] : o[DT / 2 + dt][4 * j + i]) * e + v[i] * e_o;
             }
     }
-    if (col >= cols) return;
     const int d0 = team * (HD / KW) + 4 * h;   // this lane's dims: d0 + 32 dt + 8 j + i
     if (a.cut > 1) {
-        float *po = a.part_o + (slot * COLS + col) * HD;
+        const size_t at = pc.at(piece, col);
+        if (col < cols) {
 #pragma unroll
-        for (int dt = 0; dt < DT / KW; ++dt)
+            for (int dt = 0; dt < DT / KW; ++dt)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) *(f32x4 *)(po + d0 + 32 * dt + 8 * j) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
-        if (h == 0 && team == 0) *(float2 *)(a.part_ml + 2 * (slot * COLS + col)) = float2{m_run, l_run};
+                for (int j = 0; j < 8; ++j) put_far(a.part_o + at * HD + d0 + 32 * dt + 8 * (j >> 1) + 2 * (j & 1), o[dt][2 * j], o[dt][2 * j + 1]);
+            if (h == 0 && team == 0) put_far(a.part_ml + 2 * at, m_run, l_run);
+        }
+        join_pieces<HD>(a, s, hk, unit, pc, 256 * KW);
         return;
     }
+    if (col >= cols) return;
     const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
     bf16_t *p = out_at(a, s, col, hk, G);
 #pragma unroll
@@ -413,53 +481,217 @@ __global__ __launch_bounds__(256 * KW, 2) void masked_attn_kernel(MaskedAttnArgs
         }
 }
 
-// Brings the pieces of a unit's columns together: a thread per (column, four dims).
-template <int HD, bool TREE>
-__global__ __launch_bounds__(256) void masked_join_kernel(MaskedAttnArgs a) {
-    const int G = a.Hq / a.Hkv, hk = blockIdx.x % a.Hkv, unit = blockIdx.x / a.Hkv;
+// Units of up to 32 columns (decode rows, small trees): bound by reading the cache, so nothing is shared and nothing staged.  The waves take
+// tiles of 32 keys (two blocks) in turn, straight from the pools into the operands of 32x32x16 products (every load of a wave is a contiguous
+// kilobyte, or four pieces of 256 bytes); a tile's keys are asked for as soon as the products with the ones before have been issued, and so are
+// its values.  The waves' sums meet in LDS at the end.
+template <int HD, int NW, bool TREE>
+__global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a) {
+    constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD, PAD = HD + 4;
+    extern __shared__ __attribute__((aligned(16))) float smem_few[];   // [NW][32][PAD], [NW][32][2]
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c32 = lane & 31, h = lane >> 5;
+    const int G = a.Hq / a.Hkv;
+    const int hk = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, piece = rest % a.cut, unit = rest / a.cut;
     const Span s = unit_span<TREE>(a, unit);
-    const int item = blockIdx.y * 256 + threadIdx.x, col = item / (HD / 4), d = item % (HD / 4) * 4;
-    if (s.rows <= 0 || s.dead || col >= s.rows * G) return;
-    auto at = [&](int piece) { return ((((size_t)unit * a.cut + piece) * a.Hkv + hk) * COLS + col); };
-    float top = NEG_INF, l = 0.f;
-    for (int i = 0; i < a.cut; ++i) top = fmaxf(top, a.part_ml[2 * at(i)]);
-    const float ref = top == NEG_INF ? 0.f : top;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < a.cut; ++i) {
-        const float2 ml = *(const float2 *)(a.part_ml + 2 * at(i));
-        if (ml.y == 0.f) continue;   // a piece none of whose keys the row sees
-        const float e = exp2f((ml.x - ref) * a.scale_log2);
-        l += ml.y * e;
-        acc += *(const f32x4 *)(a.part_o + at(i) * HD + d) * e;
+    if (s.rows <= 0) return;
+    const Piece pc{((size_t)unit * a.Hkv + hk) * a.cut * 32, piece, 32};
+    const int cols = s.rows * G;
+    if (s.dead) {
+        if (piece == 0)
+            for (int i = threadIdx.x; i < cols * HD; i += 64 * NW) out_at(a, s, i / HD, hk, G)[i % HD] = (bf16_t)0.f;
+        return;
     }
-    bf16x4 v;
+    const int n_tiles = (s.blocks + 1) >> 1;
+    const int t0 = (int)((int64_t)n_tiles * piece / a.cut), t1 = (int)((int64_t)n_tiles * (piece + 1) / a.cut);
+    const int32_t *tab = a.tables + (size_t)s.req * a.max_blk;
+    const float sc = a.scale_log2;
+    const int col = c32, row = min(col, cols - 1) / G;
+    const int w_last = s.first + s.rows - 1;   // position of the unit's last row (windows)
+
+    // lane l: the id of block l & 1 of a tile; -1: none, or not one of the pool
+    auto fetch_ids = [&](int t) {
+        const int j = 2 * t + (lane & 1);
+        return t < t1 && j < s.blocks ? tab[j < s.sink_blocks ? j : j + s.skip] : -1;
+    };
+    auto checked = [&](int t, int id) {
+        if ((unsigned)id < (unsigned)a.n_blocks) return id;
+        if (lane < 2 && t < t1 && 2 * t + lane < s.blocks) atomicOr(a.err_flag, 2);
+        return -1;
+    };
+    bf16x8 kf[KS], vf[2][DT];
+    auto head_of = [&](int id) { return ((size_t)max(id, 0) * a.Hkv + hk) * BLK; };   // (a block that is missing: block 0, masked)
+    auto load_k = [&](int ids) {
+        const size_t h0 = head_of(__builtin_amdgcn_readlane(ids, 0)), h1 = head_of(__builtin_amdgcn_readlane(ids, 1));
+        const bf16_t *p = a.k_pool + (c32 < 16 ? h0 : h1) + kpool_chunk_offset(c32 & 15, 8 * h);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(l == 0.f ? 0.f : acc[i] / l);
-    *(bf16x4 *)(out_at(a, s, col, hk, G) + d) = v;
+        for (int i = 0; i < KS; ++i) kf[i] = ld_bf16x8_stream(p + (i >> 1) * 512 + (i & 1) * 256);
+    };
+    auto load_v = [&](int ids) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const bf16_t *p = a.v_pool + head_of(__builtin_amdgcn_readlane(ids, b)) + c32 * 16 + 8 * h;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) vf[b][dt] = ld_bf16x8_stream(p + dt * 512);
+        }
+    };
+    int t = t0 + wave;
+    int ids = checked(t, fetch_ids(t));
+    const bool any = t < t1;
+    if (any) load_k(ids), load_v(ids);
+    int next = fetch_ids(t + NW);
+    const Sight see = row_sight<TREE>(a, s, row);
+    bf16x8 qf[KS];
+    {
+        const bf16_t *qp = a.q + (size_t)(s.row0 + row) * a.q_stride + (size_t)(hk * G + min(col, cols - 1) % G) * HD + 8 * h;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) qf[i] = ld_bf16x8(qp + 16 * i);
+    }
+    float m_run = NEG_INF, l_run = 0.f;   // running maximum of raw scores, running sum
+    f32x16 o[DT];
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+
+    for (; t < t1; t += NW) {
+        f32x16 st;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < KS; ++i) st = mfma32(kf[i], qf[i], st);
+        // the next tile, or behind the last one this one again (from the caches)
+        const bool more = t + NW < t1;
+        const int nids = more ? checked(t + NW, next) : ids;
+        next = fetch_ids(t + 2 * NW);
+        load_k(nids);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            const int e = 2 * t + b, p = 16 * (e < s.sink_blocks ? e : e + s.skip);
+            const bool there = __builtin_amdgcn_readlane(ids, b) >= 0;
+            const bool full = there && (TREE ? p + 15 < s.first : p + 15 <= s.first && (p > w_last - a.window || p + 15 < a.sinks));
+            if (!full) {   // uniform
+                const uint32_t seen = there ? see.sees16<TREE>(p) >> (4 * h) : 0u;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float x = st[8 * b + i];
+                    st[8 * b + i] = seen & (1u << ((i >> 2) * 8 + (i & 3))) ? x : NEG_INF;
+                }
+            }
+        }
+        float m_tile = NEG_INF;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) m_tile = fmaxf(m_tile, st[i]);
+        m_tile = fmaxf(m_tile, __shfl_xor(m_tile, 32, 64));
+        const float m_new = fmaxf(m_run, m_tile);
+        const float m_safe = m_new == NEG_INF ? 0.f : m_new;
+        if (__any(m_new != m_run)) {
+            const float alpha = __builtin_amdgcn_exp2f((m_run - m_safe) * sc);
+            l_run *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[dt] = o[dt] * alpha;
+            m_run = m_new;
+        }
+        const float ms = m_safe * sc;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+            bf16x8 pf;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(st[8 * b + i], sc, -ms));
+                l_run += p;
+                pf[i] = (bf16_t)p;
+            }
+            pf = by_tokens(pf);
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32(vf[b][dt], pf, o[dt]);
+        }
+        load_v(nids);
+        __builtin_amdgcn_sched_barrier(0);
+        ids = nids;
+    }
+    l_run += __shfl_xor(l_run, 32, 64);
+
+    bool odd = false;
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) odd = odd || !(fabsf(o[dt][i]) < __builtin_huge_valf());
+    float *s_o = smem_few, *s_ml = smem_few + NW * 32 * PAD;
+    if (col < cols) {
+        float *p = s_o + (wave * 32 + col) * PAD + 4 * h;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *(f32x4 *)(p + 32 * dt + 8 * j) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
+        if (h == 0) {
+            s_ml[(wave * 32 + col) * 2] = m_run;
+            s_ml[(wave * 32 + col) * 2 + 1] = l_run;
+        }
+    }
+    if (__syncthreads_or(odd && col < cols)) {
+        careful_unit<HD, TREE>(a, s, hk, 2 * t0, min(2 * t1, s.blocks), pc, 64 * NW);
+        if (a.cut > 1) join_pieces<HD>(a, s, hk, unit, pc, 64 * NW);
+        return;
+    }
+    for (int item = threadIdx.x; item < cols * (HD / 4); item += 64 * NW) {
+        const int c = item / (HD / 4), d = item % (HD / 4) * 4;
+        float top = NEG_INF, l = 0.f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) top = fmaxf(top, s_ml[(w * 32 + c) * 2]);
+        const float ref = top == NEG_INF ? 0.f : top;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            const float e = __builtin_amdgcn_exp2f((s_ml[(w * 32 + c) * 2] - ref) * sc);
+            l += s_ml[(w * 32 + c) * 2 + 1] * e;
+            acc += *(const f32x4 *)(s_o + (w * 32 + c) * PAD + d) * e;
+        }
+        if (a.cut > 1) {
+            const size_t at = pc.at(piece, c);
+            put_far(a.part_o + at * HD + d, acc[0], acc[1]);
+            put_far(a.part_o + at * HD + d + 2, acc[2], acc[3]);
+            if (d == 0) put_far(a.part_ml + 2 * at, top, l);
+            continue;
+        }
+        const float inv = l > 0.f ? 1.0f / l : 0.f;
+        bf16x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(acc[i] * inv);
+        *(bf16x4 *)(out_at(a, s, c, hk, G) + d) = v;
+    }
+    if (a.cut > 1) join_pieces<HD>(a, s, hk, unit, pc, 64 * NW);
 }
 
 constexpr int masked_lds(int hd, int kw) { return kw * 4 * 64 * hd * 2 + kw * 4 * 64 * 4; }
 
+constexpr int few_lds(int hd, int nw) { return nw * 32 * (hd + 4 + 2) * 4; }
+
 template <int HD, bool TREE>
-void launch(hipStream_t st, const MaskedAttnArgs &a, bool teams) {
+void launch(hipStream_t st, const MaskedAttnArgs &a, const MaskedForm &f) {
     const dim3 grid(a.n_units * a.cut * a.Hkv);
-    if (teams) hipLaunchKernelGGL((masked_attn_kernel<HD, 2, TREE>), grid, dim3(512), masked_lds(HD, 2), st, a);
-    else hipLaunchKernelGGL((masked_attn_kernel<HD, 1, TREE>), grid, dim3(256), masked_lds(HD, 1), st, a);
-    if (a.cut > 1) {
-        const int rows = TREE ? std::min(a.max_draft, COLS / (a.Hq / a.Hkv)) : a.ctx_lens ? 1 : COLS / (a.Hq / a.Hkv);
-        hipLaunchKernelGGL((masked_join_kernel<HD, TREE>), dim3(a.n_units * a.Hkv, (rows * (a.Hq / a.Hkv) * HD / 4 + 255) / 256), dim3(256), 0, st, a);
+    switch (f.kind) {
+        case MASKED_FEW4: hipLaunchKernelGGL((masked_few_kernel<HD, 4, TREE>), grid, dim3(256), few_lds(HD, 4), st, a); break;
+        case MASKED_FEW8: hipLaunchKernelGGL((masked_few_kernel<HD, 8, TREE>), grid, dim3(512), few_lds(HD, 8), st, a); break;
+        case MASKED_WIDE: hipLaunchKernelGGL((masked_attn_kernel<HD, 1, TREE>), grid, dim3(256), masked_lds(HD, 1), st, a); break;
+        case MASKED_TEAMS: hipLaunchKernelGGL((masked_attn_kernel<HD, 2, TREE>), grid, dim3(512), masked_lds(HD, 2), st, a); break;
     }
 }
 
 }  // namespace
 
-void launch_masked_attention(hipStream_t st, const MaskedAttnArgs &args) {
-    MaskedAttnArgs a = args;
-    const int per = COLS / (a.Hq / a.Hkv);
+MaskedForm masked_form(MaskedAttnArgs &a) {
+    const int G = a.Hq / a.Hkv;
     const bool tree = a.cu_rows != nullptr;
+    int most = 1;   // rows of a request
+    if (tree) most = a.max_draft;
+    else if (!a.ctx_lens)
+        for (int r = 0; r < a.seq.n_req; ++r) most = std::max(most, a.seq.cu[r + 1] - a.seq.cu[r]);
+    const bool few = most * G <= 32;
+    a.unit_rows = (few ? 32 : MASKED_COLS) / G;
     int keys = 0;   // most keys of a unit
     if (tree) {
-        a.units_per_req = (a.max_draft + per - 1) / per;
+        a.units_per_req = (a.max_draft + a.unit_rows - 1) / a.unit_rows;
         a.n_units = a.B * a.units_per_req;
         keys = a.max_ctx;
     } else if (a.ctx_lens) {
@@ -468,21 +700,36 @@ void launch_masked_attention(hipStream_t st, const MaskedAttnArgs &args) {
     } else {
         a.n_units = 0;
         for (int r = 0; r < a.seq.n_req; ++r) {
-            a.n_units += (a.seq.cu[r + 1] - a.seq.cu[r] + per - 1) / per;
+            a.n_units += (a.seq.cu[r + 1] - a.seq.cu[r] + a.unit_rows - 1) / a.unit_rows;
             keys = std::max(keys, a.seq.start[r] + a.seq.cu[r + 1] - a.seq.cu[r]);
         }
     }
-    if (a.n_units <= 0) return;
-    if (!tree) keys = (int)std::min<int64_t>(keys, (int64_t)a.window + a.sinks + per + 32);
-    const int wgs = a.n_units * a.Hkv, tiles = (keys + 63) / 64;
-    const bool teams = wgs <= 256;
-    a.cut = std::max(1, std::min({256 / wgs, MASKED_PIECES / wgs, (tiles + 7) / 8}));
-    if (a.hd == 128) {
-        if (tree) launch<128, true>(st, a, teams);
-        else launch<128, false>(st, a, teams);
+    if (!tree) keys = (int)std::min<int64_t>(keys, (int64_t)a.window + a.sinks + a.unit_rows + 32);
+    const int64_t wgs = (int64_t)a.n_units * a.Hkv;
+    MaskedForm f{};
+    if (wgs <= 0) return f;
+    const int tiles = (keys + 63) / 64;
+    if (few) {
+        f.kind = wgs <= 256 ? MASKED_FEW8 : MASKED_FEW4;
+        a.cut = (int)std::max<int64_t>(1, std::min<int64_t>({256 / wgs, MASKED_MAX_CUT, (tiles + 3) / 4}));
     } else {
-        if (tree) launch<64, true>(st, a, teams);
-        else launch<64, false>(st, a, teams);
+        f.kind = wgs <= 256 ? MASKED_TEAMS : MASKED_WIDE;
+        a.cut = (int)std::max<int64_t>(1, std::min<int64_t>({256 / wgs, MASKED_MAX_CUT, (tiles + 7) / 8}));
+    }
+    return f;
+}
+
+void launch_masked_attention(hipStream_t st, const MaskedAttnArgs &args) {
+    MaskedAttnArgs a = args;
+    const MaskedForm f = masked_form(a);
+    if (a.n_units <= 0) return;
+    const bool tree = a.cu_rows != nullptr;
+    if (a.hd == 128) {
+        if (tree) launch<128, true>(st, a, f);
+        else launch<128, false>(st, a, f);
+    } else {
+        if (tree) launch<64, true>(st, a, f);
+        else launch<64, false>(st, a, f);
     }
 }
 
@@ -494,4 +741,10 @@ void masked_attention_init() {
     set((const void *)masked_attn_kernel<128, 2, true>, masked_lds(128, 2));
     set((const void *)masked_attn_kernel<64, 2, false>, masked_lds(64, 2));
     set((const void *)masked_attn_kernel<64, 2, true>, masked_lds(64, 2));
+    set((const void *)masked_few_kernel<128, 4, false>, few_lds(128, 4));
+    set((const void *)masked_few_kernel<128, 4, true>, few_lds(128, 4));
+    set((const void *)masked_few_kernel<128, 8, false>, few_lds(128, 8));
+    set((const void *)masked_few_kernel<128, 8, true>, few_lds(128, 8));
+    set((const void *)masked_few_kernel<64, 8, false>, few_lds(64, 8));
+    set((const void *)masked_few_kernel<64, 8, true>, few_lds(64, 8));
 }

@@ -176,7 +176,7 @@ struct rs_ctx {
     int32_t *kv4_part_row[2] = {nullptr, nullptr};
     // scratch of windowed and tree attention whose keys are cut, and the ticket of plans, per side
     float *mask_part_o[2] = {nullptr, nullptr}, *mask_part_ml[2] = {nullptr, nullptr};
-    int32_t *plan_ticket = nullptr;
+    int32_t *plan_ticket = nullptr, *mask_tickets[2] = {nullptr, nullptr};
     CosSin *rope = nullptr;
     // One error word per side (kernels OR bits into it: 1 position outside the rotary table, 2 block id outside
     // the pool, 4 token outside the vocabulary, 8 context length outside [1, max_ctx], 16 a plan found too few free blocks,
@@ -1169,6 +1169,8 @@ int32_t alloc_masked(rs_ctx *c) {
         const size_t n = (size_t)MASKED_PIECES * MASKED_COLS;
         HIP_TRY(hipMalloc(&c->mask_part_o[s], n * c->m.head_dim * sizeof(float)));
         HIP_TRY(hipMalloc(&c->mask_part_ml[s], n * 2 * sizeof(float)));
+        HIP_TRY(hipMalloc(&c->mask_tickets[s], MASKED_PIECES * sizeof(int32_t)));
+        HIP_TRY(hipMemset(c->mask_tickets[s], 0, MASKED_PIECES * sizeof(int32_t)));
     }
     HIP_TRY(hipMalloc(&c->plan_ticket, 2 * sizeof(int32_t)));
     HIP_TRY(hipMemset(c->plan_ticket, 0, 2 * sizeof(int32_t)));
@@ -1216,6 +1218,7 @@ MaskedAttnArgs masked_args(rs_ctx *c, int side, int32_t layer, const void *q, in
     a.err_flag = c->err_flag + side;
     a.part_o = c->mask_part_o[side];
     a.part_ml = c->mask_part_ml[side];
+    a.tickets = c->mask_tickets[side];
     a.Hq = c->m.n_q_heads;
     a.Hkv = c->m.n_kv_heads;
     a.hd = c->m.head_dim;
@@ -1441,6 +1444,7 @@ int32_t rs_destroy(rs_ctx *c) {
             if (c->kv4_part_row[s]) (void)hipFree(c->kv4_part_row[s]);
             if (c->mask_part_o[s]) (void)hipFree(c->mask_part_o[s]);
             if (c->mask_part_ml[s]) (void)hipFree(c->mask_part_ml[s]);
+            if (c->mask_tickets[s]) (void)hipFree(c->mask_tickets[s]);
         }
         for (auto &kv : c->graphs) (void)hipGraphExecDestroy(kv.second);
         drop_step_graphs(c);
