@@ -133,7 +133,7 @@ void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &a);
 #define RS_FLAG_LENGTHS 32     // row counts, lengths or parents that contradict each other
 #define MASKED_COLS 128        // columns, (row, query head of a kv head), of a unit
 #define MASKED_PIECES 256      // most pieces of units whose keys are cut, in a launch
-#define MASKED_MAX_CUT 8       // and most of one unit
+#define MASKED_MAX_CUT 32      // and most of one unit
 struct MaskedAttnArgs {
     const bf16_t *q;          // rows of Hq * hd, q_stride elements apart
     size_t q_stride;
@@ -158,7 +158,7 @@ struct MaskedAttnArgs {
     int32_t *tickets = nullptr;   // [MASKED_PIECES], 0 between launches
     int unit_rows = 0, n_units = 0, units_per_req = 0, cut = 1;   // set by masked_form
 };
-// Units of up to 32 columns by four or eight waves; of up to 128 by four waves, or two teams of four.
+// Units of up to 32 columns by four or eight waves; of up to 128 by four, or by two teams of four.
 enum MaskedKind { MASKED_FEW4, MASKED_FEW8, MASKED_WIDE, MASKED_TEAMS };
 struct MaskedForm { MaskedKind kind; };
 MaskedForm masked_form(MaskedAttnArgs &a);

@@ -10,6 +10,7 @@
 // keys of a block are read once for all of them.  The blocks that any row of a unit sees are counted through (`Span`): those of the
 // sinks, then those of the windows; blocks between are not looked at, nor are their table entries.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -38,6 +39,7 @@ __device__ __forceinline__ Span unit_span(const MaskedAttnArgs &a, int u) {
         s.req = u / a.units_per_req;
         s.i0 = u % a.units_per_req * per;
         const int r0 = a.cu_rows[s.req], r1 = a.cu_rows[s.req + 1];
+        s.first = a.ctx_lens[s.req];
         if (r0 < 0 || r1 < r0 || r1 > a.max_rows || r1 - r0 > a.max_draft) {   // not a row is touched
             if (threadIdx.x == 0) atomicOr(a.err_flag, RS_FLAG_LENGTHS);
             return s;
@@ -46,7 +48,6 @@ __device__ __forceinline__ Span unit_span(const MaskedAttnArgs &a, int u) {
         s.rows = min(per, s.n - s.i0);
         if (s.rows <= 0) return s;
         s.row0 = r0 + s.i0;
-        s.first = a.ctx_lens[s.req];
         if (s.first < 0 || s.first > a.max_ctx - s.n) {
             if (threadIdx.x == 0) atomicOr(a.err_flag, 8);
             s.dead = true;
@@ -156,6 +157,7 @@ struct Piece {
 
 template <int HD>
 __device__ __forceinline__ void join_pieces(const MaskedAttnArgs &a, const Span &s, int hk, int unit, const Piece &pc, int threads) {
+    constexpr int N = 8;
     __shared__ int last;
     const int G = a.Hq / a.Hkv, cols = s.rows * G;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's sums have arrived
@@ -169,26 +171,32 @@ __device__ __forceinline__ void join_pieces(const MaskedAttnArgs &a, const Span 
     if (!last) return;
     for (int item = threadIdx.x; item < cols * (HD / 4); item += threads) {
         const int col = item / (HD / 4), d = item % (HD / 4) * 4;
-        float top = NEG_INF, l = 0.f;
-        float2 ml[MASKED_MAX_CUT], x[MASKED_MAX_CUT], y[MASKED_MAX_CUT];
-#pragma unroll
-        for (int i = 0; i < MASKED_MAX_CUT; ++i) {   // everything asked for at once
-            const size_t at = pc.at(min(i, a.cut - 1), col);
-            ml[i] = get_far(a.part_ml + 2 * at);
-            x[i] = get_far(a.part_o + at * HD + d);
-            y[i] = get_far(a.part_o + at * HD + d + 2);
-        }
-#pragma unroll
-        for (int i = 0; i < MASKED_MAX_CUT; ++i)
-            if (i < a.cut) top = fmaxf(top, ml[i].x);
-        const float ref = top == NEG_INF ? 0.f : top;
+        float top = NEG_INF, l = 0.f;   // over the pieces so far
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int i0 = 0; i0 < a.cut; i0 += N) {
+            float2 ml[N], x[N], y[N];
 #pragma unroll
-        for (int i = 0; i < MASKED_MAX_CUT; ++i) {
-            if (i >= a.cut || ml[i].y == 0.f) continue;   // (a sum of nothing: a piece none of whose keys the row sees)
-            const float e = exp2f((ml[i].x - ref) * a.scale_log2);
-            l += ml[i].y * e;
-            acc += f32x4{x[i].x, x[i].y, y[i].x, y[i].y} * e;
+            for (int i = 0; i < N; ++i) {   // asked for together
+                const size_t at = pc.at(min(i0 + i, a.cut - 1), col);
+                ml[i] = get_far(a.part_ml + 2 * at);
+                x[i] = get_far(a.part_o + at * HD + d);
+                y[i] = get_far(a.part_o + at * HD + d + 2);
+            }
+            float m = top;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i0 + i < a.cut) m = fmaxf(m, ml[i].x);
+            const float ref = m == NEG_INF ? 0.f : m, keep = exp2f((top - ref) * a.scale_log2);
+            top = m;
+            l *= keep;
+            acc = acc * keep;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (i0 + i >= a.cut || ml[i].y == 0.f) continue;   // (a sum of nothing: a piece none of whose keys the row sees)
+                const float e = exp2f((ml[i].x - ref) * a.scale_log2);
+                l += ml[i].y * e;
+                acc += f32x4{x[i].x, x[i].y, y[i].x, y[i].y} * e;
+            }
         }
         bf16x4 v;
 #pragma unroll
@@ -243,37 +251,39 @@ __device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span
     }
 }
 
-// A unit, or one of the `cut` pieces of its keys, by KW teams of four waves; team t takes every KW-th tile of 64 keys, from LDS buffers of its
-// own, and the teams' sums are brought together at the end.  S^T = K Q^T and O^T = V^T P^T, so that a lane owns one column.
-template <int HD, int KW, bool TREE>
-__global__ __launch_bounds__(256 * KW, 2) void masked_attn_kernel(MaskedAttnArgs a) {
-    constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD;
-    extern __shared__ __attribute__((aligned(1024))) bf16_t smem_masked[];
-    const int tid = threadIdx.x & 255, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int team = KW > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
+// Units of up to 128 columns, or one of the `cut` pieces of a unit's keys, by KH teams of four waves.  A wave owns 32 columns, and of a step's keys
+// (64, four blocks, for each team) those of its team.  Keys come by LDS-DMA into two buffers of K and two of V, a step ahead; all waves of a
+// team use them.  S^T = K Q^T and O^T = V^T P^T, so that a lane owns one column; the teams' sums are brought together at the end.
+// What runs beside the matrix unit is written out: the products of the next step's scores alternate with most of this one's exponentials, the
+// products with V with the rest of them and with the next step's maxima.  (A product takes 16 ns of a SIMD; an exponential, its multiplication
+// and two additions beside it one more.)
+// The exponentials' reference is the row's first maximum, moved to the running one once a score is 2^4 above it: two steps in three need no rescaling.
+constexpr int TAB_BLOCKS = 2048, BESIDE_SCORES = 24;
+template <int HD, int KH, bool TREE>
+__global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs a) {
+    constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD, BL = 4, NT = 2, BUF = 4 * KH * BLK, COLS = MASKED_COLS, T = 256 * KH;
+    extern __shared__ __attribute__((aligned(1024))) bf16_t smem_masked[];   // [2] K, [2] V of BUF, [4 KH waves][32][2] floats, [TAB_BLOCKS] ids, flag
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int cg = wave & 3, kh = wave >> 2;
     const int c32 = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hkv;
     // kv heads go to the XCDs in turn, so that a head's keys are in one L2 where there are eight of them
     const int hk = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, piece = rest % a.cut, unit = rest / a.cut;
     const Span s = unit_span<TREE>(a, unit);
     if (s.rows <= 0) return;
-    const Piece pc{((size_t)unit * a.Hkv + hk) * a.cut * MASKED_COLS, piece, MASKED_COLS};
+    const Piece pc{((size_t)unit * a.Hkv + hk) * a.cut * COLS, piece, COLS};
     const int cols = s.rows * G;
     if (s.dead) {
         if (piece == 0)
-            for (int i = threadIdx.x; i < cols * HD; i += 256 * KW) out_at(a, s, i / HD, hk, G)[i % HD] = (bf16_t)0.f;
+            for (int i = threadIdx.x; i < cols * HD; i += T) out_at(a, s, i / HD, hk, G)[i % HD] = (bf16_t)0.f;
         return;
     }
-    const int n_tiles = (s.blocks + 3) >> 2;
-    const int t0 = (int)((int64_t)n_tiles * piece / a.cut), t1 = (int)((int64_t)n_tiles * (piece + 1) / a.cut);
+    const int n_steps = (s.blocks + 4 * KH - 1) / (4 * KH);
+    const int t0 = (int)((int64_t)n_steps * piece / a.cut), t1 = (int)((int64_t)n_steps * (piece + 1) / a.cut);
     const int32_t *tab = a.tables + (size_t)s.req * a.max_blk;
     const float sc = a.scale_log2;
 
-    bf16_t *Ks = smem_masked + team * (4 * 64 * HD);   // [2][4 blocks][BLK] in the pool's order
-    bf16_t *Vs = Ks + 2 * 64 * HD;                     // [2][4 blocks][2 halves][HD][8 tokens]
-    float *x_ml = (float *)(smem_masked + KW * 4 * 64 * HD);   // [KW][4 waves][32][2]
-
-    const int col = wave * 32 + c32, row = min(col, cols - 1) / G;
+    const int col = cg * 32 + c32, row = min(col, cols - 1) / G;
     const Sight see = row_sight<TREE>(a, s, row);
     bf16x8 qf[KS];
     {
@@ -281,132 +291,221 @@ __global__ __launch_bounds__(256 * KW, 2) void masked_attn_kernel(MaskedAttnArgs
 #pragma unroll
         for (int i = 0; i < KS; ++i) qf[i] = ld_bf16x8(qp + 16 * i);
     }
-    // of the wave's rows: positions of the first and of the last
-    const int w_first = s.first + min(wave * 32, cols - 1) / G, w_last = s.first + min(wave * 32 + 31, cols - 1) / G;
-    const bool wave_idle = wave * 32 >= cols;
+    // of the wave's rows: positions of the first and of the last; steps behind what the last one sees are not the wave's
+    const int w_first = s.first + min(cg * 32, cols - 1) / G, w_last = s.first + min(cg * 32 + 31, cols - 1) / G;
+    const int w_end = cg * 32 >= cols ? t0 : TREE ? t1 : min(t1, ((w_last >> 4) - s.skip) / (4 * KH) + 1);
 
-    // lane l < 4: table entry and block id of the l-th block of a tile; -1: none, or not one of the pool
-    auto entry = [&](int t) { const int j = 4 * t + (lane & 3); return j < s.sink_blocks ? j : j + s.skip; };
-    auto fetch_ids = [&](int t) { return t < t1 && 4 * t + (lane & 3) < s.blocks ? tab[entry(t)] : -1; };
-    auto checked = [&](int t, int id) {
-        if ((unsigned)id < (unsigned)a.n_blocks) return id;
-        if (t < t1 && 4 * t + (lane & 3) < s.blocks && tid < 4) atomicOr(a.err_flag, 2);
-        return -1;
-    };
-    // Brings a tile into LDS buffer buf by LDS-DMA (16 bytes a lane, lane l's at the window's base + 16 l): wave w copies block w.  K keeps
-    // the pool's order; V's chunk (dim, half of 8 tokens) goes to [half][dim].  A block that is missing is read as block 0, and masked.
-    auto load_tile = [&](int ids, int buf) {
-        const size_t head = ((size_t)max(__builtin_amdgcn_readlane(ids, wave), 0) * a.Hkv + hk) * BLK;
-        const auto kbuf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.k_pool + head), 0, 2 * BLK, 0x00020000);
-        const auto vbuf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.v_pool + head), 0, 2 * BLK, 0x00020000);
-        bf16_t *kd = Ks + buf * 64 * HD + wave * BLK, *vd = Vs + buf * 64 * HD + wave * BLK;
-        typedef __attribute__((address_space(3))) void lds_void;
-#define KV_PIECE(i) \
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(kbuf, (lds_void *)kd, 16, lane * 16, 0, 1024 * (i), 0); \
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(vbuf, (lds_void *)(vd + (i) * 512), 16, lane * 32, ((i) % (HD / 64)) * 2048 + ((i) / (HD / 64)) * 16, 0, 0);
-        KV_PIECE(0)
-        KV_PIECE(1)
-        if constexpr (HD == 128) {
-            KV_PIECE(2)
-            KV_PIECE(3)
+    // Block ids of TAB_BLOCKS counted blocks from step tb on, in LDS: -1: none, or not one of the pool, of which there are some where *s_bad.  (Fetched
+    // step by step into registers they would be waited for by a count of the loads behind them, which the compiler takes to be none where some are
+    // under a branch: so all loads in flight would be waited for in every step.)
+    int32_t *s_tab = (int32_t *)(smem_masked + 4 * BUF) + 4 * KH * 64, *s_bad = s_tab + TAB_BLOCKS;
+    auto fill_tab = [&](int tb) {
+        for (int i = threadIdx.x; i < min(TAB_BLOCKS, 4 * KH * (t1 - tb)); i += T) {
+            const int j = 4 * KH * tb + i;
+            int id = -1;
+            if (j < s.blocks) {
+                id = tab[j < s.sink_blocks ? j : j + s.skip];
+                if ((unsigned)id >= (unsigned)a.n_blocks) {
+                    atomicOr(a.err_flag, 2);
+                    *s_bad = 1;
+                    id = -1;
+                }
+            }
+            s_tab[i] = id;
         }
-#undef KV_PIECE
+    };
+    int tb = t0;   // the first step of s_tab
+    // Wave w brings block w of a step, 16 bytes a lane (lane l's at the window's base + 16 l).  K keeps the pool's order; V's chunk (dim, half of
+    // 8 tokens) goes to [half][dim].  A block that is missing is read as block 0, and masked.
+    typedef __attribute__((address_space(3))) void lds_void;
+    auto head_of = [&](int t) {
+        const int id = __builtin_amdgcn_readfirstlane(s_tab[4 * KH * (t - tb) + wave]);
+        return ((size_t)max(id, 0) * a.Hkv + hk) * BLK;
+    };
+    auto k_at = [&](int t) { return smem_masked + ((t - t0) & 1) * BUF; };
+    auto v_at = [&](int t) { return smem_masked + (2 + ((t - t0) & 1)) * BUF; };
+    auto load_k = [&](int t) {
+        const auto buf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.k_pool + head_of(t)), 0, 2 * BLK, 0x00020000);
+        auto *d = (lds_void *)(k_at(t) + wave * BLK);   // (a constant offset counts in LDS too, a scalar one does not)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, d, 16, lane * 16, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, d, 16, lane * 16, 0, 1024, 0);
+        if constexpr (HD == 128) {
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, d, 16, lane * 16, 0, 2048, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, d, 16, lane * 16, 0, 3072, 0);
+        }
+    };
+    auto load_v = [&](int t) {
+        const auto buf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.v_pool + head_of(t)), 0, 2 * BLK, 0x00020000);
+        bf16_t *d = v_at(t) + wave * BLK;
+#pragma unroll
+        for (int i = 0; i < HD / 32; ++i)   // 64 dims of a half
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void *)(d + i * 512), 16, lane * 32, (i % (HD / 64)) * 2048 + (i / (HD / 64)) * 16, 0, 0);
     };
     auto klds = [](int r, int cc) { return (r >> 4) * BLK + kpool_chunk_offset(r & 15, cc * 8); };
     auto vlds = [](int blk, int half, int d) { return blk * BLK + half * (8 * HD) + d * 8; };
 
-    float m_run = NEG_INF, l_run = 0.f;   // running maximum of raw scores, running sum
+    // reference (raw score), where it moves, the reference in powers of 2, sum of weights
+    float ref = NEG_INF, limit = NEG_INF, ms = 0.f, l_run = 0.f;
     f32x16 o[DT];
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
+    const float behind = 4.f / sc;
 
-    const int n_it = (t1 - t0 + KW - 1) / KW;   // as many for every team: the barriers are the workgroup's
-    auto tile_at = [&](int it) { return t0 + KW * it + team; };
-    int ids = checked(tile_at(0), fetch_ids(tile_at(0))), next = fetch_ids(tile_at(1));
-    if (tile_at(0) < t1) load_tile(ids, 0);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the LDS-DMA loads have landed
+    bf16x8 pf[BL];   // weights of the wave's blocks
+    constexpr int N_W = BL * 8;
+    auto weight = [&](const f32x16 (&st)[NT], int n) {   // the n-th of the lane's weights of a step
+        const int j = n / 8, i = n % 8;
+        const float p = __builtin_amdgcn_exp2f(fmaf(st[j >> 1][8 * (j & 1) + i], sc, -ms));
+        l_run += p;
+        pf[j][i] = (bf16_t)p;
+        if (i == 7) pf[j] = by_tokens(pf[j]);
+    };
+    constexpr int N_K = NT * KS, R = 4;
+    auto scores = [&](int t, f32x16 (&st)[NT], auto between) {   // between(i): what goes beside the i-th product
+        const bf16_t *ks = k_at(t) + kh * (4 * BLK);
+        // K fragment i = (score tile i % NT, head_dim step i / NT), read R fragments ahead of its product
+        auto kread = [&](int i) { return *(const bf16x8 *)&ks[klds(32 * (i % NT) + c32, 2 * (i / NT) + h)]; };
+        bf16x8 kf[R];
+#pragma unroll
+        for (int i = 0; i < R && i < N_K; ++i) kf[i] = kread(i);
+        f32x16 zero;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) zero[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < N_K; ++i) {
+            st[i % NT] = mfma32(kf[i % R], qf[i / NT], i < NT ? zero : st[i % NT]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + R < N_K) kf[i % R] = kread(i + R);
+            between(i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    bool bad = false;   // some blocks are none of the pool
+    // hides what the wave's rows do not see of step t
+    auto mask = [&](int t, f32x16 (&st)[NT]) {
+        int pos[BL];
+        bool here[BL], full = true;
+#pragma unroll
+        for (int j = 0; j < BL; ++j) {
+            const int e = 4 * (KH * t + kh) + j, p = 16 * (e < s.sink_blocks ? e : e + s.skip);
+            here[j] = e < s.blocks && !(bad && __builtin_amdgcn_readfirstlane(s_tab[4 * (KH * (t - tb) + kh) + j]) < 0);
+            pos[j] = p;
+            full = full && here[j] && (TREE ? p + 15 < s.first : p + 15 <= w_first && (p > w_last - a.window || p + 15 < a.sinks));
+        }
+        if (full) return;
+#pragma unroll
+        for (int j = 0; j < BL; ++j) {
+            const uint32_t seen = here[j] ? see.template sees16<TREE>(pos[j]) >> (4 * h) : 0u;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float v = st[j >> 1][8 * (j & 1) + i];
+                st[j >> 1][8 * (j & 1) + i] = seen & (1u << ((i >> 2) * 8 + (i & 3))) ? v : NEG_INF;
+            }
+        }
+    };
+    auto maximum = [&](const f32x16 (&st)[NT]) {
+        float m = NEG_INF;
+#pragma unroll
+        for (int t2 = 0; t2 < NT; ++t2)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) m = fmaxf(m, st[t2][i]);
+        return m;
+    };
+    // moves the reference where a score of the step is far above it
+    auto follow = [&](float m) {
+        const uint32_t mb = __builtin_bit_cast(uint32_t, m);
+        const auto sw = __builtin_amdgcn_permlane32_swap(mb, mb, false, false);
+        m = fmaxf(__builtin_bit_cast(float, (uint32_t)sw[0]), __builtin_bit_cast(float, (uint32_t)sw[1]));
+        if (!__any(m > limit)) return;
+        const bool moves = m > limit;
+        const float alpha = moves ? __builtin_amdgcn_exp2f((ref - m) * sc) : 1.f;
+        l_run *= alpha;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt] = o[dt] * alpha;
+        ref = moves ? m : ref;
+        ms = moves ? m * sc : ms;
+        limit = moves ? m + behind : limit;
+    };
+    // products with V of step t; weights from N0 on are formed beside them (of a block in front of it), then the next step's maximum
+    constexpr int N_V = BL * DT, N0 = BESIDE_SCORES;
+    auto values = [&](int t, const f32x16 (&cur)[NT], const f32x16 (&nxt)[NT]) {
+        const bf16_t *vs = v_at(t) + kh * (4 * BLK);
+        auto vread = [&](int i) { return *(const bf16x8 *)&vs[vlds(i / DT, h, 32 * (i % DT) + c32)]; };
+        // the weights left are due before the last block's products: so many beside each product before those
+        constexpr int SLOTS = DT * (BL - 1), EACH = (N_W - N0 + SLOTS - 1) / SLOTS, RV = 4;
+        bf16x8 vf[RV];
+        float m = NEG_INF;
+#pragma unroll
+        for (int i = 0; i < RV; ++i) vf[i] = vread(i);
+#pragma unroll
+        for (int i = 0; i < N_V; ++i) {
+            o[i % DT] = mfma32(vf[i % RV], pf[i / DT], o[i % DT]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + RV < N_V) vf[i % RV] = vread(i + RV);
+#pragma unroll
+            for (int e = 0; e < EACH; ++e)
+                if (i < SLOTS && N0 + i * EACH + e < N_W) weight(cur, N0 + i * EACH + e);
+            if (i == SLOTS) m = maximum(nxt);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        return m;
+    };
+
+    if (threadIdx.x == 0) *s_bad = 0;
     __syncthreads();
-    for (int it = 0; it < n_it; ++it) {
-        const int t = tile_at(it);
-        const int nids = checked(t + KW, next);
-        if (t + KW < t1) load_tile(nids, (it + 1) & 1);
-        next = fetch_ids(t + 2 * KW);
-        // the four blocks' first positions, whether the wave's rows see all of them, and any
-        int pos[4];
-        bool full = true, some = false;
+    fill_tab(t0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int e = 4 * t + j;
-            pos[j] = 16 * (e < s.sink_blocks ? e : e + s.skip);
-            const bool there = __builtin_amdgcn_readlane(ids, j) >= 0;
-            const int p = pos[j];
-            if (TREE) {
-                full = full && there && p + 15 < s.first;
-                some = some || there;
-            } else {
-                full = full && there && p + 15 <= w_first && (p > w_last - a.window || p + 15 < a.sinks);
-                some = some || (there && p <= w_last && (p + 15 > w_first - a.window || p < a.sinks));
-            }
+    for (int i = 0; i < KS; ++i) asm volatile("" : "+v"(qf[i]));   // the queries are here: not to be waited for among the steps' loads
+    __syncthreads();
+    bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
+    // In front of step t's work: K of the step after it and V of its own have landed, nobody reads those of the step before any more; their
+    // buffers take K two steps ahead and V of the next.
+    auto turn = [&](int t) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (4 * KH * (t + 3 - tb) > TAB_BLOCKS && t + 1 < t1) {   // contexts of more than 32K tokens
+            tb = t;
+            fill_tab(tb);
+            __syncthreads();
+            bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
         }
-        if (t < t1 && some && !wave_idle) {
-            const bf16_t *ks = Ks + (it & 1) * 64 * HD;
-            const bf16_t *vs = Vs + (it & 1) * 64 * HD;
-            f32x16 st[2];
+        if (t + 2 < t1) load_k(t + 2);
+        if (t + 1 < t1) load_v(t + 1);
+    };
+    auto step = [&](int t, f32x16 (&cur)[NT], f32x16 (&nxt)[NT]) {
+        turn(t);
+        if (t >= w_end) return;
+        if (t + 1 < w_end) {
+            constexpr int EACH = (N0 + N_K - 1) / N_K;
+            scores(t + 1, nxt, [&](int i) {
 #pragma unroll
-            for (int t2 = 0; t2 < 2; ++t2)
+                for (int e = 0; e < EACH; ++e)
+                    if (i * EACH + e < N0) weight(cur, i * EACH + e);
+            });
+            mask(t + 1, nxt);
+        } else {
 #pragma unroll
-                for (int i = 0; i < 16; ++i) st[t2][i] = 0.f;
-#pragma unroll
-            for (int i = 0; i < 2 * KS; ++i) {
-                const bf16x8 kf = *(const bf16x8 *)&ks[klds(32 * (i & 1) + c32, 2 * (i >> 1) + h)];
-                st[i & 1] = mfma32(kf, qf[i >> 1], st[i & 1]);
-            }
-            if (!full) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t seen = __builtin_amdgcn_readlane(ids, j) >= 0 ? see.sees16<TREE>(pos[j]) >> (4 * h) : 0u;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const float x = st[j >> 1][8 * (j & 1) + i];
-                        st[j >> 1][8 * (j & 1) + i] = seen & (1u << ((i >> 2) * 8 + (i & 3))) ? x : NEG_INF;
-                    }
-                }
-            }
-            float m_tile = NEG_INF;
-#pragma unroll
-            for (int t2 = 0; t2 < 2; ++t2)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) m_tile = fmaxf(m_tile, st[t2][i]);
-            m_tile = fmaxf(m_tile, __shfl_xor(m_tile, 32, 64));
-            const float m_new = fmaxf(m_run, m_tile);
-            const float m_safe = m_new == NEG_INF ? 0.f : m_new;
-            if (__any(m_new != m_run)) {
-                const float alpha = __builtin_amdgcn_exp2f((m_run - m_safe) * sc);
-                l_run *= alpha;
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[dt] = o[dt] * alpha;
-                m_run = m_new;
-            }
-            const float ms = m_safe * sc;
-#pragma unroll
-            for (int blk4 = 0; blk4 < 4; ++blk4) {   // one 16-token block per product step
-                bf16x8 pf;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float p = __builtin_amdgcn_exp2f(fmaf(st[blk4 >> 1][8 * (blk4 & 1) + i], sc, -ms));
-                    l_run += p;
-                    pf[i] = (bf16_t)p;
-                }
-                pf = by_tokens(pf);
-#pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32(*(const bf16x8 *)&vs[vlds(blk4, h, 32 * dt + c32)], pf, o[dt]);
-            }
+            for (int n = 0; n < N0; ++n) weight(cur, n);
         }
-        ids = nids;
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the LDS-DMA loads have landed
-        __syncthreads();
+        const float m = values(t, cur, nxt);
+        if (t + 1 < w_end) follow(m);
+    };
+    f32x16 sa[NT], sb[NT];
+    if (t0 < t1) {
+        load_k(t0);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t0 + 1 < t1) load_k(t0 + 1);
+        load_v(t0);
+        if (t0 < w_end) {
+            scores(t0, sa, [](int) {});
+            mask(t0, sa);
+            follow(maximum(sa));
+        }
+    }
+    for (int t = t0; t < t1; t += 2) {
+        step(t, sa, sb);
+        if (t + 1 < t1) step(t + 1, sb, sa);
     }
     l_run += __shfl_xor(l_run, 32, 64);
 
@@ -416,18 +515,18 @@ __global__ __launch_bounds__(256 * KW, 2) void masked_attn_kernel(MaskedAttnArgs
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = odd || !(fabsf(o[dt][i]) < __builtin_huge_valf());
     if (__syncthreads_or(odd && col < cols)) {
-        careful_unit<HD, TREE>(a, s, hk, 4 * t0, min(4 * t1, s.blocks), pc, 256 * KW);
-        if (a.cut > 1) join_pieces<HD>(a, s, hk, unit, pc, 256 * KW);
+        careful_unit<HD, TREE>(a, s, hk, 4 * KH * t0, min(4 * KH * t1, s.blocks), pc, T);
+        if (a.cut > 1) join_pieces<HD>(a, s, hk, unit, pc, T);
         return;
     }
 
-    if (KW == 2) {
-        // both teams rescale to the common maximum; team 0 finishes the first half of head_dim, team 1 the second, each with the other's
-        // part through the K/V buffers (nobody reads those any more)
-        f32x4 *x_o = (f32x4 *)smem_masked;   // [KW][4 waves][2 DT][64]
-        float *mine = x_ml + (team * 4 + wave) * 64, *theirs = x_ml + ((1 - team) * 4 + wave) * 64;
+    if (KH == 2) {
+        // both waves of a column rescale to the common reference; the first finishes the first half of head_dim, the second the other, each with the
+        // other's part through the buffers (nobody reads those any more)
+        f32x4 *x_o = (f32x4 *)smem_masked;   // [8 waves][2 DT][64]
+        float *x_ml = (float *)(smem_masked + 4 * BUF), *mine = x_ml + wave * 64, *theirs = x_ml + (wave ^ 4) * 64;
         if (h == 0) {
-            mine[2 * c32] = m_run;
+            mine[2 * c32] = ref;
             mine[2 * c32 + 1] = l_run;
         }
 #pragma unroll
@@ -436,49 +535,58 @@ __global__ __launch_bounds__(256 * KW, 2) void masked_attn_kernel(MaskedAttnArgs
             for (int j = 0; j < 4; ++j) {
                 f32x4 v;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) v[i] = team == 0 ? o[DT / 2 + dt][4 * j + i] : o[dt][4 * j + i];
-                x_o[((team * 4 + wave) * (2 * DT) + dt * 4 + j) * 64 + lane] = v;
+                for (int i = 0; i < 4; ++i) v[i] = kh == 0 ? o[DT / 2 + dt][4 * j + i] : o[dt][4 * j + i];
+                x_o[(wave * (2 * DT) + dt * 4 + j) * 64 + lane] = v;
             }
         __syncthreads();
         const float m_o = theirs[2 * c32], l_o = theirs[2 * c32 + 1];
-        const float top = fmaxf(m_run, m_o), ref = top == NEG_INF ? 0.f : top;
-        const float e = __builtin_amdgcn_exp2f((m_run - ref) * sc), e_o = __builtin_amdgcn_exp2f((m_o - ref) * sc);
+        const float top = fmaxf(ref, m_o), base = top == NEG_INF ? 0.f : top;
+        const float e = __builtin_amdgcn_exp2f((ref - base) * sc), e_o = __builtin_amdgcn_exp2f((m_o - base) * sc);
         l_run = l_run * e + l_o * e_o;
-        m_run = top;
+        ref = top;
 #pragma unroll
         for (int dt = 0; dt < DT / 2; ++dt)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const f32x4 v = x_o[(((1 - team) * 4 + wave) * (2 * DT) + dt * 4 + j) * 64 + lane];
+                const f32x4 v = x_o[((wave ^ 4) * (2 * DT) + dt * 4 + j) * 64 + lane];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) o[dt][4 * j + i] = (team == 0 ? o[dt][4 * j + i] : o[DT / 2 + dt][4 * j + i]) * e + v[i] * e_o;
+                for (int i = 0; i < 4; ++i) o[dt][4 * j + i] = (kh == 0 ? o[dt][4 * j + i] : o[DT / 2 + dt][4 * j + i]) * e + v[i] * e_o;
             }
     }
-    const int d0 = team * (HD / KW) + 4 * h;   // this lane's dims: d0 + 32 dt + 8 j + i
+    const int d0 = kh * (HD / KH) + 4 * h;   // this lane's dims: d0 + 32 dt + 8 j + i
     if (a.cut > 1) {
         const size_t at = pc.at(piece, col);
         if (col < cols) {
 #pragma unroll
-            for (int dt = 0; dt < DT / KW; ++dt)
+            for (int dt = 0; dt < DT / KH; ++dt)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) put_far(a.part_o + at * HD + d0 + 32 * dt + 8 * (j >> 1) + 2 * (j & 1), o[dt][2 * j], o[dt][2 * j + 1]);
-            if (h == 0 && team == 0) put_far(a.part_ml + 2 * at, m_run, l_run);
+            if (h == 0 && kh == 0) put_far(a.part_ml + 2 * at, ref, l_run);
         }
-        join_pieces<HD>(a, s, hk, unit, pc, 256 * KW);
+        join_pieces<HD>(a, s, hk, unit, pc, T);
         return;
     }
-    if (col >= cols) return;
+    // rows of out are written whole: the wave's columns (of its team's dims) through LDS
+    constexpr int ROW = HD + 8;
+    if (KH == 2) __syncthreads();   // the other team's part has been read
+    bf16_t *strip = smem_masked + cg * (32 * ROW);
     const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
-    bf16_t *p = out_at(a, s, col, hk, G);
 #pragma unroll
-    for (int dt = 0; dt < DT / KW; ++dt)
+    for (int dt = 0; dt < DT / KH; ++dt)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             bf16x4 v;
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(o[dt][4 * j + i] * inv);
-            *(bf16x4 *)(p + d0 + 32 * dt + 8 * j) = v;
+            *(bf16x4 *)(strip + c32 * ROW + d0 + 32 * dt + 8 * j) = v;
         }
+    __syncthreads();
+    constexpr int CH = HD / 8;
+#pragma unroll
+    for (int i = 0; i < 32 * CH / (64 * KH); ++i) {
+        const int item = 64 * (KH * i + kh) + lane, c = item / CH, d = item % CH * 8;
+        if (cg * 32 + c < cols) st_bf16x8(out_at(a, s, cg * 32 + c, hk, G) + d, *(const bf16x8 *)(strip + c * ROW + d));
+    }
 }
 
 // Units of up to 32 columns (decode rows, small trees): bound by reading the cache, so nothing is shared and nothing staged.  The waves take
@@ -663,7 +771,7 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
     if (a.cut > 1) join_pieces<HD>(a, s, hk, unit, pc, 64 * NW);
 }
 
-constexpr int masked_lds(int hd, int kw) { return kw * 4 * 64 * hd * 2 + kw * 4 * 64 * 4; }
+constexpr int wide_lds(int hd, int kh) { return 4 * 4 * kh * 16 * hd * 2 + 4 * kh * 64 * 4 + (TAB_BLOCKS + 1) * 4; }
 
 constexpr int few_lds(int hd, int nw) { return nw * 32 * (hd + 4 + 2) * 4; }
 
@@ -673,8 +781,8 @@ void launch(hipStream_t st, const MaskedAttnArgs &a, const MaskedForm &f) {
     switch (f.kind) {
         case MASKED_FEW4: hipLaunchKernelGGL((masked_few_kernel<HD, 4, TREE>), grid, dim3(256), few_lds(HD, 4), st, a); break;
         case MASKED_FEW8: hipLaunchKernelGGL((masked_few_kernel<HD, 8, TREE>), grid, dim3(512), few_lds(HD, 8), st, a); break;
-        case MASKED_WIDE: hipLaunchKernelGGL((masked_attn_kernel<HD, 1, TREE>), grid, dim3(256), masked_lds(HD, 1), st, a); break;
-        case MASKED_TEAMS: hipLaunchKernelGGL((masked_attn_kernel<HD, 2, TREE>), grid, dim3(512), masked_lds(HD, 2), st, a); break;
+        case MASKED_WIDE: hipLaunchKernelGGL((masked_wide_kernel<HD, 1, TREE>), grid, dim3(256), wide_lds(HD, 1), st, a); break;
+        case MASKED_TEAMS: hipLaunchKernelGGL((masked_wide_kernel<HD, 2, TREE>), grid, dim3(512), wide_lds(HD, 2), st, a); break;
     }
 }
 
@@ -687,6 +795,7 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
     if (tree) most = a.max_draft;
     else if (!a.ctx_lens)
         for (int r = 0; r < a.seq.n_req; ++r) most = std::max(most, a.seq.cu[r + 1] - a.seq.cu[r]);
+    MaskedForm f{};
     const bool few = most * G <= 32;
     a.unit_rows = (few ? 32 : MASKED_COLS) / G;
     int keys = 0;   // most keys of a unit
@@ -706,12 +815,11 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
     }
     if (!tree) keys = (int)std::min<int64_t>(keys, (int64_t)a.window + a.sinks + a.unit_rows + 32);
     const int64_t wgs = (int64_t)a.n_units * a.Hkv;
-    MaskedForm f{};
     if (wgs <= 0) return f;
     const int tiles = (keys + 63) / 64;
     if (few) {
         f.kind = wgs <= 256 ? MASKED_FEW8 : MASKED_FEW4;
-        a.cut = (int)std::max<int64_t>(1, std::min<int64_t>({256 / wgs, MASKED_MAX_CUT, (tiles + 3) / 4}));
+        a.cut = (int)std::max<int64_t>(1, std::min<int64_t>({256 / wgs, MASKED_MAX_CUT, (tiles + 1) / 2}));
     } else {
         f.kind = wgs <= 256 ? MASKED_TEAMS : MASKED_WIDE;
         a.cut = (int)std::max<int64_t>(1, std::min<int64_t>({256 / wgs, MASKED_MAX_CUT, (tiles + 7) / 8}));
@@ -735,12 +843,14 @@ void launch_masked_attention(hipStream_t st, const MaskedAttnArgs &args) {
 
 void masked_attention_init() {
     auto set = [](const void *f, int lds) { (void)hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, lds); };
-    set((const void *)masked_attn_kernel<128, 1, false>, masked_lds(128, 1));
-    set((const void *)masked_attn_kernel<128, 1, true>, masked_lds(128, 1));
-    set((const void *)masked_attn_kernel<128, 2, false>, masked_lds(128, 2));
-    set((const void *)masked_attn_kernel<128, 2, true>, masked_lds(128, 2));
-    set((const void *)masked_attn_kernel<64, 2, false>, masked_lds(64, 2));
-    set((const void *)masked_attn_kernel<64, 2, true>, masked_lds(64, 2));
+    set((const void *)masked_wide_kernel<128, 1, false>, wide_lds(128, 1));
+    set((const void *)masked_wide_kernel<128, 1, true>, wide_lds(128, 1));
+    set((const void *)masked_wide_kernel<128, 2, false>, wide_lds(128, 2));
+    set((const void *)masked_wide_kernel<128, 2, true>, wide_lds(128, 2));
+    set((const void *)masked_wide_kernel<64, 1, false>, wide_lds(64, 1));
+    set((const void *)masked_wide_kernel<64, 1, true>, wide_lds(64, 1));
+    set((const void *)masked_wide_kernel<64, 2, false>, wide_lds(64, 2));
+    set((const void *)masked_wide_kernel<64, 2, true>, wide_lds(64, 2));
     set((const void *)masked_few_kernel<128, 4, false>, few_lds(128, 4));
     set((const void *)masked_few_kernel<128, 4, true>, few_lds(128, 4));
     set((const void *)masked_few_kernel<128, 8, false>, few_lds(128, 8));
