@@ -178,6 +178,7 @@ struct KvPlanArgs {
     int B, max_blk, n_blocks, free_cap, max_rows, parent_stride;
 };
 void launch_kv_plan(hipStream_t st, const KvPlanArgs &a);
+#define RS_AXES 4   // most axes of positions
 struct KvStoreArgs {
     const bf16_t *qkv;        // rows of (Hq + 2 Hkv) * hd, row_stride elements apart
     size_t row_stride;

@@ -167,29 +167,47 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void kv_plan_kernel(KvPlanArgs a) 
 // ---------------------------------------------------------------------------------------------
 // Store.  Pair i (dims i and i + hd/2) of a query or key head turns by the angle position * base^(-2i/hd), the position being the row's on
 // the pair's axis; cos and sin come from the table that was formed in float64.  Memory bound: q, k and v are read once and written once.
-// Workgroups: of 16 rows the query heads (rows x 8-dim chunks by lane, the angles in registers for all heads), then the kv heads.
-// A token's key is 16-byte pieces of its block and its value single elements, so the rows that share a block are written together: the
-// workgroup of the 16 rows among which a run of rows with the same block begins writes all of that run.
+// Workgroups for kv heads (first, as they have the longer way), then for the query heads of 16 rows (rows x 8-dim chunks by lane, the angles in
+// registers for all heads).  A token's key is 16-byte pieces of its block and its value single elements, so the rows that share a block are
+// written together: the wave of the kv_rows rows among which a run of rows with the same block begins writes all of that run.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ int pair_axis(const KvStoreArgs &a, int pair) { return (int)(a.axis[pair >> 5] >> (2 * (pair & 31)) & 3); }
 
-// cos and sin of the 8 pairs from `pair` on of a row; false: a position outside the table
-__device__ __forceinline__ bool angles(const KvStoreArgs &a, int row, int pair, CosSin cs[8]) {
-    const int half = a.hd >> 1;
-    int pos[4];
+struct Positions {   // of a row, on each axis
+    int p[RS_AXES];
+    __device__ __forceinline__ Positions at(int lane) const {
+        Positions r;
+#pragma unroll
+        for (int x = 0; x < RS_AXES; ++x) r.p[x] = __shfl(p[x], lane, 64);
+        return r;
+    }
+};
+__device__ __forceinline__ Positions positions_of(const KvStoreArgs &a, int row) {
+    Positions r;
+#pragma unroll
+    for (int x = 0; x < RS_AXES; ++x) r.p[x] = x < a.n_axes ? a.positions[(size_t)x * a.max_rows + row] : 0;
+    return r;
+}
+__device__ __forceinline__ bool in_table(const KvStoreArgs &a, const Positions &r) {
     bool ok = true;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-        pos[x] = x < a.n_axes ? a.positions[(size_t)x * a.max_rows + row] : 0;
-        ok = ok && (unsigned)pos[x] < (unsigned)a.max_pos;
+    for (int x = 0; x < RS_AXES; ++x) ok = ok && (unsigned)r.p[x] < (unsigned)a.max_pos;
+    return ok;
+}
+// cos and sin of the 8 pairs from `pair` on
+__device__ __forceinline__ void angles(const KvStoreArgs &a, const Positions &r, int pair, CosSin cs[8]) {
+    const int half = a.hd >> 1;
+    const CosSin *t = a.table + pair;
+    if (a.n_axes == 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) cs[i] = t[(size_t)r.p[0] * half + i];
+        return;
     }
-    if (!ok) return false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int x = pair_axis(a, pair + i);
-        cs[i] = a.table[(size_t)(x == 0 ? pos[0] : x == 1 ? pos[1] : x == 2 ? pos[2] : pos[3]) * half + pair + i];
+        cs[i] = t[(size_t)(x == 0 ? r.p[0] : x == 1 ? r.p[1] : x == 2 ? r.p[2] : r.p[3]) * half + i];
     }
-    return true;
 }
 __device__ __forceinline__ void turn(const CosSin cs[8], bf16x8 &lo, bf16x8 &hi) {
 #pragma unroll
@@ -202,59 +220,32 @@ __device__ __forceinline__ void turn(const CosSin cs[8], bf16x8 &lo, bf16x8 &hi)
 
 typedef uint32_t u32x4_s __attribute__((ext_vector_type(4)));
 
-// Keys of n rows of a block (lane r: row r's slot) to their places: items (row, 8 pairs), a wave's two rounds of them asked for at once.
 template <int HD>
-__device__ __forceinline__ void turn_keys(const KvStoreArgs &a, const bf16_t *src, int first, int n, int my, int lane, bf16_t *kd) {
-    constexpr int C = HD / 16, ROUNDS = 16 * C / 64;
-    bf16x8 lo[ROUNDS], hi[ROUNDS];
-    CosSin cs[ROUNDS][8];
-    bool ok[ROUNDS];
-#pragma unroll
-    for (int k = 0; k < ROUNDS; ++k) {
-        const int it = 64 * k + lane, c = it % C, r = it / C;
-        ok[k] = false;
-        if (r < n) {
-            const bf16_t *p = src + (size_t)r * a.row_stride + 8 * c;
-            lo[k] = ld_bf16x8(p), hi[k] = ld_bf16x8(p + HD / 2);
-            ok[k] = angles(a, first + r, 8 * c, cs[k]);
-        }
-    }
-#pragma unroll
-    for (int k = 0; k < ROUNDS; ++k) {
-        const int it = 64 * k + lane, c = it % C, t = __shfl(my, it / C, 64) & 15;
-        if (!ok[k]) continue;
-        turn(cs[k], lo[k], hi[k]);
-        st_bf16x8(kd + kpool_chunk_offset(t, 8 * c), lo[k]);
-        st_bf16x8(kd + kpool_chunk_offset(t, HD / 2 + 8 * c), hi[k]);
-    }
-}
-
-template <int HD>
-__global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int n_groups, int q_parts) {
+__global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_rows, int kv_groups, int kv_parts, int q_groups) {
     constexpr int C = HD / 16;   // 8-dim chunks of half a head
     constexpr int BLK = 16 * HD, PL = HD / 8;   // PL: places of a lane's V
+    constexpr int ROUNDS = 16 * C / 64;   // of items (row, 8 pairs) of a key block
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const int group = blockIdx.x % n_groups, part = blockIdx.x / n_groups;
     const int rows = a.n_rows ? min(max(*a.n_rows, 0), a.max_rows) : a.max_rows;
-    const int row0 = 16 * group;
-    if (row0 >= rows) return;
-    if (part < q_parts) {
+    if ((int)blockIdx.x >= kv_groups * kv_parts) {
         // a thread: 8 pairs of a row, in every second one of 8 heads
-        const int h0 = part * 8;
+        const int at = blockIdx.x - kv_groups * kv_parts, row0 = 16 * (at % q_groups), h0 = at / q_groups * 8;
         for (int it = tid; it < 16 * C * 2; it += 256) {
             const int c = it % C, row = row0 + it / C % 16, first = h0 + it / (16 * C);
             if (row >= rows) continue;
             const bf16_t *p = a.qkv + (size_t)row * a.row_stride + 8 * c;
+            const Positions r = positions_of(a, row);
             bf16x8 lo[4], hi[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)   // all asked for before one is written (queries in place are the thread's own)
                 if (first + 2 * k < a.Hq) lo[k] = ld_bf16x8(p + (first + 2 * k) * HD), hi[k] = ld_bf16x8(p + (first + 2 * k) * HD + HD / 2);
-            CosSin cs[8];
-            if (!angles(a, row, 8 * c, cs)) {
+            if (!in_table(a, r)) {
                 atomicOr(a.err_flag, 1);
                 continue;
             }
             if (!a.q_out) continue;
+            CosSin cs[8];
+            angles(a, r, 8 * c, cs);
             bf16_t *q = a.q_out + (size_t)row * a.q_stride + 8 * c;
 #pragma unroll
             for (int k = 0; k < 4; ++k)
@@ -266,21 +257,26 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int n_grou
         }
         return;
     }
-    const int kvh = (part - q_parts) * 4 + wave;
-    if (kvh >= a.Hkv) return;
-    // lane l: the slot of row row0 - 1 + l and its block, -1: not a row, or none
+    const int row0 = kv_rows * ((int)blockIdx.x % kv_groups), kvh = (int)blockIdx.x / kv_groups * 4 + wave;
+    if (row0 >= rows || kvh >= a.Hkv) return;
+    // lane l: slot and positions of row row0 - 1 + l, and the slot's block, -1: not a row, or none
     auto block_at = [&](int slot) { return slot < 0 || (slot >> 4) >= a.n_blocks ? -1 : slot >> 4; };
     const int r_l = row0 - 1 + lane;
-    const int sl = lane < 33 && r_l >= 0 && r_l < rows ? a.slots[r_l] : -1, bl = block_at(sl);
-    if (lane > 0 && lane < 17 && bl < 0 && sl != -1) atomicOr(a.err_flag, 2);
+    const bool is_row = lane < kv_rows + 16 && r_l >= 0 && r_l < rows;
+    const int sl = is_row ? a.slots[r_l] : -1, bl = block_at(sl);
+    const Positions ps = positions_of(a, is_row ? r_l : row0);
+    const bool mine = lane > 0 && lane <= kv_rows;
+    if (mine && bl < 0 && sl != -1) atomicOr(a.err_flag, 2);
     const int prev = __shfl_up(bl, 1, 64);
-    uint64_t starts = __ballot(lane > 0 && lane < 17 && bl >= 0 && bl != prev);
+    uint64_t starts = __ballot(mine && bl >= 0 && bl != prev);
     while (starts) {
         const int l0 = __ffsll((unsigned long long)starts) - 1;
         starts &= starts - 1;
         const int blk = __builtin_amdgcn_readlane(bl, l0);
         int first = row0 - 1 + l0;
-        int my = __shfl(sl, (l0 + lane) & 63, 64);   // lane l < 16: the slot of row first + l
+        // lane l < 16: slot and positions of row first + l
+        int my = __shfl(sl, (l0 + lane) & 63, 64);
+        Positions pos = ps.at((l0 + lane) & 63);
         if (lane >= 16) my = -1;
         for (;;) {   // 16 rows at a time: a block has no more places, but slots may name one twice
             const uint64_t same = __ballot(block_at(my) == blk);
@@ -289,23 +285,46 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int n_grou
             bf16_t *kd = a.k_pool + ((size_t)blk * a.Hkv + kvh) * BLK, *vd = a.v_pool + ((size_t)blk * a.Hkv + kvh) * BLK;
             const bf16_t *src = a.qkv + (size_t)first * a.row_stride + (size_t)(a.Hq + kvh) * HD;
             // whether the places are consecutive, and every position is in the table (a bad one is reported by the queries' workgroups)
-            bool fine = true;
-            if (lane < n) {
-                fine = (my & 15) == (__builtin_amdgcn_readfirstlane(my) & 15) + lane;
-                for (int x = 0; x < a.n_axes; ++x) fine = fine && (unsigned)a.positions[(size_t)x * a.max_rows + first + lane] < (unsigned)a.max_pos;
-            }
-            const bool plain = !__any(!fine);
-            const int t0 = __builtin_amdgcn_readfirstlane(my) & 15;
+            const int t0 = __builtin_amdgcn_readfirstlane(my) & 15, inside = in_table(a, pos);
+            const bool plain = !__any(lane < n && (!inside || (my & 15) != t0 + lane));
+
+            // V, where the places are consecutive: a lane has two dims of all rows (head_dim 64: a half-wave eight places)
+            const int dp = lane % (HD / 2), u0 = lane / (HD / 2) * 8;
+            uint32_t w[PL];
             if (plain) {
-                // V: a lane two dims of all the rows; places t0 .. t0 + n - 1 of a dim are consecutive
-                const int dp = lane % (HD / 2), u0 = lane / (HD / 2) * 8;   // (head_dim 64: a half-wave eight places)
-                uint32_t w[PL];
 #pragma unroll
                 for (int u = 0; u < PL; ++u) {
                     const int r = u0 + u - t0;
                     w[u] = r >= 0 && r < n ? *(const uint32_t *)(src + (size_t)r * a.row_stride + a.Hkv * HD + 2 * dp) : 0u;
                 }
-                turn_keys<HD>(a, src, first, n, my, lane, kd);
+            }
+            // K: items (row, 8 pairs), everything asked for at once
+            {
+                bf16x8 lo[ROUNDS], hi[ROUNDS];
+                CosSin cs[ROUNDS][8];
+                int place[ROUNDS];
+#pragma unroll
+                for (int k = 0; k < ROUNDS; ++k) {
+                    const int it = 64 * k + lane, c = it % C, r = it / C;
+                    const Positions at = pos.at(r);
+                    const int slot = __shfl(my, r, 64), ok = __shfl(inside, r, 64);
+                    place[k] = r < n && ok ? slot & 15 : -1;
+                    if (place[k] >= 0) {
+                        const bf16_t *p = src + (size_t)r * a.row_stride + 8 * c;
+                        lo[k] = ld_bf16x8(p), hi[k] = ld_bf16x8(p + HD / 2);
+                        angles(a, at, 8 * c, cs[k]);
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < ROUNDS; ++k) {
+                    const int c = (64 * k + lane) % C;
+                    if (place[k] < 0) continue;
+                    turn(cs[k], lo[k], hi[k]);
+                    st_bf16x8(kd + kpool_chunk_offset(place[k], 8 * c), lo[k]);
+                    st_bf16x8(kd + kpool_chunk_offset(place[k], HD / 2 + 8 * c), hi[k]);
+                }
+            }
+            if (plain) {
                 uint32_t ev[PL / 2], od[PL / 2];
 #pragma unroll
                 for (int j = 0; j < PL / 2; ++j) {
@@ -335,17 +354,15 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int n_grou
                     }
                 }
             } else {
-                turn_keys<HD>(a, src, first, n, my, lane, kd);
-                for (int i0 = 0; i0 < n * HD; i0 += 64) {
-                    const int it = i0 + lane, r = it % n, d = it / n, t = __shfl(my, r, 64) & 15;
-                    bool ok = it < n * HD;
-                    for (int x = 0; x < a.n_axes; ++x) ok = ok && (unsigned)a.positions[(size_t)x * a.max_rows + first + r] < (unsigned)a.max_pos;
-                    if (ok) vd[d * 16 + t] = src[(size_t)r * a.row_stride + a.Hkv * HD + d];
+                for (int i0 = 0; i0 < n * HD; i0 += 64) {   // rows in any order: element by element
+                    const int it = i0 + lane, r = it % n, d = it / n, t = __shfl(my, r, 64) & 15, ok = __shfl(inside, r, 64);
+                    if (it < n * HD && ok) vd[d * 16 + t] = src[(size_t)r * a.row_stride + a.Hkv * HD + d];
                 }
             }
             if (n < 16) break;
             first += 16;
             my = lane < 16 && first + lane < rows ? a.slots[first + lane] : -1;
+            pos = positions_of(a, min(first + lane, rows - 1));
         }
     }
 }
@@ -417,10 +434,12 @@ void launch_kv_plan(hipStream_t st, const KvPlanArgs &a) {
 }
 
 void launch_kv_store(hipStream_t st, const KvStoreArgs &a) {
-    const int groups = (a.max_rows + 15) / 16, q_parts = (a.Hq + 7) / 8, kv_parts = (a.Hkv + 3) / 4;
-    const dim3 grid(groups * (q_parts + kv_parts));
-    if (a.hd == 128) hipLaunchKernelGGL(kv_store_kernel<128>, grid, dim3(256), 0, st, a, groups, q_parts);
-    else hipLaunchKernelGGL(kv_store_kernel<64>, grid, dim3(256), 0, st, a, groups, q_parts);
+    // few rows: a wave for every four, so that short runs are not written one after the other
+    const int kv_rows = a.max_rows <= 2048 ? 4 : 16, kv_groups = (a.max_rows + kv_rows - 1) / kv_rows, kv_parts = (a.Hkv + 3) / 4;
+    const int q_groups = (a.max_rows + 15) / 16, q_parts = (a.Hq + 7) / 8;
+    const dim3 grid(kv_groups * kv_parts + q_groups * q_parts);
+    if (a.hd == 128) hipLaunchKernelGGL(kv_store_kernel<128>, grid, dim3(256), 0, st, a, kv_rows, kv_groups, kv_parts, q_groups);
+    else hipLaunchKernelGGL(kv_store_kernel<64>, grid, dim3(256), 0, st, a, kv_rows, kv_groups, kv_parts, q_groups);
 }
 
 void launch_kv_compact(hipStream_t st, const KvCompactArgs &a) {
