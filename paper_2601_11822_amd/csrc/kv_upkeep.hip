@@ -219,9 +219,17 @@ __device__ __forceinline__ void turn(const CosSin cs[8], bf16x8 &lo, bf16x8 &hi)
 }
 
 typedef uint32_t u32x4_s __attribute__((ext_vector_type(4)));
+template <bool MANY> __device__ __forceinline__ bf16x8 ld_row(const bf16_t *p) { return MANY ? ld_bf16x8_stream(p) : ld_bf16x8(p); }
+template <bool MANY> __device__ __forceinline__ void st_row(bf16_t *p, bf16x8 v) {
+    if (MANY) __builtin_nontemporal_store(v, (bf16x8 *)p);
+    else st_bf16x8(p, v);
+}
 
-template <int HD>
-__global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_rows, int kv_groups, int kv_parts, int q_groups) {
+// MANY: rows for more than the caches, which are read and written past them (16444 rows of the 8B heads, in us: 97; only the loads 97, only the
+// stores 91, both 83; with the parts of a row in workgroups far apart, so that its angles are fetched again, 108).
+template <int HD, bool MANY>
+__global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_groups, int kv_parts, int q_parts) {
+    constexpr int kv_rows = MANY ? 16 : 4;   // few rows: a wave for every four, so that short runs are not written one after the other
     constexpr int C = HD / 16;   // 8-dim chunks of half a head
     constexpr int BLK = 16 * HD, PL = HD / 8;   // PL: places of a lane's V
     constexpr int ROUNDS = 16 * C / 64;   // of items (row, 8 pairs) of a key block
@@ -229,7 +237,7 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_row
     const int rows = a.n_rows ? min(max(*a.n_rows, 0), a.max_rows) : a.max_rows;
     if ((int)blockIdx.x >= kv_groups * kv_parts) {
         // a thread: 8 pairs of a row, in every second one of 8 heads
-        const int at = blockIdx.x - kv_groups * kv_parts, row0 = 16 * (at % q_groups), h0 = at / q_groups * 8;
+        const int at = blockIdx.x - kv_groups * kv_parts, row0 = 16 * (at / q_parts), h0 = at % q_parts * 8;
         for (int it = tid; it < 16 * C * 2; it += 256) {
             const int c = it % C, row = row0 + it / C % 16, first = h0 + it / (16 * C);
             if (row >= rows) continue;
@@ -238,7 +246,7 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_row
             bf16x8 lo[4], hi[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)   // all asked for before one is written (queries in place are the thread's own)
-                if (first + 2 * k < a.Hq) lo[k] = ld_bf16x8(p + (first + 2 * k) * HD), hi[k] = ld_bf16x8(p + (first + 2 * k) * HD + HD / 2);
+                if (first + 2 * k < a.Hq) lo[k] = ld_row<MANY>(p + (first + 2 * k) * HD), hi[k] = ld_row<MANY>(p + (first + 2 * k) * HD + HD / 2);
             if (!in_table(a, r)) {
                 atomicOr(a.err_flag, 1);
                 continue;
@@ -251,13 +259,13 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_row
             for (int k = 0; k < 4; ++k)
                 if (first + 2 * k < a.Hq) {
                     turn(cs, lo[k], hi[k]);
-                    st_bf16x8(q + (first + 2 * k) * HD, lo[k]);
-                    st_bf16x8(q + (first + 2 * k) * HD + HD / 2, hi[k]);
+                    st_row<MANY>(q + (first + 2 * k) * HD, lo[k]);
+                    st_row<MANY>(q + (first + 2 * k) * HD + HD / 2, hi[k]);
                 }
         }
         return;
     }
-    const int row0 = kv_rows * ((int)blockIdx.x % kv_groups), kvh = (int)blockIdx.x / kv_groups * 4 + wave;
+    const int row0 = kv_rows * ((int)blockIdx.x / kv_parts), kvh = (int)blockIdx.x % kv_parts * 4 + wave;
     if (row0 >= rows || kvh >= a.Hkv) return;
     // lane l: slot and positions of row row0 - 1 + l, and the slot's block, -1: not a row, or none
     auto block_at = [&](int slot) { return slot < 0 || (slot >> 4) >= a.n_blocks ? -1 : slot >> 4; };
@@ -311,7 +319,7 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_row
                     place[k] = r < n && ok ? slot & 15 : -1;
                     if (place[k] >= 0) {
                         const bf16_t *p = src + (size_t)r * a.row_stride + 8 * c;
-                        lo[k] = ld_bf16x8(p), hi[k] = ld_bf16x8(p + HD / 2);
+                        lo[k] = ld_row<MANY>(p), hi[k] = ld_row<MANY>(p + HD / 2);
                         angles(a, at, 8 * c, cs[k]);
                     }
                 }
@@ -434,12 +442,12 @@ void launch_kv_plan(hipStream_t st, const KvPlanArgs &a) {
 }
 
 void launch_kv_store(hipStream_t st, const KvStoreArgs &a) {
-    // few rows: a wave for every four, so that short runs are not written one after the other
-    const int kv_rows = a.max_rows <= 2048 ? 4 : 16, kv_groups = (a.max_rows + kv_rows - 1) / kv_rows, kv_parts = (a.Hkv + 3) / 4;
-    const int q_groups = (a.max_rows + 15) / 16, q_parts = (a.Hq + 7) / 8;
-    const dim3 grid(kv_groups * kv_parts + q_groups * q_parts);
-    if (a.hd == 128) hipLaunchKernelGGL(kv_store_kernel<128>, grid, dim3(256), 0, st, a, kv_rows, kv_groups, kv_parts, q_groups);
-    else hipLaunchKernelGGL(kv_store_kernel<64>, grid, dim3(256), 0, st, a, kv_rows, kv_groups, kv_parts, q_groups);
+    const bool many = a.max_rows > 2048;   // 48 MB of the 8B heads
+    const int kv_rows = many ? 16 : 4, kv_groups = (a.max_rows + kv_rows - 1) / kv_rows, kv_parts = (a.Hkv + 3) / 4, q_parts = (a.Hq + 7) / 8;
+    const dim3 grid(kv_groups * kv_parts + (a.max_rows + 15) / 16 * q_parts);
+    auto launch = [&](auto *kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, kv_groups, kv_parts, q_parts); };
+    if (a.hd == 128) many ? launch(kv_store_kernel<128, true>) : launch(kv_store_kernel<128, false>);
+    else many ? launch(kv_store_kernel<64, true>) : launch(kv_store_kernel<64, false>);
 }
 
 void launch_kv_compact(hipStream_t st, const KvCompactArgs &a) {

@@ -1911,6 +1911,7 @@ int32_t rs_kv_store(rs_ctx *c, int32_t side, int32_t layer, const void *qkv, int
     if (q_out && (rc = check_kv4_rows("q_out", q_out, q_stride, (int64_t)m.n_q_heads * m.head_dim))) return rc;
     if ((rc = check_words("positions", positions, 4)) || (rc = check_words("slots", slots, 4))) return rc;
     if (n_rows && (rc = check_words("n_rows", n_rows, 4))) return rc;
+    static_assert(RS_MAX_AXES == RS_AXES, "the kernels' number of axes");
     if (n_axes < 1 || n_axes > RS_MAX_AXES) return fail(RS_ERR_BAD_ARG, "%d axes of positions, at most %d", n_axes, RS_MAX_AXES);
     if (n_axes > 1 && !pair_axis) return fail(RS_ERR_BAD_ARG, "no axis of each pair");
     if (max_rows < 1) return fail(RS_ERR_BAD_ARG, "%d rows", max_rows);
@@ -1919,7 +1920,7 @@ int32_t rs_kv_store(rs_ctx *c, int32_t side, int32_t layer, const void *qkv, int
         if (pair_axis[i] >= n_axes) return fail(RS_ERR_BAD_ARG, "pair %d turns with axis %d of %d", i, pair_axis[i], n_axes);
         a.axis[i >> 5] |= (uint64_t)pair_axis[i] << (2 * (i & 31));
     }
-    if ((rc = check_grid(((int64_t)max_rows / 16 + 1) * ((m.n_q_heads + 7) / 8 + (m.n_kv_heads + 3) / 4), 256))) return rc;
+    if ((rc = check_grid(((int64_t)max_rows / 4 + 1) * ((m.n_q_heads + 7) / 8 + (m.n_kv_heads + 3) / 4), 256))) return rc;
     if ((rc = check_kv4_side(c, side))) return rc;
     a.qkv = (const bf16_t *)qkv;
     a.row_stride = (size_t)row_stride;

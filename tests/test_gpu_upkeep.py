@@ -250,6 +250,23 @@ def test_store_of_shuffled_rows_with_gaps(heads, q):
     c.c.destroy()
 
 
+@pytest.mark.parametrize("heads", [(8, 2, 128), (9, 3, 128), (4, 4, 64)], ids=str)
+def test_store_of_many_rows(heads):
+    """More than 2048 rows go past the caches: prompts, one behind a cached prefix that ends inside a block, rows without a slot, queries in place."""
+    runs = [(5, 1200), (0, 999), (16, 33)]
+    c = Step(heads, 160, max_batch=1, seed=12, max_pos=3000)
+    tab = c.tables([a + b for a, b in runs])
+    slots = np.array([int(tab[r, t // 16]) * 16 + t % 16 for r, (a, b) in enumerate(runs) for t in range(a, a + b)])
+    slots[1500:1530] = -1
+    n = len(slots)
+    positions = c.g.integers(0, 3000, (2, n))
+    pair_axis = [i // 3 % 2 for i in range(c.hd // 2)]
+    qkv = R.bf16(c.g.standard_normal((n, c.Hq + 2 * c.Hkv, c.hd)))
+    got = store(c, qkv, positions, slots, 2, pair_axis, q="in place")
+    check_store(c, qkv, positions, slots, pair_axis, got, [i for i in range(n) if slots[i] >= 0], list(range(n)))
+    c.c.destroy()
+
+
 def test_store_skips_bad_rows_and_reports_them():
     c = Step((8, 2, 128), 10, max_batch=1, seed=7, max_pos=100)
     n = 20
