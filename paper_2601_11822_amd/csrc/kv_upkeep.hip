@@ -31,7 +31,7 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void kv_plan_kernel(KvPlanArgs a) 
 
     // sums over the requests, T at a time
     uint32_t carry_n = 0, carry_need = 0;
-    int bad = 0;
+    int bad = 0, held_mine = 0, need_mine = 0;   // of request tid
     int64_t tot_n = 0, tot_need = 0;
     for (int b0 = 0; b0 < a.B; b0 += T) {
         const int b = b0 + tid;
@@ -45,6 +45,7 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void kv_plan_kernel(KvPlanArgs a) 
             else need = max((int)((end + 15) >> 4) - held, 0);
         }
         tot_n += n, tot_need += need;
+        if (b0 == 0) held_mine = held, need_mine = need;
         uint32_t x = n, y = need;   // inclusive sums of the wave
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -109,6 +110,31 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void kv_plan_kernel(KvPlanArgs a) 
             if (j < s_more[i]) fresh[k] = *source(i, s_held[i] + j);
             if (a.parents && j < s_new[i]) up[k] = a.parents[(size_t)(r0 + i) * a.parent_stride + j];
         }
+        // Trees: a lane's ancestors by doubling: after k steps `mask` holds 2^k of them and `up` is the one behind; the requests' steps in turn, so
+        // that one's exchange is under way beside another's.
+        uint64_t mask[K];
+        if (a.parents) {
+            bool some = false;
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                if (up[k] < -1 || up[k] >= lane) {
+                    atomicOr(a.err_flag, RS_FLAG_LENGTHS);
+                    up[k] = -1;
+                }
+                mask[k] = 1ull << lane;
+                some = some || up[k] >= 0;
+            }
+            while (__any(some)) {
+                some = false;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const uint64_t m = __shfl(mask[k], up[k] & 63, 64);
+                    const int u = __shfl(up[k], up[k] & 63, 64);
+                    if (up[k] >= 0) mask[k] |= m, up[k] = u;
+                    some = some || up[k] >= 0;
+                }
+            }
+        }
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int i = wave / sub + k * step;
@@ -118,42 +144,22 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void kv_plan_kernel(KvPlanArgs a) 
             const int j0 = lane + 64 * part;
             if (j0 < more) tab[j0] = fresh[k];
             for (int j = j0 + 64 * parts; j < more; j += 64 * parts) tab[j] = *source(i, held + j);
-            if (a.parents) {
-                if (part > 0 || n == 0) continue;
-                // ancestors by doubling: after k steps `mask` holds 2^k of them and `u` is the one behind
-                int u = up[k];
-                if (u < -1 || u >= lane) {
-                    if (lane < n) atomicOr(a.err_flag, RS_FLAG_LENGTHS);
-                    u = -1;
-                }
-                uint64_t mask = 1ull << lane;
-#pragma unroll
-                for (int k2 = 0; k2 < 6; ++k2) {
-                    const uint64_t m = __shfl(mask, u & 63, 64);
-                    const int v = __shfl(u, u & 63, 64);
-                    if (u >= 0) mask |= m, u = v;
-                }
-                if (lane < n) {
-                    a.positions[row + lane] = len + __popcll(mask) - 1;
-                    a.slots[row + lane] = slot_of(id[k], len + lane);
-                    if (a.masks) a.masks[row + lane] = mask;
-                }
-            } else {
-                if (j0 < n) {
-                    a.positions[row + j0] = len + j0;
-                    a.slots[row + j0] = slot_of(id[k], len + j0);
-                }
-                for (int j = j0 + 64 * parts; j < n; j += 64 * parts) {
-                    a.positions[row + j] = len + j;
-                    a.slots[row + j] = slot_of(*source(i, (len + j) >> 4), len + j);
-                }
+            if (j0 < n) {
+                a.positions[row + j0] = len + (a.parents ? __popcll(mask[k]) - 1 : j0);
+                a.slots[row + j0] = slot_of(id[k], len + j0);
+                if (a.masks) a.masks[row + j0] = mask[k];
+            }
+            for (int j = j0 + 64 * parts; j < n; j += 64 * parts) {   // (chains alone: a tree has no more than 64 tokens)
+                a.positions[row + j] = len + j;
+                a.slots[row + j] = slot_of(*source(i, (len + j) >> 4), len + j);
             }
         }
     }
     if (tid == 0) s_last = wgs == 1 || arrived == wgs - 1;
     __syncthreads();
     if (!s_last) return;
-    for (int b = tid; b < a.B; b += T) {
+    if (tid < a.B) a.held_out[tid] = bad ? held_mine : held_mine + need_mine;
+    for (int b = tid + T; b < a.B; b += T) {
         const int len = a.lens[b], held = a.held[b], n = a.n_new[b];
         a.held_out[b] = bad || len == -1 ? held : max((int)(((int64_t)len + n + 15) >> 4), held);
     }
