@@ -17,11 +17,27 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 constexpr int PLAN_REQS = 64, PLAN_WAVES = 16;   // requests and waves of a workgroup
 
+// Sums that stop at 2^32 - 1: of terms of up to 2^31 - 1, a sum is right, or more than any bound.
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false); }
+// inclusive sums of a row of 16 lanes, by lane moves (1, 2, 4, 8 to the right, zeros from outside)
+__device__ __forceinline__ uint32_t row_sums(uint32_t x) {
+    x = add_sat(x, moved<0x111, 0xf>(x));
+    x = add_sat(x, moved<0x112, 0xf>(x));
+    x = add_sat(x, moved<0x114, 0xf>(x));
+    return add_sat(x, moved<0x118, 0xf>(x));
+}
+// and of the wave: lane 15 of a row to the next one (rows 1 and 3), lane 31 to the upper half
+__device__ __forceinline__ uint32_t wave_sums(uint32_t x) {
+    x = row_sums(x);
+    x = add_sat(x, moved<0x142, 0xa>(x));
+    return add_sat(x, moved<0x143, 0xc>(x));
+}
+
 __global__ __launch_bounds__(64 * PLAN_WAVES) void kv_plan_kernel(KvPlanArgs a) {
     constexpr int T = 64 * PLAN_WAVES, K = PLAN_REQS / PLAN_WAVES;
     __shared__ uint32_t s_n[PLAN_WAVES], s_need[PLAN_WAVES];
     __shared__ int s_row[PLAN_REQS], s_first[PLAN_REQS], s_len[PLAN_REQS], s_new[PLAN_REQS], s_held[PLAN_REQS], s_more[PLAN_REQS];
-    __shared__ int64_t s_tot_n[PLAN_WAVES], s_tot_need[PLAN_WAVES];
     __shared__ int s_bad, s_last;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int r0 = blockIdx.x * PLAN_REQS, mine = min(PLAN_REQS, a.B - r0);
@@ -30,9 +46,8 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void kv_plan_kernel(KvPlanArgs a) 
     const int given = *a.n_free, n_free = min(max(given, 0), a.free_cap);
 
     // sums over the requests, T at a time
-    uint32_t carry_n = 0, carry_need = 0;
+    uint32_t tot_n = 0, tot_need = 0;
     int bad = 0, held_mine = 0, need_mine = 0;   // of request tid
-    int64_t tot_n = 0, tot_need = 0;
     for (int b0 = 0; b0 < a.B; b0 += T) {
         const int b = b0 + tid;
         int n = 0, need = 0, len = -1, held = 0;
@@ -44,33 +59,21 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void kv_plan_kernel(KvPlanArgs a) 
             else if (held > a.max_blk || (int64_t)len > 16ll * held || end > 16ll * a.max_blk) bad |= 2, n = 0;
             else need = max((int)((end + 15) >> 4) - held, 0);
         }
-        tot_n += n, tot_need += need;
         if (b0 == 0) held_mine = held, need_mine = need;
-        uint32_t x = n, y = need;   // inclusive sums of the wave
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const uint32_t xo = __shfl_up(x, o, 64), yo = __shfl_up(y, o, 64);
-            if (lane >= o) x += xo, y += yo;
-        }
-        __syncthreads();   // the sums of those before have been read
+        const uint32_t x = wave_sums(n), y = wave_sums(need);
+        if (b0 > 0) __syncthreads();   // the sums of those before have been read
         if (lane == 63) s_n[wave] = x, s_need[wave] = y;
         __syncthreads();
-        uint32_t row = carry_n + x - n, first = carry_need + y - need;
-#pragma unroll
-        for (int w = 0; w < PLAN_WAVES; ++w) {
-            const uint32_t xw = s_n[w], yw = s_need[w];
-            if (w < wave) row += xw, first += yw;
-            carry_n += xw, carry_need += yw;
-        }
+        const uint32_t xs = row_sums(s_n[lane & 15]), ys = row_sums(s_need[lane & 15]);   // of the waves
+        const uint32_t xw = wave > 0 ? __builtin_amdgcn_readlane(xs, wave - 1) : 0, yw = wave > 0 ? __builtin_amdgcn_readlane(ys, wave - 1) : 0;
         const int i = b - r0;
-        if (i >= 0 && i < mine) s_row[i] = row, s_first[i] = first, s_len[i] = len, s_new[i] = n, s_held[i] = held, s_more[i] = need;
+        if (i >= 0 && i < mine) {
+            s_row[i] = add_sat(tot_n, add_sat(xw, x)) - n, s_first[i] = add_sat(tot_need, add_sat(yw, y)) - need;   // (looked at only if the totals are right)
+            s_len[i] = len, s_new[i] = n, s_held[i] = held, s_more[i] = need;
+        }
+        tot_n = add_sat(tot_n, __builtin_amdgcn_readlane(xs, 15));
+        tot_need = add_sat(tot_need, __builtin_amdgcn_readlane(ys, 15));
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        tot_n += __shfl_xor(tot_n, o, 64);
-        tot_need += __shfl_xor(tot_need, o, 64);
-    }
-    if (lane == 0) s_tot_n[wave] = tot_n, s_tot_need[wave] = tot_need;
     if (bad) atomicOr(&s_bad, bad);
     asm volatile("" ::"v"(given));   // has been read
     __syncthreads();
@@ -78,12 +81,9 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void kv_plan_kernel(KvPlanArgs a) 
     const int wgs = gridDim.x * gridDim.y;
     int arrived = 0;
     if (tid == 0 && wgs > 1) arrived = atomicAdd(a.ticket, 1);
-    tot_n = tot_need = 0;
-#pragma unroll
-    for (int w = 0; w < PLAN_WAVES; ++w) tot_n += s_tot_n[w], tot_need += s_tot_need[w];
     bad = s_bad;
-    if (!bad && tot_n > a.max_rows) bad = RS_FLAG_LENGTHS;
-    if (!bad && tot_need > n_free) bad = RS_FLAG_NO_BLOCKS;
+    if (!bad && tot_n > (uint32_t)a.max_rows) bad = RS_FLAG_LENGTHS;
+    if (!bad && tot_need > (uint32_t)n_free) bad = RS_FLAG_NO_BLOCKS;
     if (first_y) {
         for (int i = tid; i < mine; i += T) a.cu_rows[r0 + i] = bad ? 0 : s_row[i];
         if (r0 + mine == a.B && tid == 0) a.cu_rows[a.B] = bad ? 0 : (int)tot_n;

@@ -121,6 +121,28 @@ def test_a_plan_that_cannot_be_done_changes_nothing():
     c.c.destroy()
 
 
+@pytest.mark.parametrize("B,n", [(3, 2 ** 31 - 20), (4, 2 ** 30), (70, 2 ** 26), (2000, 2 ** 22 + 1)])
+def test_sums_that_pass_32_bits(B, n):
+    """Counts that fit their tables (whose entries nobody reads) and whose sum is 0, small or negative in 32 bits: too many rows, nothing is done."""
+    c = Step((1, 1, 64), 8, max_batch=1, seed=5)
+    p = Plan([0] * B, [1] * B, [0] * B, np.full((B, 1), -1, np.int32), np.arange(8, dtype=np.int32))
+    p.new.copy_(i32([n] * B))
+    torch.cuda.synchronize()
+    c.c.kv_plan(1, p.lens, p.new, p.held, p.tab, 2 ** 27 - 1, B, p.free, p.cap, p.n_free, 2 ** 31 - 1, p.cu, p.pos, p.slots, p.held_out, p.n_free_out)
+    with pytest.raises(rs.RapidServeError) as e:
+        c.c.sync(1)
+    assert e.value.code == rs.RS_ERR_BAD_ARG
+    assert p.cu.tolist() == [0] * (B + 1) and p.n_free_out.tolist() == [8] and bool((p.tab == -1).all()) and bool((p.pos == -9).all())
+    # as many rows as the bound allows, but more blocks than there are
+    p.new.copy_(i32([2 ** 31 // 4096] * B))
+    torch.cuda.synchronize()
+    c.c.kv_plan(1, p.lens, p.new, p.held, p.tab, 2 ** 27 - 1, B, p.free, p.cap, p.n_free, 2 ** 31 - 1, p.cu, p.pos, p.slots, p.held_out, p.n_free_out)
+    with pytest.raises(rs.RapidServeError) as e:
+        c.c.sync(1)
+    assert e.value.code == rs.RS_ERR_NO_BLOCKS and p.cu.tolist() == [0] * (B + 1) and bool((p.tab == -1).all())
+    c.c.destroy()
+
+
 def test_ids_outside_the_pool_and_parents_that_come_later():
     c = Step((1, 1, 64), 40, max_batch=1, seed=3)
     free = np.array([5, 40, 7], np.int32)   # taken from the end: 7, then 40, which is none
