@@ -132,7 +132,7 @@ void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &a);
 #define RS_FLAG_NO_BLOCKS 16   // a plan needs more blocks than are free
 #define RS_FLAG_LENGTHS 32     // row counts, lengths or parents that contradict each other
 #define MASKED_COLS 128        // columns, (row, query head of a kv head), of a unit
-#define MASKED_PIECES 256      // most pieces of units whose keys are cut, in a launch
+#define MASKED_PIECES 256      // most pieces of units whose keys are cut, in a launch: the compute units
 #define MASKED_MAX_CUT 32      // and most of one unit
 struct MaskedAttnArgs {
     const bf16_t *q;          // rows of Hq * hd, q_stride elements apart
@@ -156,7 +156,7 @@ struct MaskedAttnArgs {
     int max_rows = 0, max_draft = 0;
     SeqInfo seq{};            // else prompts: request r's rows are its tokens start[r] ..
     int32_t *tickets = nullptr;   // [MASKED_PIECES], 0 between launches
-    int unit_rows = 0, n_units = 0, units_per_req = 0, cut = 1;   // set by masked_form
+    int unit_rows = 0, n_units = 0, units_per_req = 0, cut = 1;   // set by masked_form (cut: of trees' units the most)
 };
 // Units of up to 32 columns by four or eight waves; of up to 128 by four, or by two teams of four.
 enum MaskedKind { MASKED_FEW4, MASKED_FEW8, MASKED_WIDE, MASKED_TEAMS };

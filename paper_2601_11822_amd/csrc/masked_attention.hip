@@ -137,10 +137,56 @@ __device__ __forceinline__ bf16_t *out_at(const MaskedAttnArgs &a, const Span &s
     return a.out + (size_t)(s.row0 + col / G) * a.out_stride + (size_t)(hk * G + col % G) * a.hd;
 }
 
-// Pieces of a unit's keys leave their sums in part_o [piece][column][hd] and part_ml (maximum of raw scores, sum); the last workgroup of a
-// (unit, kv head) to arrive brings them together, in the pieces' order, so that results do not depend on which one that is.  The sums
-// are written and read as relaxed atomics of the device's scope, which pass the XCDs' own L2 caches by; a workgroup's have arrived when
-// its waves have waited for them, in front of the ticket.  (A fence at that scope writes back and invalidates whole caches instead.)
+// A unit's keys may be cut in pieces, which leave their sums in part_o [piece][column][hd] and part_ml (maximum of raw scores, sum of weights).
+struct Piece {
+    int unit, piece, cut;   // of `cut` pieces (1: the whole unit)
+    int first, cols;        // place of the unit's first piece, columns of a place
+    int ticket;
+    __device__ __forceinline__ size_t at(int p, int col) const { return (size_t)(first + p) * cols + col; }
+};
+// The idx-th (unit, piece) of a kv head: the first pieces of all units, then the second ones, ...
+__device__ __forceinline__ Piece piece_of(const MaskedAttnArgs &a, int idx, int hk, int cols) {
+    const int u = idx % a.n_units, t = u * a.Hkv + hk;
+    return {u, idx / a.n_units, a.cut, t * a.cut, cols, t};
+}
+
+// Four dims of a column, its pieces taken in order (eight asked for together): get(i, &ml, &v).
+template <class Get>
+__device__ __forceinline__ bf16x4 join_column(const MaskedAttnArgs &a, int cut, Get get) {
+    constexpr int N = 8;
+    float top = NEG_INF, l = 0.f;   // over the pieces so far
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int i0 = 0; i0 < cut; i0 += N) {
+        float2 ml[N];
+        f32x4 x[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) get(min(i0 + i, cut - 1), ml[i], x[i]);
+        float m = top;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i0 + i < cut) m = fmaxf(m, ml[i].x);
+        const float ref = m == NEG_INF ? 0.f : m, keep = exp2f((top - ref) * a.scale_log2);
+        top = m;
+        l *= keep;
+        acc = acc * keep;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (i0 + i >= cut || ml[i].y == 0.f) continue;   // (a sum of nothing: a piece none of whose keys the row sees)
+            const float e = exp2f((ml[i].x - ref) * a.scale_log2);
+            l += ml[i].y * e;
+            acc += x[i] * e;
+        }
+    }
+    bf16x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(l == 0.f ? 0.f : acc[i] / l);
+    return v;
+}
+
+// Units of few columns: the last workgroup of a (unit, kv head) to arrive brings the pieces together, in their order, so that results do not
+// depend on which one that is.  The sums are written and read as relaxed atomics of the device's scope, which pass the XCDs' own L2 caches by;
+// a workgroup's have arrived when its waves have waited for them, in front of the ticket.  (A fence at that scope writes back and
+// invalidates whole caches instead.)  Units of many columns are joined by a launch of their own: 64 KB a piece are too much for one workgroup.
 __device__ __forceinline__ void put_far(float *p, float x, float y) {
     const uint64_t v = (uint64_t)__builtin_bit_cast(uint32_t, y) << 32 | __builtin_bit_cast(uint32_t, x);
     __hip_atomic_store((uint64_t *)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -149,58 +195,29 @@ __device__ __forceinline__ float2 get_far(const float *p) {
     const uint64_t v = __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return float2{__builtin_bit_cast(float, (uint32_t)v), __builtin_bit_cast(float, (uint32_t)(v >> 32))};
 }
-struct Piece {
-    size_t base;   // of the unit's first piece, in columns
-    int piece, cols;   // columns of a piece's place
-    __device__ __forceinline__ size_t at(int p, int col) const { return base + (size_t)p * cols + col; }
-};
-
-template <int HD>
-__device__ __forceinline__ void join_pieces(const MaskedAttnArgs &a, const Span &s, int hk, int unit, const Piece &pc, int threads) {
-    constexpr int N = 8;
+template <int HD, int T>
+__device__ __forceinline__ void join_pieces(const MaskedAttnArgs &a, const Span &s, int hk, const Piece &pc) {
     __shared__ int last;
     const int G = a.Hq / a.Hkv, cols = s.rows * G;
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // this wave's sums have arrived
     __syncthreads();
     if (threadIdx.x == 0) {
-        int32_t *ticket = a.tickets + unit * a.Hkv + hk;
-        last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == a.cut - 1;
+        int32_t *ticket = a.tickets + pc.ticket;
+        last = __hip_atomic_fetch_add(ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == pc.cut - 1;
         if (last) __hip_atomic_store(ticket, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
     if (!last) return;
-    for (int item = threadIdx.x; item < cols * (HD / 4); item += threads) {
-        const int col = item / (HD / 4), d = item % (HD / 4) * 4;
-        float top = NEG_INF, l = 0.f;   // over the pieces so far
-        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int i0 = 0; i0 < a.cut; i0 += N) {
-            float2 ml[N], x[N], y[N];
 #pragma unroll
-            for (int i = 0; i < N; ++i) {   // asked for together
-                const size_t at = pc.at(min(i0 + i, a.cut - 1), col);
-                ml[i] = get_far(a.part_ml + 2 * at);
-                x[i] = get_far(a.part_o + at * HD + d);
-                y[i] = get_far(a.part_o + at * HD + d + 2);
-            }
-            float m = top;
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (i0 + i < a.cut) m = fmaxf(m, ml[i].x);
-            const float ref = m == NEG_INF ? 0.f : m, keep = exp2f((top - ref) * a.scale_log2);
-            top = m;
-            l *= keep;
-            acc = acc * keep;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if (i0 + i >= a.cut || ml[i].y == 0.f) continue;   // (a sum of nothing: a piece none of whose keys the row sees)
-                const float e = exp2f((ml[i].x - ref) * a.scale_log2);
-                l += ml[i].y * e;
-                acc += f32x4{x[i].x, x[i].y, y[i].x, y[i].y} * e;
-            }
-        }
-        bf16x4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(l == 0.f ? 0.f : acc[i] / l);
+    for (int k = 0; k < 32 * (HD / 4) / T; ++k) {
+        const int item = T * k + threadIdx.x, col = item / (HD / 4), d = item % (HD / 4) * 4;
+        if (col >= cols) continue;
+        const bf16x4 v = join_column(a, pc.cut, [&](int i, float2 &ml, f32x4 &x) {
+            const size_t at = pc.at(i, col);
+            ml = get_far(a.part_ml + 2 * at);
+            const float2 lo = get_far(a.part_o + at * HD + d), hi = get_far(a.part_o + at * HD + d + 2);
+            x = f32x4{lo.x, lo.y, hi.x, hi.y};
+        });
         *(bf16x4 *)(out_at(a, s, col, hk, G) + d) = v;
     }
 }
@@ -240,15 +257,36 @@ __device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span
                 m = top;
             }
         }
-        if (a.cut > 1) {
+        if (pc.cut > 1) {
             const size_t at = pc.at(pc.piece, col);
-            for (int i = 0; i < D; i += 2) put_far(a.part_o + at * HD + d0 + i, o[i], o[i + 1]);
+            for (int i = 0; i < D; i += 2) put_far(a.part_o + at * HD + d0 + i, o[i], o[i + 1]);   // (whoever joins them)
             if (d0 == 0) put_far(a.part_ml + 2 * at, m, l);
         } else {
             bf16_t *p = out_at(a, s, col, hk, G) + d0;
             for (int i = 0; i < D; ++i) p[i] = (bf16_t)(l == 0.f ? 0.f : o[i] / l);
         }
     }
+}
+
+// Into how many pieces a tree's unit is cut follows from its length, in steps of `per` blocks, and all units' together, which no host knows: none is
+// to have much more than an equal share of the launch's pieces.
+__device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps, int per) {
+    if (a.cut == 1) return 1;   // (uniform, and so is the result)
+    __shared__ int64_t sums[8];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    int64_t sum = 0;   // (whole numbers: the same for every workgroup)
+    for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
+        const int n = a.cu_rows[b + 1] - a.cu_rows[b], ctx = a.ctx_lens[b];
+        if (n > 0 && n <= a.max_draft && ctx >= 0 && ctx <= a.max_ctx) sum += (int64_t)((n + a.unit_rows - 1) / a.unit_rows) * (((ctx + n + 15) / 16 + per - 1) / per);
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = 0;
+    for (int w = 0; w < waves; ++w) sum += sums[w];
+    const float share = fmaxf(1.125f * (float)sum * a.Hkv / MASKED_PIECES, 4.f);
+    return __builtin_amdgcn_readfirstlane(min(max((int)ceilf(steps / share), 1), a.cut));
 }
 
 // Units of up to 128 columns, or one of the `cut` pieces of a unit's keys, by KH teams of four waves.  A wave owns 32 columns, and of a step's keys
@@ -261,25 +299,27 @@ __device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span
 constexpr int TAB_BLOCKS = 2048, BESIDE_SCORES = 24;
 template <int HD, int KH, bool TREE>
 __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs a) {
-    constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD, BL = 4, NT = 2, BUF = 4 * KH * BLK, COLS = MASKED_COLS, T = 256 * KH;
+    constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD, BL = 4, NT = 2, BUF = 4 * KH * BLK, T = 256 * KH;
     extern __shared__ __attribute__((aligned(1024))) bf16_t smem_masked[];   // [2] K, [2] V of BUF, [4 KH waves][32][2] floats, [TAB_BLOCKS] ids, flag
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int cg = wave & 3, kh = wave >> 2;
     const int c32 = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hkv;
     // kv heads go to the XCDs in turn, so that a head's keys are in one L2 where there are eight of them
-    const int hk = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, piece = rest % a.cut, unit = rest / a.cut;
-    const Span s = unit_span<TREE>(a, unit);
+    const int hk = blockIdx.x % a.Hkv;
+    Piece pc = piece_of(a, blockIdx.x / a.Hkv, hk, MASKED_COLS);
+    const Span s = unit_span<TREE>(a, pc.unit);
     if (s.rows <= 0) return;
-    const Piece pc{((size_t)unit * a.Hkv + hk) * a.cut * COLS, piece, COLS};
     const int cols = s.rows * G;
+    if (TREE && !s.dead) pc.cut = tree_cut(a, (s.blocks + 4 * KH - 1) / (4 * KH), 4 * KH);
+    if (pc.piece >= pc.cut) return;
     if (s.dead) {
-        if (piece == 0)
+        if (pc.piece == 0)
             for (int i = threadIdx.x; i < cols * HD; i += T) out_at(a, s, i / HD, hk, G)[i % HD] = (bf16_t)0.f;
         return;
     }
     const int n_steps = (s.blocks + 4 * KH - 1) / (4 * KH);
-    const int t0 = (int)((int64_t)n_steps * piece / a.cut), t1 = (int)((int64_t)n_steps * (piece + 1) / a.cut);
+    const int t0 = (int)((int64_t)n_steps * pc.piece / pc.cut), t1 = (int)((int64_t)n_steps * (pc.piece + 1) / pc.cut);
     const int32_t *tab = a.tables + (size_t)s.req * a.max_blk;
     const float sc = a.scale_log2;
 
@@ -516,7 +556,6 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         for (int i = 0; i < 16; ++i) odd = odd || !(fabsf(o[dt][i]) < __builtin_huge_valf());
     if (__syncthreads_or(odd && col < cols)) {
         careful_unit<HD, TREE>(a, s, hk, 4 * KH * t0, min(4 * KH * t1, s.blocks), pc, T);
-        if (a.cut > 1) join_pieces<HD>(a, s, hk, unit, pc, T);
         return;
     }
 
@@ -554,16 +593,21 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
             }
     }
     const int d0 = kh * (HD / KH) + 4 * h;   // this lane's dims: d0 + 32 dt + 8 j + i
-    if (a.cut > 1) {
-        const size_t at = pc.at(piece, col);
-        if (col < cols) {
+    if (pc.cut > 1) {
+        // a column's consecutive sums are written together, through LDS
+        constexpr int ROW = HD + 4;
+        if (KH == 2) __syncthreads();   // the other team's part has been read
+        float *strip = (float *)smem_masked + cg * (32 * ROW);
 #pragma unroll
-            for (int dt = 0; dt < DT / KH; ++dt)
+        for (int dt = 0; dt < DT / KH; ++dt)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) put_far(a.part_o + at * HD + d0 + 32 * dt + 8 * (j >> 1) + 2 * (j & 1), o[dt][2 * j], o[dt][2 * j + 1]);
-            if (h == 0 && kh == 0) put_far(a.part_ml + 2 * at, ref, l_run);
+            for (int j = 0; j < 4; ++j) *(f32x4 *)(strip + c32 * ROW + d0 + 32 * dt + 8 * j) = f32x4{o[dt][4 * j], o[dt][4 * j + 1], o[dt][4 * j + 2], o[dt][4 * j + 3]};
+        if (h == 0 && kh == 0 && col < cols) *(float2 *)(a.part_ml + 2 * pc.at(pc.piece, col)) = float2{ref, l_run};
+        __syncthreads();
+        for (int i = kh; i < 32 * (HD / 4) / 64; i += KH) {
+            const int item = 64 * i + lane, c = item / (HD / 4), d = item % (HD / 4) * 4;
+            if (cg * 32 + c < cols) *(f32x4 *)(a.part_o + pc.at(pc.piece, cg * 32 + c) * HD + d) = *(const f32x4 *)(strip + c * ROW + d);
         }
-        join_pieces<HD>(a, s, hk, unit, pc, T);
         return;
     }
     // rows of out are written whole: the wave's columns (of its team's dims) through LDS
@@ -589,6 +633,24 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     }
 }
 
+// Brings the pieces of units of many columns together: a thread for four dims of a column.
+template <int HD, int KH, bool TREE>
+__global__ __launch_bounds__(256) void masked_join_kernel(MaskedAttnArgs a) {
+    const int G = a.Hq / a.Hkv, hk = blockIdx.x % a.Hkv;
+    Piece pc = piece_of(a, blockIdx.x / a.Hkv, hk, MASKED_COLS);
+    const Span s = unit_span<TREE>(a, pc.unit);
+    if (s.rows <= 0 || s.dead) return;
+    if (TREE) pc.cut = tree_cut(a, (s.blocks + 4 * KH - 1) / (4 * KH), 4 * KH);
+    const int item = blockIdx.y * 256 + threadIdx.x, col = item / (HD / 4), d = item % (HD / 4) * 4;
+    if (pc.cut == 1 || col >= s.rows * G) return;
+    const bf16x4 v = join_column(a, pc.cut, [&](int i, float2 &ml, f32x4 &x) {
+        const size_t at = pc.at(i, col);
+        ml = *(const float2 *)(a.part_ml + 2 * at);
+        x = *(const f32x4 *)(a.part_o + at * HD + d);
+    });
+    *(bf16x4 *)(out_at(a, s, col, hk, G) + d) = v;
+}
+
 // Units of up to 32 columns (decode rows, small trees): bound by reading the cache, so nothing is shared and nothing staged.  The waves take
 // tiles of 32 keys (two blocks) in turn, straight from the pools into the operands of 32x32x16 products (every load of a wave is a contiguous
 // kilobyte, or four pieces of 256 bytes); a tile's keys are asked for as soon as the products with the ones before have been issued, and so are
@@ -599,18 +661,18 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
     extern __shared__ __attribute__((aligned(16))) float smem_few[];   // [NW][32][PAD], [NW][32][2]
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c32 = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hkv;
-    const int hk = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv, piece = rest % a.cut, unit = rest / a.cut;
-    const Span s = unit_span<TREE>(a, unit);
+    const int hk = blockIdx.x % a.Hkv;
+    const Piece pc = piece_of(a, blockIdx.x / a.Hkv, hk, 32);
+    const Span s = unit_span<TREE>(a, pc.unit);
     if (s.rows <= 0) return;
-    const Piece pc{((size_t)unit * a.Hkv + hk) * a.cut * 32, piece, 32};
     const int cols = s.rows * G;
     if (s.dead) {
-        if (piece == 0)
+        if (pc.piece == 0)
             for (int i = threadIdx.x; i < cols * HD; i += 64 * NW) out_at(a, s, i / HD, hk, G)[i % HD] = (bf16_t)0.f;
         return;
     }
     const int n_tiles = (s.blocks + 1) >> 1;
-    const int t0 = (int)((int64_t)n_tiles * piece / a.cut), t1 = (int)((int64_t)n_tiles * (piece + 1) / a.cut);
+    const int t0 = (int)((int64_t)n_tiles * pc.piece / pc.cut), t1 = (int)((int64_t)n_tiles * (pc.piece + 1) / pc.cut);
     const int32_t *tab = a.tables + (size_t)s.req * a.max_blk;
     const float sc = a.scale_log2;
     const int col = c32, row = min(col, cols - 1) / G;
@@ -739,7 +801,7 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
     }
     if (__syncthreads_or(odd && col < cols)) {
         careful_unit<HD, TREE>(a, s, hk, 2 * t0, min(2 * t1, s.blocks), pc, 64 * NW);
-        if (a.cut > 1) join_pieces<HD>(a, s, hk, unit, pc, 64 * NW);
+        if (pc.cut > 1) join_pieces<HD, 64 * NW>(a, s, hk, pc);
         return;
     }
     for (int item = threadIdx.x; item < cols * (HD / 4); item += 64 * NW) {
@@ -747,16 +809,16 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
         float top = NEG_INF, l = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) top = fmaxf(top, s_ml[(w * 32 + c) * 2]);
-        const float ref = top == NEG_INF ? 0.f : top;
+        const float base = top == NEG_INF ? 0.f : top;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const float e = __builtin_amdgcn_exp2f((s_ml[(w * 32 + c) * 2] - ref) * sc);
+            const float e = __builtin_amdgcn_exp2f((s_ml[(w * 32 + c) * 2] - base) * sc);
             l += s_ml[(w * 32 + c) * 2 + 1] * e;
             acc += *(const f32x4 *)(s_o + (w * 32 + c) * PAD + d) * e;
         }
-        if (a.cut > 1) {
-            const size_t at = pc.at(piece, c);
+        if (pc.cut > 1) {
+            const size_t at = pc.at(pc.piece, c);
             put_far(a.part_o + at * HD + d, acc[0], acc[1]);
             put_far(a.part_o + at * HD + d + 2, acc[2], acc[3]);
             if (d == 0) put_far(a.part_ml + 2 * at, top, l);
@@ -768,7 +830,7 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
         for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(acc[i] * inv);
         *(bf16x4 *)(out_at(a, s, c, hk, G) + d) = v;
     }
-    if (a.cut > 1) join_pieces<HD>(a, s, hk, unit, pc, 64 * NW);
+    if (pc.cut > 1) join_pieces<HD, 64 * NW>(a, s, hk, pc);
 }
 
 constexpr int wide_lds(int hd, int kh) { return 4 * 4 * kh * 16 * hd * 2 + 4 * kh * 64 * 4 + (TAB_BLOCKS + 1) * 4; }
@@ -784,6 +846,10 @@ void launch(hipStream_t st, const MaskedAttnArgs &a, const MaskedForm &f) {
         case MASKED_WIDE: hipLaunchKernelGGL((masked_wide_kernel<HD, 1, TREE>), grid, dim3(256), wide_lds(HD, 1), st, a); break;
         case MASKED_TEAMS: hipLaunchKernelGGL((masked_wide_kernel<HD, 2, TREE>), grid, dim3(512), wide_lds(HD, 2), st, a); break;
     }
+    if (a.cut == 1) return;
+    const int cols = a.unit_rows * (a.Hq / a.Hkv);
+    const dim3 joins(a.n_units * a.Hkv, (cols * (HD / 4) + 255) / 256);
+    if (f.kind == MASKED_TEAMS) hipLaunchKernelGGL((masked_join_kernel<HD, 2, TREE>), joins, dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -817,12 +883,16 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
     const int64_t wgs = (int64_t)a.n_units * a.Hkv;
     if (wgs <= 0) return f;
     const int tiles = (keys + 63) / 64;
+    const auto cut = [&](int least) {   // pieces of `least` tiles or more, none but the first for each compute unit
+        return (int)std::max<int64_t>(1, std::min<int64_t>({MASKED_PIECES / wgs, MASKED_MAX_CUT, tiles / least}));
+    };
+    const bool alone = wgs <= MASKED_PIECES;   // every workgroup has a compute unit to itself
     if (few) {
-        f.kind = wgs <= 256 ? MASKED_FEW8 : MASKED_FEW4;
-        a.cut = (int)std::max<int64_t>(1, std::min<int64_t>({256 / wgs, MASKED_MAX_CUT, (tiles + 1) / 2}));
+        f.kind = alone ? MASKED_FEW8 : MASKED_FEW4;
+        a.cut = cut(2);
     } else {
-        f.kind = wgs <= 256 ? MASKED_TEAMS : MASKED_WIDE;
-        a.cut = (int)std::max<int64_t>(1, std::min<int64_t>({256 / wgs, MASKED_MAX_CUT, (tiles + 7) / 8}));
+        f.kind = alone ? MASKED_TEAMS : MASKED_WIDE;
+        a.cut = cut(4);
     }
     return f;
 }
