@@ -6,8 +6,8 @@
 //   tree:    j < ctx, and ctx + t for every bit t of the row's ancestor mask.
 // A row that sees nothing gets zero.  What a key holds that a row does not see, NaN included, does not reach that row.
 //
-// A UNIT is as many rows of one request and one kv head as fill 128 columns, a column being (row, query head of the group): the
-// keys of a block are read once for all of them.  The blocks that any row of a unit sees are counted through (`Span`): those of the
+// A UNIT is as many rows of one request and one kv head as fit in 128 columns, or 32, a column being (row, query head of the group): the
+// keys of a block are read once for all of them.  Where units are fewer than compute units, each one's keys are cut in pieces.  The blocks that any row of a unit sees are counted through (`Span`): those of the
 // sinks, then those of the windows; blocks between are not looked at, nor are their table entries.
 #include <algorithm>
 #include <type_traits>
@@ -268,16 +268,16 @@ __device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span
     }
 }
 
-// Into how many pieces a tree's unit is cut follows from its length, in steps of `per` blocks, and all units' together, which no host knows: none is
+// Into how many pieces a tree's unit is cut follows from its length, in steps of 64 keys, and all units' together, which no host knows: none is
 // to have much more than an equal share of the launch's pieces.
-__device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps, int per) {
+__device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps) {
     if (a.cut == 1) return 1;   // (uniform, and so is the result)
     __shared__ int64_t sums[8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     int64_t sum = 0;   // (whole numbers: the same for every workgroup)
     for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
         const int n = a.cu_rows[b + 1] - a.cu_rows[b], ctx = a.ctx_lens[b];
-        if (n > 0 && n <= a.max_draft && ctx >= 0 && ctx <= a.max_ctx) sum += (int64_t)((n + a.unit_rows - 1) / a.unit_rows) * (((ctx + n + 15) / 16 + per - 1) / per);
+        if (n > 0 && n <= a.max_draft && ctx >= 0 && ctx <= a.max_ctx) sum += (int64_t)((n + a.unit_rows - 1) / a.unit_rows) * ((ctx + n + 63) >> 6);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
@@ -290,17 +290,23 @@ __device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps, int 
 }
 
 // Units of up to 128 columns, or one of the `cut` pieces of a unit's keys, by KH teams of four waves.  A wave owns 32 columns, and of a step's keys
-// (64, four blocks, for each team) those of its team.  Keys come by LDS-DMA into two buffers of K and two of V, a step ahead; all waves of a
-// team use them.  S^T = K Q^T and O^T = V^T P^T, so that a lane owns one column; the teams' sums are brought together at the end.
+// its team's share.  Keys come by LDS-DMA into N buffers of K and N of V, used by all waves.  One team, of which two workgroups share a compute
+// unit, takes 64 keys a step and has two buffers; two teams have, for trees, four of 64 keys, and for prompts, whose rows end at
+// different steps, two of 128 (us with four buffers / with two, 8B heads: 32 trees of 32 rows behind 2300 tokens 60.3 / 64.8, sixteen behind
+// 500 to 4096 57.4 / 60.8; a prompt of 1024 rows 29.0 / 25.9, 512 rows behind 3000 under a window of 2048 39.3 / 36.5).  S^T = K Q^T and O^T = V^T P^T, so that a lane owns one column; the teams' sums are
+// brought together at the end.
 // What runs beside the matrix unit is written out: the products of the next step's scores alternate with most of this one's exponentials, the
 // products with V with the rest of them and with the next step's maxima.  (A product takes 16 ns of a SIMD; an exponential, its multiplication
 // and two additions beside it one more.)
 // The exponentials' reference is the row's first maximum, moved to the running one once a score is 2^4 above it: two steps in three need no rescaling.
-constexpr int TAB_BLOCKS = 2048, BESIDE_SCORES = 24;
+constexpr int TAB_BLOCKS = 2048;
+constexpr int step_blocks(int teams, bool tree) { return teams == 2 && !tree ? 8 : 4; }
 template <int HD, int KH, bool TREE>
 __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs a) {
-    constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD, BL = 4, NT = 2, BUF = 4 * KH * BLK, T = 256 * KH;
-    extern __shared__ __attribute__((aligned(1024))) bf16_t smem_masked[];   // [2] K, [2] V of BUF, [4 KH waves][32][2] floats, [TAB_BLOCKS] ids, flag
+    constexpr int STEP = step_blocks(KH, TREE), BL = STEP / KH, NT = BL / 2, N = 8 * KH / STEP;   // blocks of a step, a team's; its tiles of 32 keys; buffers
+    constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD, BUF = STEP * BLK, T = 256 * KH;
+    constexpr int WPB = 4 * KH / STEP, LOADS = HD / 32 / WPB;   // waves for a block; loads of a wave for a step's K, and for its V
+    extern __shared__ __attribute__((aligned(1024))) bf16_t smem_masked[];   // [N] K, [N] V of BUF, [4 KH waves][32][2] floats, [TAB_BLOCKS] ids, flag
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int cg = wave & 3, kh = wave >> 2;
     const int c32 = lane & 31, h = lane >> 5;
@@ -311,14 +317,14 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     const Span s = unit_span<TREE>(a, pc.unit);
     if (s.rows <= 0) return;
     const int cols = s.rows * G;
-    if (TREE && !s.dead) pc.cut = tree_cut(a, (s.blocks + 4 * KH - 1) / (4 * KH), 4 * KH);
+    if (TREE && !s.dead) pc.cut = tree_cut(a, (s.blocks + 3) >> 2);
     if (pc.piece >= pc.cut) return;
     if (s.dead) {
         if (pc.piece == 0)
             for (int i = threadIdx.x; i < cols * HD; i += T) out_at(a, s, i / HD, hk, G)[i % HD] = (bf16_t)0.f;
         return;
     }
-    const int n_steps = (s.blocks + 4 * KH - 1) / (4 * KH);
+    const int n_steps = (s.blocks + STEP - 1) / STEP;
     const int t0 = (int)((int64_t)n_steps * pc.piece / pc.cut), t1 = (int)((int64_t)n_steps * (pc.piece + 1) / pc.cut);
     const int32_t *tab = a.tables + (size_t)s.req * a.max_blk;
     const float sc = a.scale_log2;
@@ -333,15 +339,15 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     }
     // of the wave's rows: positions of the first and of the last; steps behind what the last one sees are not the wave's
     const int w_first = s.first + min(cg * 32, cols - 1) / G, w_last = s.first + min(cg * 32 + 31, cols - 1) / G;
-    const int w_end = cg * 32 >= cols ? t0 : TREE ? t1 : min(t1, ((w_last >> 4) - s.skip) / (4 * KH) + 1);
+    const int w_end = cg * 32 >= cols ? t0 : TREE ? t1 : min(t1, ((w_last >> 4) - s.skip) / STEP + 1);
 
     // Block ids of TAB_BLOCKS counted blocks from step tb on, in LDS: -1: none, or not one of the pool, of which there are some where *s_bad.  (Fetched
     // step by step into registers they would be waited for by a count of the loads behind them, which the compiler takes to be none where some are
     // under a branch: so all loads in flight would be waited for in every step.)
-    int32_t *s_tab = (int32_t *)(smem_masked + 4 * BUF) + 4 * KH * 64, *s_bad = s_tab + TAB_BLOCKS;
+    int32_t *s_tab = (int32_t *)(smem_masked + 2 * N * BUF) + 4 * KH * 64, *s_bad = s_tab + TAB_BLOCKS;
     auto fill_tab = [&](int tb) {
-        for (int i = threadIdx.x; i < min(TAB_BLOCKS, 4 * KH * (t1 - tb)); i += T) {
-            const int j = 4 * KH * tb + i;
+        for (int i = threadIdx.x; i < min(TAB_BLOCKS, STEP * (t1 - tb)); i += T) {
+            const int j = STEP * tb + i;
             int id = -1;
             if (j < s.blocks) {
                 id = tab[j < s.sink_blocks ? j : j + s.skip];
@@ -355,31 +361,30 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         }
     };
     int tb = t0;   // the first step of s_tab
-    // Wave w brings block w of a step, 16 bytes a lane (lane l's at the window's base + 16 l).  K keeps the pool's order; V's chunk (dim, half of
-    // 8 tokens) goes to [half][dim].  A block that is missing is read as block 0, and masked.
+    // Wave w brings block w of a step (or half w & 1 of block w / 2), 16 bytes a lane (lane l's at the window's base + 16 l).  K keeps the
+    // pool's order; V's chunk (dim, half of 8 tokens) goes to [half][dim].  A block that is missing is read as block 0, and masked.
     typedef __attribute__((address_space(3))) void lds_void;
+    const int wb = wave / WPB, wp = wave % WPB;
     auto head_of = [&](int t) {
-        const int id = __builtin_amdgcn_readfirstlane(s_tab[4 * KH * (t - tb) + wave]);
+        const int id = __builtin_amdgcn_readfirstlane(s_tab[STEP * (t - tb) + wb]);
         return ((size_t)max(id, 0) * a.Hkv + hk) * BLK;
     };
-    auto k_at = [&](int t) { return smem_masked + ((t - t0) & 1) * BUF; };
-    auto v_at = [&](int t) { return smem_masked + (2 + ((t - t0) & 1)) * BUF; };
+    auto k_at = [&](int t) { return smem_masked + ((t - t0) & (N - 1)) * BUF; };
+    auto v_at = [&](int t) { return smem_masked + (N + ((t - t0) & (N - 1))) * BUF; };
     auto load_k = [&](int t) {
         const auto buf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.k_pool + head_of(t)), 0, 2 * BLK, 0x00020000);
-        auto *d = (lds_void *)(k_at(t) + wave * BLK);   // (a constant offset counts in LDS too, a scalar one does not)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, d, 16, lane * 16, 0, 0, 0);
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, d, 16, lane * 16, 0, 1024, 0);
-        if constexpr (HD == 128) {
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, d, 16, lane * 16, 0, 2048, 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, d, 16, lane * 16, 0, 3072, 0);
-        }
+        bf16_t *d = k_at(t) + wb * BLK + wp * (BLK / 2);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void *)(d + i * 512), 16, lane * 16, wp * BLK + i * 1024, 0, 0);
     };
     auto load_v = [&](int t) {
         const auto buf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.v_pool + head_of(t)), 0, 2 * BLK, 0x00020000);
-        bf16_t *d = v_at(t) + wave * BLK;
+        bf16_t *d = v_at(t) + wb * BLK + wp * (BLK / 2);
 #pragma unroll
-        for (int i = 0; i < HD / 32; ++i)   // 64 dims of a half
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void *)(d + i * 512), 16, lane * 32, (i % (HD / 64)) * 2048 + (i / (HD / 64)) * 16, 0, 0);
+        for (int i = 0; i < LOADS; ++i) {   // 64 dims of a half of the tokens
+            const int at = wp * LOADS + i;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void *)(d + i * 512), 16, lane * 32, (at % (HD / 64)) * 2048 + (at / (HD / 64)) * 16, 0, 0);
+        }
     };
     auto klds = [](int r, int cc) { return (r >> 4) * BLK + kpool_chunk_offset(r & 15, cc * 8); };
     auto vlds = [](int blk, int half, int d) { return blk * BLK + half * (8 * HD) + d * 8; };
@@ -404,7 +409,7 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     };
     constexpr int N_K = NT * KS, R = 4;
     auto scores = [&](int t, f32x16 (&st)[NT], auto between) {   // between(i): what goes beside the i-th product
-        const bf16_t *ks = k_at(t) + kh * (4 * BLK);
+        const bf16_t *ks = k_at(t) + kh * (BL * BLK);
         // K fragment i = (score tile i % NT, head_dim step i / NT), read R fragments ahead of its product
         auto kread = [&](int i) { return *(const bf16x8 *)&ks[klds(32 * (i % NT) + c32, 2 * (i / NT) + h)]; };
         bf16x8 kf[R];
@@ -415,6 +420,8 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         for (int e = 0; e < 16; ++e) zero[e] = 0.f;
 #pragma unroll
         for (int i = 0; i < N_K; ++i) {
+            if (i == 0) __builtin_amdgcn_s_setprio(1);   // in front of the other workgroup's waves (16384 rows, window 4096: 975 us without, 963 with)
+            if (i == N_K - 1) __builtin_amdgcn_s_setprio(0);
             st[i % NT] = mfma32(kf[i % R], qf[i / NT], i < NT ? zero : st[i % NT]);
             __builtin_amdgcn_sched_barrier(0);
             if (i + R < N_K) kf[i % R] = kread(i + R);
@@ -429,8 +436,8 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         bool here[BL], full = true;
 #pragma unroll
         for (int j = 0; j < BL; ++j) {
-            const int e = 4 * (KH * t + kh) + j, p = 16 * (e < s.sink_blocks ? e : e + s.skip);
-            here[j] = e < s.blocks && !(bad && __builtin_amdgcn_readfirstlane(s_tab[4 * (KH * (t - tb) + kh) + j]) < 0);
+            const int e = STEP * t + BL * kh + j, p = 16 * (e < s.sink_blocks ? e : e + s.skip);
+            here[j] = e < s.blocks && !(bad && __builtin_amdgcn_readfirstlane(s_tab[STEP * (t - tb) + BL * kh + j]) < 0);
             pos[j] = p;
             full = full && here[j] && (TREE ? p + 15 < s.first : p + 15 <= w_first && (p > w_last - a.window || p + 15 < a.sinks));
         }
@@ -469,9 +476,9 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         limit = moves ? m + behind : limit;
     };
     // products with V of step t; weights from N0 on are formed beside them (of a block in front of it), then the next step's maximum
-    constexpr int N_V = BL * DT, N0 = BESIDE_SCORES;
+    constexpr int N_V = BL * DT, N0 = BL == 4 ? 24 : 8;
     auto values = [&](int t, const f32x16 (&cur)[NT], const f32x16 (&nxt)[NT]) {
-        const bf16_t *vs = v_at(t) + kh * (4 * BLK);
+        const bf16_t *vs = v_at(t) + kh * (BL * BLK);
         auto vread = [&](int i) { return *(const bf16x8 *)&vs[vlds(i / DT, h, 32 * (i % DT) + c32)]; };
         // the weights left are due before the last block's products: so many beside each product before those
         constexpr int SLOTS = DT * (BL - 1), EACH = (N_W - N0 + SLOTS - 1) / SLOTS, RV = 4;
@@ -500,18 +507,19 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     for (int i = 0; i < KS; ++i) asm volatile("" : "+v"(qf[i]));   // the queries are here: not to be waited for among the steps' loads
     __syncthreads();
     bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
-    // In front of step t's work: K of the step after it and V of its own have landed, nobody reads those of the step before any more; their
-    // buffers take K two steps ahead and V of the next.
+    // In front of step t's work: K of the step after it and V of its own have landed (of the wave's loads at most those behind them are in flight),
+    // nobody reads those of the step before any more; their buffers take K and V of the step N ahead.
     auto turn = [&](int t) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (4 * KH * (t + 3 - tb) > TAB_BLOCKS && t + 1 < t1) {   // contexts of more than 32K tokens
+        if (N > 2 && t + N - 1 < t1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((N - 2) * 2 * LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (STEP * (t + N + 1 - tb) > TAB_BLOCKS && t + 1 < t1) {   // contexts of more than 32K tokens
             tb = t;
             fill_tab(tb);
             __syncthreads();
             bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
         }
-        if (t + 2 < t1) load_k(t + 2);
-        if (t + 1 < t1) load_v(t + 1);
+        if (t + N < t1) load_k(t + N);
+        if (t + N - 1 < t1) load_v(t + N - 1);
     };
     auto step = [&](int t, f32x16 (&cur)[NT], f32x16 (&nxt)[NT]) {
         turn(t);
@@ -534,9 +542,13 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     f32x16 sa[NT], sb[NT];
     if (t0 < t1) {
         load_k(t0);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (t0 + 1 < t1) load_k(t0 + 1);
-        load_v(t0);
+#pragma unroll
+        for (int i = 1; i < N; ++i) {
+            if (t0 + i < t1) load_k(t0 + i);
+            if (t0 + i - 1 < t1) load_v(t0 + i - 1);
+        }
+        if (t0 + N - 1 < t1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((N - 1) * 2 * LOADS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (t0 < w_end) {
             scores(t0, sa, [](int) {});
             mask(t0, sa);
@@ -555,7 +567,7 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
 #pragma unroll
         for (int i = 0; i < 16; ++i) odd = odd || !(fabsf(o[dt][i]) < __builtin_huge_valf());
     if (__syncthreads_or(odd && col < cols)) {
-        careful_unit<HD, TREE>(a, s, hk, 4 * KH * t0, min(4 * KH * t1, s.blocks), pc, T);
+        careful_unit<HD, TREE>(a, s, hk, STEP * t0, min(STEP * t1, s.blocks), pc, T);
         return;
     }
 
@@ -563,7 +575,7 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         // both waves of a column rescale to the common reference; the first finishes the first half of head_dim, the second the other, each with the
         // other's part through the buffers (nobody reads those any more)
         f32x4 *x_o = (f32x4 *)smem_masked;   // [8 waves][2 DT][64]
-        float *x_ml = (float *)(smem_masked + 4 * BUF), *mine = x_ml + wave * 64, *theirs = x_ml + (wave ^ 4) * 64;
+        float *x_ml = (float *)(smem_masked + 2 * N * BUF), *mine = x_ml + wave * 64, *theirs = x_ml + (wave ^ 4) * 64;
         if (h == 0) {
             mine[2 * c32] = ref;
             mine[2 * c32 + 1] = l_run;
@@ -634,13 +646,13 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
 }
 
 // Brings the pieces of units of many columns together: a thread for four dims of a column.
-template <int HD, int KH, bool TREE>
+template <int HD, bool TREE>
 __global__ __launch_bounds__(256) void masked_join_kernel(MaskedAttnArgs a) {
     const int G = a.Hq / a.Hkv, hk = blockIdx.x % a.Hkv;
     Piece pc = piece_of(a, blockIdx.x / a.Hkv, hk, MASKED_COLS);
     const Span s = unit_span<TREE>(a, pc.unit);
     if (s.rows <= 0 || s.dead) return;
-    if (TREE) pc.cut = tree_cut(a, (s.blocks + 4 * KH - 1) / (4 * KH), 4 * KH);
+    if (TREE) pc.cut = tree_cut(a, (s.blocks + 3) >> 2);
     const int item = blockIdx.y * 256 + threadIdx.x, col = item / (HD / 4), d = item % (HD / 4) * 4;
     if (pc.cut == 1 || col >= s.rows * G) return;
     const bf16x4 v = join_column(a, pc.cut, [&](int i, float2 &ml, f32x4 &x) {
@@ -833,7 +845,7 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
     if (pc.cut > 1) join_pieces<HD, 64 * NW>(a, s, hk, pc);
 }
 
-constexpr int wide_lds(int hd, int kh) { return 4 * 4 * kh * 16 * hd * 2 + 4 * kh * 64 * 4 + (TAB_BLOCKS + 1) * 4; }
+constexpr int wide_lds(int hd, int kh) { return 4 * kh * 4 * 16 * hd * 2 + 4 * kh * 64 * 4 + (TAB_BLOCKS + 1) * 4; }
 
 constexpr int few_lds(int hd, int nw) { return nw * 32 * (hd + 4 + 2) * 4; }
 
@@ -849,7 +861,7 @@ void launch(hipStream_t st, const MaskedAttnArgs &a, const MaskedForm &f) {
     if (a.cut == 1) return;
     const int cols = a.unit_rows * (a.Hq / a.Hkv);
     const dim3 joins(a.n_units * a.Hkv, (cols * (HD / 4) + 255) / 256);
-    if (f.kind == MASKED_TEAMS) hipLaunchKernelGGL((masked_join_kernel<HD, 2, TREE>), joins, dim3(256), 0, st, a);
+    if (f.kind == MASKED_TEAMS) hipLaunchKernelGGL((masked_join_kernel<HD, TREE>), joins, dim3(256), 0, st, a);
 }
 
 }  // namespace
@@ -862,24 +874,23 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
     else if (!a.ctx_lens)
         for (int r = 0; r < a.seq.n_req; ++r) most = std::max(most, a.seq.cu[r + 1] - a.seq.cu[r]);
     MaskedForm f{};
-    const bool few = most * G <= 32;
+    const auto units = [&](int rows) {   // of so many rows
+        if (tree) return a.B * ((a.max_draft + rows - 1) / rows);
+        if (a.ctx_lens) return a.B;
+        int n = 0;
+        for (int r = 0; r < a.seq.n_req; ++r) n += (a.seq.cu[r + 1] - a.seq.cu[r] + rows - 1) / rows;
+        return n;
+    };
+    int keys = tree || a.ctx_lens ? a.max_ctx : 0;   // most keys of a row
+    for (int r = 0; !tree && !a.ctx_lens && r < a.seq.n_req; ++r) keys = std::max(keys, a.seq.start[r] + a.seq.cu[r + 1] - a.seq.cu[r]);
+    if (!tree) keys = (int)std::min<int64_t>(keys, (int64_t)a.window + a.sinks + 32);
+    // Units of 32 columns where a request has no more, or where reading the keys again for each of them is little: us with units of 32 / of 128,
+    // 8B heads: a tree of 16 behind 900 tokens 12.7 / 18.2, eight of them 18.2 / 21.8, one of 60 behind 3500 19.9 / 23.2, four of 32
+    // behind 4000 31.9 / 30.2, sixteen of 32 behind 500 to 4096 67.5 / 57.4; 100 rows under a window of 2048 20.4 / 20.9, 512 42.4 / 36.5.
+    const bool few = most * G <= 32 || (int64_t)units(32 / G) * a.Hkv * keys <= 256 * 1024;
     a.unit_rows = (few ? 32 : MASKED_COLS) / G;
-    int keys = 0;   // most keys of a unit
-    if (tree) {
-        a.units_per_req = (a.max_draft + a.unit_rows - 1) / a.unit_rows;
-        a.n_units = a.B * a.units_per_req;
-        keys = a.max_ctx;
-    } else if (a.ctx_lens) {
-        a.n_units = a.B;
-        keys = a.max_ctx;
-    } else {
-        a.n_units = 0;
-        for (int r = 0; r < a.seq.n_req; ++r) {
-            a.n_units += (a.seq.cu[r + 1] - a.seq.cu[r] + a.unit_rows - 1) / a.unit_rows;
-            keys = std::max(keys, a.seq.start[r] + a.seq.cu[r + 1] - a.seq.cu[r]);
-        }
-    }
-    if (!tree) keys = (int)std::min<int64_t>(keys, (int64_t)a.window + a.sinks + a.unit_rows + 32);
+    a.units_per_req = (a.max_draft + a.unit_rows - 1) / a.unit_rows;
+    a.n_units = units(a.unit_rows);
     const int64_t wgs = (int64_t)a.n_units * a.Hkv;
     if (wgs <= 0) return f;
     const int tiles = (keys + 63) / 64;
