@@ -276,8 +276,8 @@ __device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     int64_t sum = 0;   // (whole numbers: the same for every workgroup)
     for (int b = threadIdx.x; b < a.B; b += blockDim.x) {
-        const int n = a.cu_rows[b + 1] - a.cu_rows[b], ctx = a.ctx_lens[b];
-        if (n > 0 && n <= a.max_draft && ctx >= 0 && ctx <= a.max_ctx) sum += (int64_t)((n + a.unit_rows - 1) / a.unit_rows) * ((ctx + n + 63) >> 6);
+        const int n = (int)((uint32_t)a.cu_rows[b + 1] - (uint32_t)a.cu_rows[b]), ctx = a.ctx_lens[b];
+        if (n > 0 && n <= a.max_draft && ctx >= 0 && ctx <= a.max_ctx - n) sum += (int64_t)((n + a.unit_rows - 1) / a.unit_rows) * ((ctx + n + 63) >> 6);
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
