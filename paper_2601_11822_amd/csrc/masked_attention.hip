@@ -365,20 +365,22 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     // pool's order; V's chunk (dim, half of 8 tokens) goes to [half][dim].  A block that is missing is read as block 0, and masked.
     typedef __attribute__((address_space(3))) void lds_void;
     const int wb = wave / WPB, wp = wave % WPB;
-    auto head_of = [&](int t) {
-        const int id = __builtin_amdgcn_readfirstlane(s_tab[STEP * (t - tb) + wb]);
-        return ((size_t)max(id, 0) * a.Hkv + hk) * BLK;
-    };
+    auto id_of = [&](int t) { return s_tab[min(STEP * (t - tb) + wb, TAB_BLOCKS - 1)]; };   // (behind the last step: not used)
+    auto head_of = [&](int id) { return ((size_t)max(__builtin_amdgcn_readfirstlane(id), 0) * a.Hkv + hk) * BLK; };
+    size_t head_k = 0, head_v = 0;   // of the block that the wave brings next, for K; V follows a step behind
+    int id_next = -1;                // asked for a step ahead
     auto k_at = [&](int t) { return smem_masked + ((t - t0) & (N - 1)) * BUF; };
     auto v_at = [&](int t) { return smem_masked + (N + ((t - t0) & (N - 1))) * BUF; };
     auto load_k = [&](int t) {
-        const auto buf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.k_pool + head_of(t)), 0, 2 * BLK, 0x00020000);
+        head_v = head_k;
+        head_k = head_of(id_next);
+        const auto buf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.k_pool + head_k), 0, 2 * BLK, 0x00020000);
         bf16_t *d = k_at(t) + wb * BLK + wp * (BLK / 2);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void *)(d + i * 512), 16, lane * 16, wp * BLK + i * 1024, 0, 0);
     };
-    auto load_v = [&](int t) {
-        const auto buf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.v_pool + head_of(t)), 0, 2 * BLK, 0x00020000);
+    auto load_v = [&](int t, size_t head) {
+        const auto buf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.v_pool + head), 0, 2 * BLK, 0x00020000);
         bf16_t *d = v_at(t) + wb * BLK + wp * (BLK / 2);
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {   // 64 dims of a half of the tokens
@@ -407,14 +409,25 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         pf[j][i] = (bf16_t)p;
         if (i == 7) pf[j] = by_tokens(pf[j]);
     };
-    constexpr int N_K = NT * KS, R = 4;
-    auto scores = [&](int t, f32x16 (&st)[NT], auto between) {   // between(i): what goes beside the i-th product
-        const bf16_t *ks = k_at(t) + kh * (BL * BLK);
-        // K fragment i = (score tile i % NT, head_dim step i / NT), read R fragments ahead of its product
-        auto kread = [&](int i) { return *(const bf16x8 *)&ks[klds(32 * (i % NT) + c32, 2 * (i / NT) + h)]; };
-        bf16x8 kf[R];
+    // Fragments of K and V are read R ahead of their products, through one ring: while the last of K are used the first of V are read.  (With the block
+    // ids a step ahead 16384 rows under a window of 4096 take 929 us instead of 940, 64 trees of 16 rows 126.5 instead of 129.4; reading the
+    // next step's first K beside the last of V as well gives nothing more.)
+    constexpr int N_K = NT * KS, N_V = BL * DT, R = 4;
+    static_assert(N_K % R == 0 && N_V % R == 0);
+    bf16x8 ring[R];
+    auto kread = [&](int t, int i) {   // (score tile i % NT, head_dim step i / NT)
+        return *(const bf16x8 *)&(k_at(t) + kh * (BL * BLK))[klds(32 * (i % NT) + c32, 2 * (i / NT) + h)];
+    };
+    auto vread = [&](int t, int i) { return *(const bf16x8 *)&(v_at(t) + kh * (BL * BLK))[vlds(i / DT, h, 32 * (i % DT) + c32)]; };
+    auto ring_k = [&](int t) {
 #pragma unroll
-        for (int i = 0; i < R && i < N_K; ++i) kf[i] = kread(i);
+        for (int i = 0; i < R; ++i) ring[i] = kread(t, i);
+    };
+    auto ring_v = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) ring[i] = vread(t, i);
+    };
+    auto scores = [&](int t, f32x16 (&st)[NT], auto then_v, auto between) {   // then_v: V of step t - 1 next; between(i): what goes beside the i-th product
         f32x16 zero;
 #pragma unroll
         for (int e = 0; e < 16; ++e) zero[e] = 0.f;
@@ -422,9 +435,10 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         for (int i = 0; i < N_K; ++i) {
             if (i == 0) __builtin_amdgcn_s_setprio(1);   // in front of the other workgroup's waves (16384 rows, window 4096: 975 us without, 963 with)
             if (i == N_K - 1) __builtin_amdgcn_s_setprio(0);
-            st[i % NT] = mfma32(kf[i % R], qf[i / NT], i < NT ? zero : st[i % NT]);
+            st[i % NT] = mfma32(ring[i % R], qf[i / NT], i < NT ? zero : st[i % NT]);
             __builtin_amdgcn_sched_barrier(0);
-            if (i + R < N_K) kf[i % R] = kread(i + R);
+            if (i + R < N_K) ring[i % R] = kread(t, i + R);
+            else if (then_v) ring[i % R] = vread(t - 1, i + R - N_K);
             between(i);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -476,21 +490,16 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         limit = moves ? m + behind : limit;
     };
     // products with V of step t; weights from N0 on are formed beside them (of a block in front of it), then the next step's maximum
-    constexpr int N_V = BL * DT, N0 = BL == 4 ? 24 : 8;
+    constexpr int N0 = BL == 4 ? 24 : 8;
     auto values = [&](int t, const f32x16 (&cur)[NT], const f32x16 (&nxt)[NT]) {
-        const bf16_t *vs = v_at(t) + kh * (BL * BLK);
-        auto vread = [&](int i) { return *(const bf16x8 *)&vs[vlds(i / DT, h, 32 * (i % DT) + c32)]; };
         // the weights left are due before the last block's products: so many beside each product before those
-        constexpr int SLOTS = DT * (BL - 1), EACH = (N_W - N0 + SLOTS - 1) / SLOTS, RV = 4;
-        bf16x8 vf[RV];
+        constexpr int SLOTS = DT * (BL - 1), EACH = (N_W - N0 + SLOTS - 1) / SLOTS;
         float m = NEG_INF;
 #pragma unroll
-        for (int i = 0; i < RV; ++i) vf[i] = vread(i);
-#pragma unroll
         for (int i = 0; i < N_V; ++i) {
-            o[i % DT] = mfma32(vf[i % RV], pf[i / DT], o[i % DT]);
+            o[i % DT] = mfma32(ring[i % R], pf[i / DT], o[i % DT]);
             __builtin_amdgcn_sched_barrier(0);
-            if (i + RV < N_V) vf[i % RV] = vread(i + RV);
+            if (i + R < N_V) ring[i % R] = vread(t, i + R);
 #pragma unroll
             for (int e = 0; e < EACH; ++e)
                 if (i < SLOTS && N0 + i * EACH + e < N_W) weight(cur, N0 + i * EACH + e);
@@ -512,21 +521,25 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     auto turn = [&](int t) {
         if (N > 2 && t + N - 1 < t1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((N - 2) * 2 * LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (STEP * (t + N + 1 - tb) > TAB_BLOCKS && t + 1 < t1) {   // contexts of more than 32K tokens
+        if (STEP * (t + N + 2 - tb) > TAB_BLOCKS && t + 1 < t1) {   // contexts of more than 32K tokens
             tb = t;
             fill_tab(tb);
             __syncthreads();
             bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
         }
-        if (t + N < t1) load_k(t + N);
-        if (t + N - 1 < t1) load_v(t + N - 1);
+        if (t + N < t1) {
+            load_k(t + N);
+            load_v(t + N - 1, head_v);
+            id_next = id_of(t + N + 1);
+        } else if (t + N - 1 < t1) load_v(t + N - 1, head_k);
     };
     auto step = [&](int t, f32x16 (&cur)[NT], f32x16 (&nxt)[NT]) {
         turn(t);
         if (t >= w_end) return;
         if (t + 1 < w_end) {
             constexpr int EACH = (N0 + N_K - 1) / N_K;
-            scores(t + 1, nxt, [&](int i) {
+            ring_k(t + 1);
+            scores(t + 1, nxt, std::true_type(), [&](int i) {
 #pragma unroll
                 for (int e = 0; e < EACH; ++e)
                     if (i * EACH + e < N0) weight(cur, i * EACH + e);
@@ -535,22 +548,29 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         } else {
 #pragma unroll
             for (int n = 0; n < N0; ++n) weight(cur, n);
+            ring_v(t);
         }
         const float m = values(t, cur, nxt);
         if (t + 1 < w_end) follow(m);
     };
     f32x16 sa[NT], sb[NT];
     if (t0 < t1) {
+        id_next = id_of(t0);
         load_k(t0);
 #pragma unroll
         for (int i = 1; i < N; ++i) {
-            if (t0 + i < t1) load_k(t0 + i);
-            if (t0 + i - 1 < t1) load_v(t0 + i - 1);
+            id_next = id_of(t0 + i);
+            if (t0 + i < t1) {
+                load_k(t0 + i);
+                load_v(t0 + i - 1, head_v);
+            } else if (t0 + i - 1 < t1) load_v(t0 + i - 1, head_k);
         }
+        id_next = id_of(t0 + N);
         if (t0 + N - 1 < t1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((N - 1) * 2 * LOADS) : "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         if (t0 < w_end) {
-            scores(t0, sa, [](int) {});
+            ring_k(t0);
+            scores(t0, sa, std::false_type(), [](int) {});
             mask(t0, sa);
             follow(maximum(sa));
         }
