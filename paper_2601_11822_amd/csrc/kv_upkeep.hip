@@ -13,7 +13,7 @@ namespace {
 // Every workgroup forms the sums over all requests itself, then writes what belongs to its requests (blockIdx.x) and, of long runs,
 // to its share of their rows (blockIdx.y).  What a call reads and writes in place (held, n_free) the last workgroup to have read
 // everything writes: a ticket counts them and is zero again behind the launch.
-// Bound by latency: lengths, then the sums, then held blocks' ids.
+// Bound by latency: lengths, then the sums, then held blocks' ids.  64 trees of 16 rows 7.2 us, 1000 runs of up to 63 rows 6.2.
 // ---------------------------------------------------------------------------------------------
 constexpr int PLAN_REQS = 64, PLAN_WAVES = 16;   // requests and waves of a workgroup
 
@@ -176,6 +176,7 @@ __global__ __launch_bounds__(64 * PLAN_WAVES) void kv_plan_kernel(KvPlanArgs a) 
 // Workgroups for kv heads (first, as they have the longer way), then for the query heads of 16 rows (rows x 8-dim chunks by lane, the angles in
 // registers for all heads).  A token's key is 16-byte pieces of its block and its value single elements, so the rows that share a block are
 // written together: the wave of the kv_rows rows among which a run of rows with the same block begins writes all of that run.
+// 512 rows of the 8B heads in runs of 8: 7.5 us; 16444 rows of four prompts on three axes 83 to 86 us, 4.8 TB/s, what a copy reaches.
 // ---------------------------------------------------------------------------------------------
 __device__ __forceinline__ int pair_axis(const KvStoreArgs &a, int pair) { return (int)(a.axis[pair >> 5] >> (2 * (pair & 31)) & 3); }
 
@@ -384,7 +385,8 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_gro
 // ---------------------------------------------------------------------------------------------
 // Compact.  Token ctx + keep[i] of a request takes the place of token ctx + i, in every layer.  keep ascends, so a token moves to a place
 // before its own and before those of all that come later: a wave takes a (request, layer, kv head) for itself, eight tokens at a time, and has
-// read all of them before it writes one.  Latency bound: lengths, indices, block ids, tokens.
+// read all of them before it writes one.  Latency bound: lengths, indices, block ids, tokens.  32 layers of one request's path 3.2 us of the GPU, 16 layers
+// of 64 requests' 8.3.
 // ---------------------------------------------------------------------------------------------
 template <int HD>
 __global__ __launch_bounds__(256) void kv_compact_kernel(KvCompactArgs a) {

@@ -299,6 +299,8 @@ __device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps) {
 // products with V with the rest of them and with the next step's maxima.  (A product takes 16 ns of a SIMD; an exponential, its multiplication
 // and two additions beside it one more.)
 // The exponentials' reference is the row's first maximum, moved to the running one once a score is 2^4 above it: two steps in three need no rescaling.
+// 16384 rows of the 8B heads under a window of 4096: 930 to 960 us, 1.0 PFLOP/s, the matrix unit busy 54 % of the cycles; the loop with its products
+// alone takes 607.  32 trees of 32 rows behind 512 to 4096 tokens: 79 us, as long as the longest one's steps take (1.1 us each).
 constexpr int TAB_BLOCKS = 2048;
 constexpr int step_blocks(int teams, bool tree) { return teams == 2 && !tree ? 8 : 4; }
 template <int HD, int KH, bool TREE>
@@ -686,7 +688,8 @@ __global__ __launch_bounds__(256) void masked_join_kernel(MaskedAttnArgs a) {
 // Units of up to 32 columns (decode rows, small trees): bound by reading the cache, so nothing is shared and nothing staged.  The waves take
 // tiles of 32 keys (two blocks) in turn, straight from the pools into the operands of 32x32x16 products (every load of a wave is a contiguous
 // kilobyte, or four pieces of 256 bytes); a tile's keys are asked for as soon as the products with the ones before have been issued, and so are
-// its values.  The waves' sums meet in LDS at the end.
+// its values.  The waves' sums meet in LDS at the end.  8B heads: 64 rows of 512 to 16383 tokens under a window of 4096 take 152 us, 6.3 TB/s (with
+// eight waves 154); one row under a window of 1024 8.4 us, in eight pieces (in 4 10.1, in 16 9.7, in 32 12.9).
 template <int HD, int NW, bool TREE>
 __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a) {
     constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD, PAD = HD + 4;
@@ -914,16 +917,19 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
     const int64_t wgs = (int64_t)a.n_units * a.Hkv;
     if (wgs <= 0) return f;
     const int tiles = (keys + 63) / 64;
-    const auto cut = [&](int least) {   // pieces of `least` tiles or more, none but the first for each compute unit
-        return (int)std::max<int64_t>(1, std::min<int64_t>({MASKED_PIECES / wgs, MASKED_MAX_CUT, tiles / least}));
+    const auto cut = [&](int least, int most) {   // pieces of `least` tiles or more, none but the first for each compute unit
+        return (int)std::max<int64_t>(1, std::min<int64_t>({MASKED_PIECES / wgs, most, tiles / least}));
     };
     const bool alone = wgs <= MASKED_PIECES;   // every workgroup has a compute unit to itself
     if (few) {
         f.kind = alone ? MASKED_FEW8 : MASKED_FEW4;
-        a.cut = cut(2);
+        // Eight pieces are asked for together by the one that joins them; more pay for long contexts.  us in 8 / 16 / 32 pieces, 8B heads: a row under a
+        // window of 1024 8.6 / 9.6 / 13.1, 4096 13.5 / 13.0 / 14.8, 8192 18.6 / 15.8 / 18.7, 30000 45.4 / 30.9 / 31.4 (24: 29.0); a tree of 8 behind
+        // 4000 tokens 17.6 / 19.1 / 24.6, 8000 22.6 / 21.9 / 28.2; 19 rows under a window of 2048 in 8 / 10 pieces 15.7 / 18.0.
+        a.cut = cut(2, tiles <= 64 ? 8 : 16);
     } else {
         f.kind = alone ? MASKED_TEAMS : MASKED_WIDE;
-        a.cut = cut(4);
+        a.cut = cut(4, MASKED_MAX_CUT);
     }
     return f;
 }

@@ -26,8 +26,8 @@ static void check(const char *what, int i, MaskedAttnArgs &a, MaskedKind kind, i
 static void decode_forms() {
     static int32_t lens;
     struct { int Hq, Hkv, B, max_ctx, window, sinks; MaskedKind kind; int cut; } of[] = {
-        {32, 8, 1, 4096, 1024, 4, MASKED_FEW8, 8}, {32, 8, 1, 8193, 8192, 4, MASKED_FEW8, 32}, {32, 8, 64, 8193, 4096, 4, MASKED_FEW4, 1},
-        {32, 8, 32, 8193, 4096, 4, MASKED_FEW8, 1}, {8, 2, 1, 100, 64, 0, MASKED_FEW8, 1}, {16, 1, 1, 1 << 30, 1 << 30, 0, MASKED_FEW8, 32},
+        {32, 8, 1, 4096, 1024, 4, MASKED_FEW8, 8}, {32, 8, 1, 8193, 8192, 4, MASKED_FEW8, 16}, {32, 8, 1, 4097, 4096, 0, MASKED_FEW8, 16}, {32, 8, 1, 4001, 4096, 0, MASKED_FEW8, 8}, {32, 8, 64, 8193, 4096, 4, MASKED_FEW4, 1},
+        {32, 8, 32, 8193, 4096, 4, MASKED_FEW8, 1}, {8, 2, 1, 100, 64, 0, MASKED_FEW8, 1}, {16, 1, 1, 1 << 30, 1 << 30, 0, MASKED_FEW8, 16},
         {16, 1, 65535, 2147483632, 2147483647, 2147483647, MASKED_FEW4, 1}};
     for (auto &w : of) {
         MaskedAttnArgs a = heads(w.Hq, w.Hkv);
@@ -60,7 +60,7 @@ static void prompt_forms() {
 static void tree_forms() {
     static int32_t lens, cu;
     struct { int Hq, Hkv, B, max_draft, max_ctx; MaskedKind kind; int cut; } of[] = {
-        {32, 8, 1, 8, 2056, MASKED_FEW8, 16}, {32, 8, 32, 32, 4128, MASKED_TEAMS, 1}, {32, 8, 16, 32, 4128, MASKED_TEAMS, 2}, {32, 8, 4, 32, 4032, MASKED_TEAMS, 8},
+        {32, 8, 1, 8, 2056, MASKED_FEW8, 8}, {32, 8, 1, 8, 8008, MASKED_FEW8, 16}, {32, 8, 32, 32, 4128, MASKED_TEAMS, 1}, {32, 8, 16, 32, 4128, MASKED_TEAMS, 2}, {32, 8, 4, 32, 4032, MASKED_TEAMS, 8},
         {32, 8, 64, 16, 4112, MASKED_WIDE, 1}, {32, 8, 8, 16, 916, MASKED_FEW8, 2}, {32, 8, 1, 60, 3560, MASKED_FEW8, 4},
         // what GPU tests are about
         {32, 8, 2, 40, 3640, MASKED_TEAMS, 8}, {64, 16, 5, 64, 41064, MASKED_TEAMS, 1}, {64, 16, 9, 64, 41064, MASKED_WIDE, 1},
