@@ -928,7 +928,16 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
         // 4000 tokens 17.6 / 19.1 / 24.6, 8000 22.6 / 21.9 / 28.2; 19 rows under a window of 2048 in 8 / 10 pieces 15.7 / 18.0.
         a.cut = cut(2, tiles <= 64 ? 8 : 16);
     } else {
-        f.kind = alone ? MASKED_TEAMS : MASKED_WIDE;
+        // Two teams halve the longest unit's time, which two rounds of units end with where most are much shorter: us with two teams / one, 8B heads:
+        // a prompt of 1200 rows 29.3 / 35.1, 2048 51.9 / 56.7 (under a window of 1750 52.2 / 53.3, 1536 52.4 / 49.4, 512 40.1 / 30.2), 2048 behind 500
+        // 68.0 / 72.1, behind 4000 199 / 187, 1600 beside 100 41.8 / 45.2; 2500 rows (three rounds) 79.5 / 72.2; 64 query heads, 1024 rows 37.1 / 35.4.
+        int64_t seen = 0;   // by all rows
+        for (int r = 0; !tree && !a.ctx_lens && r < a.seq.n_req; ++r) {
+            const int64_t n = a.seq.cu[r + 1] - a.seq.cu[r];
+            seen += n * std::min<int64_t>(a.seq.start[r] + n / 2, (int64_t)a.window + a.sinks);
+        }
+        const bool uneven = !tree && keys >= 1152 && 5 * seen <= 3 * (int64_t)a.seq.cu[a.seq.n_req] * keys;
+        f.kind = alone || (uneven && wgs <= 2 * MASKED_PIECES) ? MASKED_TEAMS : MASKED_WIDE;
         a.cut = cut(4, MASKED_MAX_CUT);
     }
     return f;

@@ -40,7 +40,8 @@ static void decode_forms() {
 static void prompt_forms() {
     struct { int Hq, Hkv; std::vector<int> lens, starts; int window, sinks; MaskedKind kind; int cut; } of[] = {
         {32, 8, {100}, {3000}, 2048, 4, MASKED_FEW8, 2}, {32, 8, {512}, {3000}, 2048, 4, MASKED_TEAMS, 2}, {32, 8, {16384}, {0}, 4096, 4, MASKED_WIDE, 1},
-        {32, 8, {1024}, {0}, 4096, 0, MASKED_TEAMS, 1}, {32, 8, {2048}, {0}, 4096, 0, MASKED_WIDE, 1}, {32, 8, {300}, {0}, 4096, 0, MASKED_FEW4, 1},
+        {32, 8, {1024}, {0}, 4096, 0, MASKED_TEAMS, 1}, {32, 8, {2048}, {0}, 4096, 0, MASKED_TEAMS, 1}, {32, 8, {2500}, {0}, 4096, 0, MASKED_WIDE, 1}, {32, 8, {2048}, {0}, 512, 0, MASKED_WIDE, 1},
+        {32, 8, {2048}, {4000}, 8192, 0, MASKED_WIDE, 1}, {32, 8, {100, 1600}, {0, 0}, 8192, 0, MASKED_TEAMS, 1}, {64, 8, {1024}, {0}, 4096, 0, MASKED_WIDE, 1}, {32, 8, {300}, {0}, 4096, 0, MASKED_FEW4, 1},
         {32, 8, {37, 0, 1}, {5, 9, 0}, 50, 20, MASKED_FEW8, 1}, {8, 2, {0, 0}, {0, 0}, 50, 20, MASKED_FEW4, 1},
         // what GPU tests are about
         {32, 8, {100}, {3000}, 3000, 5, MASKED_TEAMS, 8}, {64, 16, {160}, {41000}, 2147483647, 0, MASKED_TEAMS, 3},
