@@ -290,10 +290,9 @@ __device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps) {
 }
 
 // Units of up to 128 columns, or one of the `cut` pieces of a unit's keys, by KH teams of four waves.  A wave owns 32 columns, and of a step's keys
-// its team's share.  Keys come by LDS-DMA into N buffers of K and N of V, used by all waves.  One team, of which two workgroups share a compute
-// unit, takes 64 keys a step and has two buffers; two teams have, for trees, four of 64 keys, and for prompts, whose rows end at
-// different steps, two of 128 (us with four buffers / with two, 8B heads: 32 trees of 32 rows behind 2300 tokens 60.3 / 64.8, sixteen behind
-// 500 to 4096 57.4 / 60.8; a prompt of 1024 rows 29.0 / 25.9, 512 rows behind 3000 under a window of 2048 39.3 / 36.5).  S^T = K Q^T and O^T = V^T P^T, so that a lane owns one column; the teams' sums are
+// (64, four blocks, for each team) those of its team.  Keys come by LDS-DMA into two buffers of K and two of V, a step ahead; all waves of a
+// team use them.  (Four buffers of half as many keys, in us with them / so: a prompt of 1024 rows 29.5 / 26.1, sixteen trees of 32 rows behind 500
+// to 4096 tokens 57.8 / 56.0, 32 of them 79.8 / 80.9.)  S^T = K Q^T and O^T = V^T P^T, so that a lane owns one column; the teams' sums are
 // brought together at the end.
 // What runs beside the matrix unit is written out: the products of the next step's scores alternate with most of this one's exponentials, the
 // products with V with the rest of them and with the next step's maxima.  (A product takes 16 ns of a SIMD; an exponential, its multiplication
@@ -302,13 +301,11 @@ __device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps) {
 // 16384 rows of the 8B heads under a window of 4096: 930 to 960 us, 1.0 PFLOP/s, the matrix unit busy 54 % of the cycles; the loop with its products
 // alone takes 607.  32 trees of 32 rows behind 512 to 4096 tokens: 79 us, as long as the longest one's steps take (1.1 us each).
 constexpr int TAB_BLOCKS = 2048;
-constexpr int step_blocks(int teams, bool tree) { return teams == 2 && !tree ? 8 : 4; }
 template <int HD, int KH, bool TREE>
 __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs a) {
-    constexpr int STEP = step_blocks(KH, TREE), BL = STEP / KH, NT = BL / 2, N = 8 * KH / STEP;   // blocks of a step, a team's; its tiles of 32 keys; buffers
+    constexpr int BL = 4, NT = 2, STEP = BL * KH;   // blocks of a team in a step, its tiles of 32 keys; blocks of a step
     constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD, BUF = STEP * BLK, T = 256 * KH;
-    constexpr int WPB = 4 * KH / STEP, LOADS = HD / 32 / WPB;   // waves for a block; loads of a wave for a step's K, and for its V
-    extern __shared__ __attribute__((aligned(1024))) bf16_t smem_masked[];   // [N] K, [N] V of BUF, [4 KH waves][32][2] floats, [TAB_BLOCKS] ids, flag
+    extern __shared__ __attribute__((aligned(1024))) bf16_t smem_masked[];   // [2] K, [2] V of BUF, [4 KH waves][32][2] floats, [TAB_BLOCKS] ids, flag
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int cg = wave & 3, kh = wave >> 2;
     const int c32 = lane & 31, h = lane >> 5;
@@ -346,7 +343,7 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     // Block ids of TAB_BLOCKS counted blocks from step tb on, in LDS: -1: none, or not one of the pool, of which there are some where *s_bad.  (Fetched
     // step by step into registers they would be waited for by a count of the loads behind them, which the compiler takes to be none where some are
     // under a branch: so all loads in flight would be waited for in every step.)
-    int32_t *s_tab = (int32_t *)(smem_masked + 2 * N * BUF) + 4 * KH * 64, *s_bad = s_tab + TAB_BLOCKS;
+    int32_t *s_tab = (int32_t *)(smem_masked + 4 * BUF) + 4 * KH * 64, *s_bad = s_tab + TAB_BLOCKS;
     auto fill_tab = [&](int tb) {
         for (int i = threadIdx.x; i < min(TAB_BLOCKS, STEP * (t1 - tb)); i += T) {
             const int j = STEP * tb + i;
@@ -363,32 +360,29 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         }
     };
     int tb = t0;   // the first step of s_tab
-    // Wave w brings block w of a step (or half w & 1 of block w / 2), 16 bytes a lane (lane l's at the window's base + 16 l).  K keeps the
+    // Wave w brings block w of a step, 16 bytes a lane (lane l's at the window's base + 16 l).  K keeps the
     // pool's order; V's chunk (dim, half of 8 tokens) goes to [half][dim].  A block that is missing is read as block 0, and masked.
     typedef __attribute__((address_space(3))) void lds_void;
-    const int wb = wave / WPB, wp = wave % WPB;
-    auto id_of = [&](int t) { return s_tab[min(STEP * (t - tb) + wb, TAB_BLOCKS - 1)]; };   // (behind the last step: not used)
+    auto id_of = [&](int t) { return s_tab[min(STEP * (t - tb) + wave, TAB_BLOCKS - 1)]; };   // (behind the last step: not used)
     auto head_of = [&](int id) { return ((size_t)max(__builtin_amdgcn_readfirstlane(id), 0) * a.Hkv + hk) * BLK; };
     size_t head_k = 0, head_v = 0;   // of the block that the wave brings next, for K; V follows a step behind
     int id_next = -1;                // asked for a step ahead
-    auto k_at = [&](int t) { return smem_masked + ((t - t0) & (N - 1)) * BUF; };
-    auto v_at = [&](int t) { return smem_masked + (N + ((t - t0) & (N - 1))) * BUF; };
+    auto k_at = [&](int t) { return smem_masked + ((t - t0) & 1) * BUF; };
+    auto v_at = [&](int t) { return smem_masked + (2 + ((t - t0) & 1)) * BUF; };
     auto load_k = [&](int t) {
         head_v = head_k;
         head_k = head_of(id_next);
         const auto buf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.k_pool + head_k), 0, 2 * BLK, 0x00020000);
-        bf16_t *d = k_at(t) + wb * BLK + wp * (BLK / 2);
+        bf16_t *d = k_at(t) + wave * BLK;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void *)(d + i * 512), 16, lane * 16, wp * BLK + i * 1024, 0, 0);
+        for (int i = 0; i < HD / 32; ++i) __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void *)(d + i * 512), 16, lane * 16, i * 1024, 0, 0);
     };
     auto load_v = [&](int t, size_t head) {
         const auto buf = __builtin_amdgcn_make_buffer_rsrc((void *)(a.v_pool + head), 0, 2 * BLK, 0x00020000);
-        bf16_t *d = v_at(t) + wb * BLK + wp * (BLK / 2);
+        bf16_t *d = v_at(t) + wave * BLK;
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {   // 64 dims of a half of the tokens
-            const int at = wp * LOADS + i;
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void *)(d + i * 512), 16, lane * 32, (at % (HD / 64)) * 2048 + (at / (HD / 64)) * 16, 0, 0);
-        }
+        for (int i = 0; i < HD / 32; ++i)   // 64 dims of a half of the tokens
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(buf, (lds_void *)(d + i * 512), 16, lane * 32, (i % (HD / 64)) * 2048 + (i / (HD / 64)) * 16, 0, 0);
     };
     auto klds = [](int r, int cc) { return (r >> 4) * BLK + kpool_chunk_offset(r & 15, cc * 8); };
     auto vlds = [](int blk, int half, int d) { return blk * BLK + half * (8 * HD) + d * 8; };
@@ -492,7 +486,7 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         limit = moves ? m + behind : limit;
     };
     // products with V of step t; weights from N0 on are formed beside them (of a block in front of it), then the next step's maximum
-    constexpr int N0 = BL == 4 ? 24 : 8;
+    constexpr int N0 = 24;
     auto values = [&](int t, const f32x16 (&cur)[NT], const f32x16 (&nxt)[NT]) {
         // the weights left are due before the last block's products: so many beside each product before those
         constexpr int SLOTS = DT * (BL - 1), EACH = (N_W - N0 + SLOTS - 1) / SLOTS;
@@ -518,22 +512,21 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     for (int i = 0; i < KS; ++i) asm volatile("" : "+v"(qf[i]));   // the queries are here: not to be waited for among the steps' loads
     __syncthreads();
     bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
-    // In front of step t's work: K of the step after it and V of its own have landed (of the wave's loads at most those behind them are in flight),
-    // nobody reads those of the step before any more; their buffers take K and V of the step N ahead.
+    // In front of step t's work: K of the step after it and V of its own have landed, nobody reads those of the step before any more; their buffers
+    // take K of the step after the next and V of the next.
     auto turn = [&](int t) {
-        if (N > 2 && t + N - 1 < t1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((N - 2) * 2 * LOADS) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        if (STEP * (t + N + 2 - tb) > TAB_BLOCKS && t + 1 < t1) {   // contexts of more than 32K tokens
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (STEP * (t + 4 - tb) > TAB_BLOCKS && t + 1 < t1) {   // contexts of more than 32K tokens
             tb = t;
             fill_tab(tb);
             __syncthreads();
             bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
         }
-        if (t + N < t1) {
-            load_k(t + N);
-            load_v(t + N - 1, head_v);
-            id_next = id_of(t + N + 1);
-        } else if (t + N - 1 < t1) load_v(t + N - 1, head_k);
+        if (t + 2 < t1) {
+            load_k(t + 2);
+            load_v(t + 1, head_v);
+            id_next = id_of(t + 3);
+        } else if (t + 1 < t1) load_v(t + 1, head_k);
     };
     auto step = [&](int t, f32x16 (&cur)[NT], f32x16 (&nxt)[NT]) {
         turn(t);
@@ -559,17 +552,13 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     if (t0 < t1) {
         id_next = id_of(t0);
         load_k(t0);
-#pragma unroll
-        for (int i = 1; i < N; ++i) {
-            id_next = id_of(t0 + i);
-            if (t0 + i < t1) {
-                load_k(t0 + i);
-                load_v(t0 + i - 1, head_v);
-            } else if (t0 + i - 1 < t1) load_v(t0 + i - 1, head_k);
-        }
-        id_next = id_of(t0 + N);
-        if (t0 + N - 1 < t1) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((N - 1) * 2 * LOADS) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        id_next = id_of(t0 + 1);
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        if (t0 + 1 < t1) {
+            load_k(t0 + 1);
+            load_v(t0, head_v);
+            id_next = id_of(t0 + 2);
+        } else load_v(t0, head_k);
         if (t0 < w_end) {
             ring_k(t0);
             scores(t0, sa, std::false_type(), [](int) {});
@@ -597,7 +586,7 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         // both waves of a column rescale to the common reference; the first finishes the first half of head_dim, the second the other, each with the
         // other's part through the buffers (nobody reads those any more)
         f32x4 *x_o = (f32x4 *)smem_masked;   // [8 waves][2 DT][64]
-        float *x_ml = (float *)(smem_masked + 2 * N * BUF), *mine = x_ml + wave * 64, *theirs = x_ml + (wave ^ 4) * 64;
+        float *x_ml = (float *)(smem_masked + 4 * BUF), *mine = x_ml + wave * 64, *theirs = x_ml + (wave ^ 4) * 64;
         if (h == 0) {
             mine[2 * c32] = ref;
             mine[2 * c32 + 1] = l_run;
