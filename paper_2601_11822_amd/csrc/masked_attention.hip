@@ -299,13 +299,13 @@ __device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps) {
 // and two additions beside it one more.)
 // The exponentials' reference is the row's first maximum, moved to the running one once a score is 2^4 above it: two steps in three need no rescaling.
 // 16384 rows of the 8B heads under a window of 4096: 930 to 960 us, 1.0 PFLOP/s, the matrix unit busy 54 % of the cycles; the loop with its products
-// alone takes 607.  32 trees of 32 rows behind 512 to 4096 tokens: 79 us, as long as the longest one's steps take (1.1 us each).
+// alone takes 607.  32 trees of 32 rows behind 512 to 4096 tokens: 74 us, as long as the longest one's steps take.
 constexpr int TAB_BLOCKS = 2048;
 template <int HD, int KH, bool TREE>
 __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs a) {
     constexpr int BL = 4, NT = 2, STEP = BL * KH;   // blocks of a team in a step, its tiles of 32 keys; blocks of a step
     constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD, BUF = STEP * BLK, T = 256 * KH;
-    extern __shared__ __attribute__((aligned(1024))) bf16_t smem_masked[];   // [2] K, [2] V of BUF, [4 KH waves][32][2] floats, [TAB_BLOCKS] ids, flag
+    extern __shared__ __attribute__((aligned(1024))) bf16_t smem_masked[];   // [2] K, [2] V of BUF, [4 KH waves][32][2] floats, [TAB_BLOCKS] ids, flag, [2] counts
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int cg = wave & 3, kh = wave >> 2;
     const int c32 = lane & 31, h = lane >> 5;
@@ -505,18 +505,36 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         return m;
     };
 
-    if (threadIdx.x == 0) *s_bad = 0;
+    if (threadIdx.x < 3) s_bad[threadIdx.x] = 0;
     __syncthreads();
     fill_tab(t0);
 #pragma unroll
     for (int i = 0; i < KS; ++i) asm volatile("" : "+v"(qf[i]));   // the queries are here: not to be waited for among the steps' loads
     __syncthreads();
     bad = __builtin_amdgcn_readfirstlane(*s_bad) != 0;
+    // All loads and reads of the team's waves so far are done.  Teams use what their own waves bring, so one need not wait for the other, and while
+    // one's waves pass from products to exponentials the other's have the matrix unit: a count in LDS in place of the workgroup's barrier (32 trees of 32
+    // rows behind 512 to 4096 tokens 81 us with the barrier, 74 so).  All four waves of a team come here equally often, and all are resident: the
+    // wait ends.
+    int32_t *met = s_bad + 1 + kh;
+    int times = 0;
+    auto meet = [&]() {
+        if (KH == 1) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            return;
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        if (lane == 0) __hip_atomic_fetch_add(met, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+        times += 4;
+        while (__builtin_amdgcn_readfirstlane(__hip_atomic_load(met, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP)) < times) {}
+        asm volatile("" ::: "memory");
+    };
     // In front of step t's work: K of the step after it and V of its own have landed, nobody reads those of the step before any more; their buffers
     // take K of the step after the next and V of the next.
     auto turn = [&](int t) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        meet();
         if (STEP * (t + 4 - tb) > TAB_BLOCKS && t + 1 < t1) {   // contexts of more than 32K tokens
+            if (KH == 2) __syncthreads();
             tb = t;
             fill_tab(tb);
             __syncthreads();
@@ -553,7 +571,7 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
         id_next = id_of(t0);
         load_k(t0);
         id_next = id_of(t0 + 1);
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        meet();
         if (t0 + 1 < t1) {
             load_k(t0 + 1);
             load_v(t0, head_v);
@@ -857,7 +875,7 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
     if (pc.cut > 1) join_pieces<HD, 64 * NW>(a, s, hk, pc);
 }
 
-constexpr int wide_lds(int hd, int kh) { return 4 * kh * 4 * 16 * hd * 2 + 4 * kh * 64 * 4 + (TAB_BLOCKS + 1) * 4; }
+constexpr int wide_lds(int hd, int kh) { return 4 * kh * 4 * 16 * hd * 2 + 4 * kh * 64 * 4 + (TAB_BLOCKS + 3) * 4; }
 
 constexpr int few_lds(int hd, int nw) { return nw * 32 * (hd + 4 + 2) * 4; }
 
