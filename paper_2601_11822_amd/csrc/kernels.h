@@ -155,7 +155,7 @@ struct MaskedAttnArgs {
     const uint64_t *masks = nullptr;
     int max_rows = 0, max_draft = 0;
     SeqInfo seq{};            // else prompts: request r's rows are its tokens start[r] ..
-    int32_t *tickets = nullptr;   // [MASKED_PIECES], 0 between launches
+    int32_t *tickets = nullptr;   // [MASKED_PIECES], 0 between launches, and [MASKED_PIECES], pieces of a tree's units
     int unit_rows = 0, n_units = 0, units_per_req = 0, cut = 1;   // set by masked_form (cut: of trees' units the most)
 };
 // Units of up to 32 columns by four or eight waves; of up to 128 by four, or by two teams of four.

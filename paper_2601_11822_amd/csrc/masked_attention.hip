@@ -271,7 +271,6 @@ __device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span
 // Into how many pieces a tree's unit is cut follows from its length, in steps of 64 keys, and all units' together, which no host knows: none is
 // to have much more than an equal share of the launch's pieces.
 __device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps) {
-    if (a.cut == 1) return 1;   // (uniform, and so is the result)
     __shared__ int64_t sums[8];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
     int64_t sum = 0;   // (whole numbers: the same for every workgroup)
@@ -316,7 +315,10 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     const Span s = unit_span<TREE>(a, pc.unit);
     if (s.rows <= 0) return;
     const int cols = s.rows * G;
-    if (TREE && !s.dead) pc.cut = tree_cut(a, (s.blocks + 3) >> 2);
+    if (TREE && a.cut > 1 && !s.dead) {
+        pc.cut = tree_cut(a, (s.blocks + 3) >> 2);
+        if (pc.piece == 0 && threadIdx.x == 0) a.tickets[MASKED_PIECES + pc.ticket] = pc.cut;   // for those who join them
+    }
     if (pc.piece >= pc.cut) return;
     if (s.dead) {
         if (pc.piece == 0)
@@ -681,7 +683,7 @@ __global__ __launch_bounds__(256) void masked_join_kernel(MaskedAttnArgs a) {
     Piece pc = piece_of(a, blockIdx.x / a.Hkv, hk, MASKED_COLS);
     const Span s = unit_span<TREE>(a, pc.unit);
     if (s.rows <= 0 || s.dead) return;
-    if (TREE) pc.cut = tree_cut(a, (s.blocks + 3) >> 2);
+    if (TREE) pc.cut = a.tickets[MASKED_PIECES + pc.ticket];
     const int item = blockIdx.y * 256 + threadIdx.x, col = item / (HD / 4), d = item % (HD / 4) * 4;
     if (pc.cut == 1 || col >= s.rows * G) return;
     const bf16x4 v = join_column(a, pc.cut, [&](int i, float2 &ml, f32x4 &x) {

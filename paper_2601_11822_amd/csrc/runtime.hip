@@ -1169,7 +1169,7 @@ int32_t alloc_masked(rs_ctx *c) {
         const size_t n = (size_t)MASKED_PIECES * MASKED_COLS;
         HIP_TRY(hipMalloc(&c->mask_part_o[s], n * c->m.head_dim * sizeof(float)));
         HIP_TRY(hipMalloc(&c->mask_part_ml[s], n * 2 * sizeof(float)));
-        HIP_TRY(hipMalloc(&c->mask_tickets[s], MASKED_PIECES * sizeof(int32_t)));
+        HIP_TRY(hipMalloc(&c->mask_tickets[s], 2 * MASKED_PIECES * sizeof(int32_t)));
         HIP_TRY(hipMemset(c->mask_tickets[s], 0, MASKED_PIECES * sizeof(int32_t)));
     }
     HIP_TRY(hipMalloc(&c->plan_ticket, 2 * sizeof(int32_t)));
