@@ -46,6 +46,7 @@ static void prompt_forms() {
         // what GPU tests are about
         {32, 8, {100}, {3000}, 3000, 5, MASKED_TEAMS, 8}, {64, 16, {160}, {41000}, 2147483647, 0, MASKED_TEAMS, 3},
         {64, 16, {300}, {41000}, 2147483647, 0, MASKED_TEAMS, 1}, {64, 16, {600}, {41000}, 2147483647, 0, MASKED_WIDE, 1},
+        {32, 8, {1300, 100}, {0, 20}, 2147483647, 0, MASKED_TEAMS, 1}, {32, 8, {1300, 100}, {0, 20}, 1250, 16, MASKED_TEAMS, 1},
         {32, 8, {600}, {41000}, 2147483647, 0, MASKED_TEAMS, 1}, {32, 8, {1200}, {41000}, 2147483647, 0, MASKED_WIDE, 1}};
     for (auto &w : of) {
         MaskedAttnArgs a = heads(w.Hq, w.Hkv);

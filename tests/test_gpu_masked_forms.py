@@ -50,6 +50,18 @@ def test_short_prompts_of_many_rows(heads, lens, starts, window, sinks):
     c.c.destroy()
 
 
+@pytest.mark.parametrize("window,sinks", [(2 ** 31 - 1, 0), (1250, 16)])
+def test_prompts_of_more_units_than_compute_units_in_two_teams(window, sinks):
+    lens, starts = [1300, 100], [0, 20]
+    c = Step((32, 8, 128), 100, max_prefill=1400, max_context=2048, seed=30)
+    tab = c.tables([1300, 120])
+    q = c.queries(1400)
+    got = W.prefill(c, tab, lens, starts, window, sinks, q)
+    W.check_prefill(f"{window}+{sinks}", c, tab, lens, starts, window, sinks, q, got, some=67)
+    assert torch.equal(got, W.prefill(c, tab, lens, starts, window, sinks, q))
+    c.c.destroy()
+
+
 # ---- more than 32K tokens ----
 LONG = 41000
 
