@@ -285,8 +285,8 @@ int32_t rs_kv4_prefill_attention(rs_ctx *ctx, int32_t layer, const void *q, int6
  * the product with V as bf16, sums are float32.  What a key or value holds that a row does not see, NaN included, does not reach the
  * row.  A block id outside the pool is never dereferenced: its tokens are seen by no row, and rs_sync reports RS_ERR_BAD_BLOCK.  The same
  * call gives the same bits, under any CU split.  How a request's keys are shared out among workgroups, and so the last bits of its
- * rows, depends on the whole launch: on its sizes (max_ctx among them), for trees on the other requests' lengths too.  out may not
- * overlap q. */
+ * rows, depends on the whole launch: on its sizes (max_ctx among them: a bound near the longest context serves best), for trees on the other
+ * requests' lengths too.  out may not overlap q. */
 
 /* Row i of q (DECODE side), the token at position ctx_lens[i] (cached already), sees the latest `window` tokens up to its own, and the first
  * `sinks` tokens of its request: positions j <= ctx_lens[i] with j > ctx_lens[i] - window or j < sinks.  window >= 1, sinks >= 0; a window

@@ -917,8 +917,9 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
     for (int r = 0; !tree && !a.ctx_lens && r < a.seq.n_req; ++r) keys = std::max(keys, a.seq.start[r] + a.seq.cu[r + 1] - a.seq.cu[r]);
     if (!tree) keys = (int)std::min<int64_t>(keys, (int64_t)a.window + a.sinks + 32);
     // Units of 32 columns where a request has no more, or where reading the keys again for each of them is little: us with units of 32 / of 128,
-    // 8B heads: a tree of 16 behind 900 tokens 12.7 / 18.2, eight of them 18.2 / 21.8, one of 60 behind 3500 19.9 / 23.2, four of 32
-    // behind 4000 31.9 / 30.2, sixteen of 32 behind 500 to 4096 67.5 / 57.4; 100 rows under a window of 2048 20.4 / 20.9, 512 42.4 / 36.5.
+    // 8B heads: a tree of 16 behind 900 tokens 12.7 / 17.8, eight of them 18.2 / 20.5, one of 60 behind 3500 19.7 / 21.6, three of 32
+    // behind 3000 25.7 / 25.7, four behind 4000 32.0 / 28.4, sixteen behind 500 to 4096 67.5 / 52.4; 100 rows under a window of 2048 20.3 / 20.6,
+    // 512 42.4 / 36.6; prompts of 200 rows 8.7 / 12.7, 400 12.1 / 15.6, 600 18.7 / 18.5.
     const bool few = most * G <= 32 || (int64_t)units(32 / G) * a.Hkv * keys <= 256 * 1024;
     a.unit_rows = (few ? 32 : MASKED_COLS) / G;
     a.units_per_req = (a.max_draft + a.unit_rows - 1) / a.unit_rows;
