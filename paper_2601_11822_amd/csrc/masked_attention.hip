@@ -150,51 +150,63 @@ __device__ __forceinline__ Piece piece_of(const MaskedAttnArgs &a, int idx, int 
     return {u, idx / a.n_units, a.cut, t * a.cut, cols, t};
 }
 
-// Four dims of a column, its pieces taken in order (eight asked for together): get(i, &ml, &v).
-template <class Get>
-__device__ __forceinline__ bf16x4 join_column(const MaskedAttnArgs &a, int cut, Get get) {
+// Four dims of each of K columns, their pieces taken in order (eight asked for together): get(k, i, &ml, &v).
+template <int K, class Get>
+__device__ __forceinline__ void join_columns(const MaskedAttnArgs &a, int cut, Get get, bf16x4 (&out)[K]) {
     constexpr int N = 8;
-    float top = NEG_INF, l = 0.f;   // over the pieces so far
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    float top[K], l[K];   // over the pieces so far
+    f32x4 acc[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) top[k] = NEG_INF, l[k] = 0.f, acc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int i0 = 0; i0 < cut; i0 += N) {
-        float2 ml[N];
-        f32x4 x[N];
+        float2 ml[K][N];
+        f32x4 x[K][N];
 #pragma unroll
-        for (int i = 0; i < N; ++i) get(min(i0 + i, cut - 1), ml[i], x[i]);
-        float m = top;
+        for (int k = 0; k < K; ++k)
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (i0 + i < cut) m = fmaxf(m, ml[i].x);
-        const float ref = m == NEG_INF ? 0.f : m, keep = exp2f((top - ref) * a.scale_log2);
-        top = m;
-        l *= keep;
-        acc = acc * keep;
+            for (int i = 0; i < N; ++i) get(k, min(i0 + i, cut - 1), ml[k][i], x[k][i]);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            if (i0 + i >= cut || ml[i].y == 0.f) continue;   // (a sum of nothing: a piece none of whose keys the row sees)
-            const float e = exp2f((ml[i].x - ref) * a.scale_log2);
-            l += ml[i].y * e;
-            acc += x[i] * e;
+        for (int k = 0; k < K; ++k) {
+            float m = top[k];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i0 + i < cut) m = fmaxf(m, ml[k][i].x);
+            const float ref = m == NEG_INF ? 0.f : m, keep = exp2f((top[k] - ref) * a.scale_log2);
+            top[k] = m;
+            l[k] *= keep;
+            acc[k] = acc[k] * keep;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                if (i0 + i >= cut || ml[k][i].y == 0.f) continue;   // (a sum of nothing: a piece none of whose keys the row sees)
+                const float e = exp2f((ml[k][i].x - ref) * a.scale_log2);
+                l[k] += ml[k][i].y * e;
+                acc[k] += x[k][i] * e;
+            }
         }
     }
-    bf16x4 v;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(l == 0.f ? 0.f : acc[i] / l);
-    return v;
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[k][i] = (bf16_t)(l[k] == 0.f ? 0.f : acc[k][i] / l[k]);
 }
 
 // Units of few columns: the last workgroup of a (unit, kv head) to arrive brings the pieces together, in their order, so that results do not
-// depend on which one that is.  The sums are written and read as relaxed atomics of the device's scope, which pass the XCDs' own L2 caches by;
-// a workgroup's have arrived when its waves have waited for them, in front of the ticket.  (A fence at that scope writes back and
-// invalidates whole caches instead.)  Units of many columns are joined by a launch of their own: 64 KB a piece are too much for one workgroup.
-__device__ __forceinline__ void put_far(float *p, float x, float y) {
-    const uint64_t v = (uint64_t)__builtin_bit_cast(uint32_t, y) << 32 | __builtin_bit_cast(uint32_t, x);
-    __hip_atomic_store((uint64_t *)p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-__device__ __forceinline__ float2 get_far(const float *p) {
-    const uint64_t v = __hip_atomic_load((const uint64_t *)p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    return float2{__builtin_bit_cast(float, (uint32_t)v), __builtin_bit_cast(float, (uint32_t)(v >> 32))};
-}
+// depend on which one that is.  The sums are written and read at the device's scope, which passes the XCDs' own L2 caches by; a workgroup's have
+// arrived when its waves have waited for them, in front of the ticket.  (A fence at that scope writes back and invalidates whole caches
+// instead.)  Units of many columns are joined by a launch of their own: 64 KB a piece are too much for one workgroup.
+struct Far {
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+    static constexpr int DEVICE = 16;   // cache policy: sc1
+    __amdgpu_buffer_rsrc_t o, ml;
+    __device__ __forceinline__ explicit Far(const MaskedAttnArgs &a)
+        : o(__builtin_amdgcn_make_buffer_rsrc(a.part_o, 0, MASKED_PIECES * MASKED_COLS * a.hd * 4, 0x00020000)),
+          ml(__builtin_amdgcn_make_buffer_rsrc(a.part_ml, 0, MASKED_PIECES * MASKED_COLS * 2 * 4, 0x00020000)) {}
+    __device__ __forceinline__ void put_o(size_t i, f32x4 v) const { __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), o, (int)(4 * i), 0, DEVICE); }
+    __device__ __forceinline__ void put_ml(size_t i, float2 v) const { __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), ml, (int)(8 * i), 0, DEVICE); }
+    __device__ __forceinline__ f32x4 get_o(size_t i) const { return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(o, (int)(4 * i), 0, DEVICE)); }
+    __device__ __forceinline__ float2 get_ml(size_t i) const { return __builtin_bit_cast(float2, __builtin_amdgcn_raw_buffer_load_b64(ml, (int)(8 * i), 0, DEVICE)); }
+};
 template <int HD, int T>
 __device__ __forceinline__ void join_pieces(const MaskedAttnArgs &a, const Span &s, int hk, const Piece &pc) {
     __shared__ int last;
@@ -208,18 +220,25 @@ __device__ __forceinline__ void join_pieces(const MaskedAttnArgs &a, const Span 
     }
     __syncthreads();
     if (!last) return;
+    const Far far(a);
+    const int d = threadIdx.x % (HD / 4) * 4, col0 = threadIdx.x / (HD / 4);
+    auto join = [&](auto items) {   // a thread's: four dims of a column, those of the columns T / (HD / 4) behind it
+        constexpr int K = items;
+        if (col0 >= cols) return;
+        bf16x4 v[K];
+        join_columns<K>(a, pc.cut, [&](int k, int i, float2 &ml, f32x4 &x) {
+            const size_t at = pc.at(i, min(col0 + k * (4 * T / HD), cols - 1));
+            ml = far.get_ml(at);
+            x = far.get_o(at * HD + d);
+        }, v);
 #pragma unroll
-    for (int k = 0; k < 32 * (HD / 4) / T; ++k) {
-        const int item = T * k + threadIdx.x, col = item / (HD / 4), d = item % (HD / 4) * 4;
-        if (col >= cols) continue;
-        const bf16x4 v = join_column(a, pc.cut, [&](int i, float2 &ml, f32x4 &x) {
-            const size_t at = pc.at(i, col);
-            ml = get_far(a.part_ml + 2 * at);
-            const float2 lo = get_far(a.part_o + at * HD + d), hi = get_far(a.part_o + at * HD + d + 2);
-            x = f32x4{lo.x, lo.y, hi.x, hi.y};
-        });
-        *(bf16x4 *)(out_at(a, s, col, hk, G) + d) = v;
-    }
+        for (int k = 0; k < K; ++k) {
+            const int col = col0 + k * (4 * T / HD);
+            if (col < cols) *(bf16x4 *)(out_at(a, s, col, hk, G) + d) = v[k];
+        }
+    };
+    if (cols <= 4 * T / HD) join(std::integral_constant<int, 1>());
+    else join(std::integral_constant<int, 32 * HD / (4 * T)>());
 }
 
 // The same sums one key after the other in float32, without the matrix unit: for units whose result is not finite.  There a weight
@@ -259,8 +278,9 @@ __device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span
         }
         if (pc.cut > 1) {
             const size_t at = pc.at(pc.piece, col);
-            for (int i = 0; i < D; i += 2) put_far(a.part_o + at * HD + d0 + i, o[i], o[i + 1]);   // (whoever joins them)
-            if (d0 == 0) put_far(a.part_ml + 2 * at, m, l);
+            const Far far(a);   // (whoever joins them)
+            for (int i = 0; i < D; i += 4) far.put_o(at * HD + d0 + i, f32x4{o[i], o[i + 1], o[i + 2], o[i + 3]});
+            if (d0 == 0) far.put_ml(at, float2{m, l});
         } else {
             bf16_t *p = out_at(a, s, col, hk, G) + d0;
             for (int i = 0; i < D; ++i) p[i] = (bf16_t)(l == 0.f ? 0.f : o[i] / l);
@@ -297,7 +317,7 @@ __device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps) {
 // products with V with the rest of them and with the next step's maxima.  (A product takes 16 ns of a SIMD; an exponential, its multiplication
 // and two additions beside it one more.)
 // The exponentials' reference is the row's first maximum, moved to the running one once a score is 2^4 above it: two steps in three need no rescaling.
-// 16384 rows of the 8B heads under a window of 4096: 902 to 960 us from card to card, 1.0 PFLOP/s at 1.8 GHz, the matrix unit busy 54 % of the cycles; the loop with its products
+// 16384 rows of the 8B heads under a window of 4096: 902 to 990 us from card to card, 1.0 PFLOP/s at 1.8 GHz, the matrix unit busy 54 % of the cycles; the loop with its products
 // alone takes 607.  32 trees of 32 rows behind 512 to 4096 tokens: 73 us, as long as the longest one's steps take.
 constexpr int TAB_BLOCKS = 2048;
 template <int HD, int KH, bool TREE>
@@ -315,7 +335,7 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     const Span s = unit_span<TREE>(a, pc.unit);
     if (s.rows <= 0) return;
     const int cols = s.rows * G;
-    if (TREE && a.cut > 1 && !s.dead) {
+    if (KH == 2 && TREE && a.cut > 1 && !s.dead) {   // (one team: more units than compute units, none is cut)
         pc.cut = tree_cut(a, (s.blocks + 3) >> 2);
         if (pc.piece == 0 && threadIdx.x == 0) a.tickets[MASKED_PIECES + pc.ticket] = pc.cut;   // for those who join them
     }
@@ -636,10 +656,10 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
             }
     }
     const int d0 = kh * (HD / KH) + 4 * h;   // this lane's dims: d0 + 32 dt + 8 j + i
-    if (pc.cut > 1) {
+    if (KH == 2 && pc.cut > 1) {
         // a column's consecutive sums are written together, through LDS
         constexpr int ROW = HD + 4;
-        if (KH == 2) __syncthreads();   // the other team's part has been read
+        __syncthreads();   // the other team's part has been read
         float *strip = (float *)smem_masked + cg * (32 * ROW);
 #pragma unroll
         for (int dt = 0; dt < DT / KH; ++dt)
@@ -686,22 +706,24 @@ __global__ __launch_bounds__(256) void masked_join_kernel(MaskedAttnArgs a) {
     if (TREE) pc.cut = a.tickets[MASKED_PIECES + pc.ticket];
     const int item = blockIdx.y * 256 + threadIdx.x, col = item / (HD / 4), d = item % (HD / 4) * 4;
     if (pc.cut == 1 || col >= s.rows * G) return;
-    const bf16x4 v = join_column(a, pc.cut, [&](int i, float2 &ml, f32x4 &x) {
+    bf16x4 v[1];
+    join_columns<1>(a, pc.cut, [&](int, int i, float2 &ml, f32x4 &x) {
         const size_t at = pc.at(i, col);
         ml = *(const float2 *)(a.part_ml + 2 * at);
         x = *(const f32x4 *)(a.part_o + at * HD + d);
-    });
-    *(bf16x4 *)(out_at(a, s, col, hk, G) + d) = v;
+    }, v);
+    *(bf16x4 *)(out_at(a, s, col, hk, G) + d) = v[0];
 }
 
 // Units of up to 32 columns (decode rows, small trees): bound by reading the cache, so nothing is shared and nothing staged.  The waves take
 // tiles of 32 keys (two blocks) in turn, straight from the pools into the operands of 32x32x16 products (every load of a wave is a contiguous
 // kilobyte, or four pieces of 256 bytes); a tile's keys are asked for as soon as the products with the ones before have been issued, and so are
 // its values.  The waves' sums meet in LDS at the end.  8B heads: 64 rows of 512 to 16383 tokens under a window of 4096 take 152 us, 6.3 TB/s (with
-// eight waves 154); one row under a window of 1024 8.4 us, in eight pieces (in 4 10.1, in 16 9.7, in 32 12.9).
+// eight waves 154); one row under a window of 1024 8.4 to 8.8 us, in eight pieces.
 template <int HD, int NW, bool TREE>
 __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a) {
     constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD, PAD = HD + 4;
+    constexpr bool CUTS = NW == 8;   // four waves: more units than compute units, none is cut
     extern __shared__ __attribute__((aligned(16))) float smem_few[];   // [NW][32][PAD], [NW][32][2]
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, c32 = lane & 31, h = lane >> 5;
     const int G = a.Hq / a.Hkv;
@@ -845,7 +867,7 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
     }
     if (__syncthreads_or(odd && col < cols)) {
         careful_unit<HD, TREE>(a, s, hk, 2 * t0, min(2 * t1, s.blocks), pc, 64 * NW);
-        if (pc.cut > 1) join_pieces<HD, 64 * NW>(a, s, hk, pc);
+        if (CUTS && pc.cut > 1) join_pieces<HD, 64 * NW>(a, s, hk, pc);
         return;
     }
     for (int item = threadIdx.x; item < cols * (HD / 4); item += 64 * NW) {
@@ -861,11 +883,11 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
             l += s_ml[(w * 32 + c) * 2 + 1] * e;
             acc += *(const f32x4 *)(s_o + (w * 32 + c) * PAD + d) * e;
         }
-        if (pc.cut > 1) {
+        if (CUTS && pc.cut > 1) {
             const size_t at = pc.at(pc.piece, c);
-            put_far(a.part_o + at * HD + d, acc[0], acc[1]);
-            put_far(a.part_o + at * HD + d + 2, acc[2], acc[3]);
-            if (d == 0) put_far(a.part_ml + 2 * at, top, l);
+            const Far far(a);
+            far.put_o(at * HD + d, acc);
+            if (d == 0) far.put_ml(at, float2{top, l});
             continue;
         }
         const float inv = l > 0.f ? 1.0f / l : 0.f;
@@ -874,7 +896,7 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
         for (int i = 0; i < 4; ++i) v[i] = (bf16_t)(acc[i] * inv);
         *(bf16x4 *)(out_at(a, s, c, hk, G) + d) = v;
     }
-    if (pc.cut > 1) join_pieces<HD, 64 * NW>(a, s, hk, pc);
+    if (CUTS && pc.cut > 1) join_pieces<HD, 64 * NW>(a, s, hk, pc);
 }
 
 constexpr int wide_lds(int hd, int kh) { return 4 * kh * 4 * 16 * hd * 2 + 4 * kh * 64 * 4 + (TAB_BLOCKS + 3) * 4; }
@@ -927,15 +949,16 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
     const int64_t wgs = (int64_t)a.n_units * a.Hkv;
     if (wgs <= 0) return f;
     const int tiles = (keys + 63) / 64;
-    const auto cut = [&](int least, int most) {   // pieces of `least` tiles or more, none but the first for each compute unit
-        return (int)std::max<int64_t>(1, std::min<int64_t>({MASKED_PIECES / wgs, most, tiles / least}));
+    const auto cut = [&](int least, int most) {   // pieces of about `least` tiles or more, none but the first for each compute unit
+        return (int)std::max<int64_t>(1, std::min<int64_t>({MASKED_PIECES / wgs, most, (tiles + least - 1) / least}));
     };
     const bool alone = wgs <= MASKED_PIECES;   // every workgroup has a compute unit to itself
     if (few) {
         f.kind = alone ? MASKED_FEW8 : MASKED_FEW4;
         // Eight pieces are asked for together by the one that joins them; more pay for long contexts.  us in 8 / 16 / 32 pieces, 8B heads: a row under a
-        // window of 1024 8.6 / 9.6 / 13.1, 4096 13.5 / 13.0 / 14.8, 8192 18.6 / 15.8 / 18.7, 30000 45.4 / 30.9 / 31.4 (24: 29.0); a tree of 8 behind
-        // 4000 tokens 17.6 / 19.1 / 24.6, 8000 22.6 / 21.9 / 28.2; 19 rows under a window of 2048 in 8 / 10 pieces 15.7 / 18.0.
+        // window of 1024 8.8 / 9.7 / 13.0, 4096 13.7 / 13.2 / 14.9, 8192 18.7 / 16.0 / 18.7, 30000 45.5 / 31.1 / 31.2 (24: 29.1); a tree of 8 behind
+        // 900 tokens 11.5 / 13.4 / 18.4 (6: 12.0), 4000 17.1 / 17.7 / 21.2, 8000 22.3 / 20.5 / 25.1; 19 rows under a window of 2048 in 8 / 10 pieces
+        // 15.4 / 16.7.
         a.cut = cut(2, tiles <= 64 ? 8 : 16);
     } else {
         // Two teams halve the longest unit's time, which two rounds of units end with where most are much shorter: us with two teams / one, 8B heads:
