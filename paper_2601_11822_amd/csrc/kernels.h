@@ -134,6 +134,7 @@ void launch_kv4_prefill(hipStream_t st, const Kv4PromptArgs &a);
 #define MASKED_COLS 128        // columns, (row, query head of a kv head), of a unit
 #define MASKED_PIECES 256      // most pieces of units whose keys are cut, in a launch: the compute units
 #define MASKED_MAX_CUT 32      // and most of one unit
+struct MaskedRun { int32_t req, units, start; };
 struct MaskedAttnArgs {
     const bf16_t *q;          // rows of Hq * hd, q_stride elements apart
     size_t q_stride;
@@ -155,6 +156,7 @@ struct MaskedAttnArgs {
     const uint64_t *masks = nullptr;
     int max_rows = 0, max_draft = 0;
     SeqInfo seq{};            // else prompts: request r's rows are its tokens start[r] ..
+    MaskedRun runs[64]{};     // and the requests, from the one whose units come last (set by masked_form)
     int32_t *tickets = nullptr;   // [MASKED_PIECES], 0 between launches, and [MASKED_PIECES], pieces of a tree's units
     int unit_rows = 0, n_units = 0, units_per_req = 0, cut = 1;   // set by masked_form (cut: of trees' units the most)
 };

@@ -56,7 +56,26 @@ static void prompt_forms() {
             masked_form(a);
             CHECK(a.n_units == 0, "no rows: %d units", a.n_units);
         } else check("prompt", int(&w - of), a, w.kind, w.cut);
+        std::vector<int> units(w.lens.size(), -1);   // each request once, with its units
+        int n = 0;
+        for (int i = 0; a.n_units && i < a.seq.n_req; ++i) {
+            const MaskedRun &r = a.runs[i];
+            CHECK(r.req >= 0 && r.req < a.seq.n_req && units[r.req] == -1, "prompt %d: run %d", int(&w - of), i);
+            units[r.req] = r.units, n += r.units;
+            CHECK(r.start == w.starts[r.req] && r.units == (w.lens[r.req] + a.unit_rows - 1) / a.unit_rows, "prompt %d: run %d", int(&w - of), i);
+        }
+        CHECK(n == a.n_units, "prompt %d: %d units of %d", int(&w - of), n, a.n_units);
     }
+}
+
+// The requests whose rows see least come last: they stand first
+static void prompt_order() {
+    MaskedAttnArgs a = heads(32, 8);
+    const int lens[] = {1500, 100, 2000, 700, 64, 0}, starts[] = {0, 3000, 500, 2000, 9, 4000}, order[] = {4, 0, 2, 3, 1, 5};
+    a.window = 4096, a.seq.n_req = 6;
+    for (int r = 0; r < 6; ++r) a.seq.cu[r + 1] = a.seq.cu[r] + lens[r], a.seq.start[r] = starts[r];
+    masked_form(a);
+    for (int i = 0; i < 6; ++i) CHECK(a.runs[i].req == order[i], "place %d: request %d", i, a.runs[i].req);
 }
 
 static void tree_forms() {
@@ -87,6 +106,7 @@ static void tree_forms() {
 int main() {
     decode_forms();
     prompt_forms();
+    prompt_order();
     tree_forms();
     std::printf(fails ? "%d failures\n" : "ok\n", fails);
     return fails != 0;
