@@ -953,9 +953,11 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
             return std::min<int64_t>(a.seq.start[r], most_seen) + std::min<int64_t>(a.seq.start[r] + a.seq.cu[r + 1] - a.seq.cu[r], most_seen);
         };
         for (int r = 0; r < a.seq.n_req; ++r) a.runs[r] = {r, (a.seq.cu[r + 1] - a.seq.cu[r] + a.unit_rows - 1) / a.unit_rows, a.seq.start[r]};
-        std::stable_sort(a.runs, a.runs + a.seq.n_req, [&](const MaskedRun &x, const MaskedRun &y) { return sees(x.req) < sees(y.req); });
+        std::sort(a.runs, a.runs + a.seq.n_req, [&](const MaskedRun &x, const MaskedRun &y) {
+            return std::make_pair(sees(x.req), x.req) < std::make_pair(sees(y.req), y.req);
+        });
     }
-    const int tiles = (keys + 63) / 64;
+    const int tiles = (int)(((int64_t)keys + 63) / 64);
     const auto cut = [&](int least, int most) {   // pieces of about `least` tiles or more, none but the first for each compute unit
         return (int)std::max<int64_t>(1, std::min<int64_t>({MASKED_PIECES / wgs, most, (tiles + least - 1) / least}));
     };

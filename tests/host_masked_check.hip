@@ -28,7 +28,7 @@ static void decode_forms() {
     struct { int Hq, Hkv, B, max_ctx, window, sinks; MaskedKind kind; int cut; } of[] = {
         {32, 8, 1, 4096, 1024, 4, MASKED_FEW8, 8}, {32, 8, 1, 8193, 8192, 4, MASKED_FEW8, 16}, {32, 8, 1, 4097, 4096, 0, MASKED_FEW8, 16}, {32, 8, 1, 4001, 4096, 0, MASKED_FEW8, 8}, {32, 8, 64, 8193, 4096, 4, MASKED_FEW4, 1},
         {32, 8, 32, 8193, 4096, 4, MASKED_FEW8, 1}, {8, 2, 1, 100, 64, 0, MASKED_FEW8, 1}, {16, 1, 1, 1 << 30, 1 << 30, 0, MASKED_FEW8, 16},
-        {16, 1, 65535, 2147483632, 2147483647, 2147483647, MASKED_FEW4, 1}};
+        {16, 1, 65535, 2147483632, 2147483647, 2147483647, MASKED_FEW4, 1}, {16, 1, 1, 2147483632, 2147483647, 2147483647, MASKED_FEW8, 16}};
     for (auto &w : of) {
         MaskedAttnArgs a = heads(w.Hq, w.Hkv);
         a.ctx_lens = &lens, a.B = w.B, a.max_ctx = w.max_ctx, a.window = w.window, a.sinks = w.sinks;
