@@ -314,7 +314,7 @@ __device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps) {
 // products with V with the rest of them and with the next step's maxima.  (A product takes 16 ns of a SIMD; an exponential, its multiplication
 // and two additions beside it one more.)
 // The exponentials' reference is the row's first maximum, moved to the running one once a score is 2^4 above it: two steps in three need no rescaling.
-// 16384 rows of the 8B heads under a window of 4096: 902 to 990 us from card to card, 1.0 PFLOP/s at 1.8 GHz, the matrix unit busy 54 % of the cycles; the loop with its products
+// 16384 rows of the 8B heads under a window of 4096: 902 to 990 us from card to card, 1.0 PFLOP/s at 1.8 GHz, the matrix unit busy 55 % of the cycles; the loop with its products
 // alone takes 607.  32 trees of 32 rows behind 512 to 4096 tokens: 73 us, as long as the longest one's steps take.
 constexpr int TAB_BLOCKS = 2048;
 template <int HD, int KH, bool TREE>
