@@ -380,7 +380,8 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     };
     int tb = t0;   // the first step of s_tab
     // Wave w brings block w of a step, 16 bytes a lane (lane l's at the window's base + 16 l).  K keeps the
-    // pool's order; V's chunk (dim, half of 8 tokens) goes to [half][dim].  A block that is missing is read as block 0, and masked.
+    // pool's order; V's chunk (dim, half of 8 tokens) goes to [half][dim].  A block that is missing is read as block 0, masked, and its values are
+    // cleared: a weight of zero times what another request's block holds may be NaN.
     typedef __attribute__((address_space(3))) void lds_void;
     auto id_of = [&](int t) { return s_tab[min(STEP * (t - tb) + wave, TAB_BLOCKS - 1)]; };   // (behind the last step: not used)
     auto head_of = [&](int id) { return ((size_t)max(__builtin_amdgcn_readfirstlane(id), 0) * a.Hkv + hk) * BLK; };
@@ -551,6 +552,12 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     // In front of step t's work: K of the step after it and V of its own have landed, nobody reads those of the step before any more; their buffers
     // take K of the step after the next and V of the next.
     auto turn = [&](int t) {
+        // the wave's own block of V, cleared if it is missing (a step before the piece's last has blocks behind the end in no case)
+        if ((t + 1 >= t1 || bad) && (STEP * t + wave >= s.blocks || (bad && __builtin_amdgcn_readfirstlane(s_tab[STEP * (t - tb) + wave]) < 0))) {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int i = 0; i < HD / 32; ++i) st_bf16x8(v_at(t) + wave * BLK + (64 * i + lane) * 8, zero_bf16x8());
+        }
         meet();
         if (STEP * (t + 4 - tb) > TAB_BLOCKS && t + 1 < t1) {   // contexts of more than 32K tokens
             if (KH == 2) __syncthreads();
@@ -752,7 +759,7 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
         return -1;
     };
     bf16x8 kf[KS], vf[2][DT];
-    auto head_of = [&](int id) { return ((size_t)max(id, 0) * a.Hkv + hk) * BLK; };   // (a block that is missing: block 0, masked)
+    auto head_of = [&](int id) { return ((size_t)max(id, 0) * a.Hkv + hk) * BLK; };   // (a block that is missing: block 0, masked, its values cleared)
     auto load_k = [&](int ids) {
         const size_t h0 = head_of(__builtin_amdgcn_readlane(ids, 0)), h1 = head_of(__builtin_amdgcn_readlane(ids, 1));
         const bf16_t *p = a.k_pool + (c32 < 16 ? h0 : h1) + kpool_chunk_offset(c32 & 15, 8 * h);
@@ -809,6 +816,10 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
                 for (int i = 0; i < 8; ++i) {
                     const float x = st[8 * b + i];
                     st[8 * b + i] = seen & (1u << ((i >> 2) * 8 + (i & 3))) ? x : NEG_INF;
+                }
+                if (!there) {
+#pragma unroll
+                    for (int dt = 0; dt < DT; ++dt) vf[b][dt] = zero_bf16x8();
                 }
             }
         }
