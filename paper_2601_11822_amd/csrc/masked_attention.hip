@@ -20,6 +20,8 @@ namespace {
 
 __device__ __forceinline__ f32x16 mfma32(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 
+typedef uint32_t u32x4_m __attribute__((ext_vector_type(4)));
+
 // What a unit's rows see.
 struct Span {
     int row0 = 0, rows = 0;      // rows of q and out
@@ -115,12 +117,27 @@ __device__ __forceinline__ Sight row_sight(const MaskedAttnArgs &a, const Span &
     }
     return v;
 }
+// What any of the unit's rows sees.  The other values of a block are cleared before they are multiplied: a weight of zero times what a place behind the
+// last token holds, or one before the window, may be NaN, and pools need not be zeroed.  (Values that some of the rows see are left to careful_unit.)
+template <bool TREE>
+__device__ __forceinline__ Sight unit_sight(const MaskedAttnArgs &a, const Span &s) {
+    Sight v{};
+    if (TREE) {
+        v.ctx = s.first + s.n;
+    } else {
+        v.hi = s.first + s.rows - 1;
+        v.lo = max(s.first - a.window + 1, 0);
+        v.sinks = a.sinks;
+    }
+    return v;
+}
+// Two values of the tokens 2j and 2j + 1 of a bit each in `seen`: which bits of them stay.
+__device__ __forceinline__ uint32_t keep_pair(uint32_t seen, int j) { return (seen >> 2 * j & 1 ? 0x0000ffffu : 0u) | (seen >> 2 * j & 2 ? 0xffff0000u : 0u); }
 
 // Weights of a block: the half-waves (same column) hold tokens 4h..4h+3 and 8+4h..8+4h+3 and trade their middle pieces; h = 0 then has tokens
 // 0-7, h = 1 tokens 8-15, the contraction slices of V's own layout.
 __device__ __forceinline__ bf16x8 by_tokens(bf16x8 p) {
-    typedef uint32_t u32x4p __attribute__((ext_vector_type(4)));
-    u32x4p w = __builtin_bit_cast(u32x4p, p);
+    u32x4_m w = __builtin_bit_cast(u32x4_m, p);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         const auto sw = __builtin_amdgcn_permlane32_swap(w[u], w[u + 2], false, false);
@@ -240,7 +257,7 @@ __device__ __forceinline__ void join_pieces(const MaskedAttnArgs &a, const Span 
 
 // The same sums one key after the other in float32, without the matrix unit: for units whose result is not finite.  There a weight
 // of zero times a value that is infinite or NaN may have reached rows that do not see that value; here it cannot.  Slow (some ms for
-// 4096 keys), and only taken where a cache holds such values.
+// 4096 keys), and only taken where a key or value that some row of the unit sees is not finite, as what no row sees is cleared.
 template <int HD, bool TREE>
 __device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span &s, int hk, int b0, int b1, const Piece &pc, int threads) {
     constexpr int D = 32;   // dims of a thread
@@ -381,7 +398,7 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     int tb = t0;   // the first step of s_tab
     // Wave w brings block w of a step, 16 bytes a lane (lane l's at the window's base + 16 l).  K keeps the
     // pool's order; V's chunk (dim, half of 8 tokens) goes to [half][dim].  A block that is missing is read as block 0, masked, and its values are
-    // cleared: a weight of zero times what another request's block holds may be NaN.
+    // cleared.
     typedef __attribute__((address_space(3))) void lds_void;
     auto id_of = [&](int t) { return s_tab[min(STEP * (t - tb) + wave, TAB_BLOCKS - 1)]; };   // (behind the last step: not used)
     auto head_of = [&](int id) { return ((size_t)max(__builtin_amdgcn_readfirstlane(id), 0) * a.Hkv + hk) * BLK; };
@@ -551,12 +568,24 @@ __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs
     };
     // In front of step t's work: K of the step after it and V of its own have landed, nobody reads those of the step before any more; their buffers
     // take K of the step after the next and V of the next.
+    const int t_edge = max(s.sink_blocks - 1, 0) / STEP;
     auto turn = [&](int t) {
-        // the wave's own block of V, cleared if it is missing (a step before the piece's last has blocks behind the end in no case)
-        if ((t + 1 >= t1 || bad) && (STEP * t + wave >= s.blocks || (bad && __builtin_amdgcn_readfirstlane(s_tab[STEP * (t - tb) + wave]) < 0))) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        // What no row sees of the wave's own block of V is cleared: places behind the end (in the last step), those behind the sinks or before the windows
+        // (blocks sink_blocks - 1 and sink_blocks), a missing block whole.
+        if (t + 1 >= t1 || bad || (!TREE && (unsigned)(t - t_edge) <= 1)) {
+            const int e = STEP * t + wave;
+            const bool here = e < s.blocks && !(bad && __builtin_amdgcn_readfirstlane(s_tab[STEP * (t - tb) + wave]) < 0);
+            const uint32_t some = here ? unit_sight<TREE>(a, s).template sees16<TREE>(16 * (e < s.sink_blocks ? e : e + s.skip)) : 0u;
+            if (some != 0xffffu) {
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 #pragma unroll
-            for (int i = 0; i < HD / 32; ++i) st_bf16x8(v_at(t) + wave * BLK + (64 * i + lane) * 8, zero_bf16x8());
+                for (int i = 0; i < HD / 32; ++i) {   // 64 dims of a half of the tokens
+                    u32x4_m *p = (u32x4_m *)(v_at(t) + wave * BLK + (64 * i + lane) * 8), w = *p;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] &= keep_pair(some >> (i / (HD / 64) * 8), j);
+                    *p = w;
+                }
+            }
         }
         meet();
         if (STEP * (t + 4 - tb) > TAB_BLOCKS && t + 1 < t1) {   // contexts of more than 32K tokens
@@ -779,7 +808,7 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
     const bool any = t < t1;
     if (any) load_k(ids), load_v(ids);
     int next = fetch_ids(t + NW);
-    const Sight see = row_sight<TREE>(a, s, row);
+    const Sight see = row_sight<TREE>(a, s, row), all = unit_sight<TREE>(a, s);
     bf16x8 qf[KS];
     {
         const bf16_t *qp = a.q + (size_t)(s.row0 + row) * a.q_stride + (size_t)(hk * G + min(col, cols - 1) % G) * HD + 8 * h;
@@ -817,9 +846,19 @@ __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a
                     const float x = st[8 * b + i];
                     st[8 * b + i] = seen & (1u << ((i >> 2) * 8 + (i & 3))) ? x : NEG_INF;
                 }
-                if (!there) {
+                const uint32_t some = there ? all.sees16<TREE>(p) : 0u;
+                if (some != 0xffffu) {   // uniform; the lane's values are those of tokens 8h ..
 #pragma unroll
-                    for (int dt = 0; dt < DT; ++dt) vf[b][dt] = zero_bf16x8();
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t keep = keep_pair(some >> (8 * h), j);
+#pragma unroll
+                        for (int dt = 0; dt < DT; ++dt) {
+                            u32x4_m w = __builtin_bit_cast(u32x4_m, vf[b][dt]);
+                            w[j] &= keep;
+                            vf[b][dt] = __builtin_bit_cast(bf16x8, w);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
             }
         }

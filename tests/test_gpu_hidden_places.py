@@ -133,3 +133,31 @@ def test_ids_that_are_none_of_the_pool(make, args):
     hidden[0] = True
     same_bits(c, hidden, lambda: call(tab))
     c.c.destroy()
+
+
+@pytest.mark.parametrize("make,args", CASES, ids=IDS)
+def test_places_that_no_row_sees(make, args):
+    """Behind the last token, before the oldest window and behind the sinks."""
+    c, tab, seen, call = make(*args)
+    hidden = torch.ones(c.n_blocks, 16, dtype=torch.bool)
+    for r, keys in enumerate(seen):
+        keys = np.array(list(keys), np.int64)
+        hidden[torch.from_numpy(tab[r][keys // 16]).long(), torch.from_numpy(keys % 16)] = False
+    same_bits(c, hidden, lambda: call(tab))
+    c.c.destroy()
+
+
+@pytest.mark.parametrize("args", PROMPTS, ids=[f"prompt_case{i}" for i in range(len(PROMPTS))])
+def test_tokens_that_only_later_rows_see(args):
+    """The last token of every prompt: rows so far before it that they share no workgroup with its own row (128 columns) are the same bits."""
+    heads, lens, starts = args[:3]
+    c, tab, _, call = prompt_case(*args)
+    per = 128 // (heads[0] // heads[1])
+    early, hidden = [], torch.zeros(c.n_blocks, 16, dtype=torch.bool)
+    for r, (n, first, at) in enumerate(zip(lens, starts, np.cumsum([0] + lens))):
+        if n > per:
+            hidden[tab[r, (first + n - 1) // 16], (first + n - 1) % 16] = True
+            early += range(at, at + n - per)
+    if early:
+        same_bits(c, hidden, lambda: call(tab)[early])
+    c.c.destroy()
