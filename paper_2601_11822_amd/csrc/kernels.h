@@ -195,6 +195,7 @@ struct KvStoreArgs {
     uint64_t axis[2];         // two bits a pair of dims
     int n_axes, max_rows, Hq, Hkv, hd, n_blocks, max_pos;
 };
+bool kv_store_past(const KvStoreArgs &a);   // whether rows go past the caches
 void launch_kv_store(hipStream_t st, const KvStoreArgs &a);
 struct KvCompactArgs {
     bf16_t *k_pool, *v_pool;  // the first of n_layers

@@ -225,23 +225,28 @@ __device__ __forceinline__ void turn(const CosSin cs[8], bf16x8 &lo, bf16x8 &hi)
     }
 }
 
+// Rows of a wave of the kv heads.  Of few rows four, so that short runs are not written one after the other by few waves; of many 16, as three waves in four would
+// only look for the beginning of a run.  us with 4 / 16, 8B heads: 64 single rows 10.3 / 31.7, 512 rows in runs of 8 8.8 / 12.6, 2048 in runs of 8 21.0 / 18.9,
+// in one run 20.0 / 11.6; 8/2 heads, 4096 rows in runs of 8 13.3 / 14.0, in one run 11.6 / 7.7.
+constexpr int STORE_SHORT = 2048;
+
 typedef uint32_t u32x4_s __attribute__((ext_vector_type(4)));
-template <bool MANY> __device__ __forceinline__ bf16x8 ld_row(const bf16_t *p) { return MANY ? ld_bf16x8_stream(p) : ld_bf16x8(p); }
-template <bool MANY> __device__ __forceinline__ void st_row(bf16_t *p, bf16x8 v) {
-    if (MANY) __builtin_nontemporal_store(v, (bf16x8 *)p);
+template <bool PAST> __device__ __forceinline__ bf16x8 ld_row(const bf16_t *p) { return PAST ? ld_bf16x8_stream(p) : ld_bf16x8(p); }
+template <bool PAST> __device__ __forceinline__ void st_row(bf16_t *p, bf16x8 v) {
+    if (PAST) __builtin_nontemporal_store(v, (bf16x8 *)p);
     else st_bf16x8(p, v);
 }
 
-// MANY: rows for more than the caches, which are read and written past them (16444 rows of the 8B heads, in us: 97; only the loads 97, only the
+// PAST: rows of so many bytes that they are read and written past the caches (16444 rows of the 8B heads, in us: 97; only the loads 97, only the
 // stores 91, both 83; with the parts of a row in workgroups far apart, so that its angles are fetched again, 108).
-template <int HD, bool MANY>
+template <int HD, bool PAST>
 __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_groups, int kv_parts, int q_parts) {
-    constexpr int kv_rows = MANY ? 16 : 4;   // few rows: a wave for every four, so that short runs are not written one after the other
     constexpr int C = HD / 16;   // 8-dim chunks of half a head
     constexpr int BLK = 16 * HD, PL = HD / 8;   // PL: places of a lane's V
     constexpr int ROUNDS = 16 * C / 64;   // of items (row, 8 pairs) of a key block
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int rows = a.n_rows ? min(max(*a.n_rows, 0), a.max_rows) : a.max_rows;
+    const int kv_rows = a.max_rows > STORE_SHORT ? 16 : 4;
     if ((int)blockIdx.x >= kv_groups * kv_parts) {
         // a thread: 8 pairs of a row, in every second one of 8 heads
         const int at = blockIdx.x - kv_groups * kv_parts, row0 = 16 * (at / q_parts), h0 = at % q_parts * 8;
@@ -253,7 +258,7 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_gro
             bf16x8 lo[4], hi[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k)   // all asked for before one is written (queries in place are the thread's own)
-                if (first + 2 * k < a.Hq) lo[k] = ld_row<MANY>(p + (first + 2 * k) * HD), hi[k] = ld_row<MANY>(p + (first + 2 * k) * HD + HD / 2);
+                if (first + 2 * k < a.Hq) lo[k] = ld_row<PAST>(p + (first + 2 * k) * HD), hi[k] = ld_row<PAST>(p + (first + 2 * k) * HD + HD / 2);
             if (!in_table(a, r)) {
                 atomicOr(a.err_flag, 1);
                 continue;
@@ -266,8 +271,8 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_gro
             for (int k = 0; k < 4; ++k)
                 if (first + 2 * k < a.Hq) {
                     turn(cs, lo[k], hi[k]);
-                    st_row<MANY>(q + (first + 2 * k) * HD, lo[k]);
-                    st_row<MANY>(q + (first + 2 * k) * HD + HD / 2, hi[k]);
+                    st_row<PAST>(q + (first + 2 * k) * HD, lo[k]);
+                    st_row<PAST>(q + (first + 2 * k) * HD + HD / 2, hi[k]);
                 }
         }
         return;
@@ -326,7 +331,7 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_gro
                     place[k] = r < n && ok ? slot & 15 : -1;
                     if (place[k] >= 0) {
                         const bf16_t *p = src + (size_t)r * a.row_stride + 8 * c;
-                        lo[k] = ld_row<MANY>(p), hi[k] = ld_row<MANY>(p + HD / 2);
+                        lo[k] = ld_row<PAST>(p), hi[k] = ld_row<PAST>(p + HD / 2);
                         angles(a, at, 8 * c, cs[k]);
                     }
                 }
@@ -449,13 +454,18 @@ void launch_kv_plan(hipStream_t st, const KvPlanArgs &a) {
     hipLaunchKernelGGL(kv_plan_kernel, dim3(x, y), dim3(64 * PLAN_WAVES), 0, st, a);
 }
 
+// What is read and written, against the caches.  One run of rows / and attention under a window of 256 over the queries, in us through the caches and past
+// them: 8B heads, 2048 rows (50 MB) 11.0 / 33.9 and 11.6 / 35.7, 4096 23.5 / 65.0 and 21.6 / 64.2, 16384 90 / 234 and 84 / 227; 64/8 heads, 2048 (84 MB)
+// 18.4 / 59.8 and 19.5 / 60.7; 8/2 heads, 4096 (25 MB) 7.5 / 26.2 and 7.7 / 27.4, 16384 (101 MB) 26.9 / 70.3 and 23.0 / 68.6.
+bool kv_store_past(const KvStoreArgs &a) { return (int64_t)a.max_rows * (a.Hq + 2 * a.Hkv) * a.hd * 4 > 80ll << 20; }
+
 void launch_kv_store(hipStream_t st, const KvStoreArgs &a) {
-    const bool many = a.max_rows > 2048;   // 48 MB of the 8B heads
-    const int kv_rows = many ? 16 : 4, kv_groups = (a.max_rows + kv_rows - 1) / kv_rows, kv_parts = (a.Hkv + 3) / 4, q_parts = (a.Hq + 7) / 8;
+    const int kv_rows = a.max_rows > STORE_SHORT ? 16 : 4, kv_groups = (a.max_rows + kv_rows - 1) / kv_rows, kv_parts = (a.Hkv + 3) / 4, q_parts = (a.Hq + 7) / 8;
     const dim3 grid(kv_groups * kv_parts + (a.max_rows + 15) / 16 * q_parts);
     auto launch = [&](auto *kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, kv_groups, kv_parts, q_parts); };
-    if (a.hd == 128) many ? launch(kv_store_kernel<128, true>) : launch(kv_store_kernel<128, false>);
-    else many ? launch(kv_store_kernel<64, true>) : launch(kv_store_kernel<64, false>);
+    const bool past = kv_store_past(a);
+    if (a.hd == 128) past ? launch(kv_store_kernel<128, true>) : launch(kv_store_kernel<128, false>);
+    else past ? launch(kv_store_kernel<64, true>) : launch(kv_store_kernel<64, false>);
 }
 
 void launch_kv_compact(hipStream_t st, const KvCompactArgs &a) {
