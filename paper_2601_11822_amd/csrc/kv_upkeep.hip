@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256) void kv_store_kernel(KvStoreArgs a, int kv_gro
     constexpr int ROUNDS = 16 * C / 64;   // of items (row, 8 pairs) of a key block
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int rows = a.n_rows ? min(max(*a.n_rows, 0), a.max_rows) : a.max_rows;
-    const int kv_rows = a.max_rows > STORE_SHORT ? 16 : 4;
+    const int kv_rows = rows > STORE_SHORT ? 16 : 4;   // (of the rows there are: the bound may be far above them)
     if ((int)blockIdx.x >= kv_groups * kv_parts) {
         // a thread: 8 pairs of a row, in every second one of 8 heads
         const int at = blockIdx.x - kv_groups * kv_parts, row0 = 16 * (at / q_parts), h0 = at % q_parts * 8;
@@ -460,7 +460,7 @@ void launch_kv_plan(hipStream_t st, const KvPlanArgs &a) {
 bool kv_store_past(const KvStoreArgs &a) { return (int64_t)a.max_rows * (a.Hq + 2 * a.Hkv) * a.hd * 4 > 80ll << 20; }
 
 void launch_kv_store(hipStream_t st, const KvStoreArgs &a) {
-    const int kv_rows = a.max_rows > STORE_SHORT ? 16 : 4, kv_groups = (a.max_rows + kv_rows - 1) / kv_rows, kv_parts = (a.Hkv + 3) / 4, q_parts = (a.Hq + 7) / 8;
+    const int kv_groups = std::max((a.max_rows + 15) / 16, (std::min(a.max_rows, STORE_SHORT) + 3) / 4), kv_parts = (a.Hkv + 3) / 4, q_parts = (a.Hq + 7) / 8;
     const dim3 grid(kv_groups * kv_parts + (a.max_rows + 15) / 16 * q_parts);
     auto launch = [&](auto *kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, kv_groups, kv_parts, q_parts); };
     const bool past = kv_store_past(a);
