@@ -179,6 +179,7 @@ struct KvPlanArgs {
     int32_t *ticket, *err_flag;           // the ticket is 0 between launches
     int B, max_blk, n_blocks, free_cap, max_rows, parent_stride;
 };
+int kv_plan_shares(const KvPlanArgs &a);   // workgroups that share 64 requests' rows
 void launch_kv_plan(hipStream_t st, const KvPlanArgs &a);
 #define RS_AXES 4   // most axes of positions
 struct KvStoreArgs {

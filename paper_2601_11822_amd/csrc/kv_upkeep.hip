@@ -447,11 +447,12 @@ __global__ __launch_bounds__(256) void kv_compact_kernel(KvCompactArgs a) {
 
 }  // namespace
 
+static int plan_groups(const KvPlanArgs &a) { return (a.B + PLAN_REQS - 1) / PLAN_REQS; }
+// long runs: some 4096 rows for each workgroup
+int kv_plan_shares(const KvPlanArgs &a) { return a.parents ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(((int64_t)a.max_rows / plan_groups(a) + 4095) / 4096, 64)); }
+
 void launch_kv_plan(hipStream_t st, const KvPlanArgs &a) {
-    const int x = (a.B + PLAN_REQS - 1) / PLAN_REQS;
-    // long runs: some 4096 rows for each workgroup
-    const int y = a.parents ? 1 : std::max(1, std::min((a.max_rows / x + 4095) / 4096, 64));
-    hipLaunchKernelGGL(kv_plan_kernel, dim3(x, y), dim3(64 * PLAN_WAVES), 0, st, a);
+    hipLaunchKernelGGL(kv_plan_kernel, dim3(plan_groups(a), kv_plan_shares(a)), dim3(64 * PLAN_WAVES), 0, st, a);
 }
 
 // What is read and written, against the caches.  One run of rows / and attention under a window of 256 over the queries, in us through the caches and past

@@ -20,7 +20,21 @@ static void store() {
     }
 }
 
+// Long runs are shared by workgroups, up to the largest bound of rows there is
+static void plan() {
+    static int32_t up;
+    struct { int B, max_rows; bool trees; int shares; } of[] = {
+        {1, 0, false, 1}, {1, 4096, false, 1}, {1, 4097, false, 2}, {64, 16384, false, 4}, {65, 16384, false, 2}, {1, 300000, false, 64}, {1, 2147483647 - 4096, false, 64},
+        {1, 2147483647 - 4094, false, 64}, {1, 2147483647, false, 64}, {64, 2147483647, true, 1}, {65535, 2147483647, false, 64}, {65535, 1000000, false, 1}};
+    for (auto &w : of) {
+        KvPlanArgs a{};
+        a.B = w.B, a.max_rows = w.max_rows, a.parents = w.trees ? &up : nullptr;
+        CHECK(kv_plan_shares(a) == w.shares, "%d requests, %d rows: %d shares", w.B, w.max_rows, kv_plan_shares(a));
+    }
+}
+
 int main() {
+    plan();
     store();
     std::printf(fails ? "%d failures\n" : "ok\n", fails);
     return fails != 0;
