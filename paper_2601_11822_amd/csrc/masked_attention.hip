@@ -6,7 +6,7 @@
 //   tree:    j < ctx, and ctx + t for every bit t of the row's ancestor mask.
 // A row that sees nothing gets zero.  What a key holds that a row does not see, NaN included, does not reach that row.
 // Scores, maxima, sums and joins are float32.  Weights go into the product with V as bf16, as over this cache everywhere: V is bf16 and the matrix unit takes
-// both factors of one type, so more bits would be a second product.  It adds some 0.0011 to the 0.0016 that the output's own rounding leaves, in quadrature.
+// both factors of one type, so more bits would be a second product.  It adds 0.0011 to 0.0015 to the 0.0016 that the output's own rounding leaves, in quadrature.
 //
 // A UNIT is as many rows of one request and one kv head as fit in 128 columns, or 32, a column being (row, query head of the group): the
 // keys of a block are read once for all of them.  Where units are fewer than compute units, each one's keys are cut in pieces.  The blocks that any row of a unit sees are counted through (`Span`): those of the
@@ -259,7 +259,7 @@ __device__ __forceinline__ void join_pieces(const MaskedAttnArgs &a, const Span 
 
 // The same sums one key after the other in float32, without the matrix unit: for units whose result is not finite.  There a weight
 // of zero times a value that is infinite or NaN may have reached rows that do not see that value; here it cannot.  Slow (some ms for
-// 4096 keys), and only taken where a key or value that some row of the unit sees is not finite, as what no row sees is cleared.
+// 4096 keys), and only taken where a key or value that some row of the unit sees is not finite: what no row sees is cleared.
 template <int HD, bool TREE>
 __device__ __forceinline__ void careful_unit(const MaskedAttnArgs &a, const Span &s, int hk, int b0, int b1, const Piece &pc, int threads) {
     constexpr int D = 32;   // dims of a thread
@@ -336,8 +336,8 @@ __device__ __forceinline__ int tree_cut(const MaskedAttnArgs &a, int steps) {
 // where bf16 is finest, and their error against float64 is that of rounding exact weights (tests/test_gpu_masked_error.py).  In us, 16384 rows under a window
 // of 4096 / 32 trees of 32 rows, and the error by that of exact weights: the maximum itself 1015 / 77.1, 0.98; twice it 995 / 76.6, 1.00; three times 992 / 76.7,
 // 1.02; a reference that follows once a score is 2^4 above it 957 / 74.4, 1.06.
-// 16384 rows of the 8B heads under a window of 4096: 902 to 990 us from card to card, 1.0 PFLOP/s at 1.8 GHz, the matrix unit busy 55 % of the cycles; the loop with its products
-// alone takes 607.  32 trees of 32 rows behind 512 to 4096 tokens: 73 us, as long as the longest one's steps take.
+// 16384 rows of the 8B heads under a window of 4096: 955 to 1060 us from card to card, 0.91 to 1.01 PFLOP/s, the matrix unit busy 48 % of the cycles; the loop with its products
+// alone takes 607.  32 trees of 32 rows behind 512 to 4096 tokens: 76 us, as long as the longest one's steps take.
 constexpr int TAB_BLOCKS = 2048;
 template <int HD, int KH, bool TREE>
 __global__ __launch_bounds__(256 * KH, 2) void masked_wide_kernel(MaskedAttnArgs a) {
@@ -758,7 +758,7 @@ __global__ __launch_bounds__(256) void masked_join_kernel(MaskedAttnArgs a) {
 // tiles of 32 keys (two blocks) in turn, straight from the pools into the operands of 32x32x16 products (every load of a wave is a contiguous
 // kilobyte, or four pieces of 256 bytes); a tile's keys are asked for as soon as the products with the ones before have been issued, and so are
 // its values.  The waves' sums meet in LDS at the end.  8B heads: 64 rows of 512 to 16383 tokens under a window of 4096 take 152 us, 6.3 TB/s (with
-// eight waves 154); one row under a window of 1024 8.4 to 8.8 us, in eight pieces.
+// eight waves 154); one row under a window of 1024 8.7 to 8.9 us, in eight pieces.
 template <int HD, int NW, bool TREE>
 __global__ __launch_bounds__(64 * NW, 2) void masked_few_kernel(MaskedAttnArgs a) {
     constexpr int KS = HD / 16, DT = HD / 32, BLK = 16 * HD, PAD = HD + 4;
@@ -992,9 +992,9 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
     for (int r = 0; !tree && !a.ctx_lens && r < a.seq.n_req; ++r) keys = std::max(keys, a.seq.start[r] + a.seq.cu[r + 1] - a.seq.cu[r]);
     if (!tree) keys = (int)std::min<int64_t>(keys, (int64_t)a.window + a.sinks + 32);
     // Units of 32 columns where a request has no more, or where reading the keys again for each of them is little: us with units of 32 / of 128,
-    // 8B heads: a tree of 16 behind 900 tokens 12.7 / 17.8, eight of them 18.2 / 20.5, one of 60 behind 3500 19.7 / 21.6, three of 32
-    // behind 3000 25.7 / 25.7, four behind 4000 32.0 / 28.4, sixteen behind 500 to 4096 67.5 / 52.4; 100 rows under a window of 2048 20.3 / 20.6,
-    // 512 42.4 / 36.6; prompts of 200 rows 8.7 / 12.7, 400 12.1 / 15.6, 600 18.7 / 18.5.
+    // 8B heads: a tree of 16 behind 900 tokens 12.0 / 16.3, eight of them 17.7 / 19.8, one of 60 behind 3500 19.1 / 22.0, three of 32
+    // behind 3000 25.4 / 26.3, four behind 4000 32.1 / 29.2, sixteen behind 500 to 4096 67.9 / 55.9; 100 rows under a window of 2048 19.4 / 21.5,
+    // 512 39.0 / 41.1; prompts of 200 rows 9.0 / 12.9, 400 12.1 / 21.1, 600 18.7 / 20.0.
     const bool few = most * G <= 32 || (int64_t)units(32 / G) * a.Hkv * keys <= 256 * 1024;
     a.unit_rows = (few ? 32 : MASKED_COLS) / G;
     a.units_per_req = (a.max_draft + a.unit_rows - 1) / a.unit_rows;
@@ -1002,7 +1002,7 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
     const int64_t wgs = (int64_t)a.n_units * a.Hkv;
     if (wgs <= 0) return f;
     // Prompts whose rows see most are begun first, so that a launch ends with short units: us without / so, 1500, 100, 2000, 700 and 64 rows behind 0, 3000, 500,
-    // 2000 and 9 144 / 117; 700 rows behind 1024, 33 behind 4000 and 1391 of 64/8 heads under a window of 512 59.2 / 54.9.
+    // 2000 and 9 158 / 129; 700 rows behind 1024, 33 behind 4000 and 1391 of 64/8 heads under a window of 512 63.5 / 58.9.
     if (!tree && !a.ctx_lens) {
         const auto sees = [&](int r) {   // the first row and the last
             const int64_t most_seen = (int64_t)a.window + a.sinks;
@@ -1017,7 +1017,10 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
     const auto cut = [&](int least, int most) {   // pieces of about `least` tiles or more, none but the first for each compute unit
         return (int)std::max<int64_t>(1, std::min<int64_t>({MASKED_PIECES / wgs, most, (tiles + least - 1) / least}));
     };
-    const bool alone = wgs <= MASKED_PIECES;   // every workgroup has a compute unit to itself
+    // Every workgroup has a compute unit to itself on the whole chip.  A partition may have fewer; the forms are the same there, so that the bits are, though one team
+    // is then often faster: us with two teams / one on 256, 192, 128 and 64 units, 32 trees of 32 77 / 93, 98 / 105, 125 / 106, 211 / 183; 2048 rows 58 / 64, 74 / 61,
+    // 99 / 79, 195 / 148.
+    const bool alone = wgs <= MASKED_PIECES;
     if (few) {
         f.kind = alone ? MASKED_FEW8 : MASKED_FEW4;
         // Eight pieces are asked for together by the one that joins them; more pay for long contexts.  us in 8 / 16 / 32 pieces, 8B heads: a row under a
@@ -1027,8 +1030,8 @@ MaskedForm masked_form(MaskedAttnArgs &a) {
         a.cut = cut(2, tiles <= 64 ? 8 : 16);
     } else {
         // Two teams halve the longest unit's time, which two rounds of units end with where most are much shorter: us with two teams / one, 8B heads:
-        // a prompt of 1200 rows 29.3 / 35.1, 2048 51.9 / 56.7 (under a window of 1750 52.2 / 53.3, 1536 52.4 / 49.4, 512 40.1 / 30.2), 2048 behind 500
-        // 68.0 / 72.1, behind 4000 199 / 187, 1600 beside 100 41.8 / 45.2; 2500 rows (three rounds) 79.5 / 72.2; 64 query heads, 1024 rows 37.1 / 35.4.
+        // a prompt of 1200 rows 32.4 / 37.9, 2048 57.7 / 63.4 (under a window of 1750 57.6 / 58.7, 1536 58.4 / 55.6, 512 42.3 / 31.9), 2048 behind 500
+        // 74.9 / 78.8, behind 4000 195 / 187, 1600 beside 100 46.2 / 49.8; 2500 rows (three rounds) 86.3 / 77.9; 64 query heads, 1024 rows 39.8 / 38.0.
         int64_t seen = 0;   // by all rows
         for (int r = 0; !tree && !a.ctx_lens && r < a.seq.n_req; ++r) {
             const int64_t n = a.seq.cu[r + 1] - a.seq.cu[r];
